@@ -7,7 +7,8 @@
  * block (section 3.1, second improvement; section 3.3).
  *
  * Conventions
- *   - Every tensor is fp32, contiguous, NCHW.  Weights: full 3x3 conv [Cout,Cin,3,3]; depthwise
+ *   - Every tensor of a block is fp32, contiguous, NCHW (the sequence operators at the end state their own types and
+ *     strides).  Weights: full 3x3 conv [Cout,Cin,3,3]; depthwise
  *     [C,1,3,3]; pointwise and shortcut 1x1 [Cout,Cin]; BatchNorm gamma, beta [C].
  *   - Pointers named *_dev are device pointers, *_host host pointers.  `hip_stream` is a hipStream_t
  *     passed as void* (NULL = the default stream).
@@ -348,6 +349,154 @@ int pbkd_kernel_kinds(void);
 const char *pbkd_kernel_kind_name(int kind);
 pbkd_status pbkd_block_profile_enable(pbkd_block_t *blk, unsigned kind_mask, int capacity);
 pbkd_status pbkd_block_profile_read(pbkd_block_t *blk, int n_kinds, double *ms_sum, int *launches);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators of sequence students.
+ *
+ * A student block of a sequence model takes the place of a teacher block as the convolutional ones do: trained on the local
+ * loss against the teacher block's activations (Eq. 3), with gradients through the student only (section 3.1).  Its
+ * cheap token mixer is a gated linear recurrence (a state per channel in place of the attention over all tokens, as the
+ * depthwise convolution is the cheap replacement of the full one), behind a root-mean-square norm; AdamW is the update such
+ * students are trained with.  Matrix products around them stay the caller's.
+ *
+ * These calls keep the conventions above (status, pbkd_last_error, asynchronous on the given stream, no device memory
+ * allocated) and hold no state of their own: a descriptor is read during the call and may be reused or freed at once.
+ * Activations are of one of three types, PBKD_F32, PBKD_BF16 or PBKD_F16, arithmetic, statistics, states and sums are fp32,
+ * and each output is rounded once (to nearest).  Rows are strided: the innermost dimension is contiguous, the others have
+ * strides in elements (any value of at least the row's length for an output; inputs may overlap or repeat).  Pointers need the
+ * alignment of their element only.  An output may be the very tensor of an input of the same call where that is stated;
+ * any other overlap of an output with another tensor of the call is undefined.  Workspaces need no initial contents,
+ * hold nothing between calls, must be 256-byte aligned and may not be used by two calls at once.
+ * Results do not depend on timing: the same inputs give the same bits. */
+enum { PBKD_F32 = 0, PBKD_BF16 = 1, PBKD_F16 = 2, PBKD_E4M3 = 3 };
+
+/* Root-mean-square norm with the residual's addition, one row of d numbers at a time:
+ *   s = x + residual,  y = s / sqrt(mean(s^2) + eps) * weight,
+ * from the unrounded fp32 sum s.  total_dev (nullable) receives s rounded to `dtype`: the residual stream that goes on, and
+ * what the backward pass reads.  residual_dev is nullable (s = x).  y_dtype == dtype: y rounded.  y_dtype == PBKD_E4M3: y in
+ * 8 bits (OCP e4m3) with a scale for each row, scale = max(max|y|, 2^-100) / 448 in scale_dev[rows], code = y / scale to
+ * nearest; a NaN keeps its place and does not count for the scale (an infinity in s makes its own place NaN, the others 0;
+ * so do numbers whose squares' sum passes fp32's range, about 1e19, without the NaN).
+ * total_dev and y_dev may be x_dev or residual_dev (not the same one; y_dev with the same type and stride only).
+ * rows >= 0, 1 <= d <= 16384 (PBKD_EUNSUPPORTED beyond), eps >= 0. */
+typedef struct {
+  long long rows;
+  int d, dtype, y_dtype;
+  float eps;
+  const void *x_dev, *residual_dev;
+  const float *weight_dev; /* [d] */
+  void *total_dev, *y_dev;
+  float *scale_dev;        /* [rows], PBKD_E4M3 only */
+  long long x_stride, residual_stride, total_stride, y_stride; /* elements between rows */
+} pbkd_rmsnorm_desc;
+pbkd_status pbkd_rmsnorm_forward(const pbkd_rmsnorm_desc *desc, void *hip_stream);
+
+/* Its backward pass, at the sum as stored: with s = total, r = 1/sqrt(mean(s^2)+eps), g = dy * weight,
+ *   dx = r * (g - s r * mean(g s r)) + dtotal,   dweight = sum over rows of dy s r   (overwritten, fp32).
+ * dtotal_dev (nullable): the gradient that arrives at the residual stream.  dx is the gradient of x and of the residual alike;
+ * dx_dev may be dy_dev or dtotal_dev (same stride).  workspace: pbkd_rmsnorm_workspace_bytes(rows, d). */
+typedef struct {
+  long long rows;
+  int d, dtype;
+  float eps;
+  const void *total_dev, *dy_dev, *dtotal_dev;
+  const float *weight_dev;
+  void *dx_dev;
+  float *dweight_dev;
+  long long total_stride, dy_stride, dtotal_stride, dx_stride;
+  void *workspace_dev;
+  size_t workspace_bytes;
+} pbkd_rmsnorm_grad_desc;
+size_t pbkd_rmsnorm_workspace_bytes(long long rows, int d); /* 0 for sizes the calls refuse */
+pbkd_status pbkd_rmsnorm_backward(const pbkd_rmsnorm_grad_desc *desc, void *hip_stream);
+
+/* Gated linear recurrence over the tokens of each sequence, channel by channel:
+ *   a_t = sigmoid(gate_t + bias),  h_t = a_t h_{t-1} + (1 - a_t) u_t,  y_t = h_t * silu(out_gate_t),
+ * with 1 - a_t formed as sigmoid(-(gate_t + bias)), h_{-1} = state (nullable: 0), no out_gate: y_t = h_t, no bias: 0.
+ * Activations are [batch, len, channels] with a batch and a token stride each.  lengths_dev (nullable) [batch]: sequence b
+ * has lengths[b] tokens (values outside 0..len count as 0 and len); what lies behind them has no influence, whatever it
+ * holds, y and the gradients are 0 there, and the state stays what it was at the last token.  state_out_dev (nullable)
+ * [batch, channels]: the last state; it may be state_dev.  saved_dev (nullable): what the backward pass needs,
+ * pbkd_recurrence_saved_bytes(); workspace: pbkd_recurrence_workspace_bytes(), the same for both directions.
+ * batch, len >= 0, channels >= 1; PBKD_EUNSUPPORTED from 2^31 tokens or batch * channels on, or batch * ceil(channels / 64)
+ * above 2^22. */
+typedef struct {
+  int batch, channels;
+  long long len;
+  int dtype;
+  const void *u_dev, *gate_dev, *out_gate_dev;
+  const float *bias_dev;    /* [channels] */
+  const int *lengths_dev;   /* [batch] */
+  const float *state_dev;   /* [batch, channels], contiguous */
+  float *state_out_dev;
+  void *y_dev;
+  long long u_batch_stride, u_stride, gate_batch_stride, gate_stride, out_gate_batch_stride, out_gate_stride, y_batch_stride, y_stride;
+  void *saved_dev;
+  size_t saved_bytes;
+  void *workspace_dev;
+  size_t workspace_bytes;
+} pbkd_recurrence_desc;
+size_t pbkd_recurrence_saved_bytes(int batch, long long len, int channels);
+size_t pbkd_recurrence_workspace_bytes(int batch, long long len, int channels);
+pbkd_status pbkd_recurrence_forward(const pbkd_recurrence_desc *desc, void *hip_stream);
+
+/* The recurrence for one token of each sequence, when text is produced token by token: `len`, saved_dev and workspace_dev of the
+ * descriptor are not used, state_dev and state_out_dev are both needed (usually the same tensor: the state is then updated in
+ * place), lengths_dev marks the rows that are idle (0: state kept, y = 0). */
+pbkd_status pbkd_recurrence_step(const pbkd_recurrence_desc *desc, void *hip_stream);
+
+/* Gradients of the recurrence from dy (and dstate_out, nullable, the gradient that arrives at the last state), from the inputs
+ * and what the forward pass saved of them: du, dgate, dout_gate (all of [batch, len, channels], strided), dbias (nullable) and
+ * dstate (nullable) in fp32, all overwritten.  h is formed again from the saved states.  du, dgate and dout_gate may be u, gate and out_gate
+ * (same strides), du may be dy. */
+typedef struct {
+  int batch, channels;
+  long long len;
+  int dtype;
+  const void *u_dev, *gate_dev, *out_gate_dev, *dy_dev;
+  const float *bias_dev;
+  const int *lengths_dev;
+  const float *dstate_out_dev;
+  void *du_dev, *dgate_dev, *dout_gate_dev;
+  float *dbias_dev, *dstate_dev;
+  long long u_batch_stride, u_stride, gate_batch_stride, gate_stride, out_gate_batch_stride, out_gate_stride, dy_batch_stride, dy_stride;
+  long long du_batch_stride, du_stride, dgate_batch_stride, dgate_stride, dout_gate_batch_stride, dout_gate_stride;
+  const void *saved_dev;
+  size_t saved_bytes;
+  void *workspace_dev;
+  size_t workspace_bytes;
+} pbkd_recurrence_grad_desc;
+pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *desc, void *hip_stream);
+
+/* One AdamW step over many tensors at once, in place.  Per element, g = grad * grad_scale:
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
+ * state_bits 32: m_dev, v_dev are fp32 [n].  state_bits 8: m_dev holds m and v_dev holds sqrt(v) as e4m3 codes [n] with an fp32
+ * scale for each 256 consecutive elements (m_scale_dev, v_scale_dev [ceil(n/256)]), scale = max(largest magnitude, 2^-100) / 448.
+ * m is rounded to nearest; sqrt(v) to one of its two neighbours at random, by their distances (to nearest, the small changes of
+ * a beta2 near 1 would be lost in three bits of mantissa), and never from above zero to zero.  New states start as zeros
+ * (codes and scales).  param_dtype PBKD_F32 or PBKD_BF16; a bf16 parameter is rounded at random too.  The random numbers are a
+ * hash of `seed` and the element's number, first + its index in the tensor (modulo 2^32): the same call gives the same
+ * bits.  copy_dev (nullable, with PBKD_F32 parameters): receives the new parameters in bf16, to nearest.
+ * grad_dtype: any of the three.  NaN and infinite gradients enter the states as the formulas say. */
+typedef struct {
+  long long n;
+  long long first;
+  int param_dtype, grad_dtype;
+  float weight_decay;
+  void *param_dev;
+  const void *grad_dev;
+  void *m_dev, *v_dev;
+  float *m_scale_dev, *v_scale_dev;
+  void *copy_dev;
+} pbkd_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, grad_scale;
+  long long step; /* 1 for the first */
+  int state_bits;
+  unsigned seed;
+} pbkd_adamw_args;
+pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *tensors_host, const pbkd_adamw_args *args, void *hip_stream);
 
 /* Message for the last error on the calling thread ("" if none). */
 const char *pbkd_last_error(void);

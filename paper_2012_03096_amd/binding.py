@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -26,6 +27,8 @@ EXPORTS = [
     "pbkd_schedule_blocks", "pbkd_distill_step_all", "pbkd_run_tasks_work_stealing", "pbkd_network_forward", "pbkd_feature_mse", "pbkd_feature_mse_noalloc", "pbkd_select_blocks", "pbkd_block_flops", "pbkd_arch_flops", "pbkd_arch_conv_kernel",
     "pbkd_block_get_tensor", "pbkd_block_set_tensor", "pbkd_last_error",
     "pbkd_kernel_kinds", "pbkd_kernel_kind_name", "pbkd_block_profile_enable", "pbkd_block_profile_read",
+    "pbkd_rmsnorm_forward", "pbkd_rmsnorm_backward", "pbkd_rmsnorm_workspace_bytes", "pbkd_recurrence_forward", "pbkd_recurrence_backward",
+    "pbkd_recurrence_step", "pbkd_recurrence_saved_bytes", "pbkd_recurrence_workspace_bytes", "pbkd_adamw_step",
 ]
 
 
@@ -128,6 +131,14 @@ def lib():
         L.pbkd_block_profile_enable.restype = ctypes.c_int
         L.pbkd_block_profile_read.argtypes = [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_double), ip]
         L.pbkd_block_profile_read.restype = ctypes.c_int
+        for f in (L.pbkd_rmsnorm_forward, L.pbkd_rmsnorm_backward, L.pbkd_recurrence_forward, L.pbkd_recurrence_backward, L.pbkd_recurrence_step):
+            f.argtypes, f.restype = [vp, vp], ctypes.c_int
+        L.pbkd_rmsnorm_workspace_bytes.argtypes = [ctypes.c_longlong, ctypes.c_int]
+        L.pbkd_rmsnorm_workspace_bytes.restype = ctypes.c_size_t
+        for f in (L.pbkd_recurrence_saved_bytes, L.pbkd_recurrence_workspace_bytes):
+            f.argtypes, f.restype = [ctypes.c_int, ctypes.c_longlong, ctypes.c_int], ctypes.c_size_t
+        L.pbkd_adamw_step.argtypes = [ctypes.c_int, vp, vp, vp]
+        L.pbkd_adamw_step.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -385,3 +396,261 @@ def feature_mse_noalloc(a, b, stream=None, n: Optional[int] = None) -> float:
     _check(lib().pbkd_feature_mse_noalloc(ctypes.c_void_p(a.data_ptr()), ctypes.c_void_p(b.data_ptr()),
                                           a.numel() if n is None else n, ctypes.byref(out), Block._sptr(stream)))
     return out.value
+
+
+# ------------------------------------------------------------------------------------------------ sequence operators
+# Root-mean-square norm, gated recurrence and AdamW (include/pbkd.h has the formulas).  All tensors are torch tensors on
+# the current GPU, outputs too: nothing is allocated by a call.  A descriptor is packed with struct (native alignment, the C struct's
+# field order): a call of a few microseconds on the GPU should not wait for a ctypes structure's.
+F32, BF16, F16, E4M3 = range(4)
+_RMSNORM = struct.Struct("@q3if6P4q")
+_RMSNORM_GRAD = struct.Struct("@q2if6P4qPN")
+_RECURRENCE = struct.Struct("@2iqi8P8qPNPN")
+_RECURRENCE_GRAD = struct.Struct("@2iqi12P14qPNPN")
+_ADAMW_ARGS = struct.Struct("@5dqiI")
+_ADAMW_TENSOR = np.dtype([("n", "i8"), ("first", "i8"), ("param_dtype", "i4"), ("grad_dtype", "i4"), ("weight_decay", "f4"), ("param", "u8"), ("grad", "u8"),
+                          ("m", "u8"), ("v", "u8"), ("m_scale", "u8"), ("v_scale", "u8"), ("copy", "u8")], align=True)
+_DTYPES = None
+
+
+def _dtypes():
+    """torch's types by the library's numbers."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    return _DTYPES
+
+
+def _code(t, name: str) -> int:
+    c = (_DTYPES or _dtypes()).get(t.dtype)
+    if c is None:
+        raise PbkdError(EINVAL, f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return c
+
+
+def _stream(stream) -> int:
+    import torch
+    return stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _gpu(t, name: str) -> int:
+    """Index of the GPU that t lies on, which must be the current one (the kernels are launched there)."""
+    import torch
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise PbkdError(EINVAL, f"{name} must lie on the current GPU, not on {t.device}")
+    return dev
+
+
+def _same(t, like, dev: int, name: str) -> int:
+    """Address of t, which has like's shape and type and lies on GPU dev."""
+    if t.dtype != like.dtype or t.shape != like.shape or t.get_device() != dev:
+        raise PbkdError(ESHAPE, f"{name} must be a {like.dtype} tensor of {tuple(like.shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _dense(t, shape, dtype, dev: int, name: str) -> int:
+    """Address of t, a contiguous tensor of this shape and type on GPU dev; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise PbkdError(ESHAPE, f"{name} must be a contiguous {dtype} tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _bytes(t, dev: int, name: str):
+    """(address, bytes) of a workspace."""
+    if t is None:
+        return 0, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        raise PbkdError(EINVAL, f"{name} must be a contiguous tensor on the same GPU")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _row_stride(t, d: int, name: str) -> int:
+    """Elements between the rows of t, whose last dimension are the rows: two dimensions with any stride, or more that are contiguous."""
+    if t.dim() == 2 and (d == 1 or t.stride(1) == 1):
+        return t.stride(0)
+    if t.is_contiguous():
+        return d
+    raise PbkdError(EINVAL, f"{name} must be contiguous, or have two dimensions with contiguous rows")
+
+
+def rmsnorm_workspace_bytes(rows: int, d: int) -> int:
+    return lib().pbkd_rmsnorm_workspace_bytes(rows, d)
+
+
+def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: float = 1e-6, stream=None) -> None:
+    """pbkd_rmsnorm_forward: y <- norm(x + residual) * weight over the last dimension, total <- x + residual.
+    y: like x, or float8_e4m3fn with scale [rows] float32."""
+    import torch
+    L, code, dev, d = _lib or lib(), _code(x, "x"), _gpu(x, "x"), x.shape[-1] if x.dim() else 0
+    if d == 0:
+        raise PbkdError(ESHAPE, "x has no elements in a row")
+    rows = x.numel() // d
+    eight = y.dtype == torch.float8_e4m3fn
+    if eight and (y.shape != x.shape or y.get_device() != dev):
+        raise PbkdError(ESHAPE, f"y must have x's shape {tuple(x.shape)} and lie on its GPU")
+    if scale is not None and not eight:
+        raise PbkdError(EINVAL, "a scale goes with a float8_e4m3fn y only")
+    _check(L.pbkd_rmsnorm_forward(_RMSNORM.pack(
+        rows, d, code, E4M3 if eight else code, eps, x.data_ptr(), 0 if residual is None else _same(residual, x, dev, "residual"),
+        _dense(weight, (d,), torch.float32, dev, "weight"), 0 if total is None else _same(total, x, dev, "total"),
+        y.data_ptr() if eight else _same(y, x, dev, "y"), _dense(scale, (rows,), torch.float32, dev, "scale"), _row_stride(x, d, "x"),
+        0 if residual is None else _row_stride(residual, d, "residual"), 0 if total is None else _row_stride(total, d, "total"), _row_stride(y, d, "y")),
+        _stream(stream)))
+
+
+def rmsnorm_backward(total, weight, dy, dx, dweight, workspace, dtotal=None, eps: float = 1e-6, stream=None) -> None:
+    """pbkd_rmsnorm_backward: dx and dweight from the sum as stored by the forward pass, dy and (optionally) the gradient that
+    arrives at the sum.  workspace: a tensor of rmsnorm_workspace_bytes(rows, d) bytes."""
+    import torch
+    L, code, dev, d = _lib or lib(), _code(total, "total"), _gpu(total, "total"), total.shape[-1] if total.dim() else 0
+    if d == 0:
+        raise PbkdError(ESHAPE, "total has no elements in a row")
+    wp, wn = _bytes(workspace, dev, "workspace")
+    _check(L.pbkd_rmsnorm_backward(_RMSNORM_GRAD.pack(
+        total.numel() // d, d, code, eps, total.data_ptr(), _same(dy, total, dev, "dy"), 0 if dtotal is None else _same(dtotal, total, dev, "dtotal"),
+        _dense(weight, (d,), torch.float32, dev, "weight"), _same(dx, total, dev, "dx"), _dense(dweight, (d,), torch.float32, dev, "dweight"),
+        _row_stride(total, d, "total"), _row_stride(dy, d, "dy"), 0 if dtotal is None else _row_stride(dtotal, d, "dtotal"), _row_stride(dx, d, "dx"), wp, wn),
+        _stream(stream)))
+
+
+def recurrence_saved_bytes(batch: int, length: int, channels: int) -> int:
+    return lib().pbkd_recurrence_saved_bytes(batch, length, channels)
+
+
+def recurrence_workspace_bytes(batch: int, length: int, channels: int) -> int:
+    return lib().pbkd_recurrence_workspace_bytes(batch, length, channels)
+
+
+def _tokens(t, name: str):
+    """(batch stride, token stride) of t [batch, len, channels]."""
+    s = t.stride()
+    if s[2] != 1 and t.shape[2] > 1:
+        raise PbkdError(EINVAL, f"{name}'s channels must be contiguous")
+    return s[0], s[1]
+
+
+def _sequence_shape(u):
+    if u.dim() != 3 or u.shape[2] == 0:
+        raise PbkdError(ESHAPE, f"u must be [batch, len, channels], not {tuple(u.shape)}")
+    return u.shape
+
+
+def recurrence_forward(u, gate, y, out_gate=None, bias=None, lengths=None, state=None, state_out=None, saved=None, workspace=None, stream=None) -> None:
+    """pbkd_recurrence_forward on [batch, len, channels] tensors: y, and the last state in state_out.  saved: a tensor of
+    recurrence_saved_bytes() for the backward pass; workspace: one of recurrence_workspace_bytes()."""
+    import torch
+    L, code, dev, (b, t, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), _sequence_shape(u)
+    f32 = torch.float32
+    sp, sn = _bytes(saved, dev, "saved")
+    wp, wn = _bytes(workspace, dev, "workspace")
+    _check(L.pbkd_recurrence_forward(_RECURRENCE.pack(
+        b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), torch.int32, dev, "lengths"), _dense(state, (b, d), f32, dev, "state"),
+        _dense(state_out, (b, d), f32, dev, "state_out"), _same(y, u, dev, "y"), *_tokens(u, "u"), *_tokens(gate, "gate"),
+        *((0, 0) if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(y, "y"), sp, sn, wp, wn), _stream(stream)))
+
+
+def recurrence_backward(u, gate, dy, saved, du, dgate, out_gate=None, dout_gate=None, bias=None, dbias=None, lengths=None, dstate_out=None, dstate=None,
+                        workspace=None, stream=None) -> None:
+    """pbkd_recurrence_backward: the gradients of recurrence_forward's inputs from dy and what it saved."""
+    import torch
+    L, code, dev, (b, t, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), _sequence_shape(u)
+    f32 = torch.float32
+    sp, sn = _bytes(saved, dev, "saved")
+    wp, wn = _bytes(workspace, dev, "workspace")
+    none = (0, 0)
+    _check(L.pbkd_recurrence_backward(_RECURRENCE_GRAD.pack(
+        b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"), _same(dy, u, dev, "dy"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), torch.int32, dev, "lengths"), _dense(dstate_out, (b, d), f32, dev, "dstate_out"),
+        _same(du, u, dev, "du"), _same(dgate, u, dev, "dgate"), 0 if dout_gate is None else _same(dout_gate, u, dev, "dout_gate"),
+        _dense(dbias, (d,), f32, dev, "dbias"), _dense(dstate, (b, d), f32, dev, "dstate"), *_tokens(u, "u"), *_tokens(gate, "gate"),
+        *(none if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(dy, "dy"), *_tokens(du, "du"), *_tokens(dgate, "dgate"),
+        *(none if dout_gate is None else _tokens(dout_gate, "dout_gate")), sp, sn, wp, wn), _stream(stream)))
+
+
+def recurrence_step(u, gate, state, y, out_gate=None, bias=None, active=None, state_out=None, stream=None) -> None:
+    """pbkd_recurrence_step: one token of each sequence, [batch, channels] rows with any stride; state [batch, channels] float32 is
+    updated in place (or goes to state_out).  active: int32 [batch], 0 for idle rows."""
+    import torch
+    if u.dim() != 2 or u.shape[1] == 0:
+        raise PbkdError(ESHAPE, f"u must be [batch, channels], not {tuple(u.shape)}")
+    L, code, dev, (b, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), u.shape
+    f32, sp = torch.float32, _dense(state, (b, d), torch.float32, dev, "state")
+    _check(L.pbkd_recurrence_step(_RECURRENCE.pack(
+        b, d, 1, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(active, (b,), torch.int32, dev, "active"), sp, sp if state_out is None else _dense(state_out, (b, d), f32, dev, "state_out"),
+        _same(y, u, dev, "y"), _row_stride(u, d, "u"), 0, _row_stride(gate, d, "gate"), 0, 0 if out_gate is None else _row_stride(out_gate, d, "out_gate"), 0,
+        _row_stride(y, d, "y"), 0, 0, 0, 0, 0), _stream(stream)))
+
+
+class AdamW:
+    """pbkd_adamw_step over a list of parameters (float32 or bfloat16, contiguous, updated in place), states in 32 or 8 bits.
+
+    states: per parameter (m, v), or (m, v, m_scale, v_scale) for 8 bits, flat tensors as the header describes them; None: zeros,
+    allocated here (the constructor then waits for its stream once, so that any stream may step).  copies: bfloat16 tensors
+    that receive the new parameters.  weight_decay: one number, or one for each parameter.  steps: how many were made already."""
+
+    def __init__(self, params, state_bits: int = 32, states=None, copies=None, weight_decay=0.0, betas=(0.9, 0.999), eps: float = 1e-8, steps: int = 0):
+        import torch
+        if state_bits not in (32, 8):
+            raise PbkdError(EINVAL, "state_bits must be 32 or 8")
+        self.params, self.copies, self.state_bits, self.betas, self.eps, self.steps = list(params), copies, state_bits, betas, eps, steps
+        n = len(self.params)
+        decays = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        for name, given in (("states", states), ("copies", copies), ("weight_decay", decays)):
+            if given is not None and len(given) != n:
+                raise PbkdError(ESHAPE, f"{len(given)} {name} for {n} parameters")
+        self._dev = _gpu(self.params[0], "a parameter") if n else -1
+        self._table = t = np.zeros(n, _ADAMW_TENSOR)
+        kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
+        sizes, rows, made = [p.numel() for p in self.params], [], []
+        first = 0
+        for i, p in enumerate(self.params):
+            code = _code(p, f"parameter {i}")
+            if code == F16:
+                raise PbkdError(EINVAL, f"parameter {i} must be float32 or bfloat16")
+            address = _dense(p, p.shape, p.dtype, self._dev, f"parameter {i}")
+            blocks = -(-sizes[i] // 256)
+            lens = (sizes[i], sizes[i], blocks, blocks)[:len(kind)]
+            if states is None:
+                made.append(tuple(torch.zeros(k, dtype=torch.uint8 if y == torch.float8_e4m3fn else y, device=p.device).view(y) for k, y in zip(lens, kind)))
+            s = made[i] if states is None else states[i]
+            if len(s) != len(kind):
+                raise PbkdError(ESHAPE, f"parameter {i}: {len(s)} state tensors, {len(kind)} are needed")
+            at = [_dense(x, (k,), y, self._dev, f"state of parameter {i}") for x, k, y in zip(s, lens, kind)] + [0, 0]
+            cp = _dense(copies[i], p.shape, torch.bfloat16, self._dev, f"copy of parameter {i}") if copies is not None else 0
+            rows.append((sizes[i], first, code, F32, decays[i], address, 0, *at[:4], cp))
+            first += blocks * 256
+        if n:
+            t[:] = rows
+        self.states = made if states is None else list(states)
+        self._sizes, self._address = sizes, t.ctypes.data
+        if states is None and n:
+            torch.cuda.current_stream().synchronize()
+
+    def step(self, grads, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, stream=None) -> None:
+        """One step with these gradients (one for each parameter, contiguous; None: the parameter and its states stay as they are).
+        seed: of the random roundings; None: the number of the step."""
+        import torch
+        L, dev, t = _lib or lib(), self._dev, self._table
+        if len(grads) != len(self._sizes):
+            raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(self._sizes)} parameters")
+        if dev >= 0 and dev != torch.cuda.current_device():
+            raise PbkdError(EINVAL, "the parameters must lie on the current GPU")
+        codes, sizes, at = [], [], []
+        for g, n in zip(grads, self._sizes):
+            if g is None:
+                codes.append(F32), sizes.append(0), at.append(0)
+                continue
+            if g.numel() != n or g.get_device() != dev or not g.is_contiguous():
+                raise PbkdError(ESHAPE, f"a gradient must be contiguous, with its parameter's {n} elements, on its GPU")
+            codes.append(_code(g, "a gradient")), sizes.append(n), at.append(g.data_ptr())
+        t["n"], t["grad_dtype"], t["grad"] = sizes, codes, at
+        number = self.steps + 1
+        _check(L.pbkd_adamw_step(len(sizes), self._address, _ADAMW_ARGS.pack(lr, *self.betas, self.eps, grad_scale, number, self.state_bits,
+                                                                             (number if seed is None else seed) & 0xFFFFFFFF), _stream(stream)))
+        self.steps = number

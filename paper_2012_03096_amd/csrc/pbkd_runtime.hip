@@ -40,6 +40,21 @@ pbkd_status fail(pbkd_status st, const char *fmt, ...) {
   return st;
 }
 
+}  // namespace
+
+namespace pbkd {
+pbkd_status set_error(pbkd_status status, const char *fmt, ...) {   // for the entry points in other files
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(status, "%s", buf);
+}
+}  // namespace pbkd
+
+namespace {
+
 #define HIPCHK(expr)                                                                      \
   do {                                                                                    \
     hipError_t e_ = (expr);                                                               \

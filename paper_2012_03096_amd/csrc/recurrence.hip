@@ -1,0 +1,533 @@
+// Gated linear recurrence over time, channel by channel, forward, backward and for single tokens:
+//
+//   x = gate + bias,  a = 1/(1+e^-x),  z = 1/(1+e^x) = 1 - a,  h_t = a_t h_{t-1} + z_t u_t,  y_t = h_t silu(o_t)
+//
+// A step is the affine map h -> a h + b (b = z u), maps compose as (A1,B1) then (A2,B2) = (A2 A1, A2 B1 + B2), so a
+// range of tokens is one pair (A, B) a channel and time can be cut into pieces.  Backward, with c_t = dy_t silu(o_t):
+//
+//   dh_t = c_t + e_t,  e_{t-1} = a_t dh_t   (the same composition from the last token on),
+//   du = z dh, dgate = dh (h_{t-1} - u) a z, do = dy h silu'(o)
+//
+// A tile is kSlice channels by a number of tokens: a thread holds L consecutive tokens of four channels, 16 threads
+// next to each other a row of kSlice channels, the 16 groups of them follow each other in time.  Each thread folds its tokens,
+// the groups' pairs are scanned over the wave's lanes and the four waves through LDS, and the tokens are gone through
+// again from the registers: each tensor is read once.
+#include "seq_common.h"
+
+namespace pbkd {
+namespace {
+
+constexpr int kSlice = 64;          // channels of a tile: 128 bytes of a 16-bit type
+constexpr int kFwdL = 8;            // tokens of a thread, forward: a tile has 16 times as many
+constexpr int kBwdL = 4;            // backward: more is held per token
+constexpr int kSaved = 16 * kBwdL;  // the forward pass saves the state in front of every backward tile
+
+struct FwdArgs {
+  const void *u, *g, *o;
+  const float *bias;
+  const int *lengths;
+  const float *h0;
+  float *hT;
+  void *y;
+  float *saved;
+  long long len, ub, us, gb, gs, ob, os, yb, ys;
+  int batch, D, slices;
+};
+
+struct BwdArgs {
+  const void *u, *g, *o, *dy;
+  const float *bias;
+  const int *lengths;
+  const float *saved, *dhT;
+  void *du, *dg, *dou;
+  float *dbias_partial, *dh0;
+  long long len, ub, us, gb, gs, ob, os, yb, ys, dub, dus, dgb, dgs, dob, dos;
+  int batch, D, slices;
+};
+
+// sigmoid(x) and sigmoid(-x), each to a few units of its own last place: both from e = exp(-|x|)
+__device__ __forceinline__ void sigmoids(float x, float &a, float &z) {
+  const float e = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
+  a = x >= 0.f ? r : s;
+  z = x >= 0.f ? s : r;
+  if (x != x) a = z = x;
+}
+
+// The four channels of a lane.  Where a row's last lanes have fewer than four (only if D is no multiple of 4) they are taken
+// one by one; lanes and channels beyond the row read its last channels again, and nothing of them is written.
+struct Lane {
+  int c;        // first channel, moved into the row
+  int n;        // channels that exist: 4, or fewer
+  bool one;     // the workgroup's loads go channel by channel
+};
+__device__ __forceinline__ Lane lane_of(int slice, int D) {
+  Lane q;
+  const int c0 = slice * kSlice + (threadIdx.x & 15) * 4;
+  q.one = (D & 3) && slice * kSlice + kSlice > D;
+  q.n = D - c0 < 4 ? (D - c0 < 0 ? 0 : D - c0) : 4;
+  q.c = q.one ? (c0 < D ? c0 : D - 1) : (c0 < D ? c0 : D - 4);
+  return q;
+}
+template <typename T>
+__device__ __forceinline__ void load4(const T *p, const Lane &q, float (&v)[4]) {
+  if (!q.one) {
+    load_n<T, 4>(p, 4, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(p[i < q.n ? i : (q.n > 0 ? q.n - 1 : 0)]);
+  }
+}
+
+__device__ __forceinline__ int length_of(const int *lengths, int b, long long len) {
+  if (!lengths) return (int)len;
+  const long long n = lengths[b];
+  return (int)(n < 0 ? 0 : n > len ? len : n);
+}
+
+// (A, B) of each lane's tokens become those of all tokens from the wave's first (reverse: last) group to the lane's own;
+// (Ae, Be) those of the groups in front of the lane's own.
+template <bool REVERSE>
+__device__ __forceinline__ void wave_scan(float (&A)[4], float (&B)[4], float (&Ae)[4], float (&Be)[4]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 16; off < 64; off *= 2) {
+    const bool in = REVERSE ? lane + off < 64 : lane >= off;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float A1 = REVERSE ? __shfl_down(A[i], off, 64) : __shfl_up(A[i], off, 64);
+      const float B1 = REVERSE ? __shfl_down(B[i], off, 64) : __shfl_up(B[i], off, 64);
+      B[i] = in ? fmaf(A[i], B1, B[i]) : B[i];
+      A[i] = in ? A[i] * A1 : A[i];
+    }
+  }
+  const bool in = REVERSE ? lane < 48 : lane >= 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float A1 = REVERSE ? __shfl_down(A[i], 16, 64) : __shfl_up(A[i], 16, 64);
+    const float B1 = REVERSE ? __shfl_down(B[i], 16, 64) : __shfl_up(B[i], 16, 64);
+    Ae[i] = in ? A1 : 1.f, Be[i] = in ? B1 : 0.f;
+  }
+}
+
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
+  constexpr int L = kFwdL, TILE = 16 * L;
+  __shared__ float2 tot[4][kSlice];
+  __shared__ float hs[2][kSlice];
+  const int slice = blockIdx.x % P.slices, b = blockIdx.x / P.slices;
+  const Lane q = lane_of(slice, P.D);
+  const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int len = length_of(P.lengths, b, P.len);
+  const long long T_ = P.len, saves = (T_ + kSaved - 1) / kSaved;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f};
+  if (P.bias) load4(P.bias + q.c, q, bias);
+  if (grp == 0) {
+    float h[4] = {0.f, 0.f, 0.f, 0.f};
+    if (P.h0) load4(P.h0 + (long long)b * P.D + q.c, q, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hs[0][cl + i] = h[i];
+  }
+  const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
+  const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
+  T *y = static_cast<T *>(P.y) + b * P.yb + q.c;
+  int flip = 0;
+  for (long long t0 = 0; t0 < T_; t0 += TILE, flip ^= 1) {
+    const long long tk = t0 + grp * L;
+    float a[L][4], bb[L][4], A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const long long t = tk + i < T_ ? tk + i : T_ - 1;     // a token that is read for nothing is one of this sequence
+      float uv[4], gv[4];
+      load4(u + t * P.us, q, uv);
+      load4(g + t * P.gs, q, gv);
+      const bool live = tk + i < len;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float z;
+        sigmoids(gv[k] + bias[k], a[i][k], z);
+        bb[i][k] = live ? z * uv[k] : 0.f;
+        a[i][k] = live ? a[i][k] : 1.f;
+        B[k] = fmaf(a[i][k], B[k], bb[i][k]);
+        A[k] *= a[i][k];
+      }
+    }
+    wave_scan<false>(A, B, Ae, Be);
+    if (lane >= 48) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tot[wave][cl + k] = make_float2(A[k], B[k]);
+    }
+    __syncthreads();
+    float h[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[k] = hs[flip][cl + k];
+      for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k].x, h[k], tot[w][cl + k].y);
+      h[k] = fmaf(Ae[k], h[k], Be[k]);
+    }
+    if (P.saved && (grp * L) % kSaved == 0 && tk < T_) {
+      float *s = P.saved + (b * saves + tk / kSaved) * P.D + q.c;
+      store_n<float, 4>(s, q.n, h);
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float out[4], ov[4];
+      if (GATED) load4(o + (tk + i < T_ ? tk + i : T_ - 1) * P.os, q, ov);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        h[k] = fmaf(a[i][k], h[k], bb[i][k]);
+        out[k] = h[k];
+        if (GATED) {
+          float s, n;
+          sigmoids(ov[k], s, n);
+          out[k] *= ov[k] * s;
+        }
+        out[k] = tk + i < len ? out[k] : 0.f;
+      }
+      if (tk + i < T_) store_n<T, 4>(y + (tk + i) * P.ys, q.n, out);
+    }
+    if (grp == 15) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) hs[flip ^ 1][cl + k] = h[k];
+    }
+    __syncthreads();
+  }
+  if (P.hT && grp == 0) {
+    float h[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h[k] = hs[flip][cl + k];
+    store_n<float, 4>(P.hT + (long long)b * P.D + q.c, q.n, h);
+  }
+}
+
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void recurrence_bwd_kernel(BwdArgs P) {
+  constexpr int L = kBwdL, TILE = 16 * L;
+  __shared__ float tot[4][kSlice][3];       // a wave's A, forward B, reverse B
+  __shared__ float es[2][kSlice];
+  const int slice = blockIdx.x % P.slices, b = blockIdx.x / P.slices;
+  const Lane q = lane_of(slice, P.D);
+  const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int len = length_of(P.lengths, b, P.len);
+  const long long T_ = P.len, tiles = (T_ + TILE - 1) / TILE;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
+  if (P.bias) load4(P.bias + q.c, q, bias);
+  if (grp == 0) {
+    float e[4] = {0.f, 0.f, 0.f, 0.f};
+    if (P.dhT) load4(P.dhT + (long long)b * P.D + q.c, q, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) es[0][cl + i] = e[i];
+  }
+  const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
+  const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
+  const T *dy = static_cast<const T *>(P.dy) + b * P.yb + q.c;
+  int flip = 0;
+  for (long long tile = tiles - 1; tile >= 0; --tile, flip ^= 1) {
+    const long long tk = tile * TILE + grp * L;
+    float a[L][4], z[L][4], hb[L][4], uv[L][4], ov[L][4], yv[L][4];
+    float A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4], Ar[4], Br[4], Ax[4], Bx[4];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const long long t = tk + i < T_ ? tk + i : T_ - 1;
+      float gv[4];
+      load4(g + t * P.gs, q, gv);
+      load4(u + t * P.us, q, uv[i]);
+      if (GATED) load4(o + t * P.os, q, ov[i]);
+      load4(dy + t * P.ys, q, yv[i]);
+      const bool live = tk + i < len;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        sigmoids(gv[k] + bias[k], a[i][k], z[i][k]);
+        a[i][k] = live ? a[i][k] : 1.f, z[i][k] = live ? z[i][k] : 0.f;
+        uv[i][k] = live ? uv[i][k] : 0.f, yv[i][k] = live ? yv[i][k] : 0.f;
+        if (GATED) ov[i][k] = live ? ov[i][k] : 0.f;
+        B[k] = fmaf(a[i][k], B[k], z[i][k] * uv[i][k]);
+        A[k] *= a[i][k];
+      }
+    }
+    float silu[L][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) Ar[k] = A[k], Br[k] = 0.f;
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        silu[i][k] = 1.f;
+        if (GATED) {
+          float n;
+          sigmoids(ov[i][k], silu[i][k], n);    // the sigmoid for now
+        }
+        const float c = GATED ? yv[i][k] * (ov[i][k] * silu[i][k]) : yv[i][k];
+        Br[k] = a[i][k] * (c + Br[k]);
+      }
+    wave_scan<false>(A, B, Ae, Be);
+    wave_scan<true>(Ar, Br, Ax, Bx);
+    if (lane >= 48) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tot[wave][cl + k][0] = A[k], tot[wave][cl + k][1] = B[k];
+    }
+    if (lane < 16) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tot[wave][cl + k][2] = Br[k];
+    }
+    __syncthreads();
+    float h[4], e[4];
+    load4(P.saved + (b * tiles + tile) * P.D + q.c, q, h);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k][0], h[k], tot[w][cl + k][1]);
+      h[k] = fmaf(Ae[k], h[k], Be[k]);
+      e[k] = es[flip][cl + k];
+      for (int w = 3; w > wave; --w) e[k] = fmaf(tot[w][cl + k][0], e[k], tot[w][cl + k][2]);
+      e[k] = fmaf(Ax[k], e[k], Bx[k]);
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        hb[i][k] = h[k];
+        h[k] = fmaf(a[i][k], h[k], z[i][k] * uv[i][k]);
+      }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+      float du[4], dg[4], dou[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float s = silu[i][k], c = GATED ? yv[i][k] * (ov[i][k] * s) : yv[i][k];
+        const float dh = c + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
+        const bool live = tk + i < len;
+        du[k] = live ? z[i][k] * dh : 0.f;
+        dg[k] = live ? dh * (hb[i][k] - uv[i][k]) * (a[i][k] * z[i][k]) : 0.f;
+        if (GATED) dou[k] = live ? yv[i][k] * hi * (s * (1.f + ov[i][k] * (1.f - s))) : 0.f;
+        e[k] = a[i][k] * dh;
+        db[k] += dg[k];
+      }
+      if (tk + i < T_) {
+        store_n<T, 4>(static_cast<T *>(P.du) + b * P.dub + (tk + i) * P.dus + q.c, q.n, du);
+        store_n<T, 4>(static_cast<T *>(P.dg) + b * P.dgb + (tk + i) * P.dgs + q.c, q.n, dg);
+        if (GATED) store_n<T, 4>(static_cast<T *>(P.dou) + b * P.dob + (tk + i) * P.dos + q.c, q.n, dou);
+      }
+    }
+    if (grp == 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) es[flip ^ 1][cl + k] = e[k];
+    }
+    __syncthreads();
+  }
+  if (P.dh0 && grp == 0) {
+    float e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = es[flip][cl + k];
+    store_n<float, 4>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
+  }
+  if (P.dbias_partial) {
+    __shared__ float sum[16][kSlice];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[grp][cl + k] = db[k];
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+      for (int r = 1; r < 16; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) db[k] += sum[r][cl + k];
+      store_n<float, 4>(P.dbias_partial + (long long)b * P.D + q.c, q.n, db);
+    }
+  }
+}
+
+// One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
+template <typename T, bool GATED>
+__global__ __launch_bounds__(64) void recurrence_step_kernel(FwdArgs P) {
+  const int quads = (P.D + 3) / 4;
+  const long long id = (long long)blockIdx.x * 64 + threadIdx.x;
+  const int b = (int)(id / quads), c = (int)(id % quads) * 4, n = P.D - c < 4 ? P.D - c : 4;
+  if (b >= P.batch) return;
+  const int len = length_of(P.lengths, b, P.len);
+  const long long saves = (P.len + kSaved - 1) / kSaved;
+  float h[4] = {0.f, 0.f, 0.f, 0.f}, bias[4] = {0.f, 0.f, 0.f, 0.f};
+  if (P.h0) load_n<float, 4>(P.h0 + (long long)b * P.D + c, n, h);
+  if (P.bias) load_n<float, 4>(P.bias + c, n, bias);
+  for (long long t = 0; t < P.len; ++t) {
+    if (P.saved && t % kSaved == 0) store_n<float, 4>(P.saved + (b * saves + t / kSaved) * P.D + c, n, h);
+    float out[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t < len) {
+      float uv[4], gv[4], ov[4];
+      load_n<T, 4>(static_cast<const T *>(P.u) + b * P.ub + t * P.us + c, n, uv);
+      load_n<T, 4>(static_cast<const T *>(P.g) + b * P.gb + t * P.gs + c, n, gv);
+      if (GATED) load_n<T, 4>(static_cast<const T *>(P.o) + b * P.ob + t * P.os + c, n, ov);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float a, z;
+        sigmoids(gv[k] + bias[k], a, z);
+        h[k] = fmaf(a, h[k], z * uv[k]);
+        out[k] = h[k];
+        if (GATED) {
+          float s, m;
+          sigmoids(ov[k], s, m);
+          out[k] *= ov[k] * s;
+        }
+      }
+    }
+    store_n<T, 4>(static_cast<T *>(P.y) + b * P.yb + t * P.ys + c, n, out);
+  }
+  if (P.hT) store_n<float, 4>(P.hT + (long long)b * P.D + c, n, h);
+}
+
+// The states' gradient of sequences without tokens.
+__global__ __launch_bounds__(256) void copy_or_zero_kernel(const float *from, float *to, long long n) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) to[i] = from ? from[i] : 0.f;
+}
+
+template <typename T>
+hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
+  if (A.len <= 16) {
+    const unsigned blocks = (unsigned)cdiv64((long long)A.batch * ((A.D + 3) / 4), 64);
+    if (A.o) recurrence_step_kernel<T, true><<<blocks, 64, 0, st>>>(A);
+    else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
+  } else {
+    if (A.o) recurrence_fwd_kernel<T, true><<<A.batch * A.slices, 256, 0, st>>>(A);
+    else recurrence_fwd_kernel<T, false><<<A.batch * A.slices, 256, 0, st>>>(A);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
+  if (A.o) recurrence_bwd_kernel<T, true><<<A.batch * A.slices, 256, 0, st>>>(A);
+  else recurrence_bwd_kernel<T, false><<<A.batch * A.slices, 256, 0, st>>>(A);
+  return hipGetLastError();
+}
+
+inline bool off(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+
+inline bool sizes_ok(int batch, long long len, int channels) {
+  return batch >= 0 && len >= 0 && channels >= 1 && (long long)batch * channels <= 0x7fffffffLL && len <= 0x7fffffffLL &&
+         (long long)batch * cdiv(channels, kSlice) <= (1LL << 22);     // a launch's threads must stay below 2^32
+}
+
+pbkd_status check_sizes(int batch, long long len, int channels, int dtype) {
+  if (batch < 0 || len < 0 || channels < 1) return set_error(PBKD_ESHAPE, "recurrence: [%d, %lld, %d]", batch, len, channels);
+  if (!sizes_ok(batch, len, channels)) return set_error(PBKD_EUNSUPPORTED, "recurrence: [%d, %lld, %d] is too large", batch, len, channels);
+  if (dtype != PBKD_F32 && dtype != PBKD_BF16 && dtype != PBKD_F16) return set_error(PBKD_EINVAL, "recurrence: dtype %d", dtype);
+  return PBKD_OK;
+}
+
+// Whether an output's rows are apart from each other, sequences in front of tokens or tokens in front of sequences.
+inline bool apart(int batch, long long len, int D, long long bs, long long ts) {
+  if (bs < 0 || ts < 0) return false;
+  if (len > 1 && ts < D) return false;
+  if (batch > 1 && bs < D) return false;
+  if (batch > 1 && len > 1 && bs < (len - 1) * ts + D && ts < (batch - 1) * bs + D) return false;
+  return true;
+}
+
+pbkd_status forward(const pbkd_recurrence_desc *q, bool step, void *hip_stream) {
+  if (!q) return set_error(PBKD_EINVAL, "recurrence: null descriptor");
+  const long long len = step ? 1 : q->len;
+  if (const pbkd_status s = check_sizes(q->batch, len, q->channels, q->dtype)) return s;
+  if (step && (!q->state_dev || !q->state_out_dev)) return set_error(PBKD_EINVAL, "recurrence: a step needs the state and where it goes");
+  const int size = q->dtype == PBKD_F32 ? 4 : 2;
+  const bool any = q->batch > 0 && len > 0;
+  if (any && (!q->u_dev || !q->gate_dev || !q->y_dev)) return set_error(PBKD_EINVAL, "recurrence: null tensor");
+  if (off(q->u_dev, size) || off(q->gate_dev, size) || off(q->out_gate_dev, size) || off(q->y_dev, size) || off(q->bias_dev, 4) || off(q->lengths_dev, 4) ||
+      off(q->state_dev, 4) || off(q->state_out_dev, 4))
+    return set_error(PBKD_EINVAL, "recurrence: a tensor is not aligned to its elements");
+  if (q->u_stride < 0 || q->u_batch_stride < 0 || q->gate_stride < 0 || q->gate_batch_stride < 0 || q->out_gate_stride < 0 || q->out_gate_batch_stride < 0)
+    return set_error(PBKD_EINVAL, "recurrence: negative stride");
+  if (any && !apart(q->batch, len, q->channels, q->y_batch_stride, q->y_stride)) return set_error(PBKD_ESHAPE, "recurrence: rows of y overlap");
+  if (!step && q->saved_dev) {
+    if (off(q->saved_dev, 4)) return set_error(PBKD_EINVAL, "recurrence: a tensor is not aligned to its elements");
+    if (q->saved_bytes < pbkd_recurrence_saved_bytes(q->batch, len, q->channels))
+      return set_error(PBKD_ENOMEM, "recurrence: saved_dev of %zu bytes is smaller than the %zu needed", q->saved_bytes, pbkd_recurrence_saved_bytes(q->batch, len, q->channels));
+  }
+  if (!step) {
+    if (!q->workspace_dev || off(q->workspace_dev, 256)) return set_error(PBKD_ENOMEM, "recurrence: the workspace must be 256-byte aligned");
+    if (q->workspace_bytes < pbkd_recurrence_workspace_bytes(q->batch, len, q->channels))
+      return set_error(PBKD_ENOMEM, "recurrence: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes,
+                       pbkd_recurrence_workspace_bytes(q->batch, len, q->channels));
+  }
+  if (q->batch == 0) return PBKD_OK;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (len == 0) {
+    const long long n = (long long)q->batch * q->channels;
+    if (q->state_out_dev) copy_or_zero_kernel<<<(unsigned)cdiv64(n, 256), 256, 0, st>>>(q->state_dev, q->state_out_dev, n);
+    SEQ_HIPCHK(hipGetLastError());
+    return PBKD_OK;
+  }
+  FwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->bias_dev, q->lengths_dev, q->state_dev, q->state_out_dev, q->y_dev,
+            step ? nullptr : static_cast<float *>(q->saved_dev), len, q->u_batch_stride, q->u_stride, q->gate_batch_stride, q->gate_stride,
+            q->out_gate_batch_stride, q->out_gate_stride, q->y_batch_stride, q->y_stride, q->batch, q->channels, cdiv(q->channels, kSlice)};
+  switch (q->dtype) {
+    case PBKD_F32: SEQ_HIPCHK(launch_fwd<float>(A, st)); break;
+    case PBKD_BF16: SEQ_HIPCHK(launch_fwd<bf16>(A, st)); break;
+    default: SEQ_HIPCHK(launch_fwd<f16>(A, st)); break;
+  }
+  return PBKD_OK;
+}
+
+}  // namespace
+}  // namespace pbkd
+
+using namespace pbkd;
+
+extern "C" {
+
+size_t pbkd_recurrence_saved_bytes(int batch, long long len, int channels) {
+  if (!sizes_ok(batch, len, channels)) return 0;
+  return (size_t)batch * cdiv64(len, kSaved) * channels * sizeof(float) + 256;
+}
+
+size_t pbkd_recurrence_workspace_bytes(int batch, long long len, int channels) {
+  if (!sizes_ok(batch, len, channels)) return 0;
+  return ((size_t)batch * channels + colsum_scratch_floats(batch, channels)) * sizeof(float) + 256;
+}
+
+pbkd_status pbkd_recurrence_forward(const pbkd_recurrence_desc *desc, void *hip_stream) { return forward(desc, false, hip_stream); }
+
+pbkd_status pbkd_recurrence_step(const pbkd_recurrence_desc *desc, void *hip_stream) { return forward(desc, true, hip_stream); }
+
+pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *q, void *hip_stream) {
+  if (!q) return set_error(PBKD_EINVAL, "recurrence: null descriptor");
+  if (const pbkd_status s = check_sizes(q->batch, q->len, q->channels, q->dtype)) return s;
+  const int size = q->dtype == PBKD_F32 ? 4 : 2;
+  const bool any = q->batch > 0 && q->len > 0;
+  if (any && (!q->u_dev || !q->gate_dev || !q->dy_dev || !q->du_dev || !q->dgate_dev || !q->saved_dev)) return set_error(PBKD_EINVAL, "recurrence: null tensor");
+  if ((q->out_gate_dev != nullptr) != (q->dout_gate_dev != nullptr)) return set_error(PBKD_EINVAL, "recurrence: out_gate and dout_gate come together");
+  if (off(q->u_dev, size) || off(q->gate_dev, size) || off(q->out_gate_dev, size) || off(q->dy_dev, size) || off(q->du_dev, size) || off(q->dgate_dev, size) ||
+      off(q->dout_gate_dev, size) || off(q->bias_dev, 4) || off(q->lengths_dev, 4) || off(q->dstate_out_dev, 4) || off(q->dbias_dev, 4) || off(q->dstate_dev, 4))
+    return set_error(PBKD_EINVAL, "recurrence: a tensor is not aligned to its elements");
+  if (q->u_stride < 0 || q->u_batch_stride < 0 || q->gate_stride < 0 || q->gate_batch_stride < 0 || q->out_gate_stride < 0 || q->out_gate_batch_stride < 0 ||
+      q->dy_stride < 0 || q->dy_batch_stride < 0)
+    return set_error(PBKD_EINVAL, "recurrence: negative stride");
+  if (any && (!apart(q->batch, q->len, q->channels, q->du_batch_stride, q->du_stride) || !apart(q->batch, q->len, q->channels, q->dgate_batch_stride, q->dgate_stride) ||
+              (q->dout_gate_dev && !apart(q->batch, q->len, q->channels, q->dout_gate_batch_stride, q->dout_gate_stride))))
+    return set_error(PBKD_ESHAPE, "recurrence: rows of a gradient overlap");
+  if (any && (off(q->saved_dev, 4) || q->saved_bytes < pbkd_recurrence_saved_bytes(q->batch, q->len, q->channels)))
+    return set_error(PBKD_ENOMEM, "recurrence: saved_dev is misaligned or smaller than the %zu bytes needed", pbkd_recurrence_saved_bytes(q->batch, q->len, q->channels));
+  if (!q->workspace_dev || off(q->workspace_dev, 256)) return set_error(PBKD_ENOMEM, "recurrence: the workspace must be 256-byte aligned");
+  if (q->workspace_bytes < pbkd_recurrence_workspace_bytes(q->batch, q->len, q->channels))
+    return set_error(PBKD_ENOMEM, "recurrence: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes,
+                     pbkd_recurrence_workspace_bytes(q->batch, q->len, q->channels));
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  float *partial = static_cast<float *>(q->workspace_dev);
+  if (any) {
+    BwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->dy_dev, q->bias_dev, q->lengths_dev, static_cast<const float *>(q->saved_dev), q->dstate_out_dev,
+              q->du_dev, q->dgate_dev, q->dout_gate_dev, q->dbias_dev ? partial : nullptr, q->dstate_dev, q->len, q->u_batch_stride, q->u_stride,
+              q->gate_batch_stride, q->gate_stride, q->out_gate_batch_stride, q->out_gate_stride, q->dy_batch_stride, q->dy_stride,
+              q->du_batch_stride, q->du_stride, q->dgate_batch_stride, q->dgate_stride, q->dout_gate_batch_stride, q->dout_gate_stride,
+              q->batch, q->channels, cdiv(q->channels, kSlice)};
+    switch (q->dtype) {
+      case PBKD_F32: SEQ_HIPCHK(launch_bwd<float>(A, st)); break;
+      case PBKD_BF16: SEQ_HIPCHK(launch_bwd<bf16>(A, st)); break;
+      default: SEQ_HIPCHK(launch_bwd<f16>(A, st)); break;
+    }
+  } else if (q->batch > 0 && q->dstate_dev) {
+    const long long n = (long long)q->batch * q->channels;
+    copy_or_zero_kernel<<<(unsigned)cdiv64(n, 256), 256, 0, st>>>(q->dstate_out_dev, q->dstate_dev, n);
+    SEQ_HIPCHK(hipGetLastError());
+  }
+  if (q->dbias_dev) SEQ_HIPCHK(launch_colsum(partial, any ? q->batch : 0, q->channels, partial + (size_t)q->batch * q->channels, q->dbias_dev, st));
+  return PBKD_OK;
+}
+
+}  // extern "C"
