@@ -11,7 +11,7 @@
 // A tile is kSlice channels by a number of tokens: a thread holds L consecutive tokens of four channels, 16 threads
 // next to each other a row of kSlice channels, the 16 groups of them follow each other in time.  Each thread folds its tokens,
 // the groups' pairs are scanned over the wave's lanes and the four waves through LDS, and the tokens are gone through
-// again from the registers: each tensor is read once.
+// again from the registers: each tensor is read once.  Tiles of all times run at once and hand the state on (below).
 #include "seq_common.h"
 
 namespace pbkd {
@@ -30,8 +30,9 @@ struct FwdArgs {
   float *hT;
   void *y;
   float *saved;
+  unsigned long long *work;
   long long len, ub, us, gb, gs, ob, os, yb, ys;
-  int batch, D, slices;
+  int batch, D, slices, tiles;
 };
 
 struct BwdArgs {
@@ -41,8 +42,9 @@ struct BwdArgs {
   const float *saved, *dhT;
   void *du, *dg, *dou;
   float *dbias_partial, *dh0;
+  unsigned long long *work;
   long long len, ub, us, gb, gs, ob, os, yb, ys, dub, dus, dgb, dgs, dob, dos;
-  int batch, D, slices;
+  int batch, D, slices, tiles;
 };
 
 // sigmoid(x) and sigmoid(-x), each to a few units of its own last place: both from e = exp(-|x|)
@@ -109,227 +111,300 @@ __device__ __forceinline__ void wave_scan(float (&A)[4], float (&B)[4], float (&
   }
 }
 
+// How tiles that follow each other in time hand on the state.  The tiles of one sequence and slice are a chain, cut into
+// segments of kSeg.  Every tile publishes its own pair (A, B), which needs nothing of the tiles in front of it; it then folds
+// the pairs of its segment's earlier tiles, and the last tile of a segment also publishes the state behind it, so that only
+// one tile in kSeg waits for one before.  All folds have a fixed order: results do not depend on who was first.
+//
+// A tile's number comes from a counter, tiles in front of it in a chain have smaller numbers, and it waits for nothing but
+// those: they were taken by workgroups that run already, so every wait ends.
+//
+// A pair travels in one 64-bit word, written and read whole at the scope of the device (the eight dies' L2 caches do not see each
+// other's writes otherwise): 0 is "not there yet", B below, A with its sign bit set above (A, a product of sigmoids, has
+// none of its own).  The words are cleared by a kernel in front.
+constexpr int kSeg = 16;
+
+__device__ __forceinline__ void put_word(unsigned long long *p, float low, unsigned high) {
+  __hip_atomic_store(p, (unsigned long long)high << 32 | __builtin_bit_cast(unsigned, low), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long peek_word(const unsigned long long *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long await_word(const unsigned long long *p, unsigned long long v) {
+  while (v == 0) {
+    __builtin_amdgcn_s_sleep(1);
+    v = peek_word(p);
+  }
+  return v;
+}
+__device__ __forceinline__ unsigned pair_high(float A) { return (A == A ? __builtin_bit_cast(unsigned, A) : 0x7FC00000u) | 0x80000000u; }
+__device__ __forceinline__ float low_of(unsigned long long v) { return __builtin_bit_cast(float, (unsigned)v); }
+__device__ __forceinline__ float high_of(unsigned long long v) { return __builtin_bit_cast(float, (unsigned)(v >> 32) & 0x7FFFFFFFu); }
+
+struct Chain {
+  unsigned long long *pairs, *states;     // [tiles][kSlice], [segments][kSlice]
+};
+// work: the counter, then the pairs and the states of all chains
+inline __host__ __device__ long long chain_words(long long chains, long long tiles) {
+  return 32 + chains * (tiles + (tiles + kSeg - 1) / kSeg) * kSlice;
+}
+__device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, int chains, int tiles) {
+  const int segs = (tiles + kSeg - 1) / kSeg;
+  return {work + 32 + (long long)chain * tiles * kSlice, work + 32 + ((long long)chains * tiles + (long long)chain * segs) * kSlice};
+}
+
+// One thread in 256 for each channel and quarter of the segment: pre[w] the pair of up to four tiles in front of tile `pos`
+// (in the order of the chain), at[] the state in front of its segment.  Only the chain's first tile reads the state in
+// front of the chain (`first`), and its pair is the constant map to the state behind it: the last tile, which may write over the
+// initial state, thereby has every reader of it behind itself.
+__device__ __forceinline__ void look_back(const Chain &q, int pos, float first, float2 (*pre)[kSlice], float *at) {
+  const int ch = threadIdx.x & 63, w = threadIdx.x >> 6, seg = pos / kSeg, in = pos % kSeg;
+  const unsigned long long *p = q.pairs + ((long long)seg * kSeg + w * 4) * kSlice + ch;
+  const unsigned long long *s = q.states + (long long)(seg - 1) * kSlice + ch;
+  unsigned long long v[4], c = 1;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = w * 4 + j < in ? peek_word(p + j * kSlice) : 1;
+  if (w == 0 && seg > 0) c = peek_word(s);
+  float A = 1.f, B = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (w * 4 + j < in) {
+      v[j] = await_word(p + j * kSlice, v[j]);
+      const float A2 = high_of(v[j]);
+      B = fmaf(A2, B, low_of(v[j]));
+      A *= A2;
+    }
+  }
+  pre[w][ch] = make_float2(A, B);
+  if (w == 0) at[ch] = seg > 0 ? low_of(await_word(s, c)) : pos == 0 ? first : 0.f;
+}
+__device__ __forceinline__ void publish_pair(const Chain &q, int pos, float A, float B, float first) {
+  put_word(q.pairs + (long long)pos * kSlice + (threadIdx.x & 63), pos == 0 ? fmaf(A, first, B) : B, pair_high(pos == 0 ? 0.f : A));
+}
+
+__global__ __launch_bounds__(256) void clear_words_kernel(unsigned long long *p, long long n) {
+  typedef unsigned long long u2 __attribute__((ext_vector_type(2)));
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n / 2; i += (long long)gridDim.x * 256) reinterpret_cast<u2 *>(p)[i] = u2{0, 0};
+}
+
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
   constexpr int L = kFwdL, TILE = 16 * L;
-  __shared__ float2 tot[4][kSlice];
-  __shared__ float hs[2][kSlice];
-  const int slice = blockIdx.x % P.slices, b = blockIdx.x / P.slices;
+  __shared__ float2 tot[4][kSlice], pre[4][kSlice];
+  __shared__ float at[kSlice];
+  __shared__ unsigned number;
+  if (threadIdx.x == 0) number = (unsigned)atomicAdd(P.work, 1ull);
+  __syncthreads();
+  const int chains = P.batch * P.slices, tile = number / chains, chain = number % chains, slice = chain % P.slices, b = chain / P.slices;
+  const Chain links = chain_of(P.work, chain, chains, P.tiles);
   const Lane q = lane_of(slice, P.D);
   const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int len = length_of(P.lengths, b, P.len);
-  const long long T_ = P.len, saves = (T_ + kSaved - 1) / kSaved;
+  const long long T_ = P.len, tk = (long long)tile * TILE + grp * L;
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
   if (P.bias) load4(P.bias + q.c, q, bias);
-  if (grp == 0) {
-    float h[4] = {0.f, 0.f, 0.f, 0.f};
-    if (P.h0) load4(P.h0 + (long long)b * P.D + q.c, q, h);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) hs[0][cl + i] = h[i];
-  }
   const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
   const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
   T *y = static_cast<T *>(P.y) + b * P.yb + q.c;
-  int flip = 0;
-  for (long long t0 = 0; t0 < T_; t0 += TILE, flip ^= 1) {
-    const long long tk = t0 + grp * L;
-    float a[L][4], bb[L][4], A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4];
+  float a[L][4], bb[L][4], A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4];
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const long long t = tk + i < T_ ? tk + i : T_ - 1;     // a token that is read for nothing is one of this sequence
-      float uv[4], gv[4];
-      load4(u + t * P.us, q, uv);
-      load4(g + t * P.gs, q, gv);
-      const bool live = tk + i < len;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float z;
-        sigmoids(gv[k] + bias[k], a[i][k], z);
-        bb[i][k] = live ? z * uv[k] : 0.f;
-        a[i][k] = live ? a[i][k] : 1.f;
-        B[k] = fmaf(a[i][k], B[k], bb[i][k]);
-        A[k] *= a[i][k];
-      }
-    }
-    wave_scan<false>(A, B, Ae, Be);
-    if (lane >= 48) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tot[wave][cl + k] = make_float2(A[k], B[k]);
-    }
-    __syncthreads();
-    float h[4];
+  for (int i = 0; i < L; ++i) {
+    const long long t = tk + i < T_ ? tk + i : T_ - 1;     // a token that is read for nothing is one of this sequence
+    float uv[4], gv[4];
+    load4(u + t * P.us, q, uv);
+    load4(g + t * P.gs, q, gv);
+    const bool live = tk + i < len;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      h[k] = hs[flip][cl + k];
-      for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k].x, h[k], tot[w][cl + k].y);
-      h[k] = fmaf(Ae[k], h[k], Be[k]);
+      float z;
+      sigmoids(gv[k] + bias[k], a[i][k], z);
+      bb[i][k] = live ? z * uv[k] : 0.f;
+      a[i][k] = live ? a[i][k] : 1.f;
+      B[k] = fmaf(a[i][k], B[k], bb[i][k]);
+      A[k] *= a[i][k];
     }
-    if (P.saved && (grp * L) % kSaved == 0 && tk < T_) {
-      float *s = P.saved + (b * saves + tk / kSaved) * P.D + q.c;
-      store_n<float, 4>(s, q.n, h);
-    }
+  }
+  wave_scan<false>(A, B, Ae, Be);
+  if (lane >= 48) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float out[4], ov[4];
-      if (GATED) load4(o + (tk + i < T_ ? tk + i : T_ - 1) * P.os, q, ov);
+    for (int k = 0; k < 4; ++k) tot[wave][cl + k] = make_float2(A[k], B[k]);
+  }
+  __syncthreads();
+  const int ch = threadIdx.x & 63, c = slice * kSlice + ch;
+  float At = 1.f, Bt = 0.f;                                // the whole tile's pair, channel ch
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        h[k] = fmaf(a[i][k], h[k], bb[i][k]);
-        out[k] = h[k];
-        if (GATED) {
-          float s, n;
-          sigmoids(ov[k], s, n);
-          out[k] *= ov[k] * s;
-        }
-        out[k] = tk + i < len ? out[k] : 0.f;
+  for (int w = 0; w < 4; ++w) Bt = fmaf(tot[w][ch].x, Bt, tot[w][ch].y), At *= tot[w][ch].x;
+  const float first = wave == 0 && tile == 0 && P.h0 && c < P.D ? P.h0[(long long)b * P.D + c] : 0.f;
+  if (wave == 0 && tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
+  look_back(links, tile, first, pre, at);
+  __syncthreads();
+  if (wave == 0 && tile % kSeg == kSeg - 1 && tile + 1 < P.tiles) {
+    float h = at[ch];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) h = fmaf(pre[w][ch].x, h, pre[w][ch].y);
+    put_word(links.states + (long long)(tile / kSeg) * kSlice + ch, fmaf(At, h, Bt), 1u);
+  }
+  float h[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    h[k] = at[cl + k];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) h[k] = fmaf(pre[w][cl + k].x, h[k], pre[w][cl + k].y);
+    for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k].x, h[k], tot[w][cl + k].y);
+    h[k] = fmaf(Ae[k], h[k], Be[k]);
+  }
+  if (P.saved && (grp * L) % kSaved == 0 && tk < T_)
+    store_n<float, 4>(P.saved + (b * ((T_ + kSaved - 1) / kSaved) + tk / kSaved) * P.D + q.c, q.n, h);
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    float out[4], ov[4];
+    if (GATED) load4(o + (tk + i < T_ ? tk + i : T_ - 1) * P.os, q, ov);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[k] = fmaf(a[i][k], h[k], bb[i][k]);
+      out[k] = h[k];
+      if (GATED) {
+        float s, n;
+        sigmoids(ov[k], s, n);
+        out[k] *= ov[k] * s;
       }
-      if (tk + i < T_) store_n<T, 4>(y + (tk + i) * P.ys, q.n, out);
+      out[k] = tk + i < len ? out[k] : 0.f;
     }
-    if (grp == 15) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) hs[flip ^ 1][cl + k] = h[k];
-    }
-    __syncthreads();
+    if (tk + i < T_) store_n<T, 4>(y + (tk + i) * P.ys, q.n, out);
   }
-  if (P.hT && grp == 0) {
-    float h[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) h[k] = hs[flip][cl + k];
-    store_n<float, 4>(P.hT + (long long)b * P.D + q.c, q.n, h);
-  }
+  if (P.hT && tile + 1 == P.tiles && grp == 15) store_n<float, 4>(P.hT + (long long)b * P.D + q.c, q.n, h);
 }
 
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void recurrence_bwd_kernel(BwdArgs P) {
   constexpr int L = kBwdL, TILE = 16 * L;
   __shared__ float tot[4][kSlice][3];       // a wave's A, forward B, reverse B
-  __shared__ float es[2][kSlice];
-  const int slice = blockIdx.x % P.slices, b = blockIdx.x / P.slices;
+  __shared__ float2 pre[4][kSlice];
+  __shared__ float at[kSlice], sum[16][kSlice];
+  __shared__ unsigned number;
+  if (threadIdx.x == 0) number = (unsigned)atomicAdd(P.work, 1ull);
+  __syncthreads();
+  const int chains = P.batch * P.slices, pos = number / chains, tile = P.tiles - 1 - pos;      // the chain starts at the last tile
+  const int chain = number % chains, slice = chain % P.slices, b = chain / P.slices;
+  const Chain links = chain_of(P.work, chain, chains, P.tiles);
   const Lane q = lane_of(slice, P.D);
   const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int len = length_of(P.lengths, b, P.len);
-  const long long T_ = P.len, tiles = (T_ + TILE - 1) / TILE;
-  float bias[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
+  const long long T_ = P.len, tk = (long long)tile * TILE + grp * L;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f}, h[4];
   if (P.bias) load4(P.bias + q.c, q, bias);
-  if (grp == 0) {
-    float e[4] = {0.f, 0.f, 0.f, 0.f};
-    if (P.dhT) load4(P.dhT + (long long)b * P.D + q.c, q, e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) es[0][cl + i] = e[i];
-  }
+  load4(P.saved + ((long long)b * P.tiles + tile) * P.D + q.c, q, h);
   const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
   const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
   const T *dy = static_cast<const T *>(P.dy) + b * P.yb + q.c;
-  int flip = 0;
-  for (long long tile = tiles - 1; tile >= 0; --tile, flip ^= 1) {
-    const long long tk = tile * TILE + grp * L;
-    float a[L][4], z[L][4], hb[L][4], uv[L][4], ov[L][4], yv[L][4];
-    float A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4], Ar[4], Br[4], Ax[4], Bx[4];
+  float a[L][4], z[L][4], hb[L][4], uv[L][4], ov[L][4], yv[L][4], silu[L][4];
+  float A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4], Ar[4], Br[4], Ax[4], Bx[4];
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const long long t = tk + i < T_ ? tk + i : T_ - 1;
-      float gv[4];
-      load4(g + t * P.gs, q, gv);
-      load4(u + t * P.us, q, uv[i]);
-      if (GATED) load4(o + t * P.os, q, ov[i]);
-      load4(dy + t * P.ys, q, yv[i]);
-      const bool live = tk + i < len;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        sigmoids(gv[k] + bias[k], a[i][k], z[i][k]);
-        a[i][k] = live ? a[i][k] : 1.f, z[i][k] = live ? z[i][k] : 0.f;
-        uv[i][k] = live ? uv[i][k] : 0.f, yv[i][k] = live ? yv[i][k] : 0.f;
-        if (GATED) ov[i][k] = live ? ov[i][k] : 0.f;
-        B[k] = fmaf(a[i][k], B[k], z[i][k] * uv[i][k]);
-        A[k] *= a[i][k];
-      }
-    }
-    float silu[L][4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) Ar[k] = A[k], Br[k] = 0.f;
-#pragma unroll
-    for (int i = L - 1; i >= 0; --i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        silu[i][k] = 1.f;
-        if (GATED) {
-          float n;
-          sigmoids(ov[i][k], silu[i][k], n);    // the sigmoid for now
-        }
-        const float c = GATED ? yv[i][k] * (ov[i][k] * silu[i][k]) : yv[i][k];
-        Br[k] = a[i][k] * (c + Br[k]);
-      }
-    wave_scan<false>(A, B, Ae, Be);
-    wave_scan<true>(Ar, Br, Ax, Bx);
-    if (lane >= 48) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tot[wave][cl + k][0] = A[k], tot[wave][cl + k][1] = B[k];
-    }
-    if (lane < 16) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tot[wave][cl + k][2] = Br[k];
-    }
-    __syncthreads();
-    float h[4], e[4];
-    load4(P.saved + (b * tiles + tile) * P.D + q.c, q, h);
+  for (int i = 0; i < L; ++i) {
+    const long long t = tk + i < T_ ? tk + i : T_ - 1;
+    float gv[4];
+    load4(g + t * P.gs, q, gv);
+    load4(u + t * P.us, q, uv[i]);
+    if (GATED) load4(o + t * P.os, q, ov[i]);
+    load4(dy + t * P.ys, q, yv[i]);
+    const bool live = tk + i < len;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k][0], h[k], tot[w][cl + k][1]);
-      h[k] = fmaf(Ae[k], h[k], Be[k]);
-      e[k] = es[flip][cl + k];
-      for (int w = 3; w > wave; --w) e[k] = fmaf(tot[w][cl + k][0], e[k], tot[w][cl + k][2]);
-      e[k] = fmaf(Ax[k], e[k], Bx[k]);
+      sigmoids(gv[k] + bias[k], a[i][k], z[i][k]);
+      a[i][k] = live ? a[i][k] : 1.f, z[i][k] = live ? z[i][k] : 0.f;
+      uv[i][k] = live ? uv[i][k] : 0.f, yv[i][k] = live ? yv[i][k] : 0.f;
+      if (GATED) ov[i][k] = live ? ov[i][k] : 0.f;
+      B[k] = fmaf(a[i][k], B[k], z[i][k] * uv[i][k]);
+      A[k] *= a[i][k];
     }
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        hb[i][k] = h[k];
-        h[k] = fmaf(a[i][k], h[k], z[i][k] * uv[i][k]);
-      }
-#pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      float du[4], dg[4], dou[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float s = silu[i][k], c = GATED ? yv[i][k] * (ov[i][k] * s) : yv[i][k];
-        const float dh = c + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
-        const bool live = tk + i < len;
-        du[k] = live ? z[i][k] * dh : 0.f;
-        dg[k] = live ? dh * (hb[i][k] - uv[i][k]) * (a[i][k] * z[i][k]) : 0.f;
-        if (GATED) dou[k] = live ? yv[i][k] * hi * (s * (1.f + ov[i][k] * (1.f - s))) : 0.f;
-        e[k] = a[i][k] * dh;
-        db[k] += dg[k];
-      }
-      if (tk + i < T_) {
-        store_n<T, 4>(static_cast<T *>(P.du) + b * P.dub + (tk + i) * P.dus + q.c, q.n, du);
-        store_n<T, 4>(static_cast<T *>(P.dg) + b * P.dgb + (tk + i) * P.dgs + q.c, q.n, dg);
-        if (GATED) store_n<T, 4>(static_cast<T *>(P.dou) + b * P.dob + (tk + i) * P.dos + q.c, q.n, dou);
-      }
-    }
-    if (grp == 0) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) es[flip ^ 1][cl + k] = e[k];
-    }
-    __syncthreads();
   }
-  if (P.dh0 && grp == 0) {
-    float e[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = es[flip][cl + k];
-    store_n<float, 4>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
+  for (int k = 0; k < 4; ++k) Ar[k] = A[k], Br[k] = 0.f;
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      silu[i][k] = 1.f;
+      if (GATED) {
+        float n;
+        sigmoids(ov[i][k], silu[i][k], n);    // the sigmoid for now
+      }
+      const float c = GATED ? yv[i][k] * (ov[i][k] * silu[i][k]) : yv[i][k];
+      Br[k] = a[i][k] * (c + Br[k]);
+    }
+  wave_scan<false>(A, B, Ae, Be);
+  wave_scan<true>(Ar, Br, Ax, Bx);
+  if (lane >= 48) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tot[wave][cl + k][0] = A[k], tot[wave][cl + k][1] = B[k];
   }
+  if (lane < 16) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tot[wave][cl + k][2] = Br[k];
+  }
+  __syncthreads();
+  const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
+  float At = 1.f, Bt = 0.f;
+#pragma unroll
+  for (int w = 3; w >= 0; --w) Bt = fmaf(tot[w][ch][0], Bt, tot[w][ch][2]), At *= tot[w][ch][0];
+  const float first = wave == 0 && pos == 0 && P.dhT && cc < P.D ? P.dhT[(long long)b * P.D + cc] : 0.f;
+  if (wave == 0 && tile > 0) publish_pair(links, pos, At, Bt, first);
+  look_back(links, pos, first, pre, at);
+  __syncthreads();
+  if (wave == 0 && pos % kSeg == kSeg - 1 && tile > 0) {
+    float e = at[ch];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) e = fmaf(pre[w][ch].x, e, pre[w][ch].y);
+    put_word(links.states + (long long)(pos / kSeg) * kSlice + ch, fmaf(At, e, Bt), 1u);
+  }
+  float e[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k][0], h[k], tot[w][cl + k][1]);
+    h[k] = fmaf(Ae[k], h[k], Be[k]);
+    e[k] = at[cl + k];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) e[k] = fmaf(pre[w][cl + k].x, e[k], pre[w][cl + k].y);
+    for (int w = 3; w > wave; --w) e[k] = fmaf(tot[w][cl + k][0], e[k], tot[w][cl + k][2]);
+    e[k] = fmaf(Ax[k], e[k], Bx[k]);
+  }
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      hb[i][k] = h[k];
+      h[k] = fmaf(a[i][k], h[k], z[i][k] * uv[i][k]);
+    }
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i) {
+    float du[4], dg[4], dou[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float s = silu[i][k], c = GATED ? yv[i][k] * (ov[i][k] * s) : yv[i][k];
+      const float dh = c + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
+      const bool live = tk + i < len;
+      du[k] = live ? z[i][k] * dh : 0.f;
+      dg[k] = live ? dh * (hb[i][k] - uv[i][k]) * (a[i][k] * z[i][k]) : 0.f;
+      if (GATED) dou[k] = live ? yv[i][k] * hi * (s * (1.f + ov[i][k] * (1.f - s))) : 0.f;
+      e[k] = a[i][k] * dh;
+      db[k] += dg[k];
+    }
+    if (tk + i < T_) {
+      store_n<T, 4>(static_cast<T *>(P.du) + b * P.dub + (tk + i) * P.dus + q.c, q.n, du);
+      store_n<T, 4>(static_cast<T *>(P.dg) + b * P.dgb + (tk + i) * P.dgs + q.c, q.n, dg);
+      if (GATED) store_n<T, 4>(static_cast<T *>(P.dou) + b * P.dob + (tk + i) * P.dos + q.c, q.n, dou);
+    }
+  }
+  if (P.dh0 && tile == 0 && grp == 0) store_n<float, 4>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
   if (P.dbias_partial) {
-    __shared__ float sum[16][kSlice];
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[grp][cl + k] = db[k];
     __syncthreads();
-    if (grp == 0) {
+    if (wave == 0 && cc < P.D) {
+      float v = 0.f;
 #pragma unroll
-      for (int r = 1; r < 16; ++r)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) db[k] += sum[r][cl + k];
-      store_n<float, 4>(P.dbias_partial + (long long)b * P.D + q.c, q.n, db);
+      for (int r = 0; r < 16; ++r) v += sum[r][ch];
+      P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = v;
     }
   }
 }
@@ -378,6 +453,11 @@ __global__ __launch_bounds__(256) void copy_or_zero_kernel(const float *from, fl
   if (i < n) to[i] = from ? from[i] : 0.f;
 }
 
+void clear_words(unsigned long long *p, long long n, hipStream_t st) {
+  const long long blocks = cdiv64(n, 512);
+  clear_words_kernel<<<(unsigned)(blocks < 2048 ? blocks : 2048), 256, 0, st>>>(p, n);
+}
+
 template <typename T>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   if (A.len <= 16) {
@@ -385,25 +465,37 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
     if (A.o) recurrence_step_kernel<T, true><<<blocks, 64, 0, st>>>(A);
     else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
   } else {
-    if (A.o) recurrence_fwd_kernel<T, true><<<A.batch * A.slices, 256, 0, st>>>(A);
-    else recurrence_fwd_kernel<T, false><<<A.batch * A.slices, 256, 0, st>>>(A);
+    const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
+    clear_words(A.work, chain_words((long long)A.batch * A.slices, A.tiles), st);
+    if (A.o) recurrence_fwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
+    else recurrence_fwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
   }
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
-  if (A.o) recurrence_bwd_kernel<T, true><<<A.batch * A.slices, 256, 0, st>>>(A);
-  else recurrence_bwd_kernel<T, false><<<A.batch * A.slices, 256, 0, st>>>(A);
+  const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
+  clear_words(A.work, chain_words((long long)A.batch * A.slices, A.tiles), st);
+  if (A.o) recurrence_bwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
+  else recurrence_bwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
 inline bool off(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
 
 inline bool sizes_ok(int batch, long long len, int channels) {
-  return batch >= 0 && len >= 0 && channels >= 1 && (long long)batch * channels <= 0x7fffffffLL && len <= 0x7fffffffLL &&
-         (long long)batch * cdiv(channels, kSlice) <= (1LL << 22);     // a launch's threads must stay below 2^32
+  if (batch < 0 || len < 0 || channels < 1 || (long long)batch * channels > 0x7fffffffLL || len > 0x7fffffffLL) return false;
+  const long long chains = (long long)batch * cdiv(channels, kSlice);
+  return chains <= (1LL << 22) && chains * cdiv64(len, kSaved) <= (1LL << 22);     // a launch's threads must stay below 2^32
 }
+
+// The workspace: the chains' words (the backward pass has the more and shorter tiles), then the bias gradient's partials, one row for
+// each backward tile of a sequence, and what their sums need.
+inline size_t work_bytes(int batch, long long len, int channels) {
+  return (size_t)chain_words((long long)batch * cdiv(channels, kSlice), cdiv64(len, kSaved)) * 8;
+}
+inline size_t partial_floats(int batch, long long len, int channels) { return (size_t)batch * cdiv64(len, kSaved) * channels; }
 
 pbkd_status check_sizes(int batch, long long len, int channels, int dtype) {
   if (batch < 0 || len < 0 || channels < 1) return set_error(PBKD_ESHAPE, "recurrence: [%d, %lld, %d]", batch, len, channels);
@@ -455,8 +547,9 @@ pbkd_status forward(const pbkd_recurrence_desc *q, bool step, void *hip_stream) 
     return PBKD_OK;
   }
   FwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->bias_dev, q->lengths_dev, q->state_dev, q->state_out_dev, q->y_dev,
-            step ? nullptr : static_cast<float *>(q->saved_dev), len, q->u_batch_stride, q->u_stride, q->gate_batch_stride, q->gate_stride,
-            q->out_gate_batch_stride, q->out_gate_stride, q->y_batch_stride, q->y_stride, q->batch, q->channels, cdiv(q->channels, kSlice)};
+            step ? nullptr : static_cast<float *>(q->saved_dev), static_cast<unsigned long long *>(q->workspace_dev), len, q->u_batch_stride, q->u_stride, q->gate_batch_stride, q->gate_stride,
+            q->out_gate_batch_stride, q->out_gate_stride, q->y_batch_stride, q->y_stride, q->batch, q->channels, cdiv(q->channels, kSlice),
+            (int)cdiv64(len, 16 * kFwdL)};
   switch (q->dtype) {
     case PBKD_F32: SEQ_HIPCHK(launch_fwd<float>(A, st)); break;
     case PBKD_BF16: SEQ_HIPCHK(launch_fwd<bf16>(A, st)); break;
@@ -479,7 +572,8 @@ size_t pbkd_recurrence_saved_bytes(int batch, long long len, int channels) {
 
 size_t pbkd_recurrence_workspace_bytes(int batch, long long len, int channels) {
   if (!sizes_ok(batch, len, channels)) return 0;
-  return ((size_t)batch * channels + colsum_scratch_floats(batch, channels)) * sizeof(float) + 256;
+  return work_bytes(batch, len, channels) + partial_floats(batch, len, channels) * sizeof(float) +
+         colsum_scratch_floats((long long)batch * cdiv64(len, kSaved), channels) * sizeof(float) + 256;
 }
 
 pbkd_status pbkd_recurrence_forward(const pbkd_recurrence_desc *desc, void *hip_stream) { return forward(desc, false, hip_stream); }
@@ -509,13 +603,14 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *q, void *h
     return set_error(PBKD_ENOMEM, "recurrence: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes,
                      pbkd_recurrence_workspace_bytes(q->batch, q->len, q->channels));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  float *partial = static_cast<float *>(q->workspace_dev);
+  float *partial = reinterpret_cast<float *>(static_cast<char *>(q->workspace_dev) + work_bytes(q->batch, q->len, q->channels));
+  const long long tiles = cdiv64(q->len, kSaved);
   if (any) {
     BwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->dy_dev, q->bias_dev, q->lengths_dev, static_cast<const float *>(q->saved_dev), q->dstate_out_dev,
-              q->du_dev, q->dgate_dev, q->dout_gate_dev, q->dbias_dev ? partial : nullptr, q->dstate_dev, q->len, q->u_batch_stride, q->u_stride,
+              q->du_dev, q->dgate_dev, q->dout_gate_dev, q->dbias_dev ? partial : nullptr, q->dstate_dev, static_cast<unsigned long long *>(q->workspace_dev), q->len, q->u_batch_stride, q->u_stride,
               q->gate_batch_stride, q->gate_stride, q->out_gate_batch_stride, q->out_gate_stride, q->dy_batch_stride, q->dy_stride,
               q->du_batch_stride, q->du_stride, q->dgate_batch_stride, q->dgate_stride, q->dout_gate_batch_stride, q->dout_gate_stride,
-              q->batch, q->channels, cdiv(q->channels, kSlice)};
+              q->batch, q->channels, cdiv(q->channels, kSlice), (int)tiles};
     switch (q->dtype) {
       case PBKD_F32: SEQ_HIPCHK(launch_bwd<float>(A, st)); break;
       case PBKD_BF16: SEQ_HIPCHK(launch_bwd<bf16>(A, st)); break;
@@ -526,7 +621,7 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *q, void *h
     copy_or_zero_kernel<<<(unsigned)cdiv64(n, 256), 256, 0, st>>>(q->dstate_out_dev, q->dstate_dev, n);
     SEQ_HIPCHK(hipGetLastError());
   }
-  if (q->dbias_dev) SEQ_HIPCHK(launch_colsum(partial, any ? q->batch : 0, q->channels, partial + (size_t)q->batch * q->channels, q->dbias_dev, st));
+  if (q->dbias_dev) SEQ_HIPCHK(launch_colsum(partial, any ? q->batch * tiles : 0, q->channels, partial + partial_floats(q->batch, q->len, q->channels), q->dbias_dev, st));
   return PBKD_OK;
 }
 
