@@ -419,7 +419,7 @@ pbkd_status pbkd_rmsnorm_backward(const pbkd_rmsnorm_grad_desc *desc, void *hip_
  * [batch, channels]: the last state; it may be state_dev.  saved_dev (nullable): what the backward pass needs,
  * pbkd_recurrence_saved_bytes(); workspace: pbkd_recurrence_workspace_bytes(), the same for both directions.
  * batch, len >= 0, channels >= 1; PBKD_EUNSUPPORTED from 2^31 tokens or batch * channels on, or batch * ceil(channels / 64) *
- * ceil(len / 64) above 2^22. */
+ * ceil(len / 64) above 2^22, or tokens more than 2^25 elements apart. */
 typedef struct {
   int batch, channels;
   long long len;

@@ -8,19 +8,21 @@
 //   dh_t = c_t + e_t,  e_{t-1} = a_t dh_t   (the same composition from the last token on),
 //   du = z dh, dgate = dh (h_{t-1} - u) a z, do = dy h silu'(o)
 //
-// A tile is kSlice channels by a number of tokens: a thread holds L consecutive tokens of four channels, 16 threads
-// next to each other a row of kSlice channels, the 16 groups of them follow each other in time.  Each thread folds its tokens,
-// the groups' pairs are scanned over the wave's lanes and the four waves through LDS, and the tokens are gone through
+// A tile is kSlice channels by a number of tokens: a thread holds L consecutive tokens of two channels, half a wave next to
+// each other a row of kSlice channels, the eight half waves of a workgroup follow each other in time.  Each thread folds its
+// tokens, the half waves' pairs are joined by an exchange between the halves and through LDS, and the tokens are gone through
 // again from the registers: each tensor is read once.  Tiles of all times run at once and hand the state on (below).
 #include "seq_common.h"
+
+#include <initializer_list>
 
 namespace pbkd {
 namespace {
 
 constexpr int kSlice = 64;          // channels of a tile: 128 bytes of a 16-bit type
-constexpr int kFwdL = 8;            // tokens of a thread, forward: a tile has 16 times as many
-constexpr int kBwdL = 4;            // backward: more is held per token
-constexpr int kSaved = 16 * kBwdL;  // the forward pass saves the state in front of every backward tile
+constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile has 8 times as many
+constexpr int kBwdL = 8;            // backward: more is held per token
+constexpr int kSaved = 8 * kBwdL;   // the forward pass saves the state in front of every backward tile
 
 struct FwdArgs {
   const void *u, *g, *o;
@@ -47,68 +49,83 @@ struct BwdArgs {
   int batch, D, slices, tiles;
 };
 
+constexpr float kLog2e = 1.44269504088896340736f;
+
 // sigmoid(x) and sigmoid(-x), each to a few units of its own last place: both from e = exp(-|x|)
 __device__ __forceinline__ void sigmoids(float x, float &a, float &z) {
-  const float e = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
+  const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
   a = x >= 0.f ? r : s;
   z = x >= 0.f ? s : r;
-  if (x != x) a = z = x;
 }
+// sigmoid(x) alone: exp(-x) may be infinite
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-// The four channels of a lane.  Where a row's last lanes have fewer than four (only if D is no multiple of 4) they are taken
-// one by one; lanes and channels beyond the row read its last channels again, and nothing of them is written.
+// The two channels of a lane.  Where a row's last lane has only one (D is odd) they are taken one by one; lanes and channels
+// beyond the row read its last channels again, and nothing of them is written.
 struct Lane {
   int c;        // first channel, moved into the row
-  int n;        // channels that exist: 4, or fewer
+  int n;        // channels that exist: 2, 1 or 0
   bool one;     // the workgroup's loads go channel by channel
 };
 __device__ __forceinline__ Lane lane_of(int slice, int D) {
   Lane q;
-  const int c0 = slice * kSlice + (threadIdx.x & 15) * 4;
-  q.one = (D & 3) && slice * kSlice + kSlice > D;
-  q.n = D - c0 < 4 ? (D - c0 < 0 ? 0 : D - c0) : 4;
-  q.c = q.one ? (c0 < D ? c0 : D - 1) : (c0 < D ? c0 : D - 4);
+  const int c0 = slice * kSlice + (threadIdx.x & 31) * 2;
+  q.one = (D & 1) && slice * kSlice + kSlice > D;
+  q.n = D - c0 < 2 ? (D - c0 < 0 ? 0 : D - c0) : 2;
+  q.c = q.one ? (c0 < D ? c0 : D - 1) : (c0 < D ? c0 : D - 2);
   return q;
 }
 template <typename T>
-__device__ __forceinline__ void load4(const T *p, const Lane &q, float (&v)[4]) {
-  if (!q.one) {
-    load_n<T, 4>(p, 4, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(p[i < q.n ? i : (q.n > 0 ? q.n - 1 : 0)]);
-  }
+using Raw = typename VecOf<T, 2>::type;
+template <typename T, bool ONE>
+__device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
+  if (!ONE) return *reinterpret_cast<const Raw<T> *>(p);
+  Raw<T> r;
+  r[0] = p[0], r[1] = p[q.n == 2 ? 1 : 0];
+  return r;
 }
+template <typename T, bool ONE>
+__device__ __forceinline__ void put2(T *p, const Lane &q, const float (&v)[2]) {
+  if (ONE) store_n<T, 2>(p, q.n, v);
+  else if (q.n) store_n<T, 2>(p, 2, v);
+}
+__device__ __forceinline__ void floats2(const float *p, const Lane &q, float (&v)[2]) {
+  const Raw<float> r = q.one ? raw2<float, true>(p, q) : raw2<float, false>(p, q);
+  v[0] = r[0], v[1] = r[1];
+}
+
+// Places of a thread's L tokens in one tensor: a base that its wave shares, and a thread's own 32-bit distance from it, which the
+// loads and stores take as they are (the empty asm keeps the compiler from joining the two in 64-bit vector arithmetic, one
+// place a token).  WHOLE tiles move the base by the stride, so that the distance stays; in others a token behind the last is moved
+// to the last.
+constexpr long long kMaxStride = 1LL << 25;      // elements between tokens: 2 * kFwdL of them, in bytes, below 2^32
+template <typename T, int L, bool WHOLE>
+struct Place {
+  const char *base;
+  long long stride;         // bytes
+  unsigned mine;            // WHOLE: the distance; else: of the channels alone
+  int token, last;          // the thread's first token and the sequence's last, counted from the base's
+  __device__ __forceinline__ Place(const void *p, long long batch_at, long long stride_, int t0, int slice, const Lane &q, long long T_) {
+    const int w0 = t0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * L, at = WHOLE || w0 < T_ ? w0 : (int)T_ - 1;
+    stride = stride_ * (long long)sizeof(T);
+    base = static_cast<const char *>(p) + (batch_at + at * stride_ + slice * kSlice) * (long long)sizeof(T);
+    token = threadIdx.x & 32 ? L : 0, last = (int)T_ - 1 - at;
+    mine = (unsigned)(q.c - slice * kSlice) * (unsigned)sizeof(T);
+    if (WHOLE) mine += (unsigned)token * (unsigned)stride;
+  }
+  __device__ __forceinline__ T *at(int i) const {
+    typedef const __attribute__((address_space(1))) char *Global;      // or the accesses become flat ones
+    Global row = (Global)(WHOLE ? base + i * stride : base);
+    asm("" : "+s"(row));
+    const unsigned far = WHOLE ? mine : mine + (unsigned)(token + i < last ? token + i : last) * (unsigned)stride;
+    return reinterpret_cast<T *>(const_cast<char *>((const char *)(row + far)));
+  }
+};
 
 __device__ __forceinline__ int length_of(const int *lengths, int b, long long len) {
   if (!lengths) return (int)len;
   const long long n = lengths[b];
   return (int)(n < 0 ? 0 : n > len ? len : n);
-}
-
-// (A, B) of each lane's tokens become those of all tokens from the wave's first (reverse: last) group to the lane's own;
-// (Ae, Be) those of the groups in front of the lane's own.
-template <bool REVERSE>
-__device__ __forceinline__ void wave_scan(float (&A)[4], float (&B)[4], float (&Ae)[4], float (&Be)[4]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int off = 16; off < 64; off *= 2) {
-    const bool in = REVERSE ? lane + off < 64 : lane >= off;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float A1 = REVERSE ? __shfl_down(A[i], off, 64) : __shfl_up(A[i], off, 64);
-      const float B1 = REVERSE ? __shfl_down(B[i], off, 64) : __shfl_up(B[i], off, 64);
-      B[i] = in ? fmaf(A[i], B1, B[i]) : B[i];
-      A[i] = in ? A[i] * A1 : A[i];
-    }
-  }
-  const bool in = REVERSE ? lane < 48 : lane >= 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float A1 = REVERSE ? __shfl_down(A[i], 16, 64) : __shfl_up(A[i], 16, 64);
-    const float B1 = REVERSE ? __shfl_down(B[i], 16, 64) : __shfl_up(B[i], 16, 64);
-    Ae[i] = in ? A1 : 1.f, Be[i] = in ? B1 : 0.f;
-  }
 }
 
 // How tiles that follow each other in time hand on the state.  The tiles of one sequence and slice are a chain, cut into
@@ -187,226 +204,254 @@ __global__ __launch_bounds__(256) void clear_words_kernel(unsigned long long *p,
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n / 2; i += (long long)gridDim.x * 256) reinterpret_cast<u2 *>(p)[i] = u2{0, 0};
 }
 
-template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
-  constexpr int L = kFwdL, TILE = 16 * L;
-  __shared__ float2 tot[4][kSlice], pre[4][kSlice];
-  __shared__ float at[kSlice];
-  __shared__ unsigned number;
-  if (threadIdx.x == 0) number = (unsigned)atomicAdd(P.work, 1ull);
-  __syncthreads();
-  const int chains = P.batch * P.slices, tile = number / chains, chain = number % chains, slice = chain % P.slices, b = chain / P.slices;
+// What a workgroup shares.
+struct Shared {
+  float tot[4][kSlice][3];           // a wave's A, forward B, reverse B
+  float2 pre[4][kSlice];
+  float at[kSlice];
+  unsigned number;
+};
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.  ONE: see Lane.
+template <typename T, bool GATED, bool WHOLE, bool ONE>
+__device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
+  constexpr int L = kFwdL, TILE = 8 * L;
+  const int chains = P.batch * P.slices, slice = chain % P.slices, b = chain / P.slices;
   const Chain links = chain_of(P.work, chain, chains, P.tiles);
-  const Lane q = lane_of(slice, P.D);
-  const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int len = length_of(P.lengths, b, P.len);
-  const long long T_ = P.len, tk = (long long)tile * TILE + grp * L;
-  float bias[4] = {0.f, 0.f, 0.f, 0.f};
-  if (P.bias) load4(P.bias + q.c, q, bias);
-  const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
-  const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
-  T *y = static_cast<T *>(P.y) + b * P.yb + q.c;
-  float a[L][4], bb[L][4], A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4];
+  const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
+  const bool upper = threadIdx.x & 32;
+  const int t0 = tile * TILE, tk = t0 + grp * L;
+  const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
+  const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
+  Raw<T> ur[L], gr[L], orr[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE>(g.at(i), q), ur[i] = raw2<T, ONE>(u.at(i), q);
+  if (GATED) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE>(o.at(i), q);
+  }
+  float bias[2] = {0.f, 0.f};
+  if (P.bias) floats2(P.bias + q.c, q, bias);
+  float a[L][2], bb[L][2], A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Ae[2], Be[2];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    const long long t = tk + i < T_ ? tk + i : T_ - 1;     // a token that is read for nothing is one of this sequence
-    float uv[4], gv[4];
-    load4(u + t * P.us, q, uv);
-    load4(g + t * P.gs, q, gv);
-    const bool live = tk + i < len;
+    const bool live = WHOLE || tk + i < len;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       float z;
-      sigmoids(gv[k] + bias[k], a[i][k], z);
-      bb[i][k] = live ? z * uv[k] : 0.f;
+      sigmoids(static_cast<float>(gr[i][k]) + bias[k], a[i][k], z);
+      bb[i][k] = live ? z * static_cast<float>(ur[i][k]) : 0.f;
       a[i][k] = live ? a[i][k] : 1.f;
       B[k] = fmaf(a[i][k], B[k], bb[i][k]);
       A[k] *= a[i][k];
     }
   }
-  wave_scan<false>(A, B, Ae, Be);
-  if (lane >= 48) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tot[wave][cl + k] = make_float2(A[k], B[k]);
+  for (int k = 0; k < 2; ++k) {
+    const float A1 = other_half(A[k]), B1 = other_half(B[k]);
+    Ae[k] = upper ? A1 : 1.f, Be[k] = upper ? B1 : 0.f;
+    if (upper) S.tot[wave][cl + k][0] = A[k] * A1, S.tot[wave][cl + k][1] = fmaf(A[k], B1, B[k]);
   }
   __syncthreads();
   const int ch = threadIdx.x & 63, c = slice * kSlice + ch;
   float At = 1.f, Bt = 0.f;                                // the whole tile's pair, channel ch
 #pragma unroll
-  for (int w = 0; w < 4; ++w) Bt = fmaf(tot[w][ch].x, Bt, tot[w][ch].y), At *= tot[w][ch].x;
+  for (int w = 0; w < 4; ++w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][1]), At *= S.tot[w][ch][0];
   const float first = wave == 0 && tile == 0 && P.h0 && c < P.D ? P.h0[(long long)b * P.D + c] : 0.f;
   if (wave == 0 && tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
-  look_back(links, tile, first, pre, at);
+  look_back(links, tile, first, S.pre, S.at);
   __syncthreads();
   if (wave == 0 && tile % kSeg == kSeg - 1 && tile + 1 < P.tiles) {
-    float h = at[ch];
+    float h = S.at[ch];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) h = fmaf(pre[w][ch].x, h, pre[w][ch].y);
+    for (int w = 0; w < 4; ++w) h = fmaf(S.pre[w][ch].x, h, S.pre[w][ch].y);
     put_word(links.states + (long long)(tile / kSeg) * kSlice + ch, fmaf(At, h, Bt), 1u);
   }
-  float h[4];
+  float h[2];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    h[k] = at[cl + k];
+  for (int k = 0; k < 2; ++k) {
+    h[k] = S.at[cl + k];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) h[k] = fmaf(pre[w][cl + k].x, h[k], pre[w][cl + k].y);
-    for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k].x, h[k], tot[w][cl + k].y);
+    for (int w = 0; w < 4; ++w) h[k] = fmaf(S.pre[w][cl + k].x, h[k], S.pre[w][cl + k].y);
+    for (int w = 0; w < wave; ++w) h[k] = fmaf(S.tot[w][cl + k][0], h[k], S.tot[w][cl + k][1]);
     h[k] = fmaf(Ae[k], h[k], Be[k]);
   }
-  if (P.saved && (grp * L) % kSaved == 0 && tk < T_)
-    store_n<float, 4>(P.saved + (b * ((T_ + kSaved - 1) / kSaved) + tk / kSaved) * P.D + q.c, q.n, h);
+  if (P.saved && (grp * L) % kSaved == 0 && tk < P.len)
+    store_n<float, 2>(P.saved + (b * ((P.len + kSaved - 1) / kSaved) + tk / kSaved) * P.D + q.c, q.n, h);
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    float out[4], ov[4];
-    if (GATED) load4(o + (tk + i < T_ ? tk + i : T_ - 1) * P.os, q, ov);
+    float out[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       h[k] = fmaf(a[i][k], h[k], bb[i][k]);
       out[k] = h[k];
       if (GATED) {
-        float s, n;
-        sigmoids(ov[k], s, n);
-        out[k] *= ov[k] * s;
+        const float ov = static_cast<float>(orr[i][k]);
+        out[k] *= ov * sigmoid(ov);
       }
-      out[k] = tk + i < len ? out[k] : 0.f;
+      out[k] = WHOLE || tk + i < len ? out[k] : 0.f;
     }
-    if (tk + i < T_) store_n<T, 4>(y + (tk + i) * P.ys, q.n, out);
+    if (WHOLE || tk + i < P.len) put2<T, ONE>(y.at(i), q, out);
   }
-  if (P.hT && tile + 1 == P.tiles && grp == 15) store_n<float, 4>(P.hT + (long long)b * P.D + q.c, q.n, h);
+  if (P.hT && tile + 1 == P.tiles && grp == 7) store_n<float, 2>(P.hT + (long long)b * P.D + q.c, q.n, h);
 }
 
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void recurrence_bwd_kernel(BwdArgs P) {
-  constexpr int L = kBwdL, TILE = 16 * L;
-  __shared__ float tot[4][kSlice][3];       // a wave's A, forward B, reverse B
-  __shared__ float2 pre[4][kSlice];
-  __shared__ float at[kSlice], sum[16][kSlice];
-  __shared__ unsigned number;
-  if (threadIdx.x == 0) number = (unsigned)atomicAdd(P.work, 1ull);
+__global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
+  __shared__ Shared S;
+  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work, 1ull);
   __syncthreads();
-  const int chains = P.batch * P.slices, pos = number / chains, tile = P.tiles - 1 - pos;      // the chain starts at the last tile
-  const int chain = number % chains, slice = chain % P.slices, b = chain / P.slices;
+  const int number = __builtin_amdgcn_readfirstlane(S.number), chains = P.batch * P.slices, tile = number / chains, chain = number % chains;
+  const Lane q = lane_of(chain % P.slices, P.D);
+  const int len = length_of(P.lengths, chain / P.slices, P.len);
+  if (q.one) fwd_tile<T, GATED, false, true>(P, S, tile, chain, q, len);
+  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false>(P, S, tile, chain, q, len);
+  else fwd_tile<T, GATED, true, false>(P, S, tile, chain, q, len);
+}
+
+template <typename T, bool GATED, bool WHOLE, bool ONE>
+__device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*sum)[kSlice], int pos, int chain, const Lane &q, int len) {
+  constexpr int L = kBwdL, TILE = 8 * L;
+  const int chains = P.batch * P.slices, slice = chain % P.slices, b = chain / P.slices;
+  const int tile = P.tiles - 1 - pos;       // the chain starts at the last tile
   const Chain links = chain_of(P.work, chain, chains, P.tiles);
-  const Lane q = lane_of(slice, P.D);
-  const int cl = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int len = length_of(P.lengths, b, P.len);
-  const long long T_ = P.len, tk = (long long)tile * TILE + grp * L;
-  float bias[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f}, h[4];
-  if (P.bias) load4(P.bias + q.c, q, bias);
-  load4(P.saved + ((long long)b * P.tiles + tile) * P.D + q.c, q, h);
-  const T *u = static_cast<const T *>(P.u) + b * P.ub + q.c, *g = static_cast<const T *>(P.g) + b * P.gb + q.c;
-  const T *o = GATED ? static_cast<const T *>(P.o) + b * P.ob + q.c : nullptr;
-  const T *dy = static_cast<const T *>(P.dy) + b * P.yb + q.c;
-  float a[L][4], z[L][4], hb[L][4], uv[L][4], ov[L][4], yv[L][4], silu[L][4];
-  float A[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, Ae[4], Be[4], Ar[4], Br[4], Ax[4], Bx[4];
+  const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
+  const bool upper = threadIdx.x & 32;
+  const int t0 = tile * TILE, tk = t0 + grp * L;
+  const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
+  const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), dy(P.dy, b * P.yb, P.ys, t0, slice, q, P.len);
+  Raw<T> ur[L], gr[L], orr[L], yr[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    const long long t = tk + i < T_ ? tk + i : T_ - 1;
-    float gv[4];
-    load4(g + t * P.gs, q, gv);
-    load4(u + t * P.us, q, uv[i]);
-    if (GATED) load4(o + t * P.os, q, ov[i]);
-    load4(dy + t * P.ys, q, yv[i]);
-    const bool live = tk + i < len;
+    gr[i] = raw2<T, ONE>(g.at(i), q);
+    ur[i] = raw2<T, ONE>(u.at(i), q);
+    yr[i] = raw2<T, ONE>(dy.at(i), q);
+    if (GATED) orr[i] = raw2<T, ONE>(o.at(i), q);
+  }
+  float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, h[2];
+  if (P.bias) floats2(P.bias + q.c, q, bias);
+  floats2(P.saved + ((long long)b * P.tiles + tile) * P.D + q.c, q, h);
+  if (!WHOLE) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      sigmoids(gv[k] + bias[k], a[i][k], z[i][k]);
-      a[i][k] = live ? a[i][k] : 1.f, z[i][k] = live ? z[i][k] : 0.f;
-      uv[i][k] = live ? uv[i][k] : 0.f, yv[i][k] = live ? yv[i][k] : 0.f;
-      if (GATED) ov[i][k] = live ? ov[i][k] : 0.f;
-      B[k] = fmaf(a[i][k], B[k], z[i][k] * uv[i][k]);
+    for (int i = 0; i < L; ++i)
+      if (tk + i >= len) {
+        ur[i][0] = ur[i][1] = yr[i][0] = yr[i][1] = T(0.f);
+        if (GATED) orr[i][0] = orr[i][1] = T(0.f);
+      }
+  }
+  float a[L][2], z[L][2], hb[L][2], sg[L][2];
+  float A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Br[2] = {0.f, 0.f}, Ae[2], Be[2], Ax[2], Bx[2];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const bool live = WHOLE || tk + i < len;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      sigmoids(static_cast<float>(gr[i][k]) + bias[k], a[i][k], z[i][k]);
+      if (!live) a[i][k] = 1.f, z[i][k] = 0.f;
+      B[k] = fmaf(a[i][k], B[k], z[i][k] * static_cast<float>(ur[i][k]));
       A[k] *= a[i][k];
     }
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) Ar[k] = A[k], Br[k] = 0.f;
-#pragma unroll
   for (int i = L - 1; i >= 0; --i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      silu[i][k] = 1.f;
-      if (GATED) {
-        float n;
-        sigmoids(ov[i][k], silu[i][k], n);    // the sigmoid for now
-      }
-      const float c = GATED ? yv[i][k] * (ov[i][k] * silu[i][k]) : yv[i][k];
+    for (int k = 0; k < 2; ++k) {
+      const float ov = GATED ? static_cast<float>(orr[i][k]) : 0.f;
+      sg[i][k] = GATED ? sigmoid(ov) : 1.f;
+      const float c = GATED ? static_cast<float>(yr[i][k]) * (ov * sg[i][k]) : static_cast<float>(yr[i][k]);
       Br[k] = a[i][k] * (c + Br[k]);
     }
-  wave_scan<false>(A, B, Ae, Be);
-  wave_scan<true>(Ar, Br, Ax, Bx);
-  if (lane >= 48) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tot[wave][cl + k][0] = A[k], tot[wave][cl + k][1] = B[k];
-  }
-  if (lane < 16) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) tot[wave][cl + k][2] = Br[k];
+  for (int k = 0; k < 2; ++k) {
+    const float A1 = other_half(A[k]), B1 = other_half(B[k]), R1 = other_half(Br[k]);
+    Ae[k] = upper ? A1 : 1.f, Be[k] = upper ? B1 : 0.f;
+    Ax[k] = upper ? 1.f : A1, Bx[k] = upper ? 0.f : R1;
+    if (upper) S.tot[wave][cl + k][0] = A[k] * A1, S.tot[wave][cl + k][1] = fmaf(A[k], B1, B[k]);
+    else S.tot[wave][cl + k][2] = fmaf(A[k], R1, Br[k]);
   }
   __syncthreads();
   const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
   float At = 1.f, Bt = 0.f;
 #pragma unroll
-  for (int w = 3; w >= 0; --w) Bt = fmaf(tot[w][ch][0], Bt, tot[w][ch][2]), At *= tot[w][ch][0];
+  for (int w = 3; w >= 0; --w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][2]), At *= S.tot[w][ch][0];
   const float first = wave == 0 && pos == 0 && P.dhT && cc < P.D ? P.dhT[(long long)b * P.D + cc] : 0.f;
   if (wave == 0 && tile > 0) publish_pair(links, pos, At, Bt, first);
-  look_back(links, pos, first, pre, at);
+  look_back(links, pos, first, S.pre, S.at);
   __syncthreads();
   if (wave == 0 && pos % kSeg == kSeg - 1 && tile > 0) {
-    float e = at[ch];
+    float e = S.at[ch];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) e = fmaf(pre[w][ch].x, e, pre[w][ch].y);
+    for (int w = 0; w < 4; ++w) e = fmaf(S.pre[w][ch].x, e, S.pre[w][ch].y);
     put_word(links.states + (long long)(pos / kSeg) * kSlice + ch, fmaf(At, e, Bt), 1u);
   }
-  float e[4];
+  float e[2];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    for (int w = 0; w < wave; ++w) h[k] = fmaf(tot[w][cl + k][0], h[k], tot[w][cl + k][1]);
+  for (int k = 0; k < 2; ++k) {
+    for (int w = 0; w < wave; ++w) h[k] = fmaf(S.tot[w][cl + k][0], h[k], S.tot[w][cl + k][1]);
     h[k] = fmaf(Ae[k], h[k], Be[k]);
-    e[k] = at[cl + k];
+    e[k] = S.at[cl + k];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) e[k] = fmaf(pre[w][cl + k].x, e[k], pre[w][cl + k].y);
-    for (int w = 3; w > wave; --w) e[k] = fmaf(tot[w][cl + k][0], e[k], tot[w][cl + k][2]);
+    for (int w = 0; w < 4; ++w) e[k] = fmaf(S.pre[w][cl + k].x, e[k], S.pre[w][cl + k].y);
+    for (int w = 3; w > wave; --w) e[k] = fmaf(S.tot[w][cl + k][0], e[k], S.tot[w][cl + k][2]);
     e[k] = fmaf(Ax[k], e[k], Bx[k]);
   }
 #pragma unroll
   for (int i = 0; i < L; ++i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       hb[i][k] = h[k];
-      h[k] = fmaf(a[i][k], h[k], z[i][k] * uv[i][k]);
+      h[k] = fmaf(a[i][k], h[k], z[i][k] * static_cast<float>(ur[i][k]));
     }
+  const Place<T, L, WHOLE> du(P.du, b * P.dub, P.dus, t0, slice, q, P.len), dgp(P.dg, b * P.dgb, P.dgs, t0, slice, q, P.len);
+  const Place<T, L, WHOLE> dop(P.dou, b * P.dob, P.dos, t0, slice, q, P.len);
 #pragma unroll
   for (int i = L - 1; i >= 0; --i) {
-    float du[4], dg[4], dou[4];
+    float dv[2], dg[2], dou[2];
+    const bool live = WHOLE || tk + i < len;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float s = silu[i][k], c = GATED ? yv[i][k] * (ov[i][k] * s) : yv[i][k];
-      const float dh = c + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
-      const bool live = tk + i < len;
-      du[k] = live ? z[i][k] * dh : 0.f;
-      dg[k] = live ? dh * (hb[i][k] - uv[i][k]) * (a[i][k] * z[i][k]) : 0.f;
-      if (GATED) dou[k] = live ? yv[i][k] * hi * (s * (1.f + ov[i][k] * (1.f - s))) : 0.f;
+    for (int k = 0; k < 2; ++k) {
+      const float s = sg[i][k], yv = static_cast<float>(yr[i][k]), ov = GATED ? static_cast<float>(orr[i][k]) : 0.f;
+      const float dh = (GATED ? yv * (ov * s) : yv) + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
+      dv[k] = live ? z[i][k] * dh : 0.f;
+      dg[k] = live ? dh * (hb[i][k] - static_cast<float>(ur[i][k])) * (a[i][k] * z[i][k]) : 0.f;
+      if (GATED) dou[k] = live ? yv * hi * (s * (1.f + ov * (1.f - s))) : 0.f;
       e[k] = a[i][k] * dh;
       db[k] += dg[k];
     }
-    if (tk + i < T_) {
-      store_n<T, 4>(static_cast<T *>(P.du) + b * P.dub + (tk + i) * P.dus + q.c, q.n, du);
-      store_n<T, 4>(static_cast<T *>(P.dg) + b * P.dgb + (tk + i) * P.dgs + q.c, q.n, dg);
-      if (GATED) store_n<T, 4>(static_cast<T *>(P.dou) + b * P.dob + (tk + i) * P.dos + q.c, q.n, dou);
+    if (WHOLE || tk + i < P.len) {
+      put2<T, ONE>(du.at(i), q, dv);
+      put2<T, ONE>(dgp.at(i), q, dg);
+      if (GATED) put2<T, ONE>(dop.at(i), q, dou);
     }
   }
-  if (P.dh0 && tile == 0 && grp == 0) store_n<float, 4>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
+  if (P.dh0 && tile == 0 && grp == 0) store_n<float, 2>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
   if (P.dbias_partial) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum[grp][cl + k] = db[k];
+    for (int k = 0; k < 2; ++k) sum[grp][cl + k] = db[k];
     __syncthreads();
     if (wave == 0 && cc < P.D) {
       float v = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) v += sum[r][ch];
+      for (int r = 0; r < 8; ++r) v += sum[r][ch];
       P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = v;
     }
   }
+}
+
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void recurrence_bwd_kernel(BwdArgs P) {
+  __shared__ Shared S;
+  __shared__ float sum[8][kSlice];
+  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work, 1ull);
+  __syncthreads();
+  const int number = __builtin_amdgcn_readfirstlane(S.number), chains = P.batch * P.slices, pos = number / chains, chain = number % chains;
+  const Lane q = lane_of(chain % P.slices, P.D);
+  const int len = length_of(P.lengths, chain / P.slices, P.len);
+  if (q.one) bwd_tile<T, GATED, false, true>(P, S, sum, pos, chain, q, len);
+  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false>(P, S, sum, pos, chain, q, len);
+  else bwd_tile<T, GATED, true, false>(P, S, sum, pos, chain, q, len);
 }
 
 // One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
@@ -435,11 +480,7 @@ __global__ __launch_bounds__(64) void recurrence_step_kernel(FwdArgs P) {
         sigmoids(gv[k] + bias[k], a, z);
         h[k] = fmaf(a, h[k], z * uv[k]);
         out[k] = h[k];
-        if (GATED) {
-          float s, m;
-          sigmoids(ov[k], s, m);
-          out[k] *= ov[k] * s;
-        }
+        if (GATED) out[k] *= ov[k] * sigmoid(ov[k]);
       }
     }
     store_n<T, 4>(static_cast<T *>(P.y) + b * P.yb + t * P.ys + c, n, out);
@@ -504,6 +545,13 @@ pbkd_status check_sizes(int batch, long long len, int channels, int dtype) {
   return PBKD_OK;
 }
 
+// Whether the strides between tokens are what the tiles take (a single token has none).
+inline bool strides_ok(long long len, std::initializer_list<long long> strides) {
+  for (long long s : strides)
+    if (len > 1 && s > kMaxStride) return false;
+  return true;
+}
+
 // Whether an output's rows are apart from each other, sequences in front of tokens or tokens in front of sequences.
 inline bool apart(int batch, long long len, int D, long long bs, long long ts) {
   if (bs < 0 || ts < 0) return false;
@@ -526,6 +574,7 @@ pbkd_status forward(const pbkd_recurrence_desc *q, bool step, void *hip_stream) 
     return set_error(PBKD_EINVAL, "recurrence: a tensor is not aligned to its elements");
   if (q->u_stride < 0 || q->u_batch_stride < 0 || q->gate_stride < 0 || q->gate_batch_stride < 0 || q->out_gate_stride < 0 || q->out_gate_batch_stride < 0)
     return set_error(PBKD_EINVAL, "recurrence: negative stride");
+  if (!strides_ok(len, {q->u_stride, q->gate_stride, q->out_gate_stride, q->y_stride})) return set_error(PBKD_EUNSUPPORTED, "recurrence: tokens more than 2^25 elements apart");
   if (any && !apart(q->batch, len, q->channels, q->y_batch_stride, q->y_stride)) return set_error(PBKD_ESHAPE, "recurrence: rows of y overlap");
   if (!step && q->saved_dev) {
     if (off(q->saved_dev, 4)) return set_error(PBKD_EINVAL, "recurrence: a tensor is not aligned to its elements");
@@ -549,7 +598,7 @@ pbkd_status forward(const pbkd_recurrence_desc *q, bool step, void *hip_stream) 
   FwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->bias_dev, q->lengths_dev, q->state_dev, q->state_out_dev, q->y_dev,
             step ? nullptr : static_cast<float *>(q->saved_dev), static_cast<unsigned long long *>(q->workspace_dev), len, q->u_batch_stride, q->u_stride, q->gate_batch_stride, q->gate_stride,
             q->out_gate_batch_stride, q->out_gate_stride, q->y_batch_stride, q->y_stride, q->batch, q->channels, cdiv(q->channels, kSlice),
-            (int)cdiv64(len, 16 * kFwdL)};
+            (int)cdiv64(len, 8 * kFwdL)};
   switch (q->dtype) {
     case PBKD_F32: SEQ_HIPCHK(launch_fwd<float>(A, st)); break;
     case PBKD_BF16: SEQ_HIPCHK(launch_fwd<bf16>(A, st)); break;
@@ -593,6 +642,8 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *q, void *h
   if (q->u_stride < 0 || q->u_batch_stride < 0 || q->gate_stride < 0 || q->gate_batch_stride < 0 || q->out_gate_stride < 0 || q->out_gate_batch_stride < 0 ||
       q->dy_stride < 0 || q->dy_batch_stride < 0)
     return set_error(PBKD_EINVAL, "recurrence: negative stride");
+  if (!strides_ok(q->len, {q->u_stride, q->gate_stride, q->out_gate_stride, q->dy_stride, q->du_stride, q->dgate_stride, q->dout_gate_stride}))
+    return set_error(PBKD_EUNSUPPORTED, "recurrence: tokens more than 2^25 elements apart");
   if (any && (!apart(q->batch, q->len, q->channels, q->du_batch_stride, q->du_stride) || !apart(q->batch, q->len, q->channels, q->dgate_batch_stride, q->dgate_stride) ||
               (q->dout_gate_dev && !apart(q->batch, q->len, q->channels, q->dout_gate_batch_stride, q->dout_gate_stride))))
     return set_error(PBKD_ESHAPE, "recurrence: rows of a gradient overlap");
