@@ -15,6 +15,7 @@
 #include "seq_common.h"
 
 #include <initializer_list>
+#include <type_traits>
 
 namespace pbkd {
 namespace {
@@ -133,8 +134,8 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, long long le
 // the pairs of its segment's earlier tiles, and the last tile of a segment also publishes the state behind it, so that only
 // one tile in kSeg waits for one before.  All folds have a fixed order: results do not depend on who was first.
 //
-// A tile's number comes from a counter, tiles in front of it in a chain have smaller numbers, and it waits for nothing but
-// those: they were taken by workgroups that run already, so every wait ends.
+// A tile's place in its chain comes from the chain's counter, and it waits for nothing but tiles with smaller numbers: they were
+// taken by workgroups that run already, so every wait ends.
 //
 // A pair travels in one 64-bit word, written and read whole at the scope of the device (the eight dies' L2 caches do not see each
 // other's writes otherwise): 0 is "not there yet", B below, A with its sign bit set above (A, a product of sigmoids, has
@@ -161,39 +162,52 @@ __device__ __forceinline__ float high_of(unsigned long long v) { return __builti
 struct Chain {
   unsigned long long *pairs, *states;     // [tiles][kSlice], [segments][kSlice]
 };
-// work: the counter, then the pairs and the states of all chains
-inline __host__ __device__ long long chain_words(long long chains, long long tiles) {
-  return 32 + chains * (tiles + (tiles + kSeg - 1) / kSeg) * kSlice;
-}
-__device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, int chains, int tiles) {
-  const int segs = (tiles + kSeg - 1) / kSeg;
-  return {work + 32 + (long long)chain * tiles * kSlice, work + 32 + ((long long)chains * tiles + (long long)chain * segs) * kSlice};
+// As many workgroups for each chain as it has tiles, those of one time step next to each other; a die takes neighbouring slices, so
+// that what it reads at a time are whole rows, which spread over all channels of its L2 (one slice in eight meets a quarter of
+// them at row lengths that are multiples of 4 KB: 8x4096x2048 forward and backward 381 us, this way 337 us).
+__device__ __forceinline__ int chain_of_workgroup(unsigned n, unsigned chains) { return xcd_contiguous(n % chains, chains); }
+
+// The words of a chain: its counter (a line of its own), its pairs, its states.
+constexpr int kCounter = 16;
+inline __host__ __device__ long long words_of_chain(long long tiles) { return kCounter + (tiles + (tiles + kSeg - 1) / kSeg) * kSlice; }
+__device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, int tiles) {
+  unsigned long long *p = work + chain * words_of_chain(tiles);
+  return {p + kCounter, p + kCounter + (long long)tiles * kSlice};
 }
 
-// One thread in 256 for each channel and quarter of the segment: pre[w] the pair of up to four tiles in front of tile `pos`
-// (in the order of the chain), at[] the state in front of its segment.  Only the chain's first tile reads the state in
-// front of the chain (`first`), and its pair is the constant map to the state behind it: the last tile, which may write over the
-// initial state, thereby has every reader of it behind itself.
-__device__ __forceinline__ void look_back(const Chain &q, int pos, float first, float2 (*pre)[kSlice], float *at) {
+// One thread in 256 for each channel and quarter of the segment.  look_early reads the words of up to four tiles in front of tile
+// `pos` and (the first wave) the state in front of its segment, which are mostly there by then, while the tile's own data
+// are on their way; look_back waits for those that were not and leaves pre[w], the pair of the four tiles in the order of
+// the chain, and at[], the state.  Only the chain's first tile reads the state in front of the chain (`first`), and its pair is
+// the constant map to the state behind it: the last tile, which may write over the initial state, thereby has every reader of it
+// behind itself.
+struct Words {
+  unsigned long long v[4], state;
+};
+__device__ __forceinline__ Words look_early(const Chain &q, int pos) {
   const int ch = threadIdx.x & 63, w = threadIdx.x >> 6, seg = pos / kSeg, in = pos % kSeg;
   const unsigned long long *p = q.pairs + ((long long)seg * kSeg + w * 4) * kSlice + ch;
-  const unsigned long long *s = q.states + (long long)(seg - 1) * kSlice + ch;
-  unsigned long long v[4], c = 1;
+  Words k;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = w * 4 + j < in ? peek_word(p + j * kSlice) : 1;
-  if (w == 0 && seg > 0) c = peek_word(s);
+  for (int j = 0; j < 4; ++j) k.v[j] = w * 4 + j < in ? peek_word(p + j * kSlice) : 1;
+  k.state = w == 0 && seg > 0 ? peek_word(q.states + (long long)(seg - 1) * kSlice + ch) : 1;
+  return k;
+}
+__device__ __forceinline__ void look_back(const Chain &q, int pos, float first, const Words &k, float2 (*pre)[kSlice], float *at) {
+  const int ch = threadIdx.x & 63, w = threadIdx.x >> 6, seg = pos / kSeg, in = pos % kSeg;
+  const unsigned long long *p = q.pairs + ((long long)seg * kSeg + w * 4) * kSlice + ch;
   float A = 1.f, B = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (w * 4 + j < in) {
-      v[j] = await_word(p + j * kSlice, v[j]);
-      const float A2 = high_of(v[j]);
-      B = fmaf(A2, B, low_of(v[j]));
+      const unsigned long long v = await_word(p + j * kSlice, k.v[j]);
+      const float A2 = high_of(v);
+      B = fmaf(A2, B, low_of(v));
       A *= A2;
     }
   }
   pre[w][ch] = make_float2(A, B);
-  if (w == 0) at[ch] = seg > 0 ? low_of(await_word(s, c)) : pos == 0 ? first : 0.f;
+  if (w == 0) at[ch] = seg > 0 ? low_of(await_word(q.states + (long long)(seg - 1) * kSlice + ch, k.state)) : pos == 0 ? first : 0.f;
 }
 __device__ __forceinline__ void publish_pair(const Chain &q, int pos, float A, float B, float first) {
   put_word(q.pairs + (long long)pos * kSlice + (threadIdx.x & 63), pos == 0 ? fmaf(A, first, B) : B, pair_high(pos == 0 ? 0.f : A));
@@ -212,14 +226,23 @@ struct Shared {
   unsigned number;
 };
 
+// What was computed from r before is not kept for later, it is computed again: registers are what limits the waves of a compute unit.
+template <typename R>
+__device__ __forceinline__ R forget(R r) {
+  using Bits = std::conditional_t<sizeof(R) == 4, unsigned, unsigned long long>;
+  Bits b = __builtin_bit_cast(Bits, r);
+  asm("" : "+v"(b));
+  return __builtin_bit_cast(R, b);
+}
+
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.  ONE: see Lane.
 template <typename T, bool GATED, bool WHOLE, bool ONE>
 __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
   constexpr int L = kFwdL, TILE = 8 * L;
-  const int chains = P.batch * P.slices, slice = chain % P.slices, b = chain / P.slices;
-  const Chain links = chain_of(P.work, chain, chains, P.tiles);
+  const int slice = chain % P.slices, b = chain / P.slices;
+  const Chain links = chain_of(P.work, chain, P.tiles);
   const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
   const bool upper = threadIdx.x & 32;
   const int t0 = tile * TILE, tk = t0 + grp * L;
@@ -234,6 +257,7 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   }
   float bias[2] = {0.f, 0.f};
   if (P.bias) floats2(P.bias + q.c, q, bias);
+  const Words words = look_early(links, tile);
   float a[L][2], bb[L][2], A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Ae[2], Be[2];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -261,7 +285,7 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   for (int w = 0; w < 4; ++w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][1]), At *= S.tot[w][ch][0];
   const float first = wave == 0 && tile == 0 && P.h0 && c < P.D ? P.h0[(long long)b * P.D + c] : 0.f;
   if (wave == 0 && tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
-  look_back(links, tile, first, S.pre, S.at);
+  look_back(links, tile, first, words, S.pre, S.at);
   __syncthreads();
   if (wave == 0 && tile % kSeg == kSeg - 1 && tile + 1 < P.tiles) {
     float h = S.at[ch];
@@ -299,11 +323,12 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
 }
 
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
   __shared__ Shared S;
-  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work, 1ull);
+  const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
+  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work + chain * words_of_chain(P.tiles), 1ull);
   __syncthreads();
-  const int number = __builtin_amdgcn_readfirstlane(S.number), chains = P.batch * P.slices, tile = number / chains, chain = number % chains;
+  const int tile = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (q.one) fwd_tile<T, GATED, false, true>(P, S, tile, chain, q, len);
@@ -314,9 +339,9 @@ __global__ __launch_bounds__(256) void recurrence_fwd_kernel(FwdArgs P) {
 template <typename T, bool GATED, bool WHOLE, bool ONE>
 __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*sum)[kSlice], int pos, int chain, const Lane &q, int len) {
   constexpr int L = kBwdL, TILE = 8 * L;
-  const int chains = P.batch * P.slices, slice = chain % P.slices, b = chain / P.slices;
+  const int slice = chain % P.slices, b = chain / P.slices;
   const int tile = P.tiles - 1 - pos;       // the chain starts at the last tile
-  const Chain links = chain_of(P.work, chain, chains, P.tiles);
+  const Chain links = chain_of(P.work, chain, P.tiles);
   const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
   const bool upper = threadIdx.x & 32;
   const int t0 = tile * TILE, tk = t0 + grp * L;
@@ -333,6 +358,7 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
   float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, h[2];
   if (P.bias) floats2(P.bias + q.c, q, bias);
   floats2(P.saved + ((long long)b * P.tiles + tile) * P.D + q.c, q, h);
+  const Words words = look_early(links, pos);
   if (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < L; ++i)
@@ -378,13 +404,18 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
   for (int w = 3; w >= 0; --w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][2]), At *= S.tot[w][ch][0];
   const float first = wave == 0 && pos == 0 && P.dhT && cc < P.D ? P.dhT[(long long)b * P.D + cc] : 0.f;
   if (wave == 0 && tile > 0) publish_pair(links, pos, At, Bt, first);
-  look_back(links, pos, first, S.pre, S.at);
+  look_back(links, pos, first, words, S.pre, S.at);
   __syncthreads();
   if (wave == 0 && pos % kSeg == kSeg - 1 && tile > 0) {
     float e = S.at[ch];
 #pragma unroll
     for (int w = 0; w < 4; ++w) e = fmaf(S.pre[w][ch].x, e, S.pre[w][ch].y);
     put_word(links.states + (long long)(pos / kSeg) * kSlice + ch, fmaf(At, e, Bt), 1u);
+  }
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    ur[i] = forget(ur[i]), yr[i] = forget(yr[i]);
+    if (GATED) orr[i] = forget(orr[i]);
   }
   float e[2];
 #pragma unroll
@@ -441,12 +472,13 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
 }
 
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void recurrence_bwd_kernel(BwdArgs P) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
   __shared__ Shared S;
   __shared__ float sum[8][kSlice];
-  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work, 1ull);
+  const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
+  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work + chain * words_of_chain(P.tiles), 1ull);
   __syncthreads();
-  const int number = __builtin_amdgcn_readfirstlane(S.number), chains = P.batch * P.slices, pos = number / chains, chain = number % chains;
+  const int pos = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (q.one) bwd_tile<T, GATED, false, true>(P, S, sum, pos, chain, q, len);
@@ -507,7 +539,7 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
     else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
   } else {
     const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
-    clear_words(A.work, chain_words((long long)A.batch * A.slices, A.tiles), st);
+    clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
     if (A.o) recurrence_fwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
     else recurrence_fwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
   }
@@ -517,7 +549,7 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
-  clear_words(A.work, chain_words((long long)A.batch * A.slices, A.tiles), st);
+  clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
   if (A.o) recurrence_bwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
   else recurrence_bwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
   return hipGetLastError();
@@ -534,7 +566,7 @@ inline bool sizes_ok(int batch, long long len, int channels) {
 // The workspace: the chains' words (the backward pass has the more and shorter tiles), then the bias gradient's partials, one row for
 // each backward tile of a sequence, and what their sums need.
 inline size_t work_bytes(int batch, long long len, int channels) {
-  return (size_t)chain_words((long long)batch * cdiv(channels, kSlice), cdiv64(len, kSaved)) * 8;
+  return (size_t)batch * cdiv(channels, kSlice) * words_of_chain(cdiv64(len, kSaved)) * 8;
 }
 inline size_t partial_floats(int batch, long long len, int channels) { return (size_t)batch * cdiv64(len, kSaved) * channels; }
 
