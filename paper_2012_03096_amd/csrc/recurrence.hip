@@ -78,8 +78,11 @@ __device__ __forceinline__ Lane lane_of(int slice, int D) {
 }
 template <typename T>
 using Raw = typename VecOf<T, 2>::type;
-template <typename T, bool ONE>
+// ALONE: no cache line has another tile's channels too.  What is read is then read past the caches; otherwise the line's second
+// reader would fetch it again (8x4096x2048 forward and backward 319 -> 305 us, but 7x1000x515 in fp32 56 -> 64 us).
+template <typename T, bool ONE, bool ALONE>
 __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
+  if (!ONE && ALONE) return __builtin_nontemporal_load(reinterpret_cast<const Raw<T> *>(p));
   if (!ONE) return *reinterpret_cast<const Raw<T> *>(p);
   Raw<T> r;
   r[0] = p[0], r[1] = p[q.n == 2 ? 1 : 0];
@@ -87,39 +90,37 @@ __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
 }
 template <typename T, bool ONE>
 __device__ __forceinline__ void put2(T *p, const Lane &q, const float (&v)[2]) {
-  if (ONE) store_n<T, 2>(p, q.n, v);
-  else if (q.n) store_n<T, 2>(p, 2, v);
+  if (ONE) {
+    store_n<T, 2>(p, q.n, v);
+  } else {                                 // lanes without channels do not come here
+    Raw<T> r;
+    r[0] = static_cast<T>(v[0]), r[1] = static_cast<T>(v[1]);
+    __builtin_nontemporal_store(r, reinterpret_cast<Raw<T> *>(p));
+  }
 }
 __device__ __forceinline__ void floats2(const float *p, const Lane &q, float (&v)[2]) {
-  const Raw<float> r = q.one ? raw2<float, true>(p, q) : raw2<float, false>(p, q);
+  const Raw<float> r = q.one ? raw2<float, true, false>(p, q) : raw2<float, false, false>(p, q);
   v[0] = r[0], v[1] = r[1];
 }
 
-// Places of a thread's L tokens in one tensor: a base that its wave shares, and a thread's own 32-bit distance from it, which the
-// loads and stores take as they are (the empty asm keeps the compiler from joining the two in 64-bit vector arithmetic, one
-// place a token).  WHOLE tiles move the base by the stride, so that the distance stays; in others a token behind the last is moved
-// to the last.
+// Places of a thread's L tokens in one tensor: a base that its wave shares, and each token's own 32-bit distance from it, which
+// the loads and stores take as they are.  In tiles that are not WHOLE a token behind the last is moved to the last.
 constexpr long long kMaxStride = 1LL << 25;      // elements between tokens: 2 * kFwdL of them, in bytes, below 2^32
 template <typename T, int L, bool WHOLE>
 struct Place {
-  const char *base;
-  long long stride;         // bytes
-  unsigned mine;            // WHOLE: the distance; else: of the channels alone
+  char *base;
+  unsigned stride, mine;    // bytes; WHOLE: the distance of the first token; else: of the channels alone
   int token, last;          // the thread's first token and the sequence's last, counted from the base's
   __device__ __forceinline__ Place(const void *p, long long batch_at, long long stride_, int t0, int slice, const Lane &q, long long T_) {
     const int w0 = t0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * L, at = WHOLE || w0 < T_ ? w0 : (int)T_ - 1;
-    stride = stride_ * (long long)sizeof(T);
-    base = static_cast<const char *>(p) + (batch_at + at * stride_ + slice * kSlice) * (long long)sizeof(T);
+    stride = (unsigned)stride_ * (unsigned)sizeof(T);
+    base = const_cast<char *>(static_cast<const char *>(p)) + (batch_at + at * stride_ + slice * kSlice) * (long long)sizeof(T);
     token = threadIdx.x & 32 ? L : 0, last = (int)T_ - 1 - at;
     mine = (unsigned)(q.c - slice * kSlice) * (unsigned)sizeof(T);
-    if (WHOLE) mine += (unsigned)token * (unsigned)stride;
+    if (WHOLE) mine += (unsigned)token * stride;
   }
   __device__ __forceinline__ T *at(int i) const {
-    typedef const __attribute__((address_space(1))) char *Global;      // or the accesses become flat ones
-    Global row = (Global)(WHOLE ? base + i * stride : base);
-    asm("" : "+s"(row));
-    const unsigned far = WHOLE ? mine : mine + (unsigned)(token + i < last ? token + i : last) * (unsigned)stride;
-    return reinterpret_cast<T *>(const_cast<char *>((const char *)(row + far)));
+    return reinterpret_cast<T *>(base + (WHOLE ? mine + i * stride : mine + (unsigned)(token + i < last ? token + i : last) * stride));
   }
 };
 
@@ -140,7 +141,7 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, long long le
 // A pair travels in one 64-bit word, written and read whole at the scope of the device (the eight dies' L2 caches do not see each
 // other's writes otherwise): 0 is "not there yet", B below, A with its sign bit set above (A, a product of sigmoids, has
 // none of its own).  The words are cleared by a kernel in front.
-constexpr int kSeg = 16;
+constexpr int kSeg = 8;      // 4: 1x65536x1280 147 -> 153 us, 16: 8x4096x2048 forward and backward 304 -> 309 us
 
 __device__ __forceinline__ void put_word(unsigned long long *p, float low, unsigned high) {
   __hip_atomic_store(p, (unsigned long long)high << 32 | __builtin_bit_cast(unsigned, low), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -175,39 +176,42 @@ __device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, i
   return {p + kCounter, p + kCounter + (long long)tiles * kSlice};
 }
 
-// One thread in 256 for each channel and quarter of the segment.  look_early reads the words of up to four tiles in front of tile
-// `pos` and (the first wave) the state in front of its segment, which are mostly there by then, while the tile's own data
-// are on their way; look_back waits for those that were not and leaves pre[w], the pair of the four tiles in the order of
-// the chain, and at[], the state.  Only the chain's first tile reads the state in front of the chain (`first`), and its pair is
-// the constant map to the state behind it: the last tile, which may write over the initial state, thereby has every reader of it
-// behind itself.
+// The first wave does this, a lane for each channel.  look_early reads the words of the segment's earlier tiles and the state in
+// front of the segment, which are mostly there by then, while the tile's own data are on their way; look_back waits for those
+// that were not and returns the state in front of the tile.  The last tile of a segment passes the state behind it on as soon as it
+// knows the one in front: one addition and one product lie between them.  Only the chain's first tile reads the state in
+// front of the chain (`first`), and its pair is the constant map to the state behind it: the last tile, which may write over the
+// initial state, thereby has every reader of it behind itself.
 struct Words {
-  unsigned long long v[4], state;
+  unsigned long long v[kSeg - 1], state;
 };
 __device__ __forceinline__ Words look_early(const Chain &q, int pos) {
-  const int ch = threadIdx.x & 63, w = threadIdx.x >> 6, seg = pos / kSeg, in = pos % kSeg;
-  const unsigned long long *p = q.pairs + ((long long)seg * kSeg + w * 4) * kSlice + ch;
+  const int ch = threadIdx.x & 63, seg = pos / kSeg, in = pos % kSeg;
+  const unsigned long long *p = q.pairs + (long long)seg * kSeg * kSlice + ch;
   Words k;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) k.v[j] = w * 4 + j < in ? peek_word(p + j * kSlice) : 1;
-  k.state = w == 0 && seg > 0 ? peek_word(q.states + (long long)(seg - 1) * kSlice + ch) : 1;
+  for (int j = 0; j < kSeg - 1; ++j) k.v[j] = j < in ? peek_word(p + j * kSlice) : 1;
+  k.state = seg > 0 ? peek_word(q.states + (long long)(seg - 1) * kSlice + ch) : 1;
   return k;
 }
-__device__ __forceinline__ void look_back(const Chain &q, int pos, float first, const Words &k, float2 (*pre)[kSlice], float *at) {
-  const int ch = threadIdx.x & 63, w = threadIdx.x >> 6, seg = pos / kSeg, in = pos % kSeg;
-  const unsigned long long *p = q.pairs + ((long long)seg * kSeg + w * 4) * kSlice + ch;
+// At, Bt: the tile's own pair
+__device__ __forceinline__ float look_back(const Chain &q, int pos, bool last, float At, float Bt, float first, const Words &k) {
+  const int ch = threadIdx.x & 63, seg = pos / kSeg, in = pos % kSeg;
+  const unsigned long long *p = q.pairs + (long long)seg * kSeg * kSlice + ch;
   float A = 1.f, B = 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (w * 4 + j < in) {
+  for (int j = 0; j < kSeg - 1; ++j) {
+    if (j < in) {
       const unsigned long long v = await_word(p + j * kSlice, k.v[j]);
       const float A2 = high_of(v);
       B = fmaf(A2, B, low_of(v));
       A *= A2;
     }
   }
-  pre[w][ch] = make_float2(A, B);
-  if (w == 0) at[ch] = seg > 0 ? low_of(await_word(q.states + (long long)(seg - 1) * kSlice + ch, k.state)) : pos == 0 ? first : 0.f;
+  const float A2 = At * A, B2 = fmaf(At, B, Bt);
+  const float at = seg > 0 ? low_of(await_word(q.states + (long long)(seg - 1) * kSlice + ch, k.state)) : pos == 0 ? first : 0.f;
+  if (in == kSeg - 1 && !last) put_word(q.states + (long long)seg * kSlice + ch, fmaf(A2, at, B2), 1u);
+  return fmaf(A, at, B);
 }
 __device__ __forceinline__ void publish_pair(const Chain &q, int pos, float A, float B, float first) {
   put_word(q.pairs + (long long)pos * kSlice + (threadIdx.x & 63), pos == 0 ? fmaf(A, first, B) : B, pair_high(pos == 0 ? 0.f : A));
@@ -219,12 +223,19 @@ __global__ __launch_bounds__(256) void clear_words_kernel(unsigned long long *p,
 }
 
 // What a workgroup shares.
-struct Shared {
-  float tot[4][kSlice][3];           // a wave's A, forward B, reverse B
-  float2 pre[4][kSlice];
+struct alignas(16) Shared {
+  float2 tot[4][kSlice], back[4][kSlice];      // each wave's pair, forward and backward in time
+  float2 part[4][kSlice];                      // what lies between the tile's start (the chain's way) and each wave's
+  float h[4][kSlice];                          // backward: the state in front of each wave
   float at[kSlice];
   unsigned number;
 };
+
+// The pairs of two channels next to each other, and the state behind them.
+__device__ __forceinline__ void apply_pairs(const float2 *p, float (&h)[2]) {
+  const float4 v = *reinterpret_cast<const float4 *>(p);
+  h[0] = fmaf(v.x, h[0], v.y), h[1] = fmaf(v.z, h[1], v.w);
+}
 
 // What was computed from r before is not kept for later, it is computed again: registers are what limits the waves of a compute unit.
 template <typename R>
@@ -238,7 +249,7 @@ __device__ __forceinline__ R forget(R r) {
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.  ONE: see Lane.
-template <typename T, bool GATED, bool WHOLE, bool ONE>
+template <typename T, bool GATED, bool WHOLE, bool ONE, bool ALONE>
 __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
   constexpr int L = kFwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -250,14 +261,15 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
   Raw<T> ur[L], gr[L], orr[L];
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE>(g.at(i), q), ur[i] = raw2<T, ONE>(u.at(i), q);
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, ALONE>(g.at(i), q), ur[i] = raw2<T, ONE, ALONE>(u.at(i), q);
   if (GATED) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE>(o.at(i), q);
+    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE, ALONE>(o.at(i), q);
   }
   float bias[2] = {0.f, 0.f};
   if (P.bias) floats2(P.bias + q.c, q, bias);
-  const Words words = look_early(links, tile);
+  Words words;
+  if (wave == 0) words = look_early(links, tile);
   float a[L][2], bb[L][2], A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Ae[2], Be[2];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -276,34 +288,33 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   for (int k = 0; k < 2; ++k) {
     const float A1 = other_half(A[k]), B1 = other_half(B[k]);
     Ae[k] = upper ? A1 : 1.f, Be[k] = upper ? B1 : 0.f;
-    if (upper) S.tot[wave][cl + k][0] = A[k] * A1, S.tot[wave][cl + k][1] = fmaf(A[k], B1, B[k]);
+    if (upper) S.tot[wave][cl + k] = make_float2(A[k] * A1, fmaf(A[k], B1, B[k]));
   }
   __syncthreads();
   const int ch = threadIdx.x & 63, c = slice * kSlice + ch;
-  float At = 1.f, Bt = 0.f;                                // the whole tile's pair, channel ch
+  if (wave == 0) {
+    float At = 1.f, Bt = 0.f, first = 0.f;                 // the whole tile's pair, channel ch
 #pragma unroll
-  for (int w = 0; w < 4; ++w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][1]), At *= S.tot[w][ch][0];
-  const float first = wave == 0 && tile == 0 && P.h0 && c < P.D ? P.h0[(long long)b * P.D + c] : 0.f;
-  if (wave == 0 && tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
-  look_back(links, tile, first, words, S.pre, S.at);
+    for (int w = 0; w < 4; ++w) Bt = fmaf(S.tot[w][ch].x, Bt, S.tot[w][ch].y), At *= S.tot[w][ch].x;
+    if (tile == 0 && P.h0 && c < P.D) first = P.h0[(long long)b * P.D + c];
+    if (tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
+    S.at[ch] = look_back(links, tile, tile + 1 == P.tiles, At, Bt, first, words);
+  } else if (wave == 1) {
+    float2 v = make_float2(1.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      S.part[w][ch] = v;
+      v = make_float2(v.x * S.tot[w][ch].x, fmaf(S.tot[w][ch].x, v.y, S.tot[w][ch].y));
+    }
+  }
   __syncthreads();
-  if (wave == 0 && tile % kSeg == kSeg - 1 && tile + 1 < P.tiles) {
-    float h = S.at[ch];
+  float h[2] = {S.at[cl], S.at[cl + 1]};
+  apply_pairs(&S.part[wave][cl], h);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) h = fmaf(S.pre[w][ch].x, h, S.pre[w][ch].y);
-    put_word(links.states + (long long)(tile / kSeg) * kSlice + ch, fmaf(At, h, Bt), 1u);
-  }
-  float h[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    h[k] = S.at[cl + k];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) h[k] = fmaf(S.pre[w][cl + k].x, h[k], S.pre[w][cl + k].y);
-    for (int w = 0; w < wave; ++w) h[k] = fmaf(S.tot[w][cl + k][0], h[k], S.tot[w][cl + k][1]);
-    h[k] = fmaf(Ae[k], h[k], Be[k]);
-  }
+  for (int k = 0; k < 2; ++k) h[k] = fmaf(Ae[k], h[k], Be[k]);
   if (P.saved && (grp * L) % kSaved == 0 && tk < P.len)
     store_n<float, 2>(P.saved + (b * ((P.len + kSaved - 1) / kSaved) + tk / kSaved) * P.D + q.c, q.n, h);
+  if (q.n == 0) return;
 #pragma unroll
   for (int i = 0; i < L; ++i) {
     float out[2];
@@ -322,7 +333,7 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   if (P.hT && tile + 1 == P.tiles && grp == 7) store_n<float, 2>(P.hT + (long long)b * P.D + q.c, q.n, h);
 }
 
-template <typename T, bool GATED>
+template <typename T, bool GATED, bool ALONE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
@@ -331,13 +342,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_ke
   const int tile = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (q.one) fwd_tile<T, GATED, false, true>(P, S, tile, chain, q, len);
-  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false>(P, S, tile, chain, q, len);
-  else fwd_tile<T, GATED, true, false>(P, S, tile, chain, q, len);
+  if (!ALONE && q.one) fwd_tile<T, GATED, false, true, false>(P, S, tile, chain, q, len);
+  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false, ALONE>(P, S, tile, chain, q, len);
+  else fwd_tile<T, GATED, true, false, ALONE>(P, S, tile, chain, q, len);
 }
 
-template <typename T, bool GATED, bool WHOLE, bool ONE>
-__device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*sum)[kSlice], int pos, int chain, const Lane &q, int len) {
+template <typename T, bool GATED, bool WHOLE, bool ONE, bool ALONE>
+__device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, int chain, const Lane &q, int len) {
   constexpr int L = kBwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
   const int tile = P.tiles - 1 - pos;       // the chain starts at the last tile
@@ -350,15 +361,16 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
   Raw<T> ur[L], gr[L], orr[L], yr[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    gr[i] = raw2<T, ONE>(g.at(i), q);
-    ur[i] = raw2<T, ONE>(u.at(i), q);
-    yr[i] = raw2<T, ONE>(dy.at(i), q);
-    if (GATED) orr[i] = raw2<T, ONE>(o.at(i), q);
+    gr[i] = raw2<T, ONE, ALONE>(g.at(i), q);
+    ur[i] = raw2<T, ONE, ALONE>(u.at(i), q);
+    yr[i] = raw2<T, ONE, ALONE>(dy.at(i), q);
+    if (GATED) orr[i] = raw2<T, ONE, ALONE>(o.at(i), q);
   }
-  float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, h[2];
+  float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
   if (P.bias) floats2(P.bias + q.c, q, bias);
-  floats2(P.saved + ((long long)b * P.tiles + tile) * P.D + q.c, q, h);
-  const Words words = look_early(links, pos);
+  if (wave == 2 && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
+  Words words;
+  if (wave == 0) words = look_early(links, pos);
   if (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < L; ++i)
@@ -384,50 +396,54 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
   for (int i = L - 1; i >= 0; --i)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const float ov = GATED ? static_cast<float>(orr[i][k]) : 0.f;
+      const float ov = GATED ? static_cast<float>(orr[i][k]) : 0.f, yv = static_cast<float>(yr[i][k]);
       sg[i][k] = GATED ? sigmoid(ov) : 1.f;
-      const float c = GATED ? static_cast<float>(yr[i][k]) * (ov * sg[i][k]) : static_cast<float>(yr[i][k]);
-      Br[k] = a[i][k] * (c + Br[k]);
+      const float c = GATED ? yv * (ov * sg[i][k]) : yv;
+      Br[k] = i == L - 1 ? c : fmaf(a[i + 1 < L ? i + 1 : i][k], Br[k], c);      // dh
     }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
+    Br[k] *= a[0][k];
     const float A1 = other_half(A[k]), B1 = other_half(B[k]), R1 = other_half(Br[k]);
     Ae[k] = upper ? A1 : 1.f, Be[k] = upper ? B1 : 0.f;
     Ax[k] = upper ? 1.f : A1, Bx[k] = upper ? 0.f : R1;
-    if (upper) S.tot[wave][cl + k][0] = A[k] * A1, S.tot[wave][cl + k][1] = fmaf(A[k], B1, B[k]);
-    else S.tot[wave][cl + k][2] = fmaf(A[k], R1, Br[k]);
+    if (upper) S.tot[wave][cl + k] = make_float2(A[k] * A1, fmaf(A[k], B1, B[k]));
+    else S.back[wave][cl + k] = make_float2(A[k] * A1, fmaf(A[k], R1, Br[k]));
   }
   __syncthreads();
   const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
-  float At = 1.f, Bt = 0.f;
+  if (wave == 0) {
+    float At = 1.f, Bt = 0.f, first = 0.f;
 #pragma unroll
-  for (int w = 3; w >= 0; --w) Bt = fmaf(S.tot[w][ch][0], Bt, S.tot[w][ch][2]), At *= S.tot[w][ch][0];
-  const float first = wave == 0 && pos == 0 && P.dhT && cc < P.D ? P.dhT[(long long)b * P.D + cc] : 0.f;
-  if (wave == 0 && tile > 0) publish_pair(links, pos, At, Bt, first);
-  look_back(links, pos, first, words, S.pre, S.at);
-  __syncthreads();
-  if (wave == 0 && pos % kSeg == kSeg - 1 && tile > 0) {
-    float e = S.at[ch];
+    for (int w = 3; w >= 0; --w) Bt = fmaf(S.back[w][ch].x, Bt, S.back[w][ch].y), At *= S.back[w][ch].x;
+    if (pos == 0 && P.dhT && cc < P.D) first = P.dhT[(long long)b * P.D + cc];
+    if (tile > 0) publish_pair(links, pos, At, Bt, first);
+    S.at[ch] = look_back(links, pos, tile == 0, At, Bt, first, words);
+  } else if (wave == 1) {
+    float2 v = make_float2(1.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) e = fmaf(S.pre[w][ch].x, e, S.pre[w][ch].y);
-    put_word(links.states + (long long)(pos / kSeg) * kSlice + ch, fmaf(At, e, Bt), 1u);
+    for (int w = 3; w >= 0; --w) {
+      S.part[w][ch] = v;
+      v = make_float2(v.x * S.back[w][ch].x, fmaf(S.back[w][ch].x, v.y, S.back[w][ch].y));
+    }
+  } else if (wave == 2) {
+    float v = saved;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      S.h[w][ch] = v;
+      v = fmaf(S.tot[w][ch].x, v, S.tot[w][ch].y);
+    }
   }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < L; ++i) {
     ur[i] = forget(ur[i]), yr[i] = forget(yr[i]);
     if (GATED) orr[i] = forget(orr[i]);
   }
-  float e[2];
+  float h[2] = {S.h[wave][cl], S.h[wave][cl + 1]}, e[2] = {S.at[cl], S.at[cl + 1]};
+  apply_pairs(&S.part[wave][cl], e);
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    for (int w = 0; w < wave; ++w) h[k] = fmaf(S.tot[w][cl + k][0], h[k], S.tot[w][cl + k][1]);
-    h[k] = fmaf(Ae[k], h[k], Be[k]);
-    e[k] = S.at[cl + k];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) e[k] = fmaf(S.pre[w][cl + k].x, e[k], S.pre[w][cl + k].y);
-    for (int w = 3; w > wave; --w) e[k] = fmaf(S.tot[w][cl + k][0], e[k], S.tot[w][cl + k][2]);
-    e[k] = fmaf(Ax[k], e[k], Bx[k]);
-  }
+  for (int k = 0; k < 2; ++k) h[k] = fmaf(Ae[k], h[k], Be[k]), e[k] = fmaf(Ax[k], e[k], Bx[k]);
 #pragma unroll
   for (int i = 0; i < L; ++i)
 #pragma unroll
@@ -437,53 +453,55 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, float (*su
     }
   const Place<T, L, WHOLE> du(P.du, b * P.dub, P.dus, t0, slice, q, P.len), dgp(P.dg, b * P.dgb, P.dgs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> dop(P.dou, b * P.dob, P.dos, t0, slice, q, P.len);
+  if (q.n > 0) {
+    float dh[2];
 #pragma unroll
-  for (int i = L - 1; i >= 0; --i) {
-    float dv[2], dg[2], dou[2];
-    const bool live = WHOLE || tk + i < len;
+    for (int i = L - 1; i >= 0; --i) {
+      float dv[2], dg[2], dou[2];
+      const bool live = WHOLE || tk + i < len;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float s = sg[i][k], yv = static_cast<float>(yr[i][k]), ov = GATED ? static_cast<float>(orr[i][k]) : 0.f;
-      const float dh = (GATED ? yv * (ov * s) : yv) + e[k], hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k];
-      dv[k] = live ? z[i][k] * dh : 0.f;
-      dg[k] = live ? dh * (hb[i][k] - static_cast<float>(ur[i][k])) * (a[i][k] * z[i][k]) : 0.f;
-      if (GATED) dou[k] = live ? yv * hi * (s * (1.f + ov * (1.f - s))) : 0.f;
-      e[k] = a[i][k] * dh;
-      db[k] += dg[k];
+      for (int k = 0; k < 2; ++k) {
+        const float s = sg[i][k], yv = static_cast<float>(yr[i][k]), ov = GATED ? static_cast<float>(orr[i][k]) : 0.f, t = ov * s;
+        const float hi = i + 1 < L ? hb[i + 1 < L ? i + 1 : i][k] : h[k], in = i == L - 1 ? e[k] : a[i + 1 < L ? i + 1 : i][k] * dh[k];
+        dh[k] = GATED ? fmaf(yv, t, in) : yv + in;
+        dv[k] = live ? z[i][k] * dh[k] : 0.f;
+        dg[k] = live ? (hb[i][k] - static_cast<float>(ur[i][k])) * a[i][k] * dv[k] : 0.f;
+        if (GATED) dou[k] = live ? yv * hi * fmaf(t, 1.f - s, s) : 0.f;
+        db[k] += dg[k];
+      }
+      if (WHOLE || tk + i < P.len) {
+        put2<T, ONE>(du.at(i), q, dv);
+        put2<T, ONE>(dgp.at(i), q, dg);
+        if (GATED) put2<T, ONE>(dop.at(i), q, dou);
+      }
     }
-    if (WHOLE || tk + i < P.len) {
-      put2<T, ONE>(du.at(i), q, dv);
-      put2<T, ONE>(dgp.at(i), q, dg);
-      if (GATED) put2<T, ONE>(dop.at(i), q, dou);
-    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) e[k] = a[0][k] * dh[k];
   }
   if (P.dh0 && tile == 0 && grp == 0) store_n<float, 2>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
   if (P.dbias_partial) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) sum[grp][cl + k] = db[k];
-    __syncthreads();
-    if (wave == 0 && cc < P.D) {
-      float v = 0.f;
-#pragma unroll
-      for (int r = 0; r < 8; ++r) v += sum[r][ch];
-      P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = v;
+    for (int k = 0; k < 2; ++k) {
+      const float v = db[k] + other_half(db[k]);
+      if (!upper) S.h[wave][cl + k] = v;        // each wave's own, which only it read
     }
+    __syncthreads();
+    if (wave == 0 && cc < P.D) P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = (S.h[0][ch] + S.h[1][ch]) + (S.h[2][ch] + S.h[3][ch]);
   }
 }
 
-template <typename T, bool GATED>
+template <typename T, bool GATED, bool ALONE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
   __shared__ Shared S;
-  __shared__ float sum[8][kSlice];
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
   if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work + chain * words_of_chain(P.tiles), 1ull);
   __syncthreads();
   const int pos = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (q.one) bwd_tile<T, GATED, false, true>(P, S, sum, pos, chain, q, len);
-  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false>(P, S, sum, pos, chain, q, len);
-  else bwd_tile<T, GATED, true, false>(P, S, sum, pos, chain, q, len);
+  if (!ALONE && q.one) bwd_tile<T, GATED, false, true, false>(P, S, pos, chain, q, len);
+  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false, ALONE>(P, S, pos, chain, q, len);
+  else bwd_tile<T, GATED, true, false, ALONE>(P, S, pos, chain, q, len);
 }
 
 // One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
@@ -531,6 +549,11 @@ void clear_words(unsigned long long *p, long long n, hipStream_t st) {
   clear_words_kernel<<<(unsigned)(blocks < 2048 ? blocks : 2048), 256, 0, st>>>(p, n);
 }
 
+// Whether a tile's rows in this tensor are whole cache lines.
+inline bool lines(const void *p, long long batch_stride, long long stride, int size) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(batch_stride * size) | (uintptr_t)(stride * size)) & 127) == 0;
+}
+
 template <typename T>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   if (A.len <= 16) {
@@ -539,9 +562,13 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
     else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
   } else {
     const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
+    const int size = sizeof(T);
+    const bool alone = A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && (!A.o || lines(A.o, A.ob, A.os, size));
     clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-    if (A.o) recurrence_fwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
-    else recurrence_fwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
+    if (A.o && alone) recurrence_fwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
+    else if (A.o) recurrence_fwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
+    else if (alone) recurrence_fwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
+    else recurrence_fwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
   }
   return hipGetLastError();
 }
@@ -549,9 +576,14 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
+  const int size = sizeof(T);
+  const bool alone = A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
+                     (!A.o || lines(A.o, A.ob, A.os, size));
   clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-  if (A.o) recurrence_bwd_kernel<T, true><<<grid, 256, 0, st>>>(A);
-  else recurrence_bwd_kernel<T, false><<<grid, 256, 0, st>>>(A);
+  if (A.o && alone) recurrence_bwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
+  else if (A.o) recurrence_bwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
+  else if (alone) recurrence_bwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
+  else recurrence_bwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
