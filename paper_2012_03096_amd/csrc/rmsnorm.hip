@@ -12,7 +12,21 @@ namespace pbkd {
 namespace {
 
 constexpr int kMaxD = 16384;         // 1024 threads x 2 items x 8 elements: four items spill in the backward kernel
-constexpr int kBwdGroups = 512;      // workgroups of the backward kernel: each leaves one row of weight-gradient partials
+
+// Threads to a row: eight elements each as long as that goes.  Measured (bf16): 16383 rows of 4096 forward to e4m3, 512 threads
+// 86 us, 256 threads with 16 elements 97 us, 64 with 64 elements 130 us; 32768 rows of 2048 backward, 256 threads 126 us, 64 with
+// 32 elements 167 us: more waves with fewer registers keep more reads on their way, which is worth the barrier in the sums.
+inline int row_threads(int d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
+
+// Workgroups of the backward kernel: two waves for each SIMD, with the next row on its way (four: 203 against 198 us for 32768 rows of
+// 2048 forward and backward, and twice the partials).  Each leaves one row of weight-gradient partials.
+constexpr int kBwdThreads = 128 * 1024;
+inline int bwd_groups(long long rows, int d) {
+  const int tpr = row_threads(d);
+  const long long groups = tpr == 64 ? cdiv64(rows, 4) : rows;
+  const int most = kBwdThreads / (tpr == 64 ? 256 : tpr);
+  return (int)(groups < most ? groups : most);
+}
 
 struct FwdArgs {
   const void *x, *res;
@@ -50,8 +64,8 @@ __device__ __forceinline__ float row_reduce(float v, float *slot) {
 }
 
 template <typename T, int TPR, int ITEMS, bool FP8>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdArgs A) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;     // rows a workgroup works on at a time
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdArgs A) {
+  constexpr int RPB = TPR == 64 ? 4 : 1;             // rows a workgroup works on at a time
   __shared__ float red[4][16];
   const int lane = threadIdx.x % TPR, d = A.d;
   float w[ITEMS][8];
@@ -141,55 +155,87 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
   }
 }
 
-// A workgroup goes through its rows with the weight gradient of its own columns in registers and leaves one row of
-// partials; with a wave to a row its four waves' sums are joined through LDS first.
+template <typename T>
+using Raw = typename VecOf<T, 8>::type;
+template <typename T>
+__device__ __forceinline__ Raw<T> raw_n(const T *p, int n) {
+  Raw<T> r;
+  if (n >= 8) {
+    r = *reinterpret_cast<const Raw<T> *>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = i < n ? p[i] : T(0.f);
+  }
+  return r;
+}
+
+// A workgroup goes through its rows with the weight gradient of its own columns in registers, the next row on its way while it
+// works on one, and leaves one row of partials; with a wave to a row its four waves' sums are joined through LDS first.
 template <typename T, int TPR, int ITEMS>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdArgs A) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdArgs A) {
+  constexpr int RPB = TPR == 64 ? 4 : 1;
+  constexpr bool AHEAD = ITEMS == 1;      // with two items the next row does not fit in the registers
   __shared__ float red[4][16];
   __shared__ float join[RPB > 1 ? (RPB - 1) * TPR * ITEMS * 8 : 1];
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = A.d;
-  float dw[ITEMS][8] = {};
-  int flip = 0;
-  for (long long row = (long long)blockIdx.x * RPB + sub; row < A.rows; row += (long long)gridDim.x * RPB, flip ^= 2) {
-    float s[ITEMS][8], g[ITEMS][8];
-    const T *tp = static_cast<const T *>(A.total) + row * A.ts, *yp = static_cast<const T *>(A.dy) + row * A.ys;
+  const T *tp = static_cast<const T *>(A.total), *yp = static_cast<const T *>(A.dy), *gp = static_cast<const T *>(A.dtotal);
+  T *xp = static_cast<T *>(A.dx);
+  float dw[ITEMS][8] = {}, w[ITEMS][8];
+  Raw<T> s[ITEMS], y[ITEMS], g[ITEMS];
+  long long row = (long long)blockIdx.x * RPB + sub;
+  const long long step = (long long)gridDim.x * RPB;
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      const int c = (k * TPR + lane) * 8;
-      load_n<T, 8>(tp + c, d - c, s[k]);
-      load_n<T, 8>(yp + c, d - c, g[k]);
+  for (int k = 0; k < ITEMS; ++k) {
+    const int c = (k * TPR + lane) * 8;
+    load_n<float, 8>(A.w + c, d - c, w[k]);
+    if (AHEAD && row < A.rows) {
+      s[k] = raw_n(tp + row * A.ts + c, d - c), y[k] = raw_n(yp + row * A.ys + c, d - c);
+      if (A.dtotal) g[k] = raw_n(gp + row * A.gs + c, d - c);
     }
-    float ss = 0.f, gs = 0.f;
+  }
+  int flip = 0;
+  for (; row < A.rows; row += step, flip ^= 2) {
+    float sv[ITEMS][8], yv[ITEMS][8], ss = 0.f, gs = 0.f;
+    Raw<T> gr[ITEMS];
+    const long long next = row + step;
+    if (!AHEAD) {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const int c = (k * TPR + lane) * 8;
+        s[k] = raw_n(tp + row * A.ts + c, d - c), y[k] = raw_n(yp + row * A.ys + c, d - c);
+        if (A.dtotal) g[k] = raw_n(gp + row * A.gs + c, d - c);
+      }
+    }
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       const int c = (k * TPR + lane) * 8;
-      float w[8];
-      load_n<float, 8>(A.w + c, d - c, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        ss = fmaf(s[k][i], s[k][i], ss);
-        gs = fmaf(g[k][i] * w[i], s[k][i], gs);
+        sv[k][i] = static_cast<float>(s[k][i]), yv[k][i] = static_cast<float>(y[k][i]);
+        ss = fmaf(sv[k][i], sv[k][i], ss);
+        gs = fmaf(yv[k][i] * w[k][i], sv[k][i], gs);
+      }
+      gr[k] = g[k];
+      if (AHEAD && next < A.rows) {
+        s[k] = raw_n(tp + next * A.ts + c, d - c), y[k] = raw_n(yp + next * A.ys + c, d - c);
+        if (A.dtotal) g[k] = raw_n(gp + next * A.gs + c, d - c);
       }
     }
     ss = row_reduce<TPR, false>(ss, red[flip]);
     gs = row_reduce<TPR, false>(gs, red[flip + 1]);
     const float r = 1.f / sqrtf(ss / d + A.eps), mean = gs * r / d;
-    T *xp = static_cast<T *>(A.dx) + row * A.xs;
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       const int c = (k * TPR + lane) * 8;
-      float w[8], e[8], v[8];
-      load_n<float, 8>(A.w + c, d - c, w);
-      if (A.dtotal) load_n<T, 8>(static_cast<const T *>(A.dtotal) + row * A.gs + c, d - c, e);
+      float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float xh = s[k][i] * r;
-        v[i] = r * (g[k][i] * w[i] - xh * mean);
-        if (A.dtotal) v[i] += e[i];
-        dw[k][i] = fmaf(g[k][i], xh, dw[k][i]);
+        const float xh = sv[k][i] * r;
+        v[i] = r * (yv[k][i] * w[k][i] - xh * mean);
+        if (A.dtotal) v[i] += static_cast<float>(gr[k][i]);
+        dw[k][i] = fmaf(yv[k][i], xh, dw[k][i]);
       }
-      store_n<T, 8>(xp + c, d - c, v);
+      store_n<T, 8>(xp + row * A.xs + c, d - c, v);
     }
   }
   if (RPB > 1) {
@@ -215,60 +261,69 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdA
   }
 }
 
-// out[slab][c] = sum of the slab's rows of partial[rows][cols]: 64 columns a workgroup, a slab of rows over its 16
-// groups of 64 threads, which are joined in order.  rows == 0 writes zeros.
+// out[slab][c] = sum of the slab's rows of partial[rows][cols]: 16 columns a workgroup, a slab's rows over 64 groups of 16
+// threads, which are joined in order.  rows == 0 writes zeros.
 __global__ __launch_bounds__(1024) void colsum_kernel(const float *partial, long long rows, int cols, int per_slab, float *out) {
-  __shared__ float part[16][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  __shared__ float part[64][17];
+  const int lane = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
   const long long lo = (long long)blockIdx.y * per_slab, hi = lo + per_slab < rows ? lo + per_slab : rows;
   float v = 0.f;
   if (c < cols) {
-#pragma unroll 8
-    for (long long r = lo + g; r < hi; r += 16) v += partial[r * cols + c];
+#pragma unroll 16
+    for (long long r = lo + g; r < hi; r += 64) v += partial[r * cols + c];
   }
   part[g][lane] = v;
   __syncthreads();
+  if (g < 8) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += part[g + 8 * k][lane];
+    part[g][lane] = v;       // only this thread reads or writes it here
+  }
+  __syncthreads();
   if (g == 0 && c < cols) {
 #pragma unroll
-    for (int k = 1; k < 16; ++k) v += part[k][lane];
+    for (int k = 1; k < 8; ++k) v += part[k][lane];
     out[(long long)blockIdx.y * cols + c] = v;
   }
 }
 
-constexpr int kSlab = 512;
+constexpr int kSlab = 2048;
+static_assert(kBwdThreads / 128 <= kSlab, "the norm's partials are summed in one pass, without scratch");
 
 template <typename T, bool FP8>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   const int d = A.d;
-#define FWD(TPR, ITEMS)                                                                                                  \
-  rmsnorm_fwd_kernel<T, TPR, ITEMS, FP8>                                                                                 \
-      <<<(unsigned)(cdiv64(A.rows, TPR < 256 ? 256 / TPR : 1) < 2048 ? cdiv64(A.rows, TPR < 256 ? 256 / TPR : 1) : 2048), \
-         TPR < 256 ? 256 : TPR, 0, st>>>(A)
-  if (d <= 512) FWD(64, 1);
-  else if (d <= 1024) FWD(64, 2);
-  else if (d <= 2048) FWD(64, 4);
-  else if (d <= 4096) FWD(256, 2);
-  else if (d <= 8192) FWD(256, 4);
-  else FWD(1024, 2);
+#define FWD(TPR, ITEMS)                                                                                              \
+  {                                                                                                                  \
+    const long long groups = cdiv64(A.rows, TPR == 64 ? 4 : 1);                                                      \
+    rmsnorm_fwd_kernel<T, TPR, ITEMS, FP8><<<(unsigned)(groups < 4096 ? groups : 4096), TPR == 64 ? 256 : TPR, 0, st>>>(A); \
+  }
+  switch (row_threads(d)) {
+    case 64: FWD(64, 1) break;
+    case 128: FWD(128, 1) break;
+    case 256: FWD(256, 1) break;
+    case 512: FWD(512, 1) break;
+    default:
+      if (d <= 8192) FWD(1024, 1)
+      else FWD(1024, 2)
+  }
 #undef FWD
   return hipGetLastError();
-}
-
-inline int bwd_groups(long long rows, int d) {
-  const long long per = d <= 2048 ? cdiv64(rows, 4) : rows;      // rows are taken four at a time by a wave each, or one at a time
-  return (int)(per < kBwdGroups ? per : kBwdGroups);
 }
 
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, int groups, hipStream_t st) {
   const int d = A.d;
-#define BWD(TPR, ITEMS) rmsnorm_bwd_kernel<T, TPR, ITEMS><<<groups, TPR < 256 ? 256 : TPR, 0, st>>>(A)
-  if (d <= 512) BWD(64, 1);
-  else if (d <= 1024) BWD(64, 2);
-  else if (d <= 2048) BWD(64, 4);
-  else if (d <= 4096) BWD(256, 2);
-  else if (d <= 8192) BWD(256, 4);
-  else BWD(1024, 2);
+#define BWD(TPR, ITEMS) rmsnorm_bwd_kernel<T, TPR, ITEMS><<<groups, TPR == 64 ? 256 : TPR, 0, st>>>(A);
+  switch (row_threads(d)) {
+    case 64: BWD(64, 1) break;
+    case 128: BWD(128, 1) break;
+    case 256: BWD(256, 1) break;
+    case 512: BWD(512, 1) break;
+    default:
+      if (d <= 8192) BWD(1024, 1)
+      else BWD(1024, 2)
+  }
 #undef BWD
   return hipGetLastError();
 }
@@ -290,10 +345,10 @@ size_t colsum_scratch_floats(long long rows, int cols) { return rows > kSlab ? (
 hipError_t launch_colsum(const float *partial, long long rows, int cols, float *scratch, float *out, hipStream_t st) {
   while (rows > kSlab) {
     const long long slabs = cdiv64(rows, kSlab);
-    colsum_kernel<<<dim3((cols + 63) / 64, (unsigned)slabs), 1024, 0, st>>>(partial, rows, cols, kSlab, scratch);
+    colsum_kernel<<<dim3((cols + 15) / 16, (unsigned)slabs), 1024, 0, st>>>(partial, rows, cols, kSlab, scratch);
     partial = scratch, scratch += slabs * cols, rows = slabs;
   }
-  colsum_kernel<<<dim3((cols + 63) / 64, 1), 1024, 0, st>>>(partial, rows, cols, kSlab, out);
+  colsum_kernel<<<dim3((cols + 15) / 16, 1), 1024, 0, st>>>(partial, rows, cols, kSlab, out);
   return hipGetLastError();
 }
 
@@ -360,7 +415,7 @@ pbkd_status pbkd_rmsnorm_backward(const pbkd_rmsnorm_grad_desc *q, void *hip_str
       default: SEQ_HIPCHK(launch_bwd<f16>(A, groups, st)); break;
     }
   }
-  SEQ_HIPCHK(launch_colsum(partial, groups, q->d, nullptr, q->dweight_dev, st));     // at most kBwdGroups rows: no scratch
+  SEQ_HIPCHK(launch_colsum(partial, groups, q->d, nullptr, q->dweight_dev, st));     // at most kSlab rows: no scratch
   return PBKD_OK;
 }
 
