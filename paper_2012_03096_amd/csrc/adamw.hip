@@ -52,7 +52,7 @@ __device__ __forceinline__ float random_e4m3(float x, unsigned up) {
   return x > 0.f ? (x < 0x1p-6f ? small : large) : x * 0.f;      // a NaN stays one
 }
 
-template <typename P, typename G, bool EIGHT>
+template <typename P, typename G, bool EIGHT, bool FAR>
 __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, long long chunk) {
 // products and sums keep their own roundings: the same figures as the formulas, operation by operation
 #pragma clang fp contract(off)
@@ -63,17 +63,17 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
   for (int k = 0; k < kRounds; ++k) {
     const long long e = base + k * kBlock, left = t.n - e;
     const int n = left < 4 ? (int)(left < 0 ? 0 : left) : 4;
-    load_n<P, 4>(static_cast<const P *>(t.p) + e, n, p[k]);
-    load_n<G, 4>(static_cast<const G *>(t.g) + e, n, g[k]);
+    load_n<P, 4, FAR>(static_cast<const P *>(t.p) + e, n, p[k]);
+    load_n<G, 4, FAR>(static_cast<const G *>(t.g) + e, n, g[k]);
     if (!EIGHT) {
-      load_n<float, 4>(static_cast<const float *>(t.m) + e, n, m[k]);
-      load_n<float, 4>(static_cast<const float *>(t.v) + e, n, v[k]);
+      load_n<float, 4, FAR>(static_cast<const float *>(t.m) + e, n, m[k]);
+      load_n<float, 4, FAR>(static_cast<const float *>(t.v) + e, n, v[k]);
     } else {
       typedef unsigned u1 __attribute__((aligned(1)));
       unsigned mc = 0, vc = 0;
       const unsigned char *mp = static_cast<const unsigned char *>(t.m) + e, *vp = static_cast<const unsigned char *>(t.v) + e;
       if (n == 4) {
-        mc = *reinterpret_cast<const u1 *>(mp), vc = *reinterpret_cast<const u1 *>(vp);
+        mc = far_load<FAR>(reinterpret_cast<const u1 *>(mp)), vc = far_load<FAR>(reinterpret_cast<const u1 *>(vp));
       } else {
         for (int i = 0; i < n; ++i) mc |= (unsigned)mp[i] << (8 * i), vc |= (unsigned)vp[i] << (8 * i);
       }
@@ -112,11 +112,11 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       mtop = fmaxf(mtop, fabsf(m[k][i]));
       vtop = fmaxf(vtop, root[i]);
     }
-    store_n<P, 4>(static_cast<P *>(t.p) + e, n, p[k]);
-    if (sizeof(P) == 4 && t.copy) store_n<bf16, 4>(static_cast<bf16 *>(t.copy) + e, n, p[k]);
+    store_n<P, 4, FAR>(static_cast<P *>(t.p) + e, n, p[k]);
+    if (sizeof(P) == 4 && t.copy) store_n<bf16, 4, FAR>(static_cast<bf16 *>(t.copy) + e, n, p[k]);
     if (!EIGHT) {
-      store_n<float, 4>(static_cast<float *>(t.m) + e, n, m[k]);
-      store_n<float, 4>(static_cast<float *>(t.v) + e, n, v[k]);
+      store_n<float, 4, FAR>(static_cast<float *>(t.m) + e, n, m[k]);
+      store_n<float, 4, FAR>(static_cast<float *>(t.v) + e, n, v[k]);
     } else {
       mtop = fmaxf(wave64_max(mtop), 0x1p-100f), vtop = fmaxf(wave64_max(vtop), 0x1p-100f);
       const float mi = 1.f / mtop * 448.f, vi = 1.f / vtop * 448.f;
@@ -131,7 +131,7 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       typedef unsigned u1 __attribute__((aligned(1)));
       unsigned char *mp = static_cast<unsigned char *>(t.m) + e, *vp = static_cast<unsigned char *>(t.v) + e;
       if (n == 4) {
-        *reinterpret_cast<u1 *>(mp) = mc, *reinterpret_cast<u1 *>(vp) = vc;
+        far_store<FAR>((u1)mc, reinterpret_cast<u1 *>(mp)), far_store<FAR>((u1)vc, reinterpret_cast<u1 *>(vp));
       } else {
         for (int i = 0; i < n; ++i) mp[i] = (unsigned char)(mc >> (8 * i)), vp[i] = (unsigned char)(vc >> (8 * i));
       }
@@ -140,7 +140,7 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
   }
 }
 
-template <bool EIGHT>
+template <bool EIGHT, bool FAR>
 __global__ __launch_bounds__(256) void adamw_kernel(Launch L) {
   int lo = 0, hi = L.tensors - 1;              // the last tensor that starts at or before this chunk
   while (lo < hi) {
@@ -151,12 +151,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(Launch L) {
   const Tensor &t = L.t[lo];
   const long long chunk = blockIdx.x - L.chunk0[lo];
   switch (L.kind[lo]) {
-    case 0: adamw_chunk<float, float, EIGHT>(L, t, chunk); break;
-    case 1: adamw_chunk<bf16, float, EIGHT>(L, t, chunk); break;
-    case 2: adamw_chunk<float, bf16, EIGHT>(L, t, chunk); break;
-    case 3: adamw_chunk<bf16, bf16, EIGHT>(L, t, chunk); break;
-    case 4: adamw_chunk<float, f16, EIGHT>(L, t, chunk); break;
-    default: adamw_chunk<bf16, f16, EIGHT>(L, t, chunk); break;
+    case 0: adamw_chunk<float, float, EIGHT, FAR>(L, t, chunk); break;
+    case 1: adamw_chunk<bf16, float, EIGHT, FAR>(L, t, chunk); break;
+    case 2: adamw_chunk<float, bf16, EIGHT, FAR>(L, t, chunk); break;
+    case 3: adamw_chunk<bf16, bf16, EIGHT, FAR>(L, t, chunk); break;
+    case 4: adamw_chunk<float, f16, EIGHT, FAR>(L, t, chunk); break;
+    default: adamw_chunk<bf16, f16, EIGHT, FAR>(L, t, chunk); break;
   }
 }
 
@@ -174,6 +174,7 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
   if (!(a->beta1 >= 0. && a->beta1 < 1. && a->beta2 >= 0. && a->beta2 < 1.)) return set_error(PBKD_EINVAL, "adamw: beta1 and beta2 must be in [0,1)");
   if (!(a->eps >= 0.) || !(a->lr >= 0.) || !(a->grad_scale == a->grad_scale)) return set_error(PBKD_EINVAL, "adamw: lr and eps must not be negative, nor grad_scale NaN");
   const bool eight = a->state_bits == 8;
+  double bytes = 0.;                           // of the whole call
   for (int i = 0; i < n_tensors; ++i) {        // all of them before the first launch
     const pbkd_adamw_tensor &t = tensors[i];
     if (t.n < 0) return set_error(PBKD_ESHAPE, "adamw: tensor %d has %lld elements", i, t.n);
@@ -188,7 +189,9 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
     if (off(t.param_dev, t.param_dtype == PBKD_F32 ? 4 : 2) || off(t.grad_dev, t.grad_dtype == PBKD_F32 ? 4 : 2) || off(t.copy_dev, 2) ||
         (!eight && (off(t.m_dev, 4) || off(t.v_dev, 4))) || (eight && (off(t.m_scale_dev, 4) || off(t.v_scale_dev, 4))))
       return set_error(PBKD_EINVAL, "adamw: tensor %d is not aligned to its elements", i);
+    bytes += (double)t.n * ((t.param_dtype == PBKD_F32 ? 8 : 4) + (t.grad_dtype == PBKD_F32 ? 4 : 2) + (eight ? 4 : 16) + (t.copy_dev ? 2 : 0));
   }
+  const bool far = bytes > kLastLevelCache;
   Launch L;
   L.seed = a->seed;
   L.b1 = (float)a->beta1, L.c1 = (float)(1. - a->beta1), L.b2 = (float)a->beta2, L.c2 = (float)(1. - a->beta2);
@@ -200,8 +203,10 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
   auto flush = [&]() -> hipError_t {
     if (L.tensors == 0) return hipSuccess;
     const unsigned grid = L.chunk0[L.tensors];
-    if (eight) adamw_kernel<true><<<grid, 256, 0, st>>>(L);
-    else adamw_kernel<false><<<grid, 256, 0, st>>>(L);
+    if (eight && far) adamw_kernel<true, true><<<grid, 256, 0, st>>>(L);
+    else if (eight) adamw_kernel<true, false><<<grid, 256, 0, st>>>(L);
+    else if (far) adamw_kernel<false, true><<<grid, 256, 0, st>>>(L);
+    else adamw_kernel<false, false><<<grid, 256, 0, st>>>(L);
     L.tensors = 0, L.chunk0[0] = 0;
     return hipGetLastError();
   };

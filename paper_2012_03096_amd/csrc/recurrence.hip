@@ -58,7 +58,7 @@ __device__ __forceinline__ void sigmoids(float x, float &a, float &z) {
   a = x >= 0.f ? r : s;
   z = x >= 0.f ? s : r;
 }
-// sigmoid(x) alone: exp(-x) may be infinite
+// sigmoid(x) far: exp(-x) may be infinite
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
 // The two channels of a lane.  Where a row's last lane has only one (D is odd) they are taken one by one; lanes and channels
@@ -78,24 +78,23 @@ __device__ __forceinline__ Lane lane_of(int slice, int D) {
 }
 template <typename T>
 using Raw = typename VecOf<T, 2>::type;
-// ALONE: no cache line has another tile's channels too.  What is read is then read past the caches; otherwise the line's second
-// reader would fetch it again (8x4096x2048 forward and backward 319 -> 305 us, but 7x1000x515 in fp32 56 -> 64 us).
-template <typename T, bool ONE, bool ALONE>
+// FAR: see far_load; and no cache line has another tile's channels too, or the line's second reader would fetch it again
+// (7x1000x515 in fp32, forward and backward: 56 -> 64 us; 8x4096x2048, whose tiles are alone with theirs: 319 -> 305 us).
+template <typename T, bool ONE, bool FAR>
 __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
-  if (!ONE && ALONE) return __builtin_nontemporal_load(reinterpret_cast<const Raw<T> *>(p));
-  if (!ONE) return *reinterpret_cast<const Raw<T> *>(p);
+  if (!ONE) return far_load<FAR>(reinterpret_cast<const Raw<T> *>(p));
   Raw<T> r;
   r[0] = p[0], r[1] = p[q.n == 2 ? 1 : 0];
   return r;
 }
-template <typename T, bool ONE>
+template <typename T, bool ONE, bool FAR>
 __device__ __forceinline__ void put2(T *p, const Lane &q, const float (&v)[2]) {
   if (ONE) {
     store_n<T, 2>(p, q.n, v);
   } else {                                 // lanes without channels do not come here
     Raw<T> r;
     r[0] = static_cast<T>(v[0]), r[1] = static_cast<T>(v[1]);
-    __builtin_nontemporal_store(r, reinterpret_cast<Raw<T> *>(p));
+    far_store<FAR>(r, reinterpret_cast<Raw<T> *>(p));
   }
 }
 __device__ __forceinline__ void floats2(const float *p, const Lane &q, float (&v)[2]) {
@@ -109,7 +108,7 @@ constexpr long long kMaxStride = 1LL << 25;      // elements between tokens: 2 *
 template <typename T, int L, bool WHOLE>
 struct Place {
   char *base;
-  unsigned stride, mine;    // bytes; WHOLE: the distance of the first token; else: of the channels alone
+  unsigned stride, mine;    // bytes; WHOLE: the distance of the first token; else: of the channels far
   int token, last;          // the thread's first token and the sequence's last, counted from the base's
   __device__ __forceinline__ Place(const void *p, long long batch_at, long long stride_, int t0, int slice, const Lane &q, long long T_) {
     const int w0 = t0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * L, at = WHOLE || w0 < T_ ? w0 : (int)T_ - 1;
@@ -249,7 +248,7 @@ __device__ __forceinline__ R forget(R r) {
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.  ONE: see Lane.
-template <typename T, bool GATED, bool WHOLE, bool ONE, bool ALONE>
+template <typename T, bool GATED, bool WHOLE, bool ONE, bool FAR>
 __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
   constexpr int L = kFwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -261,10 +260,10 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
   Raw<T> ur[L], gr[L], orr[L];
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, ALONE>(g.at(i), q), ur[i] = raw2<T, ONE, ALONE>(u.at(i), q);
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, FAR>(g.at(i), q), ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
   if (GATED) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE, ALONE>(o.at(i), q);
+    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
   }
   float bias[2] = {0.f, 0.f};
   if (P.bias) floats2(P.bias + q.c, q, bias);
@@ -328,12 +327,12 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
       }
       out[k] = WHOLE || tk + i < len ? out[k] : 0.f;
     }
-    if (WHOLE || tk + i < P.len) put2<T, ONE>(y.at(i), q, out);
+    if (WHOLE || tk + i < P.len) put2<T, ONE, FAR>(y.at(i), q, out);
   }
   if (P.hT && tile + 1 == P.tiles && grp == 7) store_n<float, 2>(P.hT + (long long)b * P.D + q.c, q.n, h);
 }
 
-template <typename T, bool GATED, bool ALONE>
+template <typename T, bool GATED, bool FAR>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
@@ -342,12 +341,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_ke
   const int tile = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (!ALONE && q.one) fwd_tile<T, GATED, false, true, false>(P, S, tile, chain, q, len);
-  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false, ALONE>(P, S, tile, chain, q, len);
-  else fwd_tile<T, GATED, true, false, ALONE>(P, S, tile, chain, q, len);
+  if (!FAR && q.one) fwd_tile<T, GATED, false, true, false>(P, S, tile, chain, q, len);
+  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false, FAR>(P, S, tile, chain, q, len);
+  else fwd_tile<T, GATED, true, false, FAR>(P, S, tile, chain, q, len);
 }
 
-template <typename T, bool GATED, bool WHOLE, bool ONE, bool ALONE>
+template <typename T, bool GATED, bool WHOLE, bool ONE, bool FAR>
 __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, int chain, const Lane &q, int len) {
   constexpr int L = kBwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -361,10 +360,10 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   Raw<T> ur[L], gr[L], orr[L], yr[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    gr[i] = raw2<T, ONE, ALONE>(g.at(i), q);
-    ur[i] = raw2<T, ONE, ALONE>(u.at(i), q);
-    yr[i] = raw2<T, ONE, ALONE>(dy.at(i), q);
-    if (GATED) orr[i] = raw2<T, ONE, ALONE>(o.at(i), q);
+    gr[i] = raw2<T, ONE, FAR>(g.at(i), q);
+    ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
+    yr[i] = raw2<T, ONE, FAR>(dy.at(i), q);
+    if (GATED) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
   }
   float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
   if (P.bias) floats2(P.bias + q.c, q, bias);
@@ -470,9 +469,9 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
         db[k] += dg[k];
       }
       if (WHOLE || tk + i < P.len) {
-        put2<T, ONE>(du.at(i), q, dv);
-        put2<T, ONE>(dgp.at(i), q, dg);
-        if (GATED) put2<T, ONE>(dop.at(i), q, dou);
+        put2<T, ONE, FAR>(du.at(i), q, dv);
+        put2<T, ONE, FAR>(dgp.at(i), q, dg);
+        if (GATED) put2<T, ONE, FAR>(dop.at(i), q, dou);
       }
     }
 #pragma unroll
@@ -490,7 +489,7 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   }
 }
 
-template <typename T, bool GATED, bool ALONE>
+template <typename T, bool GATED, bool FAR>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
@@ -499,9 +498,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_ke
   const int pos = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (!ALONE && q.one) bwd_tile<T, GATED, false, true, false>(P, S, pos, chain, q, len);
-  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false, ALONE>(P, S, pos, chain, q, len);
-  else bwd_tile<T, GATED, true, false, ALONE>(P, S, pos, chain, q, len);
+  if (!FAR && q.one) bwd_tile<T, GATED, false, true, false>(P, S, pos, chain, q, len);
+  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false, FAR>(P, S, pos, chain, q, len);
+  else bwd_tile<T, GATED, true, false, FAR>(P, S, pos, chain, q, len);
 }
 
 // One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
@@ -563,11 +562,11 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   } else {
     const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
     const int size = sizeof(T);
-    const bool alone = A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && (!A.o || lines(A.o, A.ob, A.os, size));
+    const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 4 : 3) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && (!A.o || lines(A.o, A.ob, A.os, size));
     clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-    if (A.o && alone) recurrence_fwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
+    if (A.o && far) recurrence_fwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
     else if (A.o) recurrence_fwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
-    else if (alone) recurrence_fwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
+    else if (far) recurrence_fwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
     else recurrence_fwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
   }
   return hipGetLastError();
@@ -577,12 +576,12 @@ template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
   const int size = sizeof(T);
-  const bool alone = A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
+  const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 7 : 5) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
                      (!A.o || lines(A.o, A.ob, A.os, size));
   clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-  if (A.o && alone) recurrence_bwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
+  if (A.o && far) recurrence_bwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
   else if (A.o) recurrence_bwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
-  else if (alone) recurrence_bwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
+  else if (far) recurrence_bwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
   else recurrence_bwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
   return hipGetLastError();
 }

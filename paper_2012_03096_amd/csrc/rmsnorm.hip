@@ -63,7 +63,7 @@ __device__ __forceinline__ float row_reduce(float v, float *slot) {
   return t;
 }
 
-template <typename T, int TPR, int ITEMS, bool FP8>
+template <typename T, int TPR, int ITEMS, bool FP8, bool FAR>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdArgs A) {
   constexpr int RPB = TPR == 64 ? 4 : 1;             // rows a workgroup works on at a time
   __shared__ float red[4][16];
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       const int c = (k * TPR + lane) * 8;
-      load_n<T, 8>(x + c, d - c, s[k]);
+      load_n<T, 8, FAR>(x + c, d - c, s[k]);
     }
     if (A.res) {
       const T *r = static_cast<const T *>(A.res) + row * A.rs;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
         float q[8];
-        load_n<T, 8>(r + c, d - c, q);
+        load_n<T, 8, FAR>(r + c, d - c, q);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[k][i] += q[i];
       }
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
-        store_n<T, 8>(t + c, d - c, s[k]);
+        store_n<T, 8, FAR>(t + c, d - c, s[k]);
       }
     }
 #pragma unroll
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
         q[0] = pack_e4m3(s[k][0] * inv, s[k][1] * inv, s[k][2] * inv, s[k][3] * inv);
         q[1] = pack_e4m3(s[k][4] * inv, s[k][5] * inv, s[k][6] * inv, s[k][7] * inv);
         if (c + 8 <= d) {
-          *reinterpret_cast<u2 *>(y + c) = q;
+          far_store<FAR>(q, reinterpret_cast<u2 *>(y + c));
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
-        store_n<T, 8>(y + c, d - c, s[k]);
+        store_n<T, 8, FAR>(y + c, d - c, s[k]);
       }
     }
   }
@@ -157,11 +157,11 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
 
 template <typename T>
 using Raw = typename VecOf<T, 8>::type;
-template <typename T>
+template <bool FAR, typename T>
 __device__ __forceinline__ Raw<T> raw_n(const T *p, int n) {
   Raw<T> r;
   if (n >= 8) {
-    r = *reinterpret_cast<const Raw<T> *>(p);
+    r = far_load<FAR>(reinterpret_cast<const Raw<T> *>(p));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = i < n ? p[i] : T(0.f);
@@ -171,7 +171,7 @@ __device__ __forceinline__ Raw<T> raw_n(const T *p, int n) {
 
 // A workgroup goes through its rows with the weight gradient of its own columns in registers, the next row on its way while it
 // works on one, and leaves one row of partials; with a wave to a row its four waves' sums are joined through LDS first.
-template <typename T, int TPR, int ITEMS>
+template <typename T, int TPR, int ITEMS, bool FAR>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdArgs A) {
   constexpr int RPB = TPR == 64 ? 4 : 1;
   constexpr bool AHEAD = ITEMS == 1;      // with two items the next row does not fit in the registers
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdA
     const int c = (k * TPR + lane) * 8;
     load_n<float, 8>(A.w + c, d - c, w[k]);
     if (AHEAD && row < A.rows) {
-      s[k] = raw_n(tp + row * A.ts + c, d - c), y[k] = raw_n(yp + row * A.ys + c, d - c);
-      if (A.dtotal) g[k] = raw_n(gp + row * A.gs + c, d - c);
+      s[k] = raw_n<FAR>(tp + row * A.ts + c, d - c), y[k] = raw_n<FAR>(yp + row * A.ys + c, d - c);
+      if (A.dtotal) g[k] = raw_n<FAR>(gp + row * A.gs + c, d - c);
     }
   }
   int flip = 0;
@@ -202,8 +202,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdA
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
-        s[k] = raw_n(tp + row * A.ts + c, d - c), y[k] = raw_n(yp + row * A.ys + c, d - c);
-        if (A.dtotal) g[k] = raw_n(gp + row * A.gs + c, d - c);
+        s[k] = raw_n<FAR>(tp + row * A.ts + c, d - c), y[k] = raw_n<FAR>(yp + row * A.ys + c, d - c);
+        if (A.dtotal) g[k] = raw_n<FAR>(gp + row * A.gs + c, d - c);
       }
     }
 #pragma unroll
@@ -217,8 +217,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdA
       }
       gr[k] = g[k];
       if (AHEAD && next < A.rows) {
-        s[k] = raw_n(tp + next * A.ts + c, d - c), y[k] = raw_n(yp + next * A.ys + c, d - c);
-        if (A.dtotal) g[k] = raw_n(gp + next * A.gs + c, d - c);
+        s[k] = raw_n<FAR>(tp + next * A.ts + c, d - c), y[k] = raw_n<FAR>(yp + next * A.ys + c, d - c);
+        if (A.dtotal) g[k] = raw_n<FAR>(gp + next * A.gs + c, d - c);
       }
     }
     ss = row_reduce<TPR, false>(ss, red[flip]);
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_bwd_kernel(BwdA
         if (A.dtotal) v[i] += static_cast<float>(gr[k][i]);
         dw[k][i] = fmaf(yv[k][i], xh, dw[k][i]);
       }
-      store_n<T, 8>(xp + row * A.xs + c, d - c, v);
+      store_n<T, 8, FAR>(xp + row * A.xs + c, d - c, v);
     }
   }
   if (RPB > 1) {
@@ -293,10 +293,13 @@ static_assert(kBwdThreads / 128 <= kSlab, "the norm's partials are summed in one
 template <typename T, bool FP8>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   const int d = A.d;
+  const bool far = (double)A.rows * d * (sizeof(T) * (1 + (A.res != nullptr) + (A.total != nullptr)) + (FP8 ? 1 : sizeof(T))) > kLastLevelCache;
 #define FWD(TPR, ITEMS)                                                                                              \
   {                                                                                                                  \
     const long long groups = cdiv64(A.rows, TPR == 64 ? 4 : 1);                                                      \
-    rmsnorm_fwd_kernel<T, TPR, ITEMS, FP8><<<(unsigned)(groups < 4096 ? groups : 4096), TPR == 64 ? 256 : TPR, 0, st>>>(A); \
+    const unsigned grid = (unsigned)(groups < 4096 ? groups : 4096), threads = TPR == 64 ? 256 : TPR;                 \
+    if (far) rmsnorm_fwd_kernel<T, TPR, ITEMS, FP8, true><<<grid, threads, 0, st>>>(A);                               \
+    else rmsnorm_fwd_kernel<T, TPR, ITEMS, FP8, false><<<grid, threads, 0, st>>>(A);                                  \
   }
   switch (row_threads(d)) {
     case 64: FWD(64, 1) break;
@@ -314,7 +317,13 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, int groups, hipStream_t st) {
   const int d = A.d;
-#define BWD(TPR, ITEMS) rmsnorm_bwd_kernel<T, TPR, ITEMS><<<groups, TPR == 64 ? 256 : TPR, 0, st>>>(A);
+  const bool far = (double)A.rows * d * sizeof(T) * (3 + (A.dtotal != nullptr)) > kLastLevelCache;
+#define BWD(TPR, ITEMS)                                                                             \
+  {                                                                                                 \
+    const unsigned threads = TPR == 64 ? 256 : TPR;                                                 \
+    if (far) rmsnorm_bwd_kernel<T, TPR, ITEMS, true><<<groups, threads, 0, st>>>(A);                \
+    else rmsnorm_bwd_kernel<T, TPR, ITEMS, false><<<groups, threads, 0, st>>>(A);                   \
+  }
   switch (row_threads(d)) {
     case 64: BWD(64, 1) break;
     case 128: BWD(128, 1) break;
