@@ -37,43 +37,71 @@ struct Launch {
 static_assert(sizeof(Launch) <= 4000, "kernel arguments");
 
 // A random number for each element: multiplications and xor-shifts of its number and the seed.
-__device__ __forceinline__ unsigned element_hash(unsigned i, unsigned seed) {
-  unsigned x = i * 0x9E3779B1u + seed * 0x632BE5ABu;
+constexpr unsigned kMul = 0x9E3779B1u;
+__device__ __forceinline__ unsigned element_hash(unsigned x) {       // x = number * kMul + seed * 0x632BE5AB
   x = (x ^ (x >> 16)) * 0x21F0AAADu;
   x = (x ^ (x >> 15)) * 0x735A2D97u;
   return x ^ (x >> 15);
 }
 
 // x in [0, 448] to one of the two neighbouring e4m3 values, by 20 random bits; above zero stays above zero.  In the
-// normal range the lower 20 of the float's 23 mantissa bits are cut after the addition, below 2^-6 the grid is 2^-9.
+// normal range the lower 20 of the float's 23 mantissa bits are cut after the addition; below 2^-6, where the grid is 2^-9, so
+// they are with 2^-6 added.
 __device__ __forceinline__ float random_e4m3(float x, unsigned up) {
-  const float small = fmaxf(floorf(x * 512.f + (float)up * 0x1p-20f), 1.f) * (1.f / 512.f);
-  const float large = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, x) + up) & ~0xFFFFFu);
-  return x > 0.f ? (x < 0x1p-6f ? small : large) : x * 0.f;      // a NaN stays one
+  const float base = x < 0x1p-6f ? 0x1p-6f : 0.f, least = x > 0.f ? 0x1p-9f : 0.f;
+  const float r = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, x + base) + up) & ~0xFFFFFu) - base;
+  return r < least ? least : r;      // a NaN stays one
 }
 
-template <typename P, typename G, bool EIGHT, bool FAR>
+// the maximum of numbers >= 0 over a wave, uniform: within the rows of 16 lanes, then row by row into lane 63
+__device__ __forceinline__ float wave_top(float v) {
+  v = fmaxf(v, dpp_mov<0x111>(v));      // row_shr:1, 2, 4, 8
+  v = fmaxf(v, dpp_mov<0x112>(v));
+  v = fmaxf(v, dpp_mov<0x114>(v));
+  v = fmaxf(v, dpp_mov<0x118>(v));
+  v = fmaxf(v, dpp_mov<0x142>(v));      // row_bcast:15, 31
+  v = fmaxf(v, dpp_mov<0x143>(v));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+// 1/x to a unit of its last place and its residual put right once
+__device__ __forceinline__ float reciprocal(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return fmaf(fmaf(-x, r, 1.f), r, r);
+}
+
+// The root and the quotient of the update in 8-bit kernels, which are bound by their arithmetic: the hardware's approximations with
+// the residual put right once, within 0.6 units of the last place.  (Squares below 2^-126 have the root zero.)
+__device__ __forceinline__ float root_of(float v) {
+  const float s = __builtin_amdgcn_sqrtf(v), r = fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rsqf(v), s);
+  return __builtin_amdgcn_classf(v, 0x100) ? r : s;      // positive and normal: not zero, infinite or NaN
+}
+__device__ __forceinline__ float quotient(float a, float b) {
+  const float r = __builtin_amdgcn_rcpf(b), q = a * r;
+  return fmaf(fmaf(-q, b, a), r, q);
+}
+
+// WHOLE: all of the chunk's elements exist.
+template <typename P, typename G, bool EIGHT, bool FAR, bool WHOLE>
 __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, long long chunk) {
-// products and sums keep their own roundings: the same figures as the formulas, operation by operation
-#pragma clang fp contract(off)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float p[kRounds][4], g[kRounds][4], m[kRounds][4], v[kRounds][4];
-  const long long base = chunk * kChunk + wave * (kRounds * kBlock) + lane * 4;
+  const long long base = chunk * kChunk + wave * (kRounds * kBlock) + lane * 4, left = t.n - base;
+  using Codes = typename VecOf<unsigned char, 4>::type;
 #pragma unroll
   for (int k = 0; k < kRounds; ++k) {
-    const long long e = base + k * kBlock, left = t.n - e;
-    const int n = left < 4 ? (int)(left < 0 ? 0 : left) : 4;
+    const long long e = base + k * kBlock;
+    const int n = WHOLE || left - k * kBlock >= 4 ? 4 : left - k * kBlock > 0 ? (int)(left - k * kBlock) : 0;
     load_n<P, 4, FAR>(static_cast<const P *>(t.p) + e, n, p[k]);
     load_n<G, 4, FAR>(static_cast<const G *>(t.g) + e, n, g[k]);
     if (!EIGHT) {
       load_n<float, 4, FAR>(static_cast<const float *>(t.m) + e, n, m[k]);
       load_n<float, 4, FAR>(static_cast<const float *>(t.v) + e, n, v[k]);
     } else {
-      typedef unsigned u1 __attribute__((aligned(1)));
       unsigned mc = 0, vc = 0;
       const unsigned char *mp = static_cast<const unsigned char *>(t.m) + e, *vp = static_cast<const unsigned char *>(t.v) + e;
       if (n == 4) {
-        mc = far_load<FAR>(reinterpret_cast<const u1 *>(mp)), vc = far_load<FAR>(reinterpret_cast<const u1 *>(vp));
+        mc = __builtin_bit_cast(unsigned, far_load<FAR, unsigned char, 4>(mp)), vc = __builtin_bit_cast(unsigned, far_load<FAR, unsigned char, 4>(vp));
       } else {
         for (int i = 0; i < n; ++i) mc |= (unsigned)mp[i] << (8 * i), vc |= (unsigned)vp[i] << (8 * i);
       }
@@ -86,21 +114,29 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       for (int i = 0; i < 4; ++i) v[k][i] = v[k][i] * v[k][i];
     }
   }
+  const unsigned number = (t.first + (unsigned)base) * kMul + L.seed * 0x632BE5ABu;
 #pragma unroll
   for (int k = 0; k < kRounds; ++k) {
-    const long long e = base + k * kBlock, left = t.n - e;
-    const int n = left < 4 ? (int)(left < 0 ? 0 : left) : 4;
+    const long long e = base + k * kBlock;
+    const int n = WHOLE || left - k * kBlock >= 4 ? 4 : left - k * kBlock > 0 ? (int)(left - k * kBlock) : 0;
     float root[4];
     unsigned noise[4];
     float mtop = 0.f, vtop = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float gr = g[k][i] * L.gscale;
-      m[k][i] = m[k][i] * L.b1 + gr * L.c1;
-      v[k][i] = v[k][i] * L.b2 + (gr * gr) * L.c2;
-      root[i] = sqrtf(v[k][i]);
-      const float q = p[k][i] * t.decay - m[k][i] / (root[i] * L.root + L.eps) * L.step;
-      if (EIGHT || sizeof(P) == 2) noise[i] = element_hash(t.first + (unsigned)(e + i), L.seed);
+      m[k][i] = fmaf(m[k][i], L.b1, gr * L.c1);
+      v[k][i] = fmaf(v[k][i], L.b2, gr * gr * L.c2);
+      float q;
+      if (EIGHT) {
+        root[i] = root_of(v[k][i]);
+        q = quotient(m[k][i], fmaf(root[i], L.root, L.eps));
+      } else {
+        root[i] = sqrtf(v[k][i]);
+        q = m[k][i] / fmaf(root[i], L.root, L.eps);
+      }
+      q = fmaf(-q, L.step, p[k][i] * t.decay);
+      if (EIGHT || sizeof(P) == 2) noise[i] = element_hash(number + (k * kBlock + i) * kMul);
       if (sizeof(P) == 2) {
         // to one of the two neighbours, by 16 random bits; infinities and NaN stay what they are
         const unsigned b = __builtin_bit_cast(unsigned, q);
@@ -118,8 +154,8 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       store_n<float, 4, FAR>(static_cast<float *>(t.m) + e, n, m[k]);
       store_n<float, 4, FAR>(static_cast<float *>(t.v) + e, n, v[k]);
     } else {
-      mtop = fmaxf(wave64_max(mtop), 0x1p-100f), vtop = fmaxf(wave64_max(vtop), 0x1p-100f);
-      const float mi = 1.f / mtop * 448.f, vi = 1.f / vtop * 448.f;
+      mtop = fmaxf(wave_top(mtop), 0x1p-100f), vtop = fmaxf(wave_top(vtop), 0x1p-100f);
+      const float mi = reciprocal(mtop) * 448.f, vi = reciprocal(vtop) * 448.f;
       float r[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -128,16 +164,21 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
         r[i] = random_e4m3(x > 448.f ? 448.f : x, noise[i] >> 12);
       }
       const unsigned mc = pack_e4m3(m[k][0], m[k][1], m[k][2], m[k][3]), vc = pack_e4m3(r[0], r[1], r[2], r[3]);
-      typedef unsigned u1 __attribute__((aligned(1)));
       unsigned char *mp = static_cast<unsigned char *>(t.m) + e, *vp = static_cast<unsigned char *>(t.v) + e;
       if (n == 4) {
-        far_store<FAR>((u1)mc, reinterpret_cast<u1 *>(mp)), far_store<FAR>((u1)vc, reinterpret_cast<u1 *>(vp));
+        far_store<FAR, unsigned char, 4>(__builtin_bit_cast(Codes, mc), mp), far_store<FAR, unsigned char, 4>(__builtin_bit_cast(Codes, vc), vp);
       } else {
         for (int i = 0; i < n; ++i) mp[i] = (unsigned char)(mc >> (8 * i)), vp[i] = (unsigned char)(vc >> (8 * i));
       }
       if (lane == 0 && n > 0) t.ms[e / kBlock] = mtop * (1.f / 448.f), t.vs[e / kBlock] = vtop * (1.f / 448.f);
     }
   }
+}
+
+template <typename P, typename G, bool EIGHT, bool FAR>
+__device__ __forceinline__ void adamw_piece(const Launch &L, const Tensor &t, long long chunk) {
+  if ((chunk + 1) * kChunk <= t.n) adamw_chunk<P, G, EIGHT, FAR, true>(L, t, chunk);
+  else adamw_chunk<P, G, EIGHT, false, false>(L, t, chunk);
 }
 
 template <bool EIGHT, bool FAR>
@@ -151,12 +192,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(Launch L) {
   const Tensor &t = L.t[lo];
   const long long chunk = blockIdx.x - L.chunk0[lo];
   switch (L.kind[lo]) {
-    case 0: adamw_chunk<float, float, EIGHT, FAR>(L, t, chunk); break;
-    case 1: adamw_chunk<bf16, float, EIGHT, FAR>(L, t, chunk); break;
-    case 2: adamw_chunk<float, bf16, EIGHT, FAR>(L, t, chunk); break;
-    case 3: adamw_chunk<bf16, bf16, EIGHT, FAR>(L, t, chunk); break;
-    case 4: adamw_chunk<float, f16, EIGHT, FAR>(L, t, chunk); break;
-    default: adamw_chunk<bf16, f16, EIGHT, FAR>(L, t, chunk); break;
+    case 0: adamw_piece<float, float, EIGHT, FAR>(L, t, chunk); break;
+    case 1: adamw_piece<bf16, float, EIGHT, FAR>(L, t, chunk); break;
+    case 2: adamw_piece<float, bf16, EIGHT, FAR>(L, t, chunk); break;
+    case 3: adamw_piece<bf16, bf16, EIGHT, FAR>(L, t, chunk); break;
+    case 4: adamw_piece<float, f16, EIGHT, FAR>(L, t, chunk); break;
+    default: adamw_piece<bf16, f16, EIGHT, FAR>(L, t, chunk); break;
   }
 }
 

@@ -82,7 +82,7 @@ using Raw = typename VecOf<T, 2>::type;
 // (7x1000x515 in fp32, forward and backward: 56 -> 64 us; 8x4096x2048, whose tiles are alone with theirs: 319 -> 305 us).
 template <typename T, bool ONE, bool FAR>
 __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
-  if (!ONE) return far_load<FAR>(reinterpret_cast<const Raw<T> *>(p));
+  if (!ONE) return far_load<FAR, T, 2>(p);
   Raw<T> r;
   r[0] = p[0], r[1] = p[q.n == 2 ? 1 : 0];
   return r;
@@ -94,7 +94,7 @@ __device__ __forceinline__ void put2(T *p, const Lane &q, const float (&v)[2]) {
   } else {                                 // lanes without channels do not come here
     Raw<T> r;
     r[0] = static_cast<T>(v[0]), r[1] = static_cast<T>(v[1]);
-    far_store<FAR>(r, reinterpret_cast<Raw<T> *>(p));
+    far_store<FAR, T, 2>(r, p);
   }
 }
 __device__ __forceinline__ void floats2(const float *p, const Lane &q, float (&v)[2]) {

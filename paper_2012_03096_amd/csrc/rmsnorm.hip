@@ -48,6 +48,9 @@ struct BwdArgs {
   float eps;
 };
 
+template <typename T>
+using Raw = typename VecOf<T, 8>::type;
+
 // Sum (or maximum) over the TPR threads of a row, known to all of them.  `slot` holds one float per wave; callers alternate
 // between two of them, so that the barrier inside also keeps a slot's readers ahead of its next writers.
 template <int TPR, bool MAX>
@@ -132,12 +135,11 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
-        typedef unsigned u2 __attribute__((ext_vector_type(2), aligned(1)));
-        u2 q;
+        unsigned q[2];
         q[0] = pack_e4m3(s[k][0] * inv, s[k][1] * inv, s[k][2] * inv, s[k][3] * inv);
         q[1] = pack_e4m3(s[k][4] * inv, s[k][5] * inv, s[k][6] * inv, s[k][7] * inv);
         if (c + 8 <= d) {
-          far_store<FAR>(q, reinterpret_cast<u2 *>(y + c));
+          far_store<FAR, unsigned char, 8>(__builtin_bit_cast(Raw<unsigned char>, q), y + c);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -155,13 +157,11 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
   }
 }
 
-template <typename T>
-using Raw = typename VecOf<T, 8>::type;
 template <bool FAR, typename T>
 __device__ __forceinline__ Raw<T> raw_n(const T *p, int n) {
   Raw<T> r;
   if (n >= 8) {
-    r = far_load<FAR>(reinterpret_cast<const Raw<T> *>(p));
+    r = far_load<FAR, T, 8>(p);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = i < n ? p[i] : T(0.f);

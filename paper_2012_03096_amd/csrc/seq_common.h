@@ -39,22 +39,22 @@ struct VecOf {
 // Accesses with FAR go past the caches.  It is for calls that move more than the last-level cache holds, none of which can be
 // there from the call before or for the call behind (measured on 67M parameters, 1.9 GB: 347 -> 303 us; but on 100 MB that come
 // again and again, 29 -> 36 us).
-template <bool FAR, typename V>
-__device__ __forceinline__ V far_load(const V *p) {
-  if (FAR) return __builtin_nontemporal_load(p);
-  return *p;
+template <bool FAR, typename T, int N>
+__device__ __forceinline__ typename VecOf<T, N>::type far_load(const T *p) {
+  if (FAR) return __builtin_nontemporal_load(reinterpret_cast<const typename VecOf<T, N>::type *>(p));
+  return *reinterpret_cast<const typename VecOf<T, N>::type *>(p);
 }
-template <bool FAR, typename V>
-__device__ __forceinline__ void far_store(V v, V *p) {
-  if (FAR) __builtin_nontemporal_store(v, p);
-  else *p = v;
+template <bool FAR, typename T, int N>
+__device__ __forceinline__ void far_store(typename VecOf<T, N>::type v, T *p) {
+  if (FAR) __builtin_nontemporal_store(v, reinterpret_cast<typename VecOf<T, N>::type *>(p));
+  else *reinterpret_cast<typename VecOf<T, N>::type *>(p) = v;
 }
 
 // n of the N elements exist (n <= 0: none); the others come back as zero and are not read.
 template <typename T, int N, bool FAR = false>
 __device__ __forceinline__ void load_n(const T *p, int n, float (&v)[N]) {
   if (n >= N) {
-    const typename VecOf<T, N>::type r = far_load<FAR>(reinterpret_cast<const typename VecOf<T, N>::type *>(p));
+    const typename VecOf<T, N>::type r = far_load<FAR, T, N>(p);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = static_cast<float>(r[i]);
   } else {
@@ -70,7 +70,7 @@ __device__ __forceinline__ void store_n(T *p, int n, const float (&v)[N]) {
     typename VecOf<T, N>::type r;
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = static_cast<T>(v[i]);
-    far_store<FAR>(r, reinterpret_cast<typename VecOf<T, N>::type *>(p));
+    far_store<FAR, T, N>(r, p);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
