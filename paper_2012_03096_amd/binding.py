@@ -410,42 +410,37 @@ _RECURRENCE_GRAD = struct.Struct("@2iqi12P14qPNPN")
 _ADAMW_ARGS = struct.Struct("@5dqiI")
 _ADAMW_TENSOR = np.dtype([("n", "i8"), ("first", "i8"), ("param_dtype", "i4"), ("grad_dtype", "i4"), ("weight_decay", "f4"), ("param", "u8"), ("grad", "u8"),
                           ("m", "u8"), ("v", "u8"), ("m_scale", "u8"), ("v_scale", "u8"), ("copy", "u8")], align=True)
-_DTYPES = None
+_torch = None       # set with the types by _types(), at the first call that needs them
+_CODES, _FP8, _FP32, _INT32 = {}, None, None, None
 
 
-def _dtypes():
-    """torch's types by the library's numbers."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    return _DTYPES
+def _types():
+    """torch and its types by the library's numbers; the library is loaded (and torch with it) on the way."""
+    global _torch, _CODES, _FP8, _FP32, _INT32
+    import torch
+    _CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    _FP8, _FP32, _INT32, _torch = torch.float8_e4m3fn, torch.float32, torch.int32, torch
+    return lib()
 
 
-def _code(t, name: str) -> int:
-    c = (_DTYPES or _dtypes()).get(t.dtype)
-    if c is None:
+def _first(t, name: str):
+    """(library, type's number, GPU) of a call's first tensor, which must lie on the current GPU: the kernels are launched there."""
+    L = _lib if _torch is not None and _lib is not None else _types()
+    code, dev = _CODES.get(t.dtype), t.get_device()
+    if code is None:
         raise PbkdError(EINVAL, f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
-    return c
+    if dev < 0 or dev != _torch.cuda.current_device():
+        raise PbkdError(EINVAL, f"{name} must lie on the current GPU, not on {t.device}")
+    return L, code, dev
 
 
 def _stream(stream) -> int:
-    import torch
-    return stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream
-
-
-def _gpu(t, name: str) -> int:
-    """Index of the GPU that t lies on, which must be the current one (the kernels are launched there)."""
-    import torch
-    dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
-        raise PbkdError(EINVAL, f"{name} must lie on the current GPU, not on {t.device}")
-    return dev
+    return stream.cuda_stream if stream is not None else _torch.cuda.current_stream().cuda_stream
 
 
 def _same(t, like, dev: int, name: str) -> int:
     """Address of t, which has like's shape and type and lies on GPU dev."""
-    if t.dtype != like.dtype or t.shape != like.shape or t.get_device() != dev:
+    if t.dtype is not like.dtype or t.shape != like.shape or t.get_device() != dev:
         raise PbkdError(ESHAPE, f"{name} must be a {like.dtype} tensor of {tuple(like.shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -454,7 +449,7 @@ def _dense(t, shape, dtype, dev: int, name: str) -> int:
     """Address of t, a contiguous tensor of this shape and type on GPU dev; 0 for None."""
     if t is None:
         return 0
-    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         raise PbkdError(ESHAPE, f"{name} must be a contiguous {dtype} tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -465,13 +460,14 @@ def _bytes(t, dev: int, name: str):
         return 0, 0
     if t.get_device() != dev or not t.is_contiguous():
         raise PbkdError(EINVAL, f"{name} must be a contiguous tensor on the same GPU")
-    return t.data_ptr(), t.numel() * t.element_size()
+    return t.data_ptr(), t.nbytes
 
 
 def _row_stride(t, d: int, name: str) -> int:
     """Elements between the rows of t, whose last dimension are the rows: two dimensions with any stride, or more that are contiguous."""
-    if t.dim() == 2 and (d == 1 or t.stride(1) == 1):
-        return t.stride(0)
+    s = t.stride()
+    if len(s) == 2 and (s[1] == 1 or d == 1):
+        return s[0]
     if t.is_contiguous():
         return d
     raise PbkdError(EINVAL, f"{name} must be contiguous, or have two dimensions with contiguous rows")
@@ -484,20 +480,20 @@ def rmsnorm_workspace_bytes(rows: int, d: int) -> int:
 def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: float = 1e-6, stream=None) -> None:
     """pbkd_rmsnorm_forward: y <- norm(x + residual) * weight over the last dimension, total <- x + residual.
     y: like x, or float8_e4m3fn with scale [rows] float32."""
-    import torch
-    L, code, dev, d = _lib or lib(), _code(x, "x"), _gpu(x, "x"), x.shape[-1] if x.dim() else 0
+    L, code, dev = _first(x, "x")
+    d = x.shape[-1] if x.dim() else 0
     if d == 0:
         raise PbkdError(ESHAPE, "x has no elements in a row")
     rows = x.numel() // d
-    eight = y.dtype == torch.float8_e4m3fn
+    eight = y.dtype is _FP8
     if eight and (y.shape != x.shape or y.get_device() != dev):
         raise PbkdError(ESHAPE, f"y must have x's shape {tuple(x.shape)} and lie on its GPU")
     if scale is not None and not eight:
         raise PbkdError(EINVAL, "a scale goes with a float8_e4m3fn y only")
     _check(L.pbkd_rmsnorm_forward(_RMSNORM.pack(
         rows, d, code, E4M3 if eight else code, eps, x.data_ptr(), 0 if residual is None else _same(residual, x, dev, "residual"),
-        _dense(weight, (d,), torch.float32, dev, "weight"), 0 if total is None else _same(total, x, dev, "total"),
-        y.data_ptr() if eight else _same(y, x, dev, "y"), _dense(scale, (rows,), torch.float32, dev, "scale"), _row_stride(x, d, "x"),
+        _dense(weight, (d,), _FP32, dev, "weight"), 0 if total is None else _same(total, x, dev, "total"),
+        y.data_ptr() if eight else _same(y, x, dev, "y"), _dense(scale, (rows,), _FP32, dev, "scale"), _row_stride(x, d, "x"),
         0 if residual is None else _row_stride(residual, d, "residual"), 0 if total is None else _row_stride(total, d, "total"), _row_stride(y, d, "y")),
         _stream(stream)))
 
@@ -505,14 +501,14 @@ def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: fl
 def rmsnorm_backward(total, weight, dy, dx, dweight, workspace, dtotal=None, eps: float = 1e-6, stream=None) -> None:
     """pbkd_rmsnorm_backward: dx and dweight from the sum as stored by the forward pass, dy and (optionally) the gradient that
     arrives at the sum.  workspace: a tensor of rmsnorm_workspace_bytes(rows, d) bytes."""
-    import torch
-    L, code, dev, d = _lib or lib(), _code(total, "total"), _gpu(total, "total"), total.shape[-1] if total.dim() else 0
+    L, code, dev = _first(total, "total")
+    d = total.shape[-1] if total.dim() else 0
     if d == 0:
         raise PbkdError(ESHAPE, "total has no elements in a row")
     wp, wn = _bytes(workspace, dev, "workspace")
     _check(L.pbkd_rmsnorm_backward(_RMSNORM_GRAD.pack(
         total.numel() // d, d, code, eps, total.data_ptr(), _same(dy, total, dev, "dy"), 0 if dtotal is None else _same(dtotal, total, dev, "dtotal"),
-        _dense(weight, (d,), torch.float32, dev, "weight"), _same(dx, total, dev, "dx"), _dense(dweight, (d,), torch.float32, dev, "dweight"),
+        _dense(weight, (d,), _FP32, dev, "weight"), _same(dx, total, dev, "dx"), _dense(dweight, (d,), _FP32, dev, "dweight"),
         _row_stride(total, d, "total"), _row_stride(dy, d, "dy"), 0 if dtotal is None else _row_stride(dtotal, d, "dtotal"), _row_stride(dx, d, "dx"), wp, wn),
         _stream(stream)))
 
@@ -542,14 +538,14 @@ def _sequence_shape(u):
 def recurrence_forward(u, gate, y, out_gate=None, bias=None, lengths=None, state=None, state_out=None, saved=None, workspace=None, stream=None) -> None:
     """pbkd_recurrence_forward on [batch, len, channels] tensors: y, and the last state in state_out.  saved: a tensor of
     recurrence_saved_bytes() for the backward pass; workspace: one of recurrence_workspace_bytes()."""
-    import torch
-    L, code, dev, (b, t, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), _sequence_shape(u)
-    f32 = torch.float32
+    L, code, dev = _first(u, "u")
+    b, t, d = _sequence_shape(u)
+    f32 = _FP32
     sp, sn = _bytes(saved, dev, "saved")
     wp, wn = _bytes(workspace, dev, "workspace")
     _check(L.pbkd_recurrence_forward(_RECURRENCE.pack(
         b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
-        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), torch.int32, dev, "lengths"), _dense(state, (b, d), f32, dev, "state"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), _INT32, dev, "lengths"), _dense(state, (b, d), f32, dev, "state"),
         _dense(state_out, (b, d), f32, dev, "state_out"), _same(y, u, dev, "y"), *_tokens(u, "u"), *_tokens(gate, "gate"),
         *((0, 0) if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(y, "y"), sp, sn, wp, wn), _stream(stream)))
 
@@ -557,15 +553,15 @@ def recurrence_forward(u, gate, y, out_gate=None, bias=None, lengths=None, state
 def recurrence_backward(u, gate, dy, saved, du, dgate, out_gate=None, dout_gate=None, bias=None, dbias=None, lengths=None, dstate_out=None, dstate=None,
                         workspace=None, stream=None) -> None:
     """pbkd_recurrence_backward: the gradients of recurrence_forward's inputs from dy and what it saved."""
-    import torch
-    L, code, dev, (b, t, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), _sequence_shape(u)
-    f32 = torch.float32
+    L, code, dev = _first(u, "u")
+    b, t, d = _sequence_shape(u)
+    f32 = _FP32
     sp, sn = _bytes(saved, dev, "saved")
     wp, wn = _bytes(workspace, dev, "workspace")
     none = (0, 0)
     _check(L.pbkd_recurrence_backward(_RECURRENCE_GRAD.pack(
         b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"), _same(dy, u, dev, "dy"),
-        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), torch.int32, dev, "lengths"), _dense(dstate_out, (b, d), f32, dev, "dstate_out"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), _INT32, dev, "lengths"), _dense(dstate_out, (b, d), f32, dev, "dstate_out"),
         _same(du, u, dev, "du"), _same(dgate, u, dev, "dgate"), 0 if dout_gate is None else _same(dout_gate, u, dev, "dout_gate"),
         _dense(dbias, (d,), f32, dev, "dbias"), _dense(dstate, (b, d), f32, dev, "dstate"), *_tokens(u, "u"), *_tokens(gate, "gate"),
         *(none if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(dy, "dy"), *_tokens(du, "du"), *_tokens(dgate, "dgate"),
@@ -575,14 +571,14 @@ def recurrence_backward(u, gate, dy, saved, du, dgate, out_gate=None, dout_gate=
 def recurrence_step(u, gate, state, y, out_gate=None, bias=None, active=None, state_out=None, stream=None) -> None:
     """pbkd_recurrence_step: one token of each sequence, [batch, channels] rows with any stride; state [batch, channels] float32 is
     updated in place (or goes to state_out).  active: int32 [batch], 0 for idle rows."""
-    import torch
+    L, code, dev = _first(u, "u")
     if u.dim() != 2 or u.shape[1] == 0:
         raise PbkdError(ESHAPE, f"u must be [batch, channels], not {tuple(u.shape)}")
-    L, code, dev, (b, d) = _lib or lib(), _code(u, "u"), _gpu(u, "u"), u.shape
-    f32, sp = torch.float32, _dense(state, (b, d), torch.float32, dev, "state")
+    f32, (b, d) = _FP32, u.shape
+    sp = _dense(state, (b, d), f32, dev, "state")
     _check(L.pbkd_recurrence_step(_RECURRENCE.pack(
         b, d, 1, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
-        _dense(bias, (d,), f32, dev, "bias"), _dense(active, (b,), torch.int32, dev, "active"), sp, sp if state_out is None else _dense(state_out, (b, d), f32, dev, "state_out"),
+        _dense(bias, (d,), f32, dev, "bias"), _dense(active, (b,), _INT32, dev, "active"), sp, sp if state_out is None else _dense(state_out, (b, d), f32, dev, "state_out"),
         _same(y, u, dev, "y"), _row_stride(u, d, "u"), 0, _row_stride(gate, d, "gate"), 0, 0 if out_gate is None else _row_stride(out_gate, d, "out_gate"), 0,
         _row_stride(y, d, "y"), 0, 0, 0, 0, 0), _stream(stream)))
 
@@ -604,15 +600,16 @@ class AdamW:
         for name, given in (("states", states), ("copies", copies), ("weight_decay", decays)):
             if given is not None and len(given) != n:
                 raise PbkdError(ESHAPE, f"{len(given)} {name} for {n} parameters")
-        self._dev = _gpu(self.params[0], "a parameter") if n else -1
+        _types()
+        self._dev = _first(self.params[0], "a parameter")[2] if n else -1
         self._table = t = np.zeros(n, _ADAMW_TENSOR)
         kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
         sizes, rows, made = [p.numel() for p in self.params], [], []
         first = 0
         for i, p in enumerate(self.params):
-            code = _code(p, f"parameter {i}")
-            if code == F16:
-                raise PbkdError(EINVAL, f"parameter {i} must be float32 or bfloat16")
+            code = _CODES.get(p.dtype)
+            if code not in (F32, BF16):
+                raise PbkdError(EINVAL, f"parameter {i} must be float32 or bfloat16, not {p.dtype}")
             address = _dense(p, p.shape, p.dtype, self._dev, f"parameter {i}")
             blocks = -(-sizes[i] // 256)
             lens = (sizes[i], sizes[i], blocks, blocks)[:len(kind)]
@@ -629,28 +626,31 @@ class AdamW:
             t[:] = rows
         self.states = made if states is None else list(states)
         self._sizes, self._address = sizes, t.ctypes.data
+        self._n, self._grad_dtype, self._grad, self._codes = t["n"], t["grad_dtype"], t["grad"], None
         if states is None and n:
             torch.cuda.current_stream().synchronize()
 
     def step(self, grads, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, stream=None) -> None:
         """One step with these gradients (one for each parameter, contiguous; None: the parameter and its states stay as they are).
         seed: of the random roundings; None: the number of the step."""
-        import torch
-        L, dev, t = _lib or lib(), self._dev, self._table
-        if len(grads) != len(self._sizes):
-            raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(self._sizes)} parameters")
-        if dev >= 0 and dev != torch.cuda.current_device():
+        dev, sizes = self._dev, self._sizes
+        if len(grads) != len(sizes):
+            raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(sizes)} parameters")
+        if dev >= 0 and dev != _torch.cuda.current_device():
             raise PbkdError(EINVAL, "the parameters must lie on the current GPU")
-        codes, sizes, at = [], [], []
-        for g, n in zip(grads, self._sizes):
+        codes, counts, at = [], [], []
+        for g, n in zip(grads, sizes):
             if g is None:
-                codes.append(F32), sizes.append(0), at.append(0)
+                codes.append(F32), counts.append(0), at.append(0)
                 continue
-            if g.numel() != n or g.get_device() != dev or not g.is_contiguous():
-                raise PbkdError(ESHAPE, f"a gradient must be contiguous, with its parameter's {n} elements, on its GPU")
-            codes.append(_code(g, "a gradient")), sizes.append(n), at.append(g.data_ptr())
-        t["n"], t["grad_dtype"], t["grad"] = sizes, codes, at
+            code = _CODES.get(g.dtype)
+            if code is None or g.numel() != n or g.get_device() != dev or not g.is_contiguous():
+                raise PbkdError(ESHAPE, f"a gradient must be contiguous, float32, bfloat16 or float16, with its parameter's {n} elements, on its GPU")
+            codes.append(code), counts.append(n), at.append(g.data_ptr())
+        if codes != self._codes or counts != self._counts:
+            self._n[:], self._grad_dtype[:], self._codes, self._counts = counts, codes, codes, counts
+        self._grad[:] = at
         number = self.steps + 1
-        _check(L.pbkd_adamw_step(len(sizes), self._address, _ADAMW_ARGS.pack(lr, *self.betas, self.eps, grad_scale, number, self.state_bits,
-                                                                             (number if seed is None else seed) & 0xFFFFFFFF), _stream(stream)))
+        _check(_lib.pbkd_adamw_step(len(sizes), self._address, _ADAMW_ARGS.pack(lr, *self.betas, self.eps, grad_scale, number, self.state_bits,
+                                                                               (number if seed is None else seed) & 0xFFFFFFFF), _stream(stream)))
         self.steps = number
