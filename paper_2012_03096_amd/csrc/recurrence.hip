@@ -258,6 +258,9 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   const int t0 = tile * TILE, tk = t0 + grp * L;
   const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
+  // reads come back in order: what is needed first goes first
+  float bias[2] = {0.f, 0.f};
+  if (P.bias) floats2(P.bias + q.c, q, bias);
   Raw<T> ur[L], gr[L], orr[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, FAR>(g.at(i), q), ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
@@ -265,8 +268,6 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
 #pragma unroll
     for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
   }
-  float bias[2] = {0.f, 0.f};
-  if (P.bias) floats2(P.bias + q.c, q, bias);
   Words words;
   if (wave == 0) words = look_early(links, tile);
   float a[L][2], bb[L][2], A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Ae[2], Be[2];
@@ -357,16 +358,16 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   const int t0 = tile * TILE, tk = t0 + grp * L;
   const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), dy(P.dy, b * P.yb, P.ys, t0, slice, q, P.len);
+  float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
+  if (P.bias) floats2(P.bias + q.c, q, bias);
   Raw<T> ur[L], gr[L], orr[L], yr[L];
 #pragma unroll
-  for (int i = 0; i < L; ++i) {
-    gr[i] = raw2<T, ONE, FAR>(g.at(i), q);
-    ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, FAR>(g.at(i), q), ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i) {
     yr[i] = raw2<T, ONE, FAR>(dy.at(i), q);
     if (GATED) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
   }
-  float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
-  if (P.bias) floats2(P.bias + q.c, q, bias);
   if (wave == 2 && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
   Words words;
   if (wave == 0) words = look_early(links, pos);
