@@ -685,3 +685,22 @@ def test_binding_refusals(gpu):
         with pytest.raises(pb.PbkdError):
             f()
             pytest.fail(f"call {i} was not refused")
+
+
+def test_sequence_block_learns_and_answers_token_by_token(gpu):
+    """The example's student: the local loss on a frozen block's labels falls to a tenth, and the answers token by token are those
+    of the pass over all tokens, up to the roundings of bf16 (three products and a norm on the way: 2^-6 of the output's size)."""
+    torch, pb = gpu
+    from paper_2012_03096_amd import sequence
+    losses, off = sequence.demo(d=64, batch=16, length=200, steps=400, lr=1e-2, report=399)
+    assert losses[-1] < 0.1 * losses[0] and np.isfinite(losses).all()
+    assert off < 2.0 ** -6
+    block = sequence.SequenceBlock(64, seed=5)
+    x = _randn(torch, 8, 2, 40, 64, dtype="bf16")
+    r = _randn(torch, 9, 2, 40, 64, dtype="bf16")
+    whole = block.forward(x, residual=r)
+    state, pieces, at = torch.zeros(2, 64, device="cuda"), [], 0
+    for n in (7, 1, 32):
+        pieces.append(block.forward(x[:, at:at + n].contiguous(), residual=r[:, at:at + n].contiguous(), state=state, state_out=state))
+        at += n
+    assert float((torch.cat(pieces, 1).float() - whole.float()).norm() / whole.float().norm()) < 2.0 ** -6
