@@ -410,38 +410,40 @@ _RECURRENCE_GRAD = struct.Struct("@2iqi12P14qPNPN")
 _ADAMW_ARGS = struct.Struct("@5dqiI")
 _ADAMW_TENSOR = np.dtype([("n", "i8"), ("first", "i8"), ("param_dtype", "i4"), ("grad_dtype", "i4"), ("weight_decay", "f4"), ("param", "u8"), ("grad", "u8"),
                           ("m", "u8"), ("v", "u8"), ("m_scale", "u8"), ("v_scale", "u8"), ("copy", "u8")], align=True)
-_torch = None       # set with the types by _types(), at the first call that needs them
+_torch = _current_device = None       # set with the types by _types(), at the first call that needs them
 _CODES, _FP8, _FP32, _INT32 = {}, None, None, None
 
 
 def _types():
     """torch and its types by the library's numbers; the library is loaded (and torch with it) on the way."""
-    global _torch, _CODES, _FP8, _FP32, _INT32
+    global _torch, _current_device, _CODES, _FP8, _FP32, _INT32
     import torch
     _CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    _FP8, _FP32, _INT32, _torch = torch.float8_e4m3fn, torch.float32, torch.int32, torch
+    _FP8, _FP32, _INT32, _torch, _current_device = torch.float8_e4m3fn, torch.float32, torch.int32, torch, torch.cuda.current_device
     return lib()
 
 
 def _first(t, name: str):
-    """(library, type's number, GPU) of a call's first tensor, which must lie on the current GPU: the kernels are launched there."""
+    """(library, type's number, type, shape, GPU) of a call's first tensor, which must lie on the current GPU: the kernels are launched
+    there."""
     L = _lib if _torch is not None and _lib is not None else _types()
-    code, dev = _CODES.get(t.dtype), t.get_device()
+    dtype, dev = t.dtype, t.get_device()
+    code = _CODES.get(dtype)
     if code is None:
-        raise PbkdError(EINVAL, f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
-    if dev < 0 or dev != _torch.cuda.current_device():
+        raise PbkdError(EINVAL, f"{name} must be float32, bfloat16 or float16, not {dtype}")
+    if dev < 0 or dev != _current_device():
         raise PbkdError(EINVAL, f"{name} must lie on the current GPU, not on {t.device}")
-    return L, code, dev
+    return L, code, dtype, t.shape, dev
 
 
 def _stream(stream) -> int:
     return stream.cuda_stream if stream is not None else _torch.cuda.current_stream().cuda_stream
 
 
-def _same(t, like, dev: int, name: str) -> int:
-    """Address of t, which has like's shape and type and lies on GPU dev."""
-    if t.dtype is not like.dtype or t.shape != like.shape or t.get_device() != dev:
-        raise PbkdError(ESHAPE, f"{name} must be a {like.dtype} tensor of {tuple(like.shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
+def _same(t, dtype, shape, dev: int, name: str) -> int:
+    """Address of t, a tensor of this type and shape on GPU dev."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise PbkdError(ESHAPE, f"{name} must be a {dtype} tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -480,20 +482,20 @@ def rmsnorm_workspace_bytes(rows: int, d: int) -> int:
 def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: float = 1e-6, stream=None) -> None:
     """pbkd_rmsnorm_forward: y <- norm(x + residual) * weight over the last dimension, total <- x + residual.
     y: like x, or float8_e4m3fn with scale [rows] float32."""
-    L, code, dev = _first(x, "x")
-    d = x.shape[-1] if x.dim() else 0
+    L, code, dt, shape, dev = _first(x, "x")
+    d = shape[-1] if shape else 0
     if d == 0:
         raise PbkdError(ESHAPE, "x has no elements in a row")
     rows = x.numel() // d
     eight = y.dtype is _FP8
-    if eight and (y.shape != x.shape or y.get_device() != dev):
+    if eight and (y.shape != shape or y.get_device() != dev):
         raise PbkdError(ESHAPE, f"y must have x's shape {tuple(x.shape)} and lie on its GPU")
     if scale is not None and not eight:
         raise PbkdError(EINVAL, "a scale goes with a float8_e4m3fn y only")
     _check(L.pbkd_rmsnorm_forward(_RMSNORM.pack(
-        rows, d, code, E4M3 if eight else code, eps, x.data_ptr(), 0 if residual is None else _same(residual, x, dev, "residual"),
-        _dense(weight, (d,), _FP32, dev, "weight"), 0 if total is None else _same(total, x, dev, "total"),
-        y.data_ptr() if eight else _same(y, x, dev, "y"), _dense(scale, (rows,), _FP32, dev, "scale"), _row_stride(x, d, "x"),
+        rows, d, code, E4M3 if eight else code, eps, x.data_ptr(), 0 if residual is None else _same(residual, dt, shape, dev, "residual"),
+        _dense(weight, (d,), _FP32, dev, "weight"), 0 if total is None else _same(total, dt, shape, dev, "total"),
+        y.data_ptr() if eight else _same(y, dt, shape, dev, "y"), _dense(scale, (rows,), _FP32, dev, "scale"), _row_stride(x, d, "x"),
         0 if residual is None else _row_stride(residual, d, "residual"), 0 if total is None else _row_stride(total, d, "total"), _row_stride(y, d, "y")),
         _stream(stream)))
 
@@ -501,14 +503,14 @@ def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: fl
 def rmsnorm_backward(total, weight, dy, dx, dweight, workspace, dtotal=None, eps: float = 1e-6, stream=None) -> None:
     """pbkd_rmsnorm_backward: dx and dweight from the sum as stored by the forward pass, dy and (optionally) the gradient that
     arrives at the sum.  workspace: a tensor of rmsnorm_workspace_bytes(rows, d) bytes."""
-    L, code, dev = _first(total, "total")
-    d = total.shape[-1] if total.dim() else 0
+    L, code, dt, shape, dev = _first(total, "total")
+    d = shape[-1] if shape else 0
     if d == 0:
         raise PbkdError(ESHAPE, "total has no elements in a row")
     wp, wn = _bytes(workspace, dev, "workspace")
     _check(L.pbkd_rmsnorm_backward(_RMSNORM_GRAD.pack(
-        total.numel() // d, d, code, eps, total.data_ptr(), _same(dy, total, dev, "dy"), 0 if dtotal is None else _same(dtotal, total, dev, "dtotal"),
-        _dense(weight, (d,), _FP32, dev, "weight"), _same(dx, total, dev, "dx"), _dense(dweight, (d,), _FP32, dev, "dweight"),
+        total.numel() // d, d, code, eps, total.data_ptr(), _same(dy, dt, shape, dev, "dy"), 0 if dtotal is None else _same(dtotal, dt, shape, dev, "dtotal"),
+        _dense(weight, (d,), _FP32, dev, "weight"), _same(dx, dt, shape, dev, "dx"), _dense(dweight, (d,), _FP32, dev, "dweight"),
         _row_stride(total, d, "total"), _row_stride(dy, d, "dy"), 0 if dtotal is None else _row_stride(dtotal, d, "dtotal"), _row_stride(dx, d, "dx"), wp, wn),
         _stream(stream)))
 
@@ -523,46 +525,46 @@ def recurrence_workspace_bytes(batch: int, length: int, channels: int) -> int:
 
 def _tokens(t, name: str):
     """(batch stride, token stride) of t [batch, len, channels]."""
-    s = t.stride()
-    if s[2] != 1 and t.shape[2] > 1:
+    b, s, c = t.stride()
+    if c != 1 and t.shape[2] > 1:
         raise PbkdError(EINVAL, f"{name}'s channels must be contiguous")
-    return s[0], s[1]
+    return b, s
 
 
-def _sequence_shape(u):
-    if u.dim() != 3 or u.shape[2] == 0:
-        raise PbkdError(ESHAPE, f"u must be [batch, len, channels], not {tuple(u.shape)}")
-    return u.shape
+def _sequence_shape(shape):
+    if len(shape) != 3 or shape[2] == 0:
+        raise PbkdError(ESHAPE, f"u must be [batch, len, channels], not {tuple(shape)}")
+    return shape
 
 
 def recurrence_forward(u, gate, y, out_gate=None, bias=None, lengths=None, state=None, state_out=None, saved=None, workspace=None, stream=None) -> None:
     """pbkd_recurrence_forward on [batch, len, channels] tensors: y, and the last state in state_out.  saved: a tensor of
     recurrence_saved_bytes() for the backward pass; workspace: one of recurrence_workspace_bytes()."""
-    L, code, dev = _first(u, "u")
-    b, t, d = _sequence_shape(u)
+    L, code, dt, shape, dev = _first(u, "u")
+    b, t, d = _sequence_shape(shape)
     f32 = _FP32
     sp, sn = _bytes(saved, dev, "saved")
     wp, wn = _bytes(workspace, dev, "workspace")
     _check(L.pbkd_recurrence_forward(_RECURRENCE.pack(
-        b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
+        b, d, t, code, u.data_ptr(), _same(gate, dt, shape, dev, "gate"), 0 if out_gate is None else _same(out_gate, dt, shape, dev, "out_gate"),
         _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), _INT32, dev, "lengths"), _dense(state, (b, d), f32, dev, "state"),
-        _dense(state_out, (b, d), f32, dev, "state_out"), _same(y, u, dev, "y"), *_tokens(u, "u"), *_tokens(gate, "gate"),
+        _dense(state_out, (b, d), f32, dev, "state_out"), _same(y, dt, shape, dev, "y"), *_tokens(u, "u"), *_tokens(gate, "gate"),
         *((0, 0) if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(y, "y"), sp, sn, wp, wn), _stream(stream)))
 
 
 def recurrence_backward(u, gate, dy, saved, du, dgate, out_gate=None, dout_gate=None, bias=None, dbias=None, lengths=None, dstate_out=None, dstate=None,
                         workspace=None, stream=None) -> None:
     """pbkd_recurrence_backward: the gradients of recurrence_forward's inputs from dy and what it saved."""
-    L, code, dev = _first(u, "u")
-    b, t, d = _sequence_shape(u)
+    L, code, dt, shape, dev = _first(u, "u")
+    b, t, d = _sequence_shape(shape)
     f32 = _FP32
     sp, sn = _bytes(saved, dev, "saved")
     wp, wn = _bytes(workspace, dev, "workspace")
     none = (0, 0)
     _check(L.pbkd_recurrence_backward(_RECURRENCE_GRAD.pack(
-        b, d, t, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"), _same(dy, u, dev, "dy"),
+        b, d, t, code, u.data_ptr(), _same(gate, dt, shape, dev, "gate"), 0 if out_gate is None else _same(out_gate, dt, shape, dev, "out_gate"), _same(dy, dt, shape, dev, "dy"),
         _dense(bias, (d,), f32, dev, "bias"), _dense(lengths, (b,), _INT32, dev, "lengths"), _dense(dstate_out, (b, d), f32, dev, "dstate_out"),
-        _same(du, u, dev, "du"), _same(dgate, u, dev, "dgate"), 0 if dout_gate is None else _same(dout_gate, u, dev, "dout_gate"),
+        _same(du, dt, shape, dev, "du"), _same(dgate, dt, shape, dev, "dgate"), 0 if dout_gate is None else _same(dout_gate, dt, shape, dev, "dout_gate"),
         _dense(dbias, (d,), f32, dev, "dbias"), _dense(dstate, (b, d), f32, dev, "dstate"), *_tokens(u, "u"), *_tokens(gate, "gate"),
         *(none if out_gate is None else _tokens(out_gate, "out_gate")), *_tokens(dy, "dy"), *_tokens(du, "du"), *_tokens(dgate, "dgate"),
         *(none if dout_gate is None else _tokens(dout_gate, "dout_gate")), sp, sn, wp, wn), _stream(stream)))
@@ -571,15 +573,15 @@ def recurrence_backward(u, gate, dy, saved, du, dgate, out_gate=None, dout_gate=
 def recurrence_step(u, gate, state, y, out_gate=None, bias=None, active=None, state_out=None, stream=None) -> None:
     """pbkd_recurrence_step: one token of each sequence, [batch, channels] rows with any stride; state [batch, channels] float32 is
     updated in place (or goes to state_out).  active: int32 [batch], 0 for idle rows."""
-    L, code, dev = _first(u, "u")
-    if u.dim() != 2 or u.shape[1] == 0:
-        raise PbkdError(ESHAPE, f"u must be [batch, channels], not {tuple(u.shape)}")
-    f32, (b, d) = _FP32, u.shape
+    L, code, dt, shape, dev = _first(u, "u")
+    if len(shape) != 2 or shape[1] == 0:
+        raise PbkdError(ESHAPE, f"u must be [batch, channels], not {tuple(shape)}")
+    f32, (b, d) = _FP32, shape
     sp = _dense(state, (b, d), f32, dev, "state")
     _check(L.pbkd_recurrence_step(_RECURRENCE.pack(
-        b, d, 1, code, u.data_ptr(), _same(gate, u, dev, "gate"), 0 if out_gate is None else _same(out_gate, u, dev, "out_gate"),
+        b, d, 1, code, u.data_ptr(), _same(gate, dt, shape, dev, "gate"), 0 if out_gate is None else _same(out_gate, dt, shape, dev, "out_gate"),
         _dense(bias, (d,), f32, dev, "bias"), _dense(active, (b,), _INT32, dev, "active"), sp, sp if state_out is None else _dense(state_out, (b, d), f32, dev, "state_out"),
-        _same(y, u, dev, "y"), _row_stride(u, d, "u"), 0, _row_stride(gate, d, "gate"), 0, 0 if out_gate is None else _row_stride(out_gate, d, "out_gate"), 0,
+        _same(y, dt, shape, dev, "y"), _row_stride(u, d, "u"), 0, _row_stride(gate, d, "gate"), 0, 0 if out_gate is None else _row_stride(out_gate, d, "out_gate"), 0,
         _row_stride(y, d, "y"), 0, 0, 0, 0, 0), _stream(stream)))
 
 
@@ -601,7 +603,7 @@ class AdamW:
             if given is not None and len(given) != n:
                 raise PbkdError(ESHAPE, f"{len(given)} {name} for {n} parameters")
         _types()
-        self._dev = _first(self.params[0], "a parameter")[2] if n else -1
+        self._dev = _first(self.params[0], "a parameter")[4] if n else -1
         self._table = t = np.zeros(n, _ADAMW_TENSOR)
         kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
         sizes, rows, made = [p.numel() for p in self.params], [], []
@@ -636,7 +638,7 @@ class AdamW:
         dev, sizes = self._dev, self._sizes
         if len(grads) != len(sizes):
             raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(sizes)} parameters")
-        if dev >= 0 and dev != _torch.cuda.current_device():
+        if dev >= 0 and dev != _current_device():
             raise PbkdError(EINVAL, "the parameters must lie on the current GPU")
         codes, counts, at = [], [], []
         for g, n in zip(grads, sizes):
