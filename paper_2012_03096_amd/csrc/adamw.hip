@@ -3,7 +3,7 @@
 //   m <- b1 m + (1-b1) g,  v <- b2 v + (1-b2) g^2,  p <- p (1 - lr wd) - (lr/bc1) m / (sqrt(v)/sqrt(bc2) + eps)
 //
 // One launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments: nothing has to be copied to
-// the device first, and a captured call keeps them.  A workgroup owns a chunk of kChunk elements of one tensor, found by a
+// the device first, and a captured call keeps them.  A workgroup owns a chunk of elements of one tensor, found by a
 // search over the tensors' first chunks; four consecutive elements go to a lane, so that a wave's 256 are just one block of
 // the 8-bit states and its maximum is a reduction over the wave.  Bound by memory.
 #include "seq_common.h"
@@ -12,8 +12,10 @@ namespace pbkd {
 namespace {
 
 constexpr int kBlock = 256;                    // elements that share a scale
-constexpr int kRounds = 4;                     // blocks of a wave
-constexpr int kChunk = 4 * kRounds * kBlock;   // elements of a workgroup: four waves
+// Elements of a workgroup: four waves, of a block each in every round.  Calls that go past the caches are long enough for four rounds;
+// others have too few workgroups then (6M bf16 parameters 17.6 against 18.4 us, 201M 553 against 542 us).
+constexpr int rounds_of(bool far) { return far ? 4 : 2; }
+constexpr int chunk_of(bool far) { return 4 * rounds_of(far) * kBlock; }
 constexpr int kTensors = 40;                   // descriptors of a launch: 72 bytes each, below the 4 KB of a kernel's arguments
 
 struct Tensor {
@@ -33,6 +35,7 @@ struct Launch {
   int tensors;
   unsigned seed;
   float b1, c1, b2, c2, eps, gscale, step, root;   // c = 1 - b, step = lr / bc1, root = 1 / sqrt(bc2)
+  float c1g, rb2, rc2g;                            // 8-bit states: c1 gscale, sqrt(b2), sqrt(c2) gscale
 };
 static_assert(sizeof(Launch) <= 4000, "kernel arguments");
 
@@ -70,8 +73,9 @@ __device__ __forceinline__ float reciprocal(float x) {
   return fmaf(fmaf(-x, r, 1.f), r, r);
 }
 
-// The root and the quotient of the update in 8-bit kernels, which are bound by their arithmetic: the hardware's approximations with
-// the residual put right once, within 0.6 units of the last place.  (Squares below 2^-126 have the root zero.)
+// The root and the quotient of the update in 8-bit kernels, whose arithmetic takes as long as their memory: the hardware's
+// approximations with the residual put right once, within 0.6 units of the last place (random rounding of a bf16 parameter
+// looks at bits far below its own).  Squares below 2^-126 have the root zero.
 __device__ __forceinline__ float root_of(float v) {
   const float s = __builtin_amdgcn_sqrtf(v), r = fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rsqf(v), s);
   return __builtin_amdgcn_classf(v, 0x100) ? r : s;      // positive and normal: not zero, infinite or NaN
@@ -82,8 +86,9 @@ __device__ __forceinline__ float quotient(float a, float b) {
 }
 
 // WHOLE: all of the chunk's elements exist.
-template <typename P, typename G, bool EIGHT, bool FAR, bool WHOLE>
+template <typename P, typename G, bool EIGHT, bool FAR, bool WHOLE, int kRounds>
 __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, long long chunk) {
+  constexpr int kChunk = 4 * kRounds * kBlock;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float p[kRounds][4], g[kRounds][4], m[kRounds][4], v[kRounds][4];
   const long long base = chunk * kChunk + wave * (kRounds * kBlock) + lane * 4, left = t.n - base;
@@ -108,10 +113,10 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       const float sm = n > 0 ? t.ms[e / kBlock] : 0.f, sv = n > 0 ? t.vs[e / kBlock] : 0.f;
       const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mc, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mc, true);
       const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(vc, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(vc, true);
-      m[k][0] = m01[0] * sm, m[k][1] = m01[1] * sm, m[k][2] = m23[0] * sm, m[k][3] = m23[1] * sm;
-      v[k][0] = v01[0] * sv, v[k][1] = v01[1] * sv, v[k][2] = v23[0] * sv, v[k][3] = v23[1] * sv;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[k][i] = v[k][i] * v[k][i];
+      // already with their factors of this step: b1 m and sqrt(b2) sqrt(v)
+      const float smb = sm * L.b1, svb = sv * L.rb2;
+      m[k][0] = m01[0] * smb, m[k][1] = m01[1] * smb, m[k][2] = m23[0] * smb, m[k][3] = m23[1] * smb;
+      v[k][0] = v01[0] * svb, v[k][1] = v01[1] * svb, v[k][2] = v23[0] * svb, v[k][3] = v23[1] * svb;
     }
   }
   const unsigned number = (t.first + (unsigned)base) * kMul + L.seed * 0x632BE5ABu;
@@ -124,14 +129,17 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
     float mtop = 0.f, vtop = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float gr = g[k][i] * L.gscale;
-      m[k][i] = fmaf(m[k][i], L.b1, gr * L.c1);
-      v[k][i] = fmaf(v[k][i], L.b2, gr * gr * L.c2);
       float q;
       if (EIGHT) {
+        const float u = g[k][i] * L.rc2g;
+        m[k][i] = fmaf(g[k][i], L.c1g, m[k][i]);
+        v[k][i] = fmaf(u, u, v[k][i] * v[k][i]);
         root[i] = root_of(v[k][i]);
         q = quotient(m[k][i], fmaf(root[i], L.root, L.eps));
       } else {
+        const float gr = g[k][i] * L.gscale;
+        m[k][i] = fmaf(m[k][i], L.b1, gr * L.c1);
+        v[k][i] = fmaf(v[k][i], L.b2, gr * gr * L.c2);
         root[i] = sqrtf(v[k][i]);
         q = m[k][i] / fmaf(root[i], L.root, L.eps);
       }
@@ -177,8 +185,9 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
 
 template <typename P, typename G, bool EIGHT, bool FAR>
 __device__ __forceinline__ void adamw_piece(const Launch &L, const Tensor &t, long long chunk) {
-  if ((chunk + 1) * kChunk <= t.n) adamw_chunk<P, G, EIGHT, FAR, true>(L, t, chunk);
-  else adamw_chunk<P, G, EIGHT, false, false>(L, t, chunk);
+  constexpr int kRounds = rounds_of(FAR);
+  if ((chunk + 1) * chunk_of(FAR) <= t.n) adamw_chunk<P, G, EIGHT, FAR, true, kRounds>(L, t, chunk);
+  else adamw_chunk<P, G, EIGHT, false, false, kRounds>(L, t, chunk);
 }
 
 // Six waves a SIMD are worth 3 % with 32-bit states, and cost the 8-bit kernel as much.
@@ -238,6 +247,7 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
   L.seed = a->seed;
   L.b1 = (float)a->beta1, L.c1 = (float)(1. - a->beta1), L.b2 = (float)a->beta2, L.c2 = (float)(1. - a->beta2);
   L.eps = (float)a->eps, L.gscale = (float)a->grad_scale;
+  L.c1g = (float)((1. - a->beta1) * a->grad_scale), L.rb2 = (float)sqrt(a->beta2), L.rc2g = (float)(sqrt(1. - a->beta2) * a->grad_scale);
   L.step = (float)(a->lr / (1. - pow(a->beta1, (double)a->step)));
   L.root = (float)(1. / sqrt(1. - pow(a->beta2, (double)a->step)));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -254,7 +264,7 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
   };
   for (int i = 0; i < n_tensors; ++i) {
     const pbkd_adamw_tensor &t = tensors[i];
-    const long long chunks = cdiv64(t.n, kChunk);   // at most 2^22; a launch's threads must stay below 2^32
+    const long long chunks = cdiv64(t.n, chunk_of(far));   // at most 2^22 (what is not far is small); a launch's threads must stay below 2^32
     if (chunks == 0) continue;
     if (L.tensors == kTensors || L.chunk0[L.tensors] + chunks > (1LL << 23)) SEQ_HIPCHK(flush());
     const int k = L.tensors++;
