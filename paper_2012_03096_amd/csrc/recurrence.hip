@@ -61,45 +61,58 @@ __device__ __forceinline__ void sigmoids(float x, float &a, float &z) {
 // sigmoid(x) far: exp(-x) may be infinite
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-// The two channels of a lane.  Where a row's last lane has only one (D is odd) they are taken one by one; lanes and channels
-// beyond the row read its last channels again, and nothing of them is written.
+// The two channels of a lane.  A row's last lane may have only one (D is odd): it reads the last two and moves its own to the front.
+// Lanes beyond the row read its last channels again, and nothing of them is written.
 struct Lane {
-  int c;        // first channel, moved into the row
+  int c;        // first channel that is read
   int n;        // channels that exist: 2, 1 or 0
-  bool one;     // the workgroup's loads go channel by channel
+  bool odd;     // a lane of the workgroup has only one
 };
+// How a workgroup's lanes take their channels: all two by two; a lane may have one; the row has no two.
+enum { PAIRS, ODD, SINGLE };
 __device__ __forceinline__ Lane lane_of(int slice, int D) {
   Lane q;
-  const int c0 = slice * kSlice + (threadIdx.x & 31) * 2;
-  q.one = (D & 1) && slice * kSlice + kSlice > D;
+  const int c0 = slice * kSlice + (threadIdx.x & 31) * 2, last = D > 2 ? D - 2 : 0;
+  q.odd = (D & 1) && slice * kSlice + kSlice > D;
   q.n = D - c0 < 2 ? (D - c0 < 0 ? 0 : D - c0) : 2;
-  q.c = q.one ? (c0 < D ? c0 : D - 1) : (c0 < D ? c0 : D - 2);
+  q.c = c0 < last ? c0 : last;
   return q;
 }
 template <typename T>
 using Raw = typename VecOf<T, 2>::type;
 // FAR: see far_load; and no cache line has another tile's channels too, or the line's second reader would fetch it again
 // (7x1000x515 in fp32, forward and backward: 56 -> 64 us; 8x4096x2048, whose tiles are alone with theirs: 319 -> 305 us).
-template <typename T, bool ONE, bool FAR>
+template <typename T, int HOW, bool FAR>
 __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
-  if (!ONE) return far_load<FAR, T, 2>(p);
   Raw<T> r;
-  r[0] = p[0], r[1] = p[q.n == 2 ? 1 : 0];
+  if (HOW == SINGLE) {
+    r[0] = r[1] = *p;
+  } else {
+    r = far_load<FAR, T, 2>(p);
+    if (HOW == ODD) r[0] = q.n == 1 ? r[1] : r[0];
+  }
   return r;
 }
-template <typename T, bool ONE, bool FAR>
+// lanes without channels do not come here
+template <typename T, int HOW, bool FAR>
 __device__ __forceinline__ void put2(T *p, const Lane &q, const float (&v)[2]) {
-  if (ONE) {
-    store_n<T, 2>(p, q.n, v);
-  } else {                                 // lanes without channels do not come here
+  if (HOW != PAIRS && q.n == 1) {
+    p[HOW == SINGLE ? 0 : 1] = static_cast<T>(v[0]);      // its place was moved with its reads
+  } else {
     Raw<T> r;
     r[0] = static_cast<T>(v[0]), r[1] = static_cast<T>(v[1]);
     far_store<FAR, T, 2>(r, p);
   }
 }
+// fp32 rows of channels, by the lane's own place
+template <int HOW>
 __device__ __forceinline__ void floats2(const float *p, const Lane &q, float (&v)[2]) {
-  const Raw<float> r = q.one ? raw2<float, true, false>(p, q) : raw2<float, false, false>(p, q);
+  const Raw<float> r = raw2<float, HOW, false>(p + q.c, q);
   v[0] = r[0], v[1] = r[1];
+}
+template <int HOW>
+__device__ __forceinline__ void put_floats2(float *p, const Lane &q, const float (&v)[2]) {
+  if (q.n > 0) put2<float, HOW, false>(p + q.c, q, v);
 }
 
 // Places of a thread's L tokens in one tensor: a base that its wave shares, and each token's own 32-bit distance from it, which
@@ -113,9 +126,10 @@ struct Place {
   __device__ __forceinline__ Place(const void *p, long long batch_at, long long stride_, int t0, int slice, const Lane &q, long long T_) {
     const int w0 = t0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * L, at = WHOLE || w0 < T_ ? w0 : (int)T_ - 1;
     stride = (unsigned)stride_ * (unsigned)sizeof(T);
-    base = const_cast<char *>(static_cast<const char *>(p)) + (batch_at + at * stride_ + slice * kSlice) * (long long)sizeof(T);
+    const int c0 = slice > 0 ? slice * kSlice - 2 : 0;      // a slice's only lane may read from the channel in front
+    base = const_cast<char *>(static_cast<const char *>(p)) + (batch_at + at * stride_ + c0) * (long long)sizeof(T);
     token = threadIdx.x & 32 ? L : 0, last = (int)T_ - 1 - at;
-    mine = (unsigned)(q.c - slice * kSlice) * (unsigned)sizeof(T);
+    mine = (unsigned)(q.c - c0) * (unsigned)sizeof(T);
     if (WHOLE) mine += (unsigned)token * stride;
   }
   __device__ __forceinline__ T *at(int i) const {
@@ -247,8 +261,8 @@ __device__ __forceinline__ R forget(R r) {
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
-// WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.  ONE: see Lane.
-template <typename T, bool GATED, bool WHOLE, bool ONE, bool FAR>
+// WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.
+template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR>
 __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
   constexpr int L = kFwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -260,13 +274,13 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
   // reads come back in order: what is needed first goes first
   float bias[2] = {0.f, 0.f};
-  if (P.bias) floats2(P.bias + q.c, q, bias);
+  if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L];
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, FAR>(g.at(i), q), ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
   if (GATED) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
+    for (int i = 0; i < L; ++i) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
   }
   Words words;
   if (wave == 0) words = look_early(links, tile);
@@ -313,7 +327,7 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
 #pragma unroll
   for (int k = 0; k < 2; ++k) h[k] = fmaf(Ae[k], h[k], Be[k]);
   if (P.saved && (grp * L) % kSaved == 0 && tk < P.len)
-    store_n<float, 2>(P.saved + (b * ((P.len + kSaved - 1) / kSaved) + tk / kSaved) * P.D + q.c, q.n, h);
+    put_floats2<HOW>(P.saved + (b * ((P.len + kSaved - 1) / kSaved) + tk / kSaved) * P.D, q, h);
   if (q.n == 0) return;
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -328,9 +342,9 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
       }
       out[k] = WHOLE || tk + i < len ? out[k] : 0.f;
     }
-    if (WHOLE || tk + i < P.len) put2<T, ONE, FAR>(y.at(i), q, out);
+    if (WHOLE || tk + i < P.len) put2<T, HOW, FAR>(y.at(i), q, out);
   }
-  if (P.hT && tile + 1 == P.tiles && grp == 7) store_n<float, 2>(P.hT + (long long)b * P.D + q.c, q.n, h);
+  if (P.hT && tile + 1 == P.tiles && grp == 7) put_floats2<HOW>(P.hT + (long long)b * P.D, q, h);
 }
 
 template <typename T, bool GATED, bool FAR>
@@ -342,12 +356,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_ke
   const int tile = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (!FAR && q.one) fwd_tile<T, GATED, false, true, false>(P, S, tile, chain, q, len);
-  else if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, false, FAR>(P, S, tile, chain, q, len);
-  else fwd_tile<T, GATED, true, false, FAR>(P, S, tile, chain, q, len);
+  if (FAR) {                 // rows are whole cache lines
+    if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, PAIRS, FAR>(P, S, tile, chain, q, len);
+    else fwd_tile<T, GATED, true, PAIRS, FAR>(P, S, tile, chain, q, len);
+  } else if (P.D == 1) {
+    fwd_tile<T, GATED, false, SINGLE, false>(P, S, tile, chain, q, len);
+  } else if ((tile + 1) * (8LL * kFwdL) > len) {
+    fwd_tile<T, GATED, false, ODD, false>(P, S, tile, chain, q, len);
+  } else if (q.odd) {
+    fwd_tile<T, GATED, true, ODD, false>(P, S, tile, chain, q, len);
+  } else {
+    fwd_tile<T, GATED, true, PAIRS, false>(P, S, tile, chain, q, len);
+  }
 }
 
-template <typename T, bool GATED, bool WHOLE, bool ONE, bool FAR>
+template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR>
 __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, int chain, const Lane &q, int len) {
   constexpr int L = kBwdL, TILE = 8 * L;
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -359,14 +382,14 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), dy(P.dy, b * P.yb, P.ys, t0, slice, q, P.len);
   float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
-  if (P.bias) floats2(P.bias + q.c, q, bias);
+  if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L], yr[L];
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, ONE, FAR>(g.at(i), q), ur[i] = raw2<T, ONE, FAR>(u.at(i), q);
+  for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
 #pragma unroll
   for (int i = L - 1; i >= 0; --i) {
-    yr[i] = raw2<T, ONE, FAR>(dy.at(i), q);
-    if (GATED) orr[i] = raw2<T, ONE, FAR>(o.at(i), q);
+    yr[i] = raw2<T, HOW, FAR>(dy.at(i), q);
+    if (GATED) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
   }
   if (wave == 2 && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
   Words words;
@@ -470,15 +493,15 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
         db[k] += dg[k];
       }
       if (WHOLE || tk + i < P.len) {
-        put2<T, ONE, FAR>(du.at(i), q, dv);
-        put2<T, ONE, FAR>(dgp.at(i), q, dg);
-        if (GATED) put2<T, ONE, FAR>(dop.at(i), q, dou);
+        put2<T, HOW, FAR>(du.at(i), q, dv);
+        put2<T, HOW, FAR>(dgp.at(i), q, dg);
+        if (GATED) put2<T, HOW, FAR>(dop.at(i), q, dou);
       }
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) e[k] = a[0][k] * dh[k];
   }
-  if (P.dh0 && tile == 0 && grp == 0) store_n<float, 2>(P.dh0 + (long long)b * P.D + q.c, q.n, e);
+  if (P.dh0 && tile == 0 && grp == 0) put_floats2<HOW>(P.dh0 + (long long)b * P.D, q, e);
   if (P.dbias_partial) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -499,9 +522,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_ke
   const int pos = __builtin_amdgcn_readfirstlane(S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
-  if (!FAR && q.one) bwd_tile<T, GATED, false, true, false>(P, S, pos, chain, q, len);
-  else if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, false, FAR>(P, S, pos, chain, q, len);
-  else bwd_tile<T, GATED, true, false, FAR>(P, S, pos, chain, q, len);
+  if (FAR) {                 // rows are whole cache lines
+    if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, PAIRS, FAR>(P, S, pos, chain, q, len);
+    else bwd_tile<T, GATED, true, PAIRS, FAR>(P, S, pos, chain, q, len);
+  } else if (P.D == 1) {
+    bwd_tile<T, GATED, false, SINGLE, false>(P, S, pos, chain, q, len);
+  } else if ((P.tiles - pos) * (8LL * kBwdL) > len) {
+    bwd_tile<T, GATED, false, ODD, false>(P, S, pos, chain, q, len);
+  } else if (q.odd) {
+    bwd_tile<T, GATED, true, ODD, false>(P, S, pos, chain, q, len);
+  } else {
+    bwd_tile<T, GATED, true, PAIRS, false>(P, S, pos, chain, q, len);
+  }
 }
 
 // One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
