@@ -276,11 +276,16 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   float bias[2] = {0.f, 0.f};
   if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L];
+  if (WHOLE || t0 < len) {
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
-  if (GATED) {
+    for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
+    if (GATED) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
+      for (int i = 0; i < L; ++i) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
+    }
+  } else {                   // behind the sequence: nothing to read, only zeros to write and the state to pass on
+#pragma unroll
+    for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = Raw<T>{};
   }
   Words words;
   if (wave == 0) words = look_early(links, tile);
@@ -384,12 +389,17 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
   if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L], yr[L];
+  if (WHOLE || t0 < len) {
 #pragma unroll
-  for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
+    for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
 #pragma unroll
-  for (int i = L - 1; i >= 0; --i) {
-    yr[i] = raw2<T, HOW, FAR>(dy.at(i), q);
-    if (GATED) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
+    for (int i = L - 1; i >= 0; --i) {
+      yr[i] = raw2<T, HOW, FAR>(dy.at(i), q);
+      if (GATED) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = yr[i] = Raw<T>{};
   }
   if (wave == 2 && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
   Words words;
