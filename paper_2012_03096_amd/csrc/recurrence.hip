@@ -244,6 +244,14 @@ struct alignas(16) Shared {
   unsigned number;
 };
 
+// A chain of one tile has no words, nor are they cleared for it.
+__device__ __forceinline__ int place_in_chain(unsigned long long *work, int chain, int tiles, Shared &S) {
+  if (tiles == 1) return 0;
+  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(work + chain * words_of_chain(tiles), 1ull);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(S.number);
+}
+
 // The pairs of two channels next to each other, and the state behind them.
 __device__ __forceinline__ void apply_pairs(const float2 *p, float (&h)[2]) {
   const float4 v = *reinterpret_cast<const float4 *>(p);
@@ -356,9 +364,7 @@ template <typename T, bool GATED, bool FAR>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
-  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work + chain * words_of_chain(P.tiles), 1ull);
-  __syncthreads();
-  const int tile = __builtin_amdgcn_readfirstlane(S.number);
+  const int tile = place_in_chain(P.work, chain, P.tiles, S);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (FAR) {                 // rows are whole cache lines
@@ -527,9 +533,7 @@ template <typename T, bool GATED, bool FAR>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
-  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(P.work + chain * words_of_chain(P.tiles), 1ull);
-  __syncthreads();
-  const int pos = __builtin_amdgcn_readfirstlane(S.number);
+  const int pos = place_in_chain(P.work, chain, P.tiles, S);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (FAR) {                 // rows are whole cache lines
@@ -606,7 +610,7 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
     const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
     const int size = sizeof(T);
     const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 4 : 3) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && (!A.o || lines(A.o, A.ob, A.os, size));
-    clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
+    if (A.tiles > 1) clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
     if (A.o && far) recurrence_fwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
     else if (A.o) recurrence_fwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
     else if (far) recurrence_fwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
@@ -621,7 +625,7 @@ hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const int size = sizeof(T);
   const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 7 : 5) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
                      (!A.o || lines(A.o, A.ob, A.os, size));
-  clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
+  if (A.tiles > 1) clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
   if (A.o && far) recurrence_bwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
   else if (A.o) recurrence_bwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
   else if (far) recurrence_bwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);

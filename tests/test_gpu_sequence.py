@@ -704,3 +704,75 @@ def test_sequence_block_learns_and_answers_token_by_token(gpu):
         pieces.append(block.forward(x[:, at:at + n].contiguous(), residual=r[:, at:at + n].contiguous(), state=state, state_out=state))
         at += n
     assert float((torch.cat(pieces, 1).float() - whole.float()).norm() / whole.float().norm()) < 2.0 ** -6
+
+
+# ------------------------------------------- calls beyond the last-level cache: the same bits as in smaller pieces
+def test_rmsnorm_of_many_rows(gpu):
+    torch, pb = gpu
+    rows, d, cut = 60001, 1280, 23456
+    x, r = (torch.randn(rows, d, device="cuda").bfloat16() for _ in range(2))
+    w = 1.0 + _randn(torch, 3, d, scale=0.3)
+    y, total, q, scale = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, d, device="cuda", dtype=torch.float8_e4m3fn), torch.empty(rows, device="cuda")
+    pb.rmsnorm_forward(x, w, y, residual=r, total=total)
+    pb.rmsnorm_forward(x, w, q, residual=r, total=total, scale=scale)
+    dx, dw = torch.empty_like(x), torch.empty(d, device="cuda")
+    ws = torch.empty(pb.rmsnorm_workspace_bytes(rows, d), device="cuda", dtype=torch.uint8)
+    pb.rmsnorm_backward(total, w, x, dx, dw, ws, dtotal=r)
+    for part in (slice(0, 1000), slice(cut, cut + 1001), slice(rows - 7, rows)):
+        a, b, e, f, g = torch.empty_like(x[part]), torch.empty_like(x[part]), torch.empty_like(q[part]), torch.empty_like(scale[part]), torch.empty_like(x[part])
+        pb.rmsnorm_forward(x[part], w, a, residual=r[part], total=b)
+        pb.rmsnorm_forward(x[part], w, e, residual=r[part], scale=f)
+        pb.rmsnorm_backward(b, w, x[part], g, torch.empty_like(dw), ws, dtotal=r[part])
+        assert torch.equal(a, y[part]) and torch.equal(b, total[part]) and torch.equal(e.view(torch.uint8), q[part].view(torch.uint8)) and torch.equal(f, scale[part])
+        assert torch.equal(g, dx[part])
+    ref = torch.zeros(d, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(ref)
+    for i in range(0, rows, 8192):
+        s, dy = total[i:i + 8192].double(), x[i:i + 8192].double()
+        t = dy * s * torch.rsqrt((s * s).mean(1, keepdim=True) + 1e-6)
+        ref, size = ref + t.sum(0), size + t.abs().sum(0)
+    _within(_np(dw), ref.cpu().numpy(), ((64 + rows / 32) * E * size).cpu().numpy(), "dweight")
+
+
+@pytest.mark.parametrize("gated", [True, False])
+def test_recurrence_of_much_data(gpu, gated):
+    torch, pb = gpu
+    b, t, d = 6, 9000, 1280
+    make = lambda: torch.randn(b, t, d, device="cuda").bfloat16()                                    # noqa: E731
+    q = {"u": make(), "gate": make(), "out_gate": make() if gated else None, "bias": torch.rand(d, device="cuda") * 6, "state": torch.randn(b, d, device="cuda"),
+         "lengths": torch.tensor([t, t - 1, 4000, 0, t, 1], dtype=torch.int32).cuda()}
+    f = _forward(torch, pb, q)
+    dy, dT = make(), torch.randn(b, d, device="cuda")
+    g = _backward(torch, pb, q, f, dy, dT)
+    for i in range(b):                               # one sequence a call stays below the cache's size
+        one = {k: (v if k == "bias" else v[i:i + 1]) if v is not None else None for k, v in q.items()}
+        f1 = _forward(torch, pb, one)
+        g1 = _backward(torch, pb, one, f1, dy[i:i + 1], dT[i:i + 1])
+        assert torch.equal(f1["y"], f["y"][i:i + 1]) and torch.equal(f1["state"], f["state"][i:i + 1])
+        assert all(torch.equal(g1[k], g[k][i:i + 1]) for k in ("du", "dgate", "dstate") + (("dout_gate",) if gated else ()))
+
+
+@pytest.mark.parametrize("bits,param,grad", [(32, "f32", "f32"), (8, "f32", "bf16"), (8, "bf16", "bf16")])
+def test_adamw_of_many_elements(gpu, bits, param, grad):
+    torch, pb = gpu
+    n, cut = 40_000_123, 256 * 54321
+    make = lambda kind, s: (torch.randn(n, device="cuda") * s).to(_type(torch, kind))                # noqa: E731
+    p, g = make(param, 0.1), make(grad, 0.01)
+    blocks = -(-n // 256)
+    if bits == 32:
+        st = [make("f32", 0.003), make("f32", 0.01).square()]
+    else:
+        st = [(torch.randn(n, device="cuda") * 60).clamp(-448, 448).to(torch.float8_e4m3fn), (torch.rand(n, device="cuda") * 448).to(torch.float8_e4m3fn),
+              torch.rand(blocks, device="cuda") * 1e-4 + 1e-6, torch.rand(blocks, device="cuda") * 1e-4 + 1e-6]
+    p2, st2 = p.clone(), [x.clone() for x in st]
+    c, c2 = ([torch.empty(n, dtype=torch.bfloat16, device="cuda") for _ in range(2)] if param == "f32" else (None, None))
+    pb.AdamW([p], state_bits=bits, states=[tuple(st)], copies=[c] if c is not None else None, weight_decay=0.1).step([g], 0.01)
+    for a, e in ((0, cut), (cut, n)):                # the second piece with the elements' numbers of the whole
+        for a2 in range(a, e, 256 * 30000):          # pieces below the cache's size
+            e2 = min(e, a2 + 256 * 30000)
+            piece = [x[a2:e2] for x in st2[:2]] + [x[a2 // 256:-(-e2 // 256)] for x in st2[2:]]
+            opt = pb.AdamW([p2[a2:e2]], state_bits=bits, states=[tuple(piece)], copies=[c2[a2:e2]] if c2 is not None else None, weight_decay=0.1)
+            opt._table["first"] = a2
+            opt.step([g[a2:e2]], 0.01)
+    assert torch.equal(p, p2) and all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(st, st2))
+    assert c is None or torch.equal(c, c2)
