@@ -573,6 +573,34 @@ def test_adamw_random_rounding_is_fair_and_never_reaches_zero(gpu):
     assert c[0] == 448 and c[5] == 0 and (np.delete(c, [0, 5]) == 2.0 ** -9).all()
 
 
+def test_adamw_codes_are_those_of_separate_operations(gpu):
+    """The 8-bit states of fp32 arithmetic with every product, sum, root and quotient rounded by itself, code for code: products
+    fused into their sums would move about four codes in a million over the middle between two, here some ten."""
+    torch, pb = gpu
+    f, n, b1, b2, scale = np.float32, 3 * 1048576 + 77, 0.9, 0.999, 0.37
+    ps, gs, states = _adamw_setup(torch, [n], "f32", "bf16", 8, seed=9)
+    m8, v8, sm, sv = [x.clone() for x in states[0]]
+    opt = pb.AdamW(ps, state_bits=8, states=states, betas=(b1, b2), steps=6)
+    opt.step(gs, 0.01, grad_scale=scale)
+    at = lambda t: np.repeat(t.cpu().numpy(), 256)[:n]                                     # noqa: E731
+    g = gs[0].float().cpu().numpy() * f(scale)
+    m, v = m8.float().cpu().numpy() * at(sm), v8.float().cpu().numpy() * at(sv)
+    m = m * f(b1) + g * f(1 - b1)
+    root = np.sqrt((v * v) * f(b2) + (g * g) * f(1 - b2))
+    up = (osq.element_hash(n, 7) >> 12).astype(np.uint32)
+    for k, x in ((0, m), (1, root)):
+        top = np.abs(np.concatenate([x, np.zeros(-n % 256, f)]).reshape(-1, 256)).max(1)
+        assert x.dtype == top.dtype == f
+        assert (states[0][2 + k].cpu().numpy() == top * f(1 / 448)).all()
+        x = np.minimum(x * np.repeat(f(1) / top * f(448), 256)[:n], f(448))
+        if k == 1:
+            low = np.where(x < f(2.0 ** -6), f(2.0 ** -6), f(0))
+            r = ((((x + low).view(np.uint32) + up) & np.uint32(0xFFF00000)).view(f)) - low
+            x = np.where(x > 0, np.maximum(r, f(2.0 ** -9)), f(0))
+        want = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8)
+        assert torch.equal(states[0][k].cpu().view(torch.uint8), want)
+
+
 def test_adamw_not_finite(gpu):
     torch, pb = gpu
     p, g = torch.ones(600, device="cuda"), torch.ones(600, device="cuda")
