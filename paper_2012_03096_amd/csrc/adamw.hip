@@ -84,9 +84,9 @@ __device__ __forceinline__ float quotient(float a, float b) {
   return fmaf(fmaf(-q, b, a), r, q);
 }
 
-// a b + c d with every product and the sum rounded.  What is coded in 8 bits takes its steps as the formula has them: a code near the middle
-// between two is then the same however the step was computed, on the host or one operation a kernel.  Fused, 700 of 201M codes were
-// others; 6M bf16 parameters took 17.4 instead of 18.2 us, 201M 542 either way.
+// a b + c d with every product and the sum rounded.  What ends in 8 bits, or in bf16 by a random number, takes its steps as the formula
+// has them: a value near the middle between two codes is then coded the same however the steps were computed, on the host or one
+// operation a kernel.  Fused, 700 of 201M codes were others; 6M bf16 parameters took 17.4 instead of 18.4 us, 201M 542 either way.
 __device__ __forceinline__ float sum_of_products(float a, float b, float c, float d) {
 #pragma clang fp contract(off)
   return a * b + c * d;
@@ -134,21 +134,12 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
     float mtop = 0.f, vtop = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float q;
-      if (EIGHT) {
-        const float gr = g[k][i] * L.gscale;
-        m[k][i] = sum_of_products(m[k][i], L.b1, gr, L.c1);
-        v[k][i] = sum_of_products(v[k][i] * v[k][i], L.b2, gr * gr, L.c2);
-        root[i] = root_of(v[k][i]);
-        q = quotient(m[k][i], fmaf(root[i], L.root, L.eps));
-      } else {
-        const float gr = g[k][i] * L.gscale;
-        m[k][i] = fmaf(m[k][i], L.b1, gr * L.c1);
-        v[k][i] = fmaf(v[k][i], L.b2, gr * gr * L.c2);
-        root[i] = sqrtf(v[k][i]);
-        q = m[k][i] / fmaf(root[i], L.root, L.eps);
-      }
-      q = fmaf(-q, L.step, p[k][i] * t.decay);
+      const float gr = g[k][i] * L.gscale, square = EIGHT ? v[k][i] * v[k][i] : v[k][i];
+      m[k][i] = sum_of_products(m[k][i], L.b1, gr, L.c1);
+      v[k][i] = sum_of_products(square, L.b2, gr * gr, L.c2);
+      root[i] = EIGHT ? root_of(v[k][i]) : sqrtf(v[k][i]);
+      const float below = sum_of_products(root[i], L.root, L.eps, 1.f);
+      const float q = sum_of_products(p[k][i], t.decay, EIGHT ? quotient(m[k][i], below) : m[k][i] / below, -L.step);
       if (EIGHT || sizeof(P) == 2) noise[i] = element_hash(number + (k * kBlock + i) * kMul);
       if (sizeof(P) == 2) {
         // to one of the two neighbours, by 16 random bits; infinities and NaN stay what they are

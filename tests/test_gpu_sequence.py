@@ -601,6 +601,36 @@ def test_adamw_codes_are_those_of_separate_operations(gpu):
         assert torch.equal(states[0][k].cpu().view(torch.uint8), want)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+def test_adamw_steps_are_those_of_separate_operations(gpu, bits, param):
+    """Parameters and 32-bit states of fp32 arithmetic with every product, sum, root and quotient rounded by itself, bit for bit, so
+    that random rounding to bf16 decides alike.  (The 8-bit kernels' roots and quotients miss the nearest number about once in
+    2^21 times: one unit of the last place of an fp32 parameter's move, below one of the parameter's own.)"""
+    torch, pb = gpu
+    f, n, b1, b2, lr, wd, step = np.float32, 1048576 + 77, 0.9, 0.999, 0.01, np.float64(np.float32(0.1)), 7
+    ps, gs, states = _adamw_setup(torch, [n], param, "f32", bits, seed=19)
+    p = ps[0].float().cpu().numpy()
+    m, v = [x.float().cpu().numpy() for x in states[0][:2]]
+    if bits == 8:
+        at = lambda t: np.repeat(t.cpu().numpy(), 256)[:n]                                 # noqa: E731
+        m, v = m * at(states[0][2]), np.square(v * at(states[0][3]))
+    pb.AdamW(ps, state_bits=bits, states=states, betas=(b1, b2), weight_decay=wd, steps=step - 1).step(gs, lr)
+    g = gs[0].cpu().numpy()
+    m, v = m * f(b1) + g * f(1 - b1), v * f(b2) + (g * g) * f(1 - b2)
+    move = m / (np.sqrt(v) * f(1 / np.sqrt(1 - b2 ** step)) + f(1e-8)) * f(lr / (1 - b1 ** step))
+    p = p * f(1 - lr * wd) - move
+    assert p.dtype == move.dtype == f
+    if param == "bf16":
+        p = ((p.view(np.uint32) + (osq.element_hash(n, step) & 0xFFFF).astype(np.uint32)) & np.uint32(0xFFFF0000)).view(f)
+    got = ps[0].float().cpu().numpy()
+    if bits == 32:
+        assert (got == p).all() and (states[0][0].cpu().numpy() == m).all() and (states[0][1].cpu().numpy() == v).all()
+    else:
+        other = np.abs(got.astype(np.float64) - p) / (np.spacing(np.abs(p)) if param == "f32" else 2.0 ** -7 * np.abs(p) + 1e-30)
+        assert (other > 0).sum() <= n * 2.0 ** -18 and other.max() <= 1
+
+
 def test_adamw_not_finite(gpu):
     torch, pb = gpu
     p, g = torch.ones(600, device="cuda"), torch.ones(600, device="cuda")
