@@ -177,6 +177,19 @@ def test_rmsnorm_rows_of_zeros_and_what_is_not_finite(gpu):
     assert np.isfinite(s).all() and (s > 0).all() and np.abs(q[4] * s[4] - 1e-27).max() < 1e-31
 
 
+@pytest.mark.parametrize("x_scale,w_scale", [(1e15, 1e30), (1e16, 1e-20), (1e-15, 1e-25), (1e-17, 1e35), (1e-12, 1e-29)])
+@pytest.mark.parametrize("d", [40, 300, 9000])
+def test_rmsnorm_8_bits_of_far_magnitudes(gpu, x_scale, w_scale, d):
+    """The sum times the weight would pass fp32's range, or fall under it, where the output is far from both ends."""
+    torch, pb = gpu
+    x, w = _randn(torch, 1, 6, d, scale=x_scale), _randn(torch, 2, d, scale=w_scale)
+    y, _, _ = osq.rmsnorm(_np(x), _np(w), eps=0.0)
+    q, scale = torch.empty(6, d, device="cuda", dtype=torch.float8_e4m3fn), torch.empty(6, device="cuda")
+    pb.rmsnorm_forward(x, w, q, scale=scale, eps=0.0)
+    torch.cuda.synchronize()
+    _check_codes(torch, _np(q), _np(scale), y, "e4m3")
+
+
 def test_rmsnorm_without_rows(gpu):
     torch, pb = gpu
     x, w, dw = torch.empty(0, 8, device="cuda"), torch.ones(8, device="cuda"), torch.full((8,), 3.0, device="cuda")
