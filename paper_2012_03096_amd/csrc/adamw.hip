@@ -5,7 +5,11 @@
 // One launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments: nothing has to be copied to
 // the device first, and a captured call keeps them.  A workgroup owns a chunk of elements of one tensor, found by a
 // search over the tensors' first chunks; four consecutive elements go to a lane, so that a wave's 256 are just one block of
-// the 8-bit states and its maximum is a reduction over the wave.  Bound by memory.
+// the 8-bit states and its maximum is a reduction over the wave.
+//
+// Bound by memory: 67M fp32 parameters with 32-bit states 303 us, 6.2 TB/s; 201M fp32 parameters, bf16 gradients and copies,
+// 8-bit states 541 us, 6.0 TB/s.  Smaller calls are bound by the last-level cache and their arithmetic (6M bf16 parameters, 8-bit
+// states, 18.4 us), eight tensors of a convolutional block by the launch (8.1 us, 4.9 of them the kernel).
 #include "seq_common.h"
 
 namespace pbkd {

@@ -12,6 +12,13 @@
 // each other a row of kSlice channels, the eight half waves of a workgroup follow each other in time.  Each thread folds its
 // tokens, the half waves' pairs are joined by an exchange between the halves and through LDS, and the tokens are gone through
 // again from the registers: each tensor is read once.  Tiles of all times run at once and hand the state on (below).
+//
+// Bound by memory, then by the wait for the state.  A row of a tile is 128 bytes of a 16-bit type (a slice of 128 channels in workgroups of
+// 512 threads reads better alone, but its registers allow half as many tiles at a time: 8x4096x2048 324 us against 288).
+// Measured (bf16, with the output gate): 1x65536x1280 forward 143 us, 4.7 TB/s, without the waits it would be 120; 8x4096x2048
+// forward and backward 288 us, 5.1 TB/s (forward 105, backward 182, the rest clears words and sums the bias gradient); fp32
+// 7x1000x515, padded, 47 us; one token of 64 sequences of 2048 channels 3.6 us, which is a launch's own length.  One workgroup going
+// through a chain alone took 8.8 ms for the first of these.
 #include "seq_common.h"
 
 #include <initializer_list>
@@ -21,8 +28,9 @@ namespace pbkd {
 namespace {
 
 constexpr int kSlice = 64;          // channels of a tile: 128 bytes of a 16-bit type
-constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile has 8 times as many
+constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile has 8 times as many (8: 1x65536x1280 182 us against 143)
 constexpr int kBwdL = 8;            // backward: more is held per token
+constexpr int kMostSteps = 64;      // tokens that may be taken one after the other
 constexpr int kSaved = 8 * kBwdL;   // the forward pass saves the state in front of every backward tile
 
 struct FwdArgs {
@@ -81,7 +89,7 @@ __device__ __forceinline__ Lane lane_of(int slice, int D) {
 template <typename T>
 using Raw = typename VecOf<T, 2>::type;
 // FAR: see far_load; and no cache line has another tile's channels too, or the line's second reader would fetch it again
-// (7x1000x515 in fp32, forward and backward: 56 -> 64 us; 8x4096x2048, whose tiles are alone with theirs: 319 -> 305 us).
+// (7x1000x515 in fp32, forward and backward, with it: 64 us, without: 56; 8x4096x2048, whose tiles are alone with theirs: 305, without: 319).
 template <typename T, int HOW, bool FAR>
 __device__ __forceinline__ Raw<T> raw2(const T *p, const Lane &q) {
   Raw<T> r;
@@ -154,7 +162,7 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, long long le
 // A pair travels in one 64-bit word, written and read whole at the scope of the device (the eight dies' L2 caches do not see each
 // other's writes otherwise): 0 is "not there yet", B below, A with its sign bit set above (A, a product of sigmoids, has
 // none of its own).  The words are cleared by a kernel in front.
-constexpr int kSeg = 8;      // 4: 1x65536x1280 147 -> 153 us, 16: 8x4096x2048 forward and backward 304 -> 309 us
+constexpr int kSeg = 8;      // 1x65536x1280: 147 us, with 4 153; 8x4096x2048 forward and backward: 304 us, with 16 309
 
 __device__ __forceinline__ void put_word(unsigned long long *p, float low, unsigned high) {
   __hip_atomic_store(p, (unsigned long long)high << 32 | __builtin_bit_cast(unsigned, low), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -230,6 +238,7 @@ __device__ __forceinline__ void publish_pair(const Chain &q, int pos, float A, f
   put_word(q.pairs + (long long)pos * kSlice + (threadIdx.x & 63), pos == 0 ? fmaf(A, first, B) : B, pair_high(pos == 0 ? 0.f : A));
 }
 
+// 9 MB (8x4096x2048 backward) in 5.8 us, most of it one kernel waiting for another.
 __global__ __launch_bounds__(256) void clear_words_kernel(unsigned long long *p, long long n) {
   typedef unsigned long long u2 __attribute__((ext_vector_type(2)));
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n / 2; i += (long long)gridDim.x * 256) reinterpret_cast<u2 *>(p)[i] = u2{0, 0};
@@ -277,21 +286,21 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   const Chain links = chain_of(P.work, chain, P.tiles);
   const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
   const bool upper = threadIdx.x & 32;
-  const int t0 = tile * TILE, tk = t0 + grp * L;
+  const int t0 = tile * TILE, tk = t0 + grp * L, first = t0 + __builtin_amdgcn_readfirstlane(wave) * 2 * L;      // the wave's first token
   const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), y(P.y, b * P.yb, P.ys, t0, slice, q, P.len);
   // reads come back in order: what is needed first goes first
   float bias[2] = {0.f, 0.f};
   if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L];
-  if (WHOLE || t0 < len) {
+  if (WHOLE || first < len) {
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
     if (GATED) {
 #pragma unroll
       for (int i = 0; i < L; ++i) orr[i] = raw2<T, HOW, FAR>(o.at(i), q);
     }
-  } else {                   // behind the sequence: nothing to read, only zeros to write and the state to pass on
+  } else {                   // behind the sequence: nothing to read, only zeros to write (in the sequence's tokens) and the state to pass on
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = Raw<T>{};
   }
@@ -389,13 +398,13 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   const Chain links = chain_of(P.work, chain, P.tiles);
   const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
   const bool upper = threadIdx.x & 32;
-  const int t0 = tile * TILE, tk = t0 + grp * L;
+  const int t0 = tile * TILE, tk = t0 + grp * L, first = t0 + __builtin_amdgcn_readfirstlane(wave) * 2 * L;      // the wave's first token
   const Place<T, L, WHOLE> u(P.u, b * P.ub, P.us, t0, slice, q, P.len), g(P.g, b * P.gb, P.gs, t0, slice, q, P.len);
   const Place<T, L, WHOLE> o(P.o, b * P.ob, P.os, t0, slice, q, P.len), dy(P.dy, b * P.yb, P.ys, t0, slice, q, P.len);
   float bias[2] = {0.f, 0.f}, db[2] = {0.f, 0.f}, saved = 0.f;
   if (P.bias) floats2<HOW>(P.bias, q, bias);
   Raw<T> ur[L], gr[L], orr[L], yr[L];
-  if (WHOLE || t0 < len) {
+  if (WHOLE || first < len) {
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = raw2<T, HOW, FAR>(g.at(i), q), ur[i] = raw2<T, HOW, FAR>(u.at(i), q);
 #pragma unroll
@@ -550,36 +559,70 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_ke
   }
 }
 
-// One thread takes four channels of a sequence through its tokens, one after the other: single tokens and pieces of a few.
+// One thread takes four channels of a sequence through its tokens, one after the other: single tokens and short pieces, for which a
+// tile of 128 tokens would be mostly empty.  Bound by latency, with many sequences by memory (256x24x4096 31 us, 6.6 TB/s out of the
+// last-level cache).  Measured in us, steps against tiles (bf16, with the output gate):
+//   tokens         16            24            32            48            64
+//   1x1280      4.7 /  6.8    6.3 /  6.7    7.9 /  6.7   11.1 /  6.8   14.4 /  6.9
+//   32x2048        -          6.8 /  9.0    8.5 /  8.9   11.9 / 10.1   15.6 / 11.3
+//   64x2048     5.5 / 15.0    7.3 / 15.4    9.3 / 16.1   15.7 / 20.3   19.9 / 22.8
+//   256x4096   21.6 / 97.5   30.6 / 98.3   40.3 /  131   84.5 /  161    113 /  172
+constexpr int kFewSteps = 24, kManyThreads = 32768;
+constexpr int kAhead = 8;      // tokens on their way together (4: 5.0 against 4.7 us for 1x16x1280)
 template <typename T, bool GATED>
 __global__ __launch_bounds__(64) void recurrence_step_kernel(FwdArgs P) {
+  using Four = typename VecOf<T, 4>::type;
   const int quads = (P.D + 3) / 4;
   const long long id = (long long)blockIdx.x * 64 + threadIdx.x;
   const int b = (int)(id / quads), c = (int)(id % quads) * 4, n = P.D - c < 4 ? P.D - c : 4;
   if (b >= P.batch) return;
   const int len = length_of(P.lengths, b, P.len);
-  const long long saves = (P.len + kSaved - 1) / kSaved;
+  const T *u = static_cast<const T *>(P.u) + b * P.ub + c, *g = static_cast<const T *>(P.g) + b * P.gb + c, *o = static_cast<const T *>(P.o) + b * P.ob + c;
+  T *y = static_cast<T *>(P.y) + b * P.yb + c;
   float h[4] = {0.f, 0.f, 0.f, 0.f}, bias[4] = {0.f, 0.f, 0.f, 0.f};
   if (P.h0) load_n<float, 4>(P.h0 + (long long)b * P.D + c, n, h);
   if (P.bias) load_n<float, 4>(P.bias + c, n, bias);
-  for (long long t = 0; t < P.len; ++t) {
-    if (P.saved && t % kSaved == 0) store_n<float, 4>(P.saved + (b * saves + t / kSaved) * P.D + c, n, h);
-    float out[4] = {0.f, 0.f, 0.f, 0.f};
-    if (t < len) {
-      float uv[4], gv[4], ov[4];
-      load_n<T, 4>(static_cast<const T *>(P.u) + b * P.ub + t * P.us + c, n, uv);
-      load_n<T, 4>(static_cast<const T *>(P.g) + b * P.gb + t * P.gs + c, n, gv);
-      if (GATED) load_n<T, 4>(static_cast<const T *>(P.o) + b * P.ob + t * P.os + c, n, ov);
+  auto token = [&](const float (&uv)[4], const float (&gv)[4], const float (&ov)[4], float (&out)[4]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float a, z;
-        sigmoids(gv[k] + bias[k], a, z);
-        h[k] = fmaf(a, h[k], z * uv[k]);
-        out[k] = h[k];
-        if (GATED) out[k] *= ov[k] * sigmoid(ov[k]);
+    for (int k = 0; k < 4; ++k) {
+      float a, z;
+      sigmoids(gv[k] + bias[k], a, z);
+      h[k] = fmaf(a, h[k], z * uv[k]);
+      out[k] = h[k];
+      if (GATED) out[k] *= ov[k] * sigmoid(ov[k]);
+    }
+  };
+  if (P.saved) store_n<float, 4>(P.saved + (long long)b * P.D + c, n, h);
+  static_assert(kMostSteps <= kSaved, "one saved state");
+  int t = 0;
+  if (n == 4) {
+    for (; t + kAhead <= len; t += kAhead) {
+      Four ur[kAhead], gr[kAhead], orr[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        gr[i] = far_load<false, T, 4>(g + (t + i) * P.gs), ur[i] = far_load<false, T, 4>(u + (t + i) * P.us);
+        if (GATED) orr[i] = far_load<false, T, 4>(o + (t + i) * P.os);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        float uv[4], gv[4], ov[4] = {}, out[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) uv[k] = static_cast<float>(ur[i][k]), gv[k] = static_cast<float>(gr[i][k]), ov[k] = GATED ? static_cast<float>(orr[i][k]) : 0.f;
+        token(uv, gv, ov, out);
+        store_n<T, 4>(y + (t + i) * P.ys, 4, out);
       }
     }
-    store_n<T, 4>(static_cast<T *>(P.y) + b * P.yb + t * P.ys + c, n, out);
+  }
+  for (; t < P.len; ++t) {
+    float out[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t < len) {
+      float uv[4], gv[4], ov[4] = {};
+      load_n<T, 4>(g + t * P.gs, n, gv);
+      load_n<T, 4>(u + t * P.us, n, uv);
+      if (GATED) load_n<T, 4>(o + t * P.os, n, ov);
+      token(uv, gv, ov, out);
+    }
+    store_n<T, 4>(y + t * P.ys, n, out);
   }
   if (P.hT) store_n<float, 4>(P.hT + (long long)b * P.D + c, n, h);
 }
@@ -602,8 +645,9 @@ inline bool lines(const void *p, long long batch_stride, long long stride, int s
 
 template <typename T>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
-  if (A.len <= 16) {
-    const unsigned blocks = (unsigned)cdiv64((long long)A.batch * ((A.D + 3) / 4), 64);
+  const long long threads = (long long)A.batch * ((A.D + 3) / 4);
+  if (A.len <= kFewSteps || (A.len <= kMostSteps && threads >= kManyThreads)) {
+    const unsigned blocks = (unsigned)cdiv64(threads, 64);
     if (A.o) recurrence_step_kernel<T, true><<<blocks, 64, 0, st>>>(A);
     else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
   } else {

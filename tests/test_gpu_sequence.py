@@ -267,6 +267,13 @@ def test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, sta
     assert torch.equal(out["y"], bare["y"])
 
 
+@pytest.mark.parametrize("b,t,d", [(3, 23, 70), (2, 24, 64), (3, 25, 70), (5, 8, 1), (1100, 33, 122), (1040, 64, 127), (1030, 65, 129), (513, 63, 256)])
+@pytest.mark.parametrize("dtype,gated,ragged,state", [("f32", True, True, True), ("bf16", False, True, False), ("f16", True, False, True)])
+def test_recurrence_of_short_pieces(gpu, b, t, d, dtype, gated, ragged, state):
+    """Around the lengths and numbers of sequences up to which a thread takes the tokens one after the other."""
+    test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, state)
+
+
 @pytest.mark.parametrize("t,d", [(5, 6), (130, 70), (700, 64)])
 def test_recurrence_gradient_is_the_slope_of_the_loss(gpu, t, d):
     """A step along the kernels' gradient changes the (64-bit) loss by the gradient's square, to first order."""
