@@ -594,24 +594,30 @@ __global__ __launch_bounds__(64) void recurrence_step_kernel(FwdArgs P) {
   };
   if (P.saved) store_n<float, 4>(P.saved + (long long)b * P.D + c, n, h);
   static_assert(kMostSteps <= kSaved, "one saved state");
+  // kAhead tokens from t on; those behind the last are the last again and not used
+  auto tokens = [&](auto whole, int t) {
+    constexpr int N = kAhead;
+    Four ur[N], gr[N], orr[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = whole.value || t + i < len ? t + i : len - 1;
+      gr[i] = far_load<false, T, 4>(g + at * P.gs), ur[i] = far_load<false, T, 4>(u + at * P.us);
+      if (GATED) orr[i] = far_load<false, T, 4>(o + at * P.os);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (!whole.value && t + i >= len) return;
+      float uv[4], gv[4], ov[4] = {}, out[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) uv[k] = static_cast<float>(ur[i][k]), gv[k] = static_cast<float>(gr[i][k]), ov[k] = GATED ? static_cast<float>(orr[i][k]) : 0.f;
+      token(uv, gv, ov, out);
+      store_n<T, 4>(y + (t + i) * P.ys, 4, out);
+    }
+  };
   int t = 0;
   if (n == 4) {
-    for (; t + kAhead <= len; t += kAhead) {
-      Four ur[kAhead], gr[kAhead], orr[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        gr[i] = far_load<false, T, 4>(g + (t + i) * P.gs), ur[i] = far_load<false, T, 4>(u + (t + i) * P.us);
-        if (GATED) orr[i] = far_load<false, T, 4>(o + (t + i) * P.os);
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        float uv[4], gv[4], ov[4] = {}, out[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) uv[k] = static_cast<float>(ur[i][k]), gv[k] = static_cast<float>(gr[i][k]), ov[k] = GATED ? static_cast<float>(orr[i][k]) : 0.f;
-        token(uv, gv, ov, out);
-        store_n<T, 4>(y + (t + i) * P.ys, 4, out);
-      }
-    }
+    for (; t + kAhead <= len; t += kAhead) tokens(std::true_type{}, t);
+    if (t + 1 < len) tokens(std::false_type{}, t), t = len;
   }
   for (; t < P.len; ++t) {
     float out[4] = {0.f, 0.f, 0.f, 0.f};
