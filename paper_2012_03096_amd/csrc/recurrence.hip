@@ -390,9 +390,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_ke
   }
 }
 
-template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR>
+// A tile of W waves, which share three roles between them.
+template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR, int W>
 __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, int chain, const Lane &q, int len) {
-  constexpr int L = kBwdL, TILE = 8 * L;
+  constexpr int L = kBwdL, TILE = 2 * W * L;
+  const auto mine = [](int role) { return W == 1 || (int)(threadIdx.x >> 6) == role % W; };
   const int slice = chain % P.slices, b = chain / P.slices;
   const int tile = P.tiles - 1 - pos;       // the chain starts at the last tile
   const Chain links = chain_of(P.work, chain, P.tiles);
@@ -416,7 +418,7 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = yr[i] = Raw<T>{};
   }
-  if (wave == 2 && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
+  if (mine(2) && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
   Words words;
   if (wave == 0) words = look_early(links, pos);
   if (!WHOLE) {
@@ -460,24 +462,26 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
   }
   __syncthreads();
   const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
-  if (wave == 0) {
+  if (mine(0)) {
     float At = 1.f, Bt = 0.f, first = 0.f;
 #pragma unroll
-    for (int w = 3; w >= 0; --w) Bt = fmaf(S.back[w][ch].x, Bt, S.back[w][ch].y), At *= S.back[w][ch].x;
+    for (int w = W - 1; w >= 0; --w) Bt = fmaf(S.back[w][ch].x, Bt, S.back[w][ch].y), At *= S.back[w][ch].x;
     if (pos == 0 && P.dhT && cc < P.D) first = P.dhT[(long long)b * P.D + cc];
     if (tile > 0) publish_pair(links, pos, At, Bt, first);
     S.at[ch] = look_back(links, pos, tile == 0, At, Bt, first, words);
-  } else if (wave == 1) {
+  }
+  if (mine(1)) {
     float2 v = make_float2(1.f, 0.f);
 #pragma unroll
-    for (int w = 3; w >= 0; --w) {
+    for (int w = W - 1; w >= 0; --w) {
       S.part[w][ch] = v;
       v = make_float2(v.x * S.back[w][ch].x, fmaf(S.back[w][ch].x, v.y, S.back[w][ch].y));
     }
-  } else if (wave == 2) {
+  }
+  if (mine(2)) {
     float v = saved;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       S.h[w][ch] = v;
       v = fmaf(S.tot[w][ch].x, v, S.tot[w][ch].y);
     }
@@ -534,28 +538,33 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
       if (!upper) S.h[wave][cl + k] = v;        // each wave's own, which only it read
     }
     __syncthreads();
-    if (wave == 0 && cc < P.D) P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = (S.h[0][ch] + S.h[1][ch]) + (S.h[2][ch] + S.h[3][ch]);
+    if (wave == 0 && cc < P.D) {
+      float v = S.h[0][ch];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v += S.h[w][ch];
+      P.dbias_partial[((long long)b * P.tiles + tile) * P.D + cc] = v;
+    }
   }
 }
 
-template <typename T, bool GATED, bool FAR>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
+template <typename T, bool GATED, bool FAR, int W>
+__global__ __launch_bounds__(64 * W, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
   __shared__ Shared S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
   const int pos = place_in_chain(P.work, chain, P.tiles, S);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (FAR) {                 // rows are whole cache lines
-    if ((P.tiles - pos) * (8LL * kBwdL) > len) bwd_tile<T, GATED, false, PAIRS, FAR>(P, S, pos, chain, q, len);
-    else bwd_tile<T, GATED, true, PAIRS, FAR>(P, S, pos, chain, q, len);
+    if ((P.tiles - pos) * (2LL * W * kBwdL) > len) bwd_tile<T, GATED, false, PAIRS, FAR, W>(P, S, pos, chain, q, len);
+    else bwd_tile<T, GATED, true, PAIRS, FAR, W>(P, S, pos, chain, q, len);
   } else if (P.D == 1) {
-    bwd_tile<T, GATED, false, SINGLE, false>(P, S, pos, chain, q, len);
-  } else if ((P.tiles - pos) * (8LL * kBwdL) > len) {
-    bwd_tile<T, GATED, false, ODD, false>(P, S, pos, chain, q, len);
+    bwd_tile<T, GATED, false, SINGLE, false, W>(P, S, pos, chain, q, len);
+  } else if ((P.tiles - pos) * (2LL * W * kBwdL) > len) {
+    bwd_tile<T, GATED, false, ODD, false, W>(P, S, pos, chain, q, len);
   } else if (q.odd) {
-    bwd_tile<T, GATED, true, ODD, false>(P, S, pos, chain, q, len);
+    bwd_tile<T, GATED, true, ODD, false, W>(P, S, pos, chain, q, len);
   } else {
-    bwd_tile<T, GATED, true, PAIRS, false>(P, S, pos, chain, q, len);
+    bwd_tile<T, GATED, true, PAIRS, false, W>(P, S, pos, chain, q, len);
   }
 }
 
@@ -676,10 +685,18 @@ hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 7 : 5) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
                      (!A.o || lines(A.o, A.ob, A.os, size));
   if (A.tiles > 1) clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-  if (A.o && far) recurrence_bwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
-  else if (A.o) recurrence_bwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
-  else if (far) recurrence_bwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
-  else recurrence_bwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
+  // Short sequences take tiles of fewer waves, of which more fit on a compute unit.  Measured in us, four waves against one (16 tokens) or two
+  // (32): bf16 with the output gate, 1x16x1280 6.3 / 4.5, 64x16x2048 19.4 / 7.5, 256x16x4096 127 / 38;
+  // 1x32x1280 6.4 / 4.7, 64x32x2048 21.7 / 14.1, 256x32x4096 109 / 101, 256x17x4096 137 / 77.
+  const int waves = A.len <= 2 * kBwdL ? 1 : A.len <= 4 * kBwdL ? 2 : 4;
+  if (A.o && waves == 1) recurrence_bwd_kernel<T, true, false, 1><<<grid, 64, 0, st>>>(A);
+  else if (waves == 1) recurrence_bwd_kernel<T, false, false, 1><<<grid, 64, 0, st>>>(A);
+  else if (A.o && waves == 2) recurrence_bwd_kernel<T, true, false, 2><<<grid, 128, 0, st>>>(A);
+  else if (waves == 2) recurrence_bwd_kernel<T, false, false, 2><<<grid, 128, 0, st>>>(A);
+  else if (A.o && far) recurrence_bwd_kernel<T, true, true, 4><<<grid, 256, 0, st>>>(A);
+  else if (A.o) recurrence_bwd_kernel<T, true, false, 4><<<grid, 256, 0, st>>>(A);
+  else if (far) recurrence_bwd_kernel<T, false, true, 4><<<grid, 256, 0, st>>>(A);
+  else recurrence_bwd_kernel<T, false, false, 4><<<grid, 256, 0, st>>>(A);
   return hipGetLastError();
 }
 

@@ -274,6 +274,13 @@ def test_recurrence_of_short_pieces(gpu, b, t, d, dtype, gated, ragged, state):
     test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, state)
 
 
+@pytest.mark.parametrize("b,t,d", [(4, 15, 66), (7, 16, 64), (3, 17, 129), (260, 31, 65), (5, 32, 64), (4, 33, 70), (300, 16, 515), (6, 47, 3)])
+@pytest.mark.parametrize("dtype,gated,ragged,state", [("f32", False, True, True), ("bf16", True, False, True), ("bf16", True, True, False), ("f16", False, False, False)])
+def test_recurrence_of_sequences_shorter_than_a_tile(gpu, b, t, d, dtype, gated, ragged, state):
+    """Around the lengths at which the backward pass takes tiles of one, two and four waves."""
+    test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, state)
+
+
 @pytest.mark.parametrize("t,d", [(5, 6), (130, 70), (700, 64)])
 def test_recurrence_gradient_is_the_slope_of_the_loss(gpu, t, d):
     """A step along the kernels' gradient changes the (64-bit) loss by the gradient's square, to first order."""
