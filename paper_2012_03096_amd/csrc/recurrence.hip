@@ -9,13 +9,13 @@
 //   du = z dh, dgate = dh (h_{t-1} - u) a z, do = dy h silu'(o)
 //
 // A tile is kSlice channels by a number of tokens: a thread holds L consecutive tokens of two channels, half a wave next to
-// each other a row of kSlice channels, the eight half waves of a workgroup follow each other in time.  Each thread folds its
+// each other a row of kSlice channels, the half waves of a workgroup (of four waves mostly) follow each other in time.  Each thread folds its
 // tokens, the half waves' pairs are joined by an exchange between the halves and through LDS, and the tokens are gone through
 // again from the registers: each tensor is read once.  Tiles of all times run at once and hand the state on (below).
 //
 // Bound by memory, then by the wait for the state.  A row of a tile is 128 bytes of a 16-bit type (a slice of 128 channels in workgroups of
 // 512 threads reads better alone, but its registers allow half as many tiles at a time: 8x4096x2048 324 us against 288).
-// Measured (bf16, with the output gate): 1x65536x1280 forward 143 us, 4.7 TB/s, without the waits it would be 120; 8x4096x2048
+// Measured (bf16, with the output gate): 1x65536x1280 forward 133 us, 5.1 TB/s; 8x4096x2048
 // forward and backward 288 us, 5.1 TB/s (forward 105, backward 182, the rest clears words and sums the bias gradient); fp32
 // 7x1000x515, padded, 47 us; one token of 64 sequences of 2048 channels 3.6 us, which is a launch's own length.  One workgroup going
 // through a chain alone took 8.8 ms for the first of these.
@@ -28,10 +28,10 @@ namespace pbkd {
 namespace {
 
 constexpr int kSlice = 64;          // channels of a tile: 128 bytes of a 16-bit type
-constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile has 8 times as many (8: 1x65536x1280 182 us against 143)
+constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile of four waves has 8 times as many (8: 1x65536x1280 182 us against 143)
 constexpr int kBwdL = 8;            // backward: more is held per token
 constexpr int kMostSteps = 64;      // tokens that may be taken one after the other
-constexpr int kSaved = 8 * kBwdL;   // the forward pass saves the state in front of every backward tile
+constexpr int kSaved = 8 * kBwdL;   // the forward pass saves the state in front of every backward tile of four waves
 
 struct FwdArgs {
   const void *u, *g, *o;
@@ -245,20 +245,21 @@ __global__ __launch_bounds__(256) void clear_words_kernel(unsigned long long *p,
 }
 
 // What a workgroup shares.
+template <int W>
 struct alignas(16) Shared {
-  float2 tot[4][kSlice], back[4][kSlice];      // each wave's pair, forward and backward in time
-  float2 part[4][kSlice];                      // what lies between the tile's start (the chain's way) and each wave's
-  float h[4][kSlice];                          // backward: the state in front of each wave
+  float2 tot[W][kSlice], back[W][kSlice];      // each wave's pair, forward and backward in time
+  float2 part[W][kSlice];                      // what lies between the tile's start (the chain's way) and each wave's
+  float h[W][kSlice];                          // backward: the state in front of each wave
   float at[kSlice];
   unsigned number;
 };
 
 // A chain of one tile has no words, nor are they cleared for it.
-__device__ __forceinline__ int place_in_chain(unsigned long long *work, int chain, int tiles, Shared &S) {
+__device__ __forceinline__ int place_in_chain(unsigned long long *work, int chain, int tiles, unsigned &number) {
   if (tiles == 1) return 0;
-  if (threadIdx.x == 0) S.number = (unsigned)atomicAdd(work + chain * words_of_chain(tiles), 1ull);
+  if (threadIdx.x == 0) number = (unsigned)atomicAdd(work + chain * words_of_chain(tiles), 1ull);
   __syncthreads();
-  return __builtin_amdgcn_readfirstlane(S.number);
+  return __builtin_amdgcn_readfirstlane(number);
 }
 
 // The pairs of two channels next to each other, and the state behind them.
@@ -279,9 +280,9 @@ __device__ __forceinline__ R forget(R r) {
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // WHOLE: all tokens of the tile are the sequence's own: no place is moved, nothing is masked.
-template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR>
-__device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, int chain, const Lane &q, int len) {
-  constexpr int L = kFwdL, TILE = 8 * L;
+template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR, int W>
+__device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared<W> &S, int tile, int chain, const Lane &q, int len) {
+  constexpr int L = kFwdL, TILE = 2 * W * L;
   const int slice = chain % P.slices, b = chain / P.slices;
   const Chain links = chain_of(P.work, chain, P.tiles);
   const int cl = (threadIdx.x & 31) * 2, grp = threadIdx.x >> 5, wave = threadIdx.x >> 6;
@@ -331,14 +332,14 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
   if (wave == 0) {
     float At = 1.f, Bt = 0.f, first = 0.f;                 // the whole tile's pair, channel ch
 #pragma unroll
-    for (int w = 0; w < 4; ++w) Bt = fmaf(S.tot[w][ch].x, Bt, S.tot[w][ch].y), At *= S.tot[w][ch].x;
+    for (int w = 0; w < W; ++w) Bt = fmaf(S.tot[w][ch].x, Bt, S.tot[w][ch].y), At *= S.tot[w][ch].x;
     if (tile == 0 && P.h0 && c < P.D) first = P.h0[(long long)b * P.D + c];
     if (tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
     S.at[ch] = look_back(links, tile, tile + 1 == P.tiles, At, Bt, first, words);
   } else if (wave == 1) {
     float2 v = make_float2(1.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       S.part[w][ch] = v;
       v = make_float2(v.x * S.tot[w][ch].x, fmaf(S.tot[w][ch].x, v.y, S.tot[w][ch].y));
     }
@@ -366,33 +367,33 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared &S, int tile, 
     }
     if (WHOLE || tk + i < P.len) put2<T, HOW, FAR>(y.at(i), q, out);
   }
-  if (P.hT && tile + 1 == P.tiles && grp == 7) put_floats2<HOW>(P.hT + (long long)b * P.D, q, h);
+  if (P.hT && tile + 1 == P.tiles && grp == 2 * W - 1) put_floats2<HOW>(P.hT + (long long)b * P.D, q, h);
 }
 
-template <typename T, bool GATED, bool FAR>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
-  __shared__ Shared S;
+template <typename T, bool GATED, bool FAR, int W>
+__global__ __launch_bounds__(64 * W, sizeof(T) == 4 ? 3 : 4) void recurrence_fwd_kernel(FwdArgs P) {
+  __shared__ Shared<W> S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
-  const int tile = place_in_chain(P.work, chain, P.tiles, S);
+  const int tile = place_in_chain(P.work, chain, P.tiles, S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (FAR) {                 // rows are whole cache lines
-    if ((tile + 1) * (8LL * kFwdL) > len) fwd_tile<T, GATED, false, PAIRS, FAR>(P, S, tile, chain, q, len);
-    else fwd_tile<T, GATED, true, PAIRS, FAR>(P, S, tile, chain, q, len);
+    if ((tile + 1) * (2LL * W * kFwdL) > len) fwd_tile<T, GATED, false, PAIRS, FAR, W>(P, S, tile, chain, q, len);
+    else fwd_tile<T, GATED, true, PAIRS, FAR, W>(P, S, tile, chain, q, len);
   } else if (P.D == 1) {
-    fwd_tile<T, GATED, false, SINGLE, false>(P, S, tile, chain, q, len);
-  } else if ((tile + 1) * (8LL * kFwdL) > len) {
-    fwd_tile<T, GATED, false, ODD, false>(P, S, tile, chain, q, len);
+    fwd_tile<T, GATED, false, SINGLE, false, W>(P, S, tile, chain, q, len);
+  } else if ((tile + 1) * (2LL * W * kFwdL) > len) {
+    fwd_tile<T, GATED, false, ODD, false, W>(P, S, tile, chain, q, len);
   } else if (q.odd) {
-    fwd_tile<T, GATED, true, ODD, false>(P, S, tile, chain, q, len);
+    fwd_tile<T, GATED, true, ODD, false, W>(P, S, tile, chain, q, len);
   } else {
-    fwd_tile<T, GATED, true, PAIRS, false>(P, S, tile, chain, q, len);
+    fwd_tile<T, GATED, true, PAIRS, false, W>(P, S, tile, chain, q, len);
   }
 }
 
 // A tile of W waves, which share three roles between them.
 template <typename T, bool GATED, bool WHOLE, int HOW, bool FAR, int W>
-__device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, int chain, const Lane &q, int len) {
+__device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared<W> &S, int pos, int chain, const Lane &q, int len) {
   constexpr int L = kBwdL, TILE = 2 * W * L;
   const auto mine = [](int role) { return W == 1 || (int)(threadIdx.x >> 6) == role % W; };
   const int slice = chain % P.slices, b = chain / P.slices;
@@ -418,7 +419,7 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = yr[i] = Raw<T>{};
   }
-  if (mine(2) && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[((long long)b * P.tiles + tile) * P.D + slice * kSlice + (threadIdx.x & 63)];
+  if (mine(2) && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[(b * ((P.len + kSaved - 1) / kSaved) + t0 / kSaved) * P.D + slice * kSlice + (threadIdx.x & 63)];
   Words words;
   if (wave == 0) words = look_early(links, pos);
   if (!WHOLE) {
@@ -548,10 +549,10 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared &S, int pos, i
 }
 
 template <typename T, bool GATED, bool FAR, int W>
-__global__ __launch_bounds__(64 * W, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
-  __shared__ Shared S;
+__global__ __launch_bounds__(64 * W, W == 8 ? 4 : sizeof(T) == 4 ? 2 : 3) void recurrence_bwd_kernel(BwdArgs P) {
+  __shared__ Shared<W> S;
   const int chain = chain_of_workgroup(blockIdx.x, P.batch * P.slices);
-  const int pos = place_in_chain(P.work, chain, P.tiles, S);
+  const int pos = place_in_chain(P.work, chain, P.tiles, S.number);
   const Lane q = lane_of(chain % P.slices, P.D);
   const int len = length_of(P.lengths, chain / P.slices, P.len);
   if (FAR) {                 // rows are whole cache lines
@@ -576,6 +577,7 @@ __global__ __launch_bounds__(64 * W, sizeof(T) == 4 ? 2 : 3) void recurrence_bwd
 //   32x2048        -          6.8 /  9.0    8.5 /  8.9   11.9 / 10.1   15.6 / 11.3
 //   64x2048     5.5 / 15.0    7.3 / 15.4    9.3 / 16.1   15.7 / 20.3   19.9 / 22.8
 //   256x4096   21.6 / 97.5   30.6 / 98.3   40.3 /  131   84.5 /  161    113 /  172
+constexpr int kFewChains = 128, kLongChain = 8192;
 constexpr int kFewSteps = 24, kManyThreads = 32768;
 constexpr int kAhead = 8;      // tokens on their way together (4: 5.0 against 4.7 us for 1x16x1280)
 template <typename T, bool GATED>
@@ -658,25 +660,54 @@ inline bool lines(const void *p, long long batch_stride, long long stride, int s
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(batch_stride * size) | (uintptr_t)(stride * size)) & 127) == 0;
 }
 
+// Whether tiles have eight waves.  A chain hands its state from segment to segment, about 1.8 us each; few long chains are bound by that, and tiles
+// of twice the tokens halve it.  Many chains hide it, and want small workgroups.  Measured in us, four / eight waves (bf16 with the output gate):
+//                     chains  forward     backward                           chains  forward     backward
+//   1x131072x64          1     94 /  53   156 /  90      8x8192x512            64     63 /  60   115 / 110
+//   1x65536x1280        20    147 / 133   282 / 254      4x16384x1280          80    137 / 129   264 / 249
+//   1x16384x1280        20   47.3 / 47.9 79.7 / 73.9     8x8192x1280          160    134 / 135   252 / 252
+//   1x65536x4096        64    428 / 407   799 / 780      8x8192x2048          256    193 / 200
+// fp32's registers leave a compute unit one workgroup of eight waves (1x65536x1280 forward 244 / 249).
+inline bool tall_tiles(int batch, long long len, int slices, int size) { return size == 2 && (long long)batch * slices <= kFewChains && len >= kLongChain; }
+
 template <typename T>
-hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
+hipError_t launch_fwd(FwdArgs A, hipStream_t st) {
   const long long threads = (long long)A.batch * ((A.D + 3) / 4);
   if (A.len <= kFewSteps || (A.len <= kMostSteps && threads >= kManyThreads)) {
     const unsigned blocks = (unsigned)cdiv64(threads, 64);
     if (A.o) recurrence_step_kernel<T, true><<<blocks, 64, 0, st>>>(A);
     else recurrence_step_kernel<T, false><<<blocks, 64, 0, st>>>(A);
   } else {
-    const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
     const int size = sizeof(T);
     const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 4 : 3) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && (!A.o || lines(A.o, A.ob, A.os, size));
+    const int waves = tall_tiles(A.batch, A.len, A.slices, size) ? 8 : 4;
+    A.tiles = (int)cdiv64(A.len, 2 * waves * kFwdL);
+    const unsigned grid = (unsigned)A.batch * A.slices * A.tiles;
     if (A.tiles > 1) clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-    if (A.o && far) recurrence_fwd_kernel<T, true, true><<<grid, 256, 0, st>>>(A);
-    else if (A.o) recurrence_fwd_kernel<T, true, false><<<grid, 256, 0, st>>>(A);
-    else if (far) recurrence_fwd_kernel<T, false, true><<<grid, 256, 0, st>>>(A);
-    else recurrence_fwd_kernel<T, false, false><<<grid, 256, 0, st>>>(A);
+    if constexpr (sizeof(T) == 2) {
+      if (waves == 8) {
+        if (A.o && far) recurrence_fwd_kernel<T, true, true, 8><<<grid, 512, 0, st>>>(A);
+        else if (A.o) recurrence_fwd_kernel<T, true, false, 8><<<grid, 512, 0, st>>>(A);
+        else if (far) recurrence_fwd_kernel<T, false, true, 8><<<grid, 512, 0, st>>>(A);
+        else recurrence_fwd_kernel<T, false, false, 8><<<grid, 512, 0, st>>>(A);
+        return hipGetLastError();
+      }
+    }
+    if (A.o && far) recurrence_fwd_kernel<T, true, true, 4><<<grid, 256, 0, st>>>(A);
+    else if (A.o) recurrence_fwd_kernel<T, true, false, 4><<<grid, 256, 0, st>>>(A);
+    else if (far) recurrence_fwd_kernel<T, false, true, 4><<<grid, 256, 0, st>>>(A);
+    else recurrence_fwd_kernel<T, false, false, 4><<<grid, 256, 0, st>>>(A);
   }
   return hipGetLastError();
 }
+
+// Short sequences take tiles of fewer waves, of which more fit on a compute unit.  Measured in us, four waves against one (16 tokens) or two
+// (32): bf16 with the output gate, 1x16x1280 6.3 / 4.5, 64x16x2048 19.4 / 7.5, 256x16x4096 127 / 38;
+// 1x32x1280 6.4 / 4.7, 64x32x2048 21.7 / 14.1, 256x32x4096 109 / 101, 256x17x4096 137 / 77.
+inline int bwd_waves(int batch, long long len, int slices, int size) {
+  return len <= 2 * kBwdL ? 1 : len <= 4 * kBwdL ? 2 : tall_tiles(batch, len, slices, size) ? 8 : 4;
+}
+inline long long bwd_tiles(int batch, long long len, int channels, int size) { return cdiv64(len, 2 * bwd_waves(batch, len, cdiv(channels, kSlice), size) * kBwdL); }
 
 template <typename T>
 hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
@@ -685,15 +716,19 @@ hipError_t launch_bwd(const BwdArgs &A, hipStream_t st) {
   const bool far = (double)A.batch * A.len * A.D * size * (A.o ? 7 : 5) > kLastLevelCache && A.D * size % 128 == 0 && lines(A.u, A.ub, A.us, size) && lines(A.g, A.gb, A.gs, size) && lines(A.dy, A.yb, A.ys, size) &&
                      (!A.o || lines(A.o, A.ob, A.os, size));
   if (A.tiles > 1) clear_words(A.work, (long long)A.batch * A.slices * words_of_chain(A.tiles), st);
-  // Short sequences take tiles of fewer waves, of which more fit on a compute unit.  Measured in us, four waves against one (16 tokens) or two
-  // (32): bf16 with the output gate, 1x16x1280 6.3 / 4.5, 64x16x2048 19.4 / 7.5, 256x16x4096 127 / 38;
-  // 1x32x1280 6.4 / 4.7, 64x32x2048 21.7 / 14.1, 256x32x4096 109 / 101, 256x17x4096 137 / 77.
-  const int waves = A.len <= 2 * kBwdL ? 1 : A.len <= 4 * kBwdL ? 2 : 4;
+  const int waves = bwd_waves(A.batch, A.len, A.slices, size);
   if (A.o && waves == 1) recurrence_bwd_kernel<T, true, false, 1><<<grid, 64, 0, st>>>(A);
   else if (waves == 1) recurrence_bwd_kernel<T, false, false, 1><<<grid, 64, 0, st>>>(A);
   else if (A.o && waves == 2) recurrence_bwd_kernel<T, true, false, 2><<<grid, 128, 0, st>>>(A);
   else if (waves == 2) recurrence_bwd_kernel<T, false, false, 2><<<grid, 128, 0, st>>>(A);
-  else if (A.o && far) recurrence_bwd_kernel<T, true, true, 4><<<grid, 256, 0, st>>>(A);
+  else if (waves == 8) {
+    if constexpr (sizeof(T) == 2) {
+      if (A.o && far) recurrence_bwd_kernel<T, true, true, 8><<<grid, 512, 0, st>>>(A);
+      else if (A.o) recurrence_bwd_kernel<T, true, false, 8><<<grid, 512, 0, st>>>(A);
+      else if (far) recurrence_bwd_kernel<T, false, true, 8><<<grid, 512, 0, st>>>(A);
+      else recurrence_bwd_kernel<T, false, false, 8><<<grid, 512, 0, st>>>(A);
+    }
+  } else if (A.o && far) recurrence_bwd_kernel<T, true, true, 4><<<grid, 256, 0, st>>>(A);
   else if (A.o) recurrence_bwd_kernel<T, true, false, 4><<<grid, 256, 0, st>>>(A);
   else if (far) recurrence_bwd_kernel<T, false, true, 4><<<grid, 256, 0, st>>>(A);
   else recurrence_bwd_kernel<T, false, false, 4><<<grid, 256, 0, st>>>(A);
@@ -832,7 +867,7 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *q, void *h
                      pbkd_recurrence_workspace_bytes(q->batch, q->len, q->channels));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   float *partial = reinterpret_cast<float *>(static_cast<char *>(q->workspace_dev) + work_bytes(q->batch, q->len, q->channels));
-  const long long tiles = cdiv64(q->len, kSaved);
+  const long long tiles = bwd_tiles(q->batch, q->len, q->channels, size);
   if (any) {
     BwdArgs A{q->u_dev, q->gate_dev, q->out_gate_dev, q->dy_dev, q->bias_dev, q->lengths_dev, static_cast<const float *>(q->saved_dev), q->dstate_out_dev,
               q->du_dev, q->dgate_dev, q->dout_gate_dev, q->dbias_dev ? partial : nullptr, q->dstate_dev, static_cast<unsigned long long *>(q->workspace_dev), q->len, q->u_batch_stride, q->u_stride,

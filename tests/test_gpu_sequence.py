@@ -281,6 +281,13 @@ def test_recurrence_of_sequences_shorter_than_a_tile(gpu, b, t, d, dtype, gated,
     test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, state)
 
 
+@pytest.mark.parametrize("b,t,d", [(1, 8191, 64), (1, 8192, 64), (2, 8321, 70), (3, 9001, 5), (1, 12345, 1), (5, 8200, 130)])
+@pytest.mark.parametrize("dtype,gated,ragged,state", [("bf16", True, True, True), ("f16", False, False, True), ("f16", True, False, False), ("f32", True, True, False)])
+def test_recurrence_of_long_chains(gpu, b, t, d, dtype, gated, ragged, state):
+    """Few long sequences, from 8192 tokens of 16 bits on in taller tiles."""
+    test_recurrence_forward_and_backward(gpu, b, t, d, dtype, gated, ragged, state)
+
+
 @pytest.mark.parametrize("t,d", [(5, 6), (130, 70), (700, 64)])
 def test_recurrence_gradient_is_the_slope_of_the_loss(gpu, t, d):
     """A step along the kernels' gradient changes the (64-bit) loss by the gradient's square, to first order."""
