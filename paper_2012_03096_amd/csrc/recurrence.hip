@@ -15,7 +15,7 @@
 //
 // Bound by memory, then by the wait for the state.  A row of a tile is 128 bytes of a 16-bit type (a slice of 128 channels in workgroups of
 // 512 threads reads better alone, but its registers allow half as many tiles at a time: 8x4096x2048 324 us against 288).
-// Measured (bf16, with the output gate): 1x65536x1280 forward 133 us, 5.1 TB/s; 8x4096x2048
+// Measured (bf16, with the output gate): 1x65536x1280 forward 128 us, 5.2 TB/s; 8x4096x2048
 // forward and backward 288 us, 5.1 TB/s (forward 105, backward 182, the rest clears words and sums the bias gradient); fp32
 // 7x1000x515, padded, 47 us; one token of 64 sequences of 2048 channels 3.6 us, which is a launch's own length.  One workgroup going
 // through a chain alone took 8.8 ms for the first of these.
@@ -170,8 +170,10 @@ __device__ __forceinline__ void put_word(unsigned long long *p, float low, unsig
 __device__ __forceinline__ unsigned long long peek_word(const unsigned long long *p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// All lanes of the wave come here together and leave together: lanes that wait under a mask of their own are where the compiler, short
+// of registers, was seen to copy others' under that mask.
 __device__ __forceinline__ unsigned long long await_word(const unsigned long long *p, unsigned long long v) {
-  while (v == 0) {
+  while (__any(v == 0)) {
     __builtin_amdgcn_s_sleep(1);
     v = peek_word(p);
   }
@@ -203,27 +205,37 @@ __device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, i
 // knows the one in front: one addition and one product lie between them.  Only the chain's first tile reads the state in
 // front of the chain (`first`), and its pair is the constant map to the state behind it: the last tile, which may write over the
 // initial state, thereby has every reader of it behind itself.
+// EARLY of the pairs' words are read early.  Seven cost registers for as long as the tile's data are on their way, and tiles of eight waves,
+// which have the fewest, spill: with three 1x65536x1280 backward takes 237 us instead of 254, 1x65536x4096 728 instead of 778.
+// With four waves all of them are: 8x2048x2047 forward and backward 193 us, with three 197.
+constexpr int early_words(int waves) { return waves == 8 ? 3 : kSeg - 1; }
+template <int EARLY>
 struct Words {
-  unsigned long long v[kSeg - 1], state;
+  unsigned long long v[EARLY], state;
 };
-__device__ __forceinline__ Words look_early(const Chain &q, int pos) {
+template <int EARLY>
+__device__ __forceinline__ Words<EARLY> look_early(const Chain &q, int pos) {
   const int ch = threadIdx.x & 63, seg = pos / kSeg, in = pos % kSeg;
   const unsigned long long *p = q.pairs + (long long)seg * kSeg * kSlice + ch;
-  Words k;
+  Words<EARLY> k;
 #pragma unroll
-  for (int j = 0; j < kSeg - 1; ++j) k.v[j] = j < in ? peek_word(p + j * kSlice) : 1;
+  for (int j = 0; j < EARLY; ++j) k.v[j] = j < in ? peek_word(p + j * kSlice) : 1;
   k.state = seg > 0 ? peek_word(q.states + (long long)(seg - 1) * kSlice + ch) : 1;
   return k;
 }
 // At, Bt: the tile's own pair
-__device__ __forceinline__ float look_back(const Chain &q, int pos, bool last, float At, float Bt, float first, const Words &k) {
+template <int EARLY>
+__device__ __forceinline__ float look_back(const Chain &q, int pos, bool last, float At, float Bt, float first, const Words<EARLY> &k) {
   const int ch = threadIdx.x & 63, seg = pos / kSeg, in = pos % kSeg;
   const unsigned long long *p = q.pairs + (long long)seg * kSeg * kSlice + ch;
+  unsigned long long late[kSeg - 1];
+#pragma unroll
+  for (int j = EARLY; j < kSeg - 1; ++j) late[j] = j < in ? peek_word(p + j * kSlice) : 1;
   float A = 1.f, B = 0.f;
 #pragma unroll
   for (int j = 0; j < kSeg - 1; ++j) {
     if (j < in) {
-      const unsigned long long v = await_word(p + j * kSlice, k.v[j]);
+      const unsigned long long v = await_word(p + j * kSlice, j < EARLY ? k.v[j < EARLY ? j : 0] : late[j]);
       const float A2 = high_of(v);
       B = fmaf(A2, B, low_of(v));
       A *= A2;
@@ -305,8 +317,8 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared<W> &S, int til
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = Raw<T>{};
   }
-  Words words;
-  if (wave == 0) words = look_early(links, tile);
+  Words<early_words(W)> words;
+  if (wave == 0) words = look_early<early_words(W)>(links, tile);
   float a[L][2], bb[L][2], A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, Ae[2], Be[2];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -333,7 +345,7 @@ __device__ __forceinline__ void fwd_tile(const FwdArgs &P, Shared<W> &S, int til
     float At = 1.f, Bt = 0.f, first = 0.f;                 // the whole tile's pair, channel ch
 #pragma unroll
     for (int w = 0; w < W; ++w) Bt = fmaf(S.tot[w][ch].x, Bt, S.tot[w][ch].y), At *= S.tot[w][ch].x;
-    if (tile == 0 && P.h0 && c < P.D) first = P.h0[(long long)b * P.D + c];
+    if (tile == 0 && P.h0) first = P.h0[(long long)b * P.D + (c < P.D ? c : P.D - 1)];
     if (tile + 1 < P.tiles) publish_pair(links, tile, At, Bt, first);
     S.at[ch] = look_back(links, tile, tile + 1 == P.tiles, At, Bt, first, words);
   } else if (wave == 1) {
@@ -419,9 +431,10 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared<W> &S, int pos
 #pragma unroll
     for (int i = 0; i < L; ++i) gr[i] = ur[i] = orr[i] = yr[i] = Raw<T>{};
   }
-  if (mine(2) && slice * kSlice + (threadIdx.x & 63) < P.D) saved = P.saved[(b * ((P.len + kSaved - 1) / kSaved) + t0 / kSaved) * P.D + slice * kSlice + (threadIdx.x & 63)];
-  Words words;
-  if (wave == 0) words = look_early(links, pos);
+  const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
+  if (mine(2)) saved = P.saved[(b * ((P.len + kSaved - 1) / kSaved) + t0 / kSaved) * P.D + (cc < P.D ? cc : P.D - 1)];
+  Words<early_words(W)> words;
+  if (wave == 0) words = look_early<early_words(W)>(links, pos);
   if (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < L; ++i)
@@ -462,12 +475,11 @@ __device__ __forceinline__ void bwd_tile(const BwdArgs &P, Shared<W> &S, int pos
     else S.back[wave][cl + k] = make_float2(A[k] * A1, fmaf(A[k], R1, Br[k]));
   }
   __syncthreads();
-  const int ch = threadIdx.x & 63, cc = slice * kSlice + ch;
   if (mine(0)) {
     float At = 1.f, Bt = 0.f, first = 0.f;
 #pragma unroll
     for (int w = W - 1; w >= 0; --w) Bt = fmaf(S.back[w][ch].x, Bt, S.back[w][ch].y), At *= S.back[w][ch].x;
-    if (pos == 0 && P.dhT && cc < P.D) first = P.dhT[(long long)b * P.D + cc];
+    if (pos == 0 && P.dhT) first = P.dhT[(long long)b * P.D + (cc < P.D ? cc : P.D - 1)];
     if (tile > 0) publish_pair(links, pos, At, Bt, first);
     S.at[ch] = look_back(links, pos, tile == 0, At, Bt, first, words);
   }
@@ -663,10 +675,10 @@ inline bool lines(const void *p, long long batch_stride, long long stride, int s
 // Whether tiles have eight waves.  A chain hands its state from segment to segment, about 1.8 us each; few long chains are bound by that, and tiles
 // of twice the tokens halve it.  Many chains hide it, and want small workgroups.  Measured in us, four / eight waves (bf16 with the output gate):
 //                     chains  forward     backward                           chains  forward     backward
-//   1x131072x64          1     94 /  53   156 /  90      8x8192x512            64     63 /  60   115 / 110
-//   1x65536x1280        20    147 / 133   282 / 254      4x16384x1280          80    137 / 129   264 / 249
-//   1x16384x1280        20   47.3 / 47.9 79.7 / 73.9     8x8192x1280          160    134 / 135   252 / 252
-//   1x65536x4096        64    428 / 407   799 / 780      8x8192x2048          256    193 / 200
+//   1x131072x64          1     94 /  53   156 /  88      8x8192x512            64     63 /  59   115 / 104
+//   1x65536x1280        20    147 / 128   282 / 237      4x16384x1280          80    137 / 127   264 / 237
+//   1x16384x1280        20   47.3 / 47.8 79.7 / 69.5     8x8192x1280          160    134 / 131   252 / 245
+//   1x65536x4096        64    428 / 396   799 / 724      8x8192x2048          256    193 / 200
 // fp32's registers leave a compute unit one workgroup of eight waves (1x65536x1280 forward 244 / 249).
 inline bool tall_tiles(int batch, long long len, int slices, int size) { return size == 2 && (long long)batch * slices <= kFewChains && len >= kLongChain; }
 
