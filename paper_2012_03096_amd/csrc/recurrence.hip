@@ -14,10 +14,10 @@
 // again from the registers: each tensor is read once.  Tiles of all times run at once and hand the state on (below).
 //
 // Bound by memory, then by the wait for the state.  A row of a tile is 128 bytes of a 16-bit type (a slice of 128 channels in workgroups of
-// 512 threads reads better alone, but its registers allow half as many tiles at a time: 8x4096x2048 324 us against 288).
+// 512 threads reads better alone, but half as many tiles fit at a time: 8x4096x2048 324 us against 288).
 // Measured (bf16, with the output gate): 1x65536x1280 forward 128 us, 5.2 TB/s; 8x4096x2048
 // forward and backward 288 us, 5.1 TB/s (forward 105, backward 182, the rest clears words and sums the bias gradient); fp32
-// 7x1000x515, padded, 47 us; one token of 64 sequences of 2048 channels 3.6 us, which is a launch's own length.  One workgroup going
+// 7x1000x515, padded, 46 us; one token of 64 sequences of 2048 channels 3.6 us, which is a launch's own length.  One workgroup going
 // through a chain alone took 8.8 ms for the first of these.
 #include "seq_common.h"
 
@@ -28,7 +28,7 @@ namespace pbkd {
 namespace {
 
 constexpr int kSlice = 64;          // channels of a tile: 128 bytes of a 16-bit type
-constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile of four waves has 8 times as many (8: 1x65536x1280 182 us against 143)
+constexpr int kFwdL = 16;           // tokens of a thread, forward: a tile of four waves has 8 times as many (8: 1x65536x1280 182 us, then 143)
 constexpr int kBwdL = 8;            // backward: more is held per token
 constexpr int kMostSteps = 64;      // tokens that may be taken one after the other
 constexpr int kSaved = 8 * kBwdL;   // the forward pass saves the state in front of every backward tile of four waves
@@ -162,7 +162,7 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, long long le
 // A pair travels in one 64-bit word, written and read whole at the scope of the device (the eight dies' L2 caches do not see each
 // other's writes otherwise): 0 is "not there yet", B below, A with its sign bit set above (A, a product of sigmoids, has
 // none of its own).  The words are cleared by a kernel in front.
-constexpr int kSeg = 8;      // 1x65536x1280: 147 us, with 4 153; 8x4096x2048 forward and backward: 304 us, with 16 309
+constexpr int kSeg = 8;      // forward with 4, 8 and 16, us: 1x131072x64 82, 53, 46; 1x65536x1280 131, 130, 140; 8x4096x2048 108, 108, 168
 
 __device__ __forceinline__ void put_word(unsigned long long *p, float low, unsigned high) {
   __hip_atomic_store(p, (unsigned long long)high << 32 | __builtin_bit_cast(unsigned, low), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
