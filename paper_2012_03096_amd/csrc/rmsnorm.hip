@@ -108,6 +108,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
       for (int i = 0; i < 8; ++i) ss = fmaf(s[k][i], s[k][i], ss);
     ss = row_reduce<TPR, false>(ss, red[flip]);
     const float rms = sqrtf(ss / d + A.eps), r = 1.f / rms;
+    const bool mend = r > 0.f && r < __builtin_inff();
     if (A.total) {
       T *t = static_cast<T *>(A.total) + row * A.ts;
 #pragma unroll
@@ -116,33 +117,33 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
         store_n<T, 8, FAR>(t + c, d - c, s[k]);
       }
     }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // s / rms to its last place: the product's remainder is put right.  Each step is rounded as the formula has it, so that a code in the
+        // middle between two falls as it does where the steps are operations of their own: of 435 codes in 759M that are not the nearest to
+        // the exact ones 375 are theirs too; s w over its own maximum, two roundings less, has 312, but other ones
+        float q = s[k][i] * r;
+        q = mend ? fmaf(fmaf(-q, rms, s[k][i]), r, q) : q;
+        s[k][i] = q * w[k][i];
+      }
     if (FP8) {
-      // y over its row's maximum is s w over its own: the codes take two roundings (with s / rms first, four: 171 against 101 of 277M
-      // codes were not the nearest), and rms goes into the scale only.  s is brought near 1 by a power of two, which rounds nothing, so
-      // that s w passes fp32's range only where y does.
-      const bool usual = rms > 0.f && rms < __builtin_inff();
-      const float near = usual ? __builtin_bit_cast(float, (254u << 23) - (__builtin_bit_cast(unsigned, rms) & 0x7F800000u)) : r;
-      const float rest = usual ? rms * near : 1.f;      // in [1, 2)
-      float most = 0.f;
+      float top = 0x1p-100f;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s[k][i] = s[k][i] * near * w[k][i];
-          most = fmaxf(most, fabsf(s[k][i]));
-        }
-      most = row_reduce<TPR, true>(most, red[flip + 1]);
-      const float top = most / rest;
-      const bool tiny = !(top >= 0x1p-100f);
-      const float up = tiny ? 448.f * 0x1p100f / rest : 448.f / most;   // |y| up exceeds 448 by rounding only, far below where e4m3 would overflow
-      if (lane == 0) A.scale[row] = (tiny ? 0x1p-100f : top) * (1.f / 448.f);
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(s[k][i]));
+      top = row_reduce<TPR, true>(top, red[flip + 1]);
+      const float inv = 1.f / top * 448.f;   // |y| inv exceeds 448 by rounding only, far below where e4m3 would overflow
+      if (lane == 0) A.scale[row] = top * (1.f / 448.f);
       unsigned char *y = static_cast<unsigned char *>(A.y) + row * A.ys;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         const int c = (k * TPR + lane) * 8;
         unsigned q[2];
-        q[0] = pack_e4m3(s[k][0] * up, s[k][1] * up, s[k][2] * up, s[k][3] * up);
-        q[1] = pack_e4m3(s[k][4] * up, s[k][5] * up, s[k][6] * up, s[k][7] * up);
+        q[0] = pack_e4m3(s[k][0] * inv, s[k][1] * inv, s[k][2] * inv, s[k][3] * inv);
+        q[1] = pack_e4m3(s[k][4] * inv, s[k][5] * inv, s[k][6] * inv, s[k][7] * inv);
         if (c + 8 <= d) {
           far_store<FAR, unsigned char, 8>(__builtin_bit_cast(Raw<unsigned char>, q), y + c);
         } else {
@@ -152,15 +153,6 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_fwd_kernel(FwdA
         }
       }
     } else {
-      const bool mend = r > 0.f && r < __builtin_inff();
-#pragma unroll
-      for (int k = 0; k < ITEMS; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float q = s[k][i] * r;
-          q = mend ? fmaf(fmaf(-q, rms, s[k][i]), r, q) : q;      // s / rms to its last place
-          s[k][i] = q * w[k][i];
-        }
       T *y = static_cast<T *>(A.y) + row * A.ys;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
