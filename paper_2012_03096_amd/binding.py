@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from itertools import chain
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -590,7 +591,10 @@ class AdamW:
 
     states: per parameter (m, v), or (m, v, m_scale, v_scale) for 8 bits, flat tensors as the header describes them; None: zeros,
     allocated here (the constructor then waits for its stream once, so that any stream may step).  copies: bfloat16 tensors
-    that receive the new parameters.  weight_decay: one number, or one for each parameter.  steps: how many were made already."""
+    that receive the new parameters.  weight_decay: one number, or one for each parameter.  steps: how many were made already.
+
+    params, states and copies are lists of this object.  Each step goes to where their tensors lie then, so data or tensors may be
+    exchanged between steps; what is no longer of its first type and size is refused."""
 
     def __init__(self, params, state_bits: int = 32, states=None, copies=None, weight_decay=0.0, betas=(0.9, 0.999), eps: float = 1e-8, steps: int = 0):
         import torch
@@ -605,32 +609,50 @@ class AdamW:
         _types()
         self._dev = _first(self.params[0], "a parameter")[4] if n else -1
         self._table = t = np.zeros(n, _ADAMW_TENSOR)
-        kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
-        sizes, rows, made = [p.numel() for p in self.params], [], []
+        self._kind = kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
+        self._sizes, self._shapes, self._dtypes, made = [p.numel() for p in self.params], [p.shape for p in self.params], [p.dtype for p in self.params], []
         first = 0
         for i, p in enumerate(self.params):
             code = _CODES.get(p.dtype)
             if code not in (F32, BF16):
                 raise PbkdError(EINVAL, f"parameter {i} must be float32 or bfloat16, not {p.dtype}")
-            address = _dense(p, p.shape, p.dtype, self._dev, f"parameter {i}")
-            blocks = -(-sizes[i] // 256)
-            lens = (sizes[i], sizes[i], blocks, blocks)[:len(kind)]
             if states is None:
-                made.append(tuple(torch.zeros(k, dtype=torch.uint8 if y == torch.float8_e4m3fn else y, device=p.device).view(y) for k, y in zip(lens, kind)))
-            s = made[i] if states is None else states[i]
-            if len(s) != len(kind):
-                raise PbkdError(ESHAPE, f"parameter {i}: {len(s)} state tensors, {len(kind)} are needed")
-            at = [_dense(x, (k,), y, self._dev, f"state of parameter {i}") for x, k, y in zip(s, lens, kind)] + [0, 0]
-            cp = _dense(copies[i], p.shape, torch.bfloat16, self._dev, f"copy of parameter {i}") if copies is not None else 0
-            rows.append((sizes[i], first, code, F32, decays[i], address, 0, *at[:4], cp))
-            first += blocks * 256
-        if n:
-            t[:] = rows
+                made.append(tuple(torch.zeros(k, dtype=torch.uint8 if y == torch.float8_e4m3fn else y, device=p.device).view(y) for k, y in zip(self._state_sizes(i), kind)))
+            t[i]["first"], t[i]["param_dtype"], t[i]["weight_decay"] = first, code, decays[i]
+            first += -(-self._sizes[i] // 256) * 256
         self.states = made if states is None else list(states)
-        self._sizes, self._address = sizes, t.ctypes.data
-        self._n, self._grad_dtype, self._grad, self._codes = t["n"], t["grad_dtype"], t["grad"], None
+        self._address = t.ctypes.data
+        self._n, self._grad_dtype, self._grad, self._codes, self._at = t["n"], t["grad_dtype"], t["grad"], None, None
+        self._take_addresses()
         if states is None and n:
             torch.cuda.current_stream().synchronize()
+
+    def _state_sizes(self, i: int):
+        n = self._sizes[i]
+        return (n, n, -(-n // 256), -(-n // 256))[:len(self._kind)]
+
+    def _where(self):
+        """Addresses of all parameters, states and copies, as one list."""
+        at = [*map(_torch.Tensor.data_ptr, chain(self.params, chain.from_iterable(self.states)))]
+        return at if self.copies is None else at + [0 if c is None else c.data_ptr() for c in self.copies]
+
+    def _take_addresses(self) -> None:
+        """Looks at every tensor, which must be of the type and size it had at first, and writes its address into the table."""
+        n, names = len(self._sizes), ("m", "v", "m_scale", "v_scale")
+        for name, given in (("parameters", self.params), ("states", self.states), ("copies", self.copies)):
+            if given is not None and len(given) != n:
+                raise PbkdError(ESHAPE, f"{len(given)} {name}, {n} are needed")
+        at = {k: [] for k in ("param", "copy", *names[:len(self._kind)])}
+        for i, (p, s) in enumerate(zip(self.params, self.states)):
+            at["param"].append(_dense(p, self._shapes[i], self._dtypes[i], self._dev, f"parameter {i}"))
+            if len(s) != len(self._kind):
+                raise PbkdError(ESHAPE, f"parameter {i}: {len(s)} state tensors, {len(self._kind)} are needed")
+            for x, k, y, name in zip(s, self._state_sizes(i), self._kind, names):
+                at[name].append(_dense(x, (k,), y, self._dev, f"state of parameter {i}"))
+            at["copy"].append(_dense(self.copies[i], self._shapes[i], _torch.bfloat16, self._dev, f"copy of parameter {i}") if self.copies is not None else 0)
+        for k, v in at.items():
+            self._table[k] = v
+        self._seen = self._where()
 
     def step(self, grads, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, stream=None) -> None:
         """One step with these gradients (one for each parameter, contiguous; None: the parameter and its states stay as they are).
@@ -640,18 +662,24 @@ class AdamW:
             raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(sizes)} parameters")
         if dev >= 0 and dev != _current_device():
             raise PbkdError(EINVAL, "the parameters must lie on the current GPU")
-        codes, counts, at = [], [], []
-        for g, n in zip(grads, sizes):
-            if g is None:
-                codes.append(F32), counts.append(0), at.append(0)
-                continue
-            code = _CODES.get(g.dtype)
-            if code is None or g.numel() != n or g.get_device() != dev or not g.is_contiguous():
-                raise PbkdError(ESHAPE, f"a gradient must be contiguous, float32, bfloat16 or float16, with its parameter's {n} elements, on its GPU")
-            codes.append(code), counts.append(n), at.append(g.data_ptr())
+        if self._where() != self._seen:
+            self._take_addresses()
+        t = _torch.Tensor
+        if not all(map(t.is_contiguous, self.params)):       # data may be viewed otherwise at the same place (a shorter view: its gradient tells)
+            raise PbkdError(ESHAPE, "a parameter is no longer contiguous")
+        live, want, counts = grads, sizes, sizes
+        if any([g is None for g in grads]):
+            live, want = [g for g in grads if g is not None], [n for g, n in zip(grads, sizes) if g is not None]
+            counts = [0 if g is None else n for g, n in zip(grads, sizes)]
+        codes, at = [_CODES.get(g.dtype) for g in live], [*map(t.data_ptr, live)]
+        if None in codes or [*map(t.numel, live)] != want or not all(map(t.is_contiguous, live)) or set(map(t.get_device, live)) - {dev}:
+            raise PbkdError(ESHAPE, "a gradient must be contiguous, float32, bfloat16 or float16, with its parameter's elements, on its GPU")
+        if live is not grads:
+            codes, at = ([next(x) if g is not None else 0 for g in grads] for x in (iter(codes), iter(at)))
         if codes != self._codes or counts != self._counts:
             self._n[:], self._grad_dtype[:], self._codes, self._counts = counts, codes, codes, counts
-        self._grad[:] = at
+        if at != self._at:
+            self._grad[:] = self._at = at
         number = self.steps + 1
         _check(_lib.pbkd_adamw_step(len(sizes), self._address, _ADAMW_ARGS.pack(lr, *self.betas, self.eps, grad_scale, number, self.state_bits,
                                                                                (number if seed is None else seed) & 0xFFFFFFFF), _stream(stream)))

@@ -868,3 +868,41 @@ def test_adamw_of_many_elements(gpu, bits, param, grad):
             opt.step([g[a2:e2]], 0.01)
     assert torch.equal(p, p2) and all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(st, st2))
     assert c is None or torch.equal(c, c2)
+
+
+# ------------------------------------------------------------------------------- tensors that move between steps
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_follows_its_tensors(gpu, bits):
+    """A parameter's data, states and copies are exchanged between steps: the step works on the new ones, as an optimizer that always
+    had them does, and writes nothing into the old ones."""
+    torch, pb = gpu
+    sizes = [300, 4097, 1]
+    ps, gs, states = _adamw_setup(torch, sizes, "f32", "f32", bits)
+    copies = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for n in sizes]
+    opt = pb.AdamW(ps, state_bits=bits, states=states, copies=copies, weight_decay=0.1)
+    ref = pb.AdamW([p.clone() for p in ps], state_bits=bits, states=[tuple(x.clone() for x in s) for s in states], weight_decay=0.1)
+    raw = lambda t: t.view(torch.uint8).clone()                                            # noqa: E731
+    for k in range(4):
+        old = []
+        if k == 1:
+            old = [(p.data, raw(p.data)) for p in ps]
+            for p in ps:
+                p.data = p.data.clone()
+        elif k == 2:
+            old = [(x, raw(x)) for x in opt.states[1]] + [(c, raw(c)) for c in copies]
+            opt.states[1] = tuple(x.clone() for x in opt.states[1])
+            for i, n in enumerate(sizes):
+                copies[i] = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+        elif k == 3:
+            opt.params[0], copies[2] = ps[0].clone(), None
+            old = [(ps[0], raw(ps[0]))]
+        opt.step(gs, 0.01)
+        ref.step(gs, 0.01)
+        assert all(torch.equal(a, b) for a, b in zip(opt.params, ref.params)), k
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for s, t in zip(opt.states, ref.states) for a, b in zip(s, t)), k
+        assert all(torch.equal(c, p.to(torch.bfloat16)) for c, p in zip(copies, opt.params) if c is not None), k
+        assert all(torch.equal(t.view(torch.uint8), was) for t, was in old), k
+    ps[1].data = torch.zeros(4096, device="cuda")
+    with pytest.raises(pb.PbkdError):
+        opt.step(gs, 0.01)
+    assert opt.steps == 4

@@ -195,3 +195,105 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
         pb.rmsnorm_forward(x.double(), torch.ones(8), x)
     with pytest.raises(pb.PbkdError):
         pb.AdamW([], state_bits=4)
+
+
+class _Recorder:
+    """Stands in for the library: keeps the table of each step that reaches it (host tensors: nothing may run on their addresses)."""
+
+    def __init__(self):
+        self.tables = []
+
+    def pbkd_adamw_step(self, n, table, args, stream):
+        self.tables.append(np.frombuffer((ctypes.c_char * (n * pb._ADAMW_TENSOR.itemsize)).from_address(table), pb._ADAMW_TENSOR).copy())
+        return 0
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    torch = pytest.importorskip("torch")
+    pb._types()
+    seen = _Recorder()
+    monkeypatch.setattr(pb, "_lib", seen)
+    monkeypatch.setattr(pb, "_current_device", lambda: -1)
+    monkeypatch.setattr(pb, "_first", lambda t, name: (seen, pb._CODES.get(t.dtype), t.dtype, t.shape, -1))
+    return torch, seen
+
+
+def _adamw_on_host(torch, bits, copies=True):
+    params = [torch.zeros(6, 50), torch.zeros(300)]
+    kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    states = [tuple([torch.zeros(300).to(kind), torch.zeros(300).to(kind)] + ([] if bits == 32 else [torch.zeros(2), torch.zeros(2)])) for _ in params]
+    return pb.AdamW(params, state_bits=bits, states=states, copies=[p.bfloat16() for p in params] if copies else None)
+
+
+def _addresses(opt):
+    names = ("m", "v", "m_scale", "v_scale")[:len(opt.states[0])]
+    out = {"param": [p.data_ptr() for p in opt.params], **{k: [s[i].data_ptr() for s in opt.states] for i, k in enumerate(names)}}
+    if opt.copies is not None:
+        out["copy"] = [c.data_ptr() if c is not None else 0 for c in opt.copies]
+    return out
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_goes_to_where_its_tensors_are(recorded, bits):
+    """A parameter's data, a state or a copy that was exchanged for another tensor of the same type and size: the next step takes the
+    new one (the old one's memory may belong to somebody else by then)."""
+    torch, seen = recorded
+    opt = _adamw_on_host(torch, bits)
+    grads = [torch.zeros(6, 50), torch.zeros(300)]
+
+    def step():
+        opt.step(grads, 0.1, stream=_Stream)
+        table, want = seen.tables[-1], _addresses(opt)
+        for k, v in want.items():
+            assert table[k].tolist() == v, k
+        assert table["n"].tolist() == [300, 300]
+
+    step()
+    opt.params[0].data = torch.ones(6, 50)
+    step()
+    opt.params[1] = torch.ones(300)
+    step()
+    opt.states[1] = tuple(x.clone() for x in opt.states[1])
+    step()
+    opt.copies[0] = torch.zeros(6, 50, dtype=torch.bfloat16)
+    step()
+    opt.copies[1] = None
+    step()
+    opt.params[1].set_(torch.zeros(1000), 700, (300,))
+    step()
+
+
+@pytest.mark.parametrize("change", ["shorter", "shorter at its place", "longer", "type", "layout", "copy", "state", "state type", "count"])
+def test_adamw_refuses_tensors_that_are_not_what_they_were(recorded, change):
+    torch, seen = recorded
+    opt = _adamw_on_host(torch, 32)
+    grads = [torch.zeros(6, 50), torch.zeros(300)]
+    opt.step(grads, 0.1, stream=_Stream)
+    p = opt.params[0]
+    if change == "shorter":
+        p.data = torch.zeros(5, 50)
+    elif change == "shorter at its place":
+        p.data = p.data[:5]
+        grads[0] = torch.zeros(5, 50)
+    elif change == "longer":
+        p.resize_(7, 50)
+    elif change == "type":
+        p.data = p.data.bfloat16()
+    elif change == "layout":
+        p.data = p.data.view(50, 6).t()
+    elif change == "copy":
+        opt.copies[0] = torch.zeros(6, 49, dtype=torch.bfloat16)
+    elif change == "state":
+        opt.states[0] = (torch.zeros(299), opt.states[0][1])
+    elif change == "state type":
+        opt.states[0] = (torch.zeros(300, dtype=torch.float64), opt.states[0][1])
+    else:
+        opt.params.append(torch.zeros(3))
+    with pytest.raises(pb.PbkdError):
+        opt.step(grads, 0.1, stream=_Stream)
+    assert len(seen.tables) == 1 and opt.steps == 1
