@@ -81,14 +81,19 @@ class SequenceBlock:
 
     def distill_step(self, x, target, lr: float, residual=None, lengths=None):
         """One distillation step: forward, mean squared difference from target over the real tokens (Eq. 3), backward through this block
-        only, AdamW.  Returns the loss of the forward pass as a tensor on the GPU: the call waits for nothing."""
+        only, AdamW.  What x, residual and target hold behind a sequence has no influence.  Returns the loss of the forward pass as a
+        tensor on the GPU: the call waits for nothing."""
         b, t, d = x.shape
+        if lengths is not None:
+            # the weights' gradients sum over all rows: 0 * NaN of a padded one would be NaN in every weight
+            live = (torch.arange(t, device=x.device) < lengths[:, None])[:, :, None]
+            x = torch.where(live, x, 0.0)
+            residual = torch.where(live, residual, 0.0) if residual is not None else None
         out, z, q = self._forward(x, residual, lengths, None, None, True)
         diff = out.float() - target.float()
         count = b * t * d
         if lengths is not None:
-            live = torch.arange(t, device=x.device) < lengths[:, None]
-            diff = torch.where(live[:, :, None], diff, 0.0)
+            diff = torch.where(live, diff, 0.0)
             count = live.sum().clamp_min(1) * d
         loss = diff.square().sum() / count
         dout = (diff * (2.0 / count)).to(torch.bfloat16).view(-1, d)

@@ -906,3 +906,25 @@ def test_adamw_follows_its_tensors(gpu, bits):
     with pytest.raises(pb.PbkdError):
         opt.step(gs, 0.01)
     assert opt.steps == 4
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf"), 3.0])
+@pytest.mark.parametrize("residual", [True, False])
+def test_sequence_block_what_lies_behind_a_sequence_has_no_influence(gpu, junk, residual):
+    """Steps on a padded batch: loss, gradients, weights and states are those of a batch that is padded with zeros, bit for bit."""
+    torch, pb = gpu
+    from paper_2012_03096_amd import sequence
+    b, t, d = 5, 50, 64
+    lengths = torch.tensor([t, 0, 1, 23, t - 1], dtype=torch.int32).cuda()
+    gone = (torch.arange(t, device="cuda")[None] >= lengths[:, None])[:, :, None]
+    x, r, target = (_randn(torch, k, b, t, d, dtype="bf16") for k in (1, 2, 3))
+    seen = []
+    for fill in (0.0, junk):
+        block = sequence.SequenceBlock(d, seed=5)
+        given = x.masked_fill(gone, fill)
+        was = given.clone()
+        loss = [block.distill_step(given, target.masked_fill(gone, fill), 1e-2, residual=r.masked_fill(gone, fill) if residual else None, lengths=lengths) for _ in range(3)]
+        assert torch.equal(given.view(torch.int16), was.view(torch.int16))
+        seen.append([float(v) for v in loss] + [v.clone() for v in (*block.grads, *block.params, *block.copies, *(s.view(torch.uint8) for st in block.optimizer.states for s in st))])
+    assert np.isfinite(seen[0][:3]).all() and seen[0][:3] == seen[1][:3]
+    assert all(torch.isfinite(v.float()).all() for v in seen[1][3:15]) and all(torch.equal(a, c) for a, c in zip(seen[0][3:], seen[1][3:]))
