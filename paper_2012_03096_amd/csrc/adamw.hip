@@ -54,9 +54,9 @@ __device__ __forceinline__ unsigned element_hash(unsigned x) {       // x = numb
 // normal range the lower 20 of the float's 23 mantissa bits are cut after the addition; below 2^-6, where the grid is 2^-9, so
 // they are with 2^-6 added.
 __device__ __forceinline__ float random_e4m3(float x, unsigned up) {
-  const float base = x < 0x1p-6f ? 0x1p-6f : 0.f, least = x > 0.f ? 0x1p-9f : 0.f;
+  const float base = x < 0x1p-6f ? 0x1p-6f : 0.f;
   const float r = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, x + base) + up) & ~0xFFFFFu) - base;
-  return r < least ? least : r;      // a NaN stays one
+  return x > 0.f ? fmaxf(r, 0x1p-9f) : x;      // a NaN stays one: the sum above may carry out of its mantissa
 }
 
 // the maximum of numbers >= 0 over a wave, uniform: within the rows of 16 lanes, then row by row into lane 63

@@ -928,3 +928,16 @@ def test_sequence_block_what_lies_behind_a_sequence_has_no_influence(gpu, junk, 
         seen.append([float(v) for v in loss] + [v.clone() for v in (*block.grads, *block.params, *block.copies, *(s.view(torch.uint8) for st in block.optimizer.states for s in st))])
     assert np.isfinite(seen[0][:3]).all() and seen[0][:3] == seen[1][:3]
     assert all(torch.isfinite(v.float()).all() for v in seen[1][3:15]) and all(torch.equal(a, c) for a, c in zip(seen[0][3:], seen[1][3:]))
+
+
+# ------------------------------------------------------------------------ 8-bit states of what is not finite
+@pytest.mark.parametrize("bits", [0x7FC00000, 0x7F800001, 0x7FFF0000, 0x7FFFFFFF, 0xFFC00000, 0xFFFF0000, 0xFFFFFFFF])
+def test_adamw_8_bits_of_any_nan(gpu, bits):
+    """A gradient of NaN, whatever its sign and mantissa, leaves NaN in both states and the parameter, by any random number."""
+    torch, pb = gpu
+    g = torch.from_numpy(np.full(256, bits, np.uint32).view(np.float32)).cuda()
+    for seed in range(8):
+        p = torch.ones(256, device="cuda")
+        opt = pb.AdamW([p], state_bits=8)
+        opt.step([g], 0.1, seed=seed)
+        assert torch.isnan(opt.states[0][0].float()).all() and torch.isnan(opt.states[0][1].float()).all() and torch.isnan(p).all(), seed
