@@ -473,12 +473,13 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *desc, void
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
  * state_bits 32: m_dev, v_dev are fp32 [n].  state_bits 8: m_dev holds m and v_dev holds sqrt(v) as e4m3 codes [n] with an fp32
  * scale for each 256 consecutive elements (m_scale_dev, v_scale_dev [ceil(n/256)]), scale = max(largest magnitude, 2^-100) / 448.
+ * A NaN or an infinity is held as NaN in its own place and does not count for the scale: the elements beside it stay what they are.
  * m is rounded to nearest; sqrt(v) to one of its two neighbours at random, by their distances (to nearest, the small changes of
  * a beta2 near 1 would be lost in three bits of mantissa), and never from above zero to zero.  New states start as zeros
  * (codes and scales).  param_dtype PBKD_F32 or PBKD_BF16; a bf16 parameter is rounded at random too.  The random numbers are a
  * hash of `seed` and the element's number, first + its index in the tensor (modulo 2^32): the same call gives the same
  * bits.  copy_dev (nullable, with PBKD_F32 parameters): receives the new parameters in bf16, to nearest.
- * grad_dtype: any of the three.  NaN and infinite gradients enter the states as the formulas say. */
+ * grad_dtype: any of the three.  NaN and infinite gradients enter their own element's states and parameter as the formulas say. */
 typedef struct {
   long long n;
   long long first;

@@ -70,11 +70,15 @@ __device__ __forceinline__ float wave_top(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
-// 1/x to a unit of its last place and its residual put right once
+// 1/x to a unit of its last place and its residual put right once; x below 2^126, or the result would be below fp32's normal range
 __device__ __forceinline__ float reciprocal(float x) {
   const float r = __builtin_amdgcn_rcpf(x);
   return fmaf(fmaf(-x, r, 1.f), r, r);
 }
+
+// A block with an infinite value has its scale from the others, and NaN in that place: 8 bits hold no infinity, and an infinite scale
+// would lose the block's other 255 values.
+__device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) < __builtin_inff() ? x : __builtin_nanf(""); }
 
 // The root and the quotient of the update in 8-bit kernels, whose arithmetic takes as long as their memory: the hardware's
 // approximations with the residual put right once, within 0.6 units of the last place (random rounding of a bf16 parameter
@@ -163,7 +167,14 @@ __device__ __forceinline__ void adamw_chunk(const Launch &L, const Tensor &t, lo
       store_n<float, 4, FAR>(static_cast<float *>(t.v) + e, n, v[k]);
     } else {
       mtop = fmaxf(wave_top(mtop), 0x1p-100f), vtop = fmaxf(wave_top(vtop), 0x1p-100f);
-      const float mi = reciprocal(mtop) * 448.f, vi = reciprocal(vtop) * 448.f;
+      float mi = reciprocal(mtop) * 448.f, vi = reciprocal(vtop) * 448.f;
+      if (fmaxf(mtop, vtop) >= 0x1p126f) {     // the same for the whole wave
+        mtop = vtop = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[k][i] = finite_or_nan(m[k][i]), root[i] = finite_or_nan(root[i]), mtop = fmaxf(mtop, fabsf(m[k][i])), vtop = fmaxf(vtop, root[i]);
+        mtop = fmaxf(wave_top(mtop), 0x1p-100f), vtop = fmaxf(wave_top(vtop), 0x1p-100f);
+        mi = 448.f / mtop, vi = 448.f / vtop;
+      }
       float r[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

@@ -941,3 +941,49 @@ def test_adamw_8_bits_of_any_nan(gpu, bits):
         opt = pb.AdamW([p], state_bits=8)
         opt.step([g], 0.1, seed=seed)
         assert torch.isnan(opt.states[0][0].float()).all() and torch.isnan(opt.states[0][1].float()).all() and torch.isnan(p).all(), seed
+
+
+@pytest.mark.parametrize("bad,param,grad", [(b, p, g) for b in (float("inf"), -float("inf"), float("nan"), 1e20)
+                                            for p, g in (("f32", "f32"), ("f32", "bf16"), ("bf16", "f16")) if b != 1e20 or g != "f16"])
+def test_adamw_8_bits_beside_what_is_not_finite(gpu, bad, param, grad):
+    """One gradient of a block is infinite, NaN or has a square past fp32's range: its own element is lost (the last one's second moment
+    only), the others' parameters, codes and scales are those beside a zero in its place, in this step and the next."""
+    torch, pb = gpu
+    n, at = 600, [3, 300, 599]
+
+    def run(value):
+        p, g, g2 = (_randn(torch, k, n, scale=0.1) for k in (1, 2, 3))
+        p[at], g[at], g2[at] = 0.0, value, 0.0
+        p, g, g2 = p.to(_type(torch, param)), g.to(_type(torch, grad)), g2.to(_type(torch, grad))
+        opt = pb.AdamW([p], state_bits=8)
+        out = []
+        for v in (g, g2):
+            opt.step([v], 0.01)
+            out.append([x.clone() for x in (p, *opt.states[0])])
+        return out
+
+    keep = np.delete(np.arange(n), at)
+    for k, (a, z) in enumerate(zip(run(bad), run(0.0))):
+        for j, name in enumerate(("param", "m", "v", "m_scale", "v_scale")):
+            if bad == 1e20 and name in ("m", "m_scale"):
+                continue                           # a finite first moment counts for its scale
+            x, y = _np(a[j]), _np(z[j])
+            if name.endswith("scale"):
+                assert (x == y).all() and np.isfinite(x).all(), (k, name)
+            else:
+                assert name == "param" and bad == 1e20 and k == 1 or (x[keep] == y[keep]).all(), (k, name)
+                assert np.isfinite(x[keep]).all(), (k, name)
+                lost = np.isnan(x[at])
+                assert lost.all() if name == "v" or bad != 1e20 or name == "param" and k == 1 else True, (k, name)
+
+
+def test_adamw_8_bits_of_the_largest_numbers(gpu):
+    """First moments around fp32's largest number, where the reciprocal of their maximum is below its normal range."""
+    torch, pb = gpu
+    f = torch.linspace(0.0, 1.0, 256, device="cuda") * 3.4e38
+    p = torch.zeros(256, device="cuda")
+    opt = pb.AdamW([p], state_bits=8, betas=(0.0, 0.999))
+    opt.step([f], 0.0)
+    x = _np(f) / _np(f).max() * 448.0
+    _within(_np(opt.states[0][0]), x, 0.5 * osq.e4m3_spacing(x) * (1 + 1e-3), "codes")
+    _within(_np(opt.states[0][2]), [_np(f).max() / 448.0], 4 * E * 1e36, "scale")
