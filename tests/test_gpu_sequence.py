@@ -987,3 +987,19 @@ def test_adamw_8_bits_of_the_largest_numbers(gpu):
     x = _np(f) / _np(f).max() * 448.0
     _within(_np(opt.states[0][0]), x, 0.5 * osq.e4m3_spacing(x) * (1 + 1e-3), "codes")
     _within(_np(opt.states[0][2]), [_np(f).max() / 448.0], 4 * E * 1e36, "scale")
+
+
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-8, 0.0])
+def test_adamw_8_bits_move_at_the_ends_of_the_range(gpu, param, eps):
+    """The first step from nothing is the same with states in 8 as in 32 bits, also where the quotient's denominator is infinite
+    (a gradient whose square passes fp32's range: no move) or zero, and where the gradient is."""
+    torch, pb = gpu
+    g = _randn(torch, 1, 512)
+    g[:8] = torch.tensor([1e20, -1e20, 3.4e38, 0.0, -0.0, 1e-30, float("inf"), float("nan")])
+    p, q = (_randn(torch, 2, 512, dtype=param) for _ in range(2))
+    pb.AdamW([p], weight_decay=0.1, eps=eps).step([g], 0.01)
+    pb.AdamW([q], weight_decay=0.1, eps=eps, state_bits=8).step([g], 0.01)
+    a, b = _np(p), _np(q)
+    assert (np.isnan(a[:8]) == np.isnan(b[:8])).all() and (np.isnan(a[:8]) == [False, False, False, eps == 0.0, eps == 0.0, False, True, True]).all(), (a[:8], b[:8])
+    _within(b, a, np.abs(a) * (2 * E if param == "f32" else 2.0 ** -7) + 0.01 * 4 * E, "parameters")
