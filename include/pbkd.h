@@ -479,7 +479,9 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *desc, void
  * (codes and scales).  param_dtype PBKD_F32 or PBKD_BF16; a bf16 parameter is rounded at random too.  The random numbers are a
  * hash of `seed` and the element's number, first + its index in the tensor (modulo 2^32): the same call gives the same
  * bits.  copy_dev (nullable, with PBKD_F32 parameters): receives the new parameters in bf16, to nearest.
- * grad_dtype: any of the three.  NaN and infinite gradients enter their own element's states and parameter as the formulas say. */
+ * grad_dtype: any of the three.  NaN and infinite gradients enter their own element's states and parameter as the formulas say.
+ * The step's number, lr and seed are fixed by the call, so a graph would repeat one step for ever: PBKD_EUNSUPPORTED on a stream that is
+ * being captured. */
 typedef struct {
   long long n;
   long long first;

@@ -656,7 +656,8 @@ class AdamW:
 
     def step(self, grads, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, stream=None) -> None:
         """One step with these gradients (one for each parameter, contiguous; None: the parameter and its states stay as they are).
-        seed: of the random roundings; None: the number of the step."""
+        seed: of the random roundings; None: the number of the step.  Refused while the stream is captured: a graph would repeat this
+        very step, its bias corrections and random numbers with it."""
         dev, sizes = self._dev, self._sizes
         if len(grads) != len(sizes):
             raise PbkdError(ESHAPE, f"{len(grads)} gradients for {len(sizes)} parameters")

@@ -3,7 +3,7 @@
 //   m <- b1 m + (1-b1) g,  v <- b2 v + (1-b2) g^2,  p <- p (1 - lr wd) - (lr/bc1) m / (sqrt(v)/sqrt(bc2) + eps)
 //
 // One launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments: nothing has to be copied to
-// the device first, and a captured call keeps them.  A workgroup owns a chunk of elements of one tensor, found by a
+// the device first.  So do the step's own numbers, for which reason a call is refused while its stream is captured.  A workgroup owns a chunk of elements of one tensor, found by a
 // search over the tensors' first chunks; four consecutive elements go to a lane, so that a wave's 256 are just one block of
 // the 8-bit states and its maximum is a reduction over the wave.
 //
@@ -254,6 +254,13 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
       return set_error(PBKD_EINVAL, "adamw: tensor %d is not aligned to its elements", i);
     bytes += (double)t.n * ((t.param_dtype == PBKD_F32 ? 8 : 4) + (t.grad_dtype == PBKD_F32 ? 4 : 2) + (eight ? 4 : 16) + (t.copy_dev ? 2 : 0));
   }
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (bytes > 0. && st) {                      // the null stream cannot be captured
+    hipStreamCaptureStatus capture;
+    SEQ_HIPCHK(hipStreamIsCapturing(st, &capture));
+    if (capture != hipStreamCaptureStatusNone)
+      return set_error(PBKD_EUNSUPPORTED, "adamw: a captured step would repeat its bias corrections, learning rate and random numbers; capture what is around it");
+  }
   const bool far = bytes > kLastLevelCache;
   Launch L;
   L.seed = a->seed;
@@ -261,7 +268,6 @@ extern "C" pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *t
   L.eps = (float)a->eps, L.gscale = (float)a->grad_scale;
   L.step = (float)(a->lr / (1. - pow(a->beta1, (double)a->step)));
   L.root = (float)(1. / sqrt(1. - pow(a->beta2, (double)a->step)));
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
   L.tensors = 0, L.chunk0[0] = 0;
   auto flush = [&]() -> hipError_t {
     if (L.tensors == 0) return hipSuccess;

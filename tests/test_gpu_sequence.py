@@ -1003,3 +1003,31 @@ def test_adamw_8_bits_move_at_the_ends_of_the_range(gpu, param, eps):
     a, b = _np(p), _np(q)
     assert (np.isnan(a[:8]) == np.isnan(b[:8])).all() and (np.isnan(a[:8]) == [False, False, False, eps == 0.0, eps == 0.0, False, True, True]).all(), (a[:8], b[:8])
     _within(b, a, np.abs(a) * (2 * E if param == "f32" else 2.0 ** -7) + 0.01 * 4 * E, "parameters")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_is_refused_in_a_capture(gpu, bits):
+    """A replayed step would not count on.  The refusal leaves the capture, and the optimizer, as they were."""
+    torch, pb = gpu
+    x, w = _randn(torch, 1, 4, 64), torch.ones(64, device="cuda")
+    y, g, p = torch.zeros_like(x), _randn(torch, 2, 300), _randn(torch, 3, 300)
+    opt, ref = (pb.AdamW([q], state_bits=bits) for q in (p, p.clone()))
+    pb.rmsnorm_forward(x, w, y)
+    want, before = y.clone(), p.clone()
+    torch.cuda.synchronize()
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        with pytest.raises(pb.PbkdError) as refused:
+            opt.step([g], 0.1)
+        pb.rmsnorm_forward(x, w, y)
+    assert refused.value.status == pb.EUNSUPPORTED and opt.steps == 0
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(p, before)
+    for _ in range(2):
+        opt.step([g], 0.1)
+        ref.step([g], 0.1, stream=s)
+        torch.cuda.synchronize()
+    assert opt.steps == 2 and torch.equal(p, ref.params[0])
