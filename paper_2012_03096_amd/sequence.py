@@ -13,6 +13,7 @@ plain matrix products and torch's, in bf16.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -36,22 +37,30 @@ class SequenceBlock:
         self.norm, self.w_in, self.bias, self.w_out = self.params
         self.grads = [torch.empty_like(p) if p.dim() == 1 else torch.empty_like(c) for p, c in zip(self.params, self.copies)]
         self.optimizer = pb.AdamW(self.params, state_bits=state_bits, copies=self.copies, weight_decay=[0.0, weight_decay, 0.0, weight_decay])
-        self._buffers = {}
+        self._buffers, self._views = {}, {}
+
+    def _buffer(self, name: str, *shape, dtype=torch.bfloat16):
+        """A buffer of the block for what is called `name`, as large as the largest that was asked for."""
+        n, have = math.prod(shape), self._buffers.get(name)
+        if have is None or have.numel() < n:
+            self._buffers.pop(name, None)
+            have = self._buffers[name] = torch.empty(n, dtype=dtype, device=self.params[0].device)
+        return have[:n].view(shape)
 
     def _sized(self, b: int, t: int, training: bool):
-        """Activations, their gradients and the operators' workspaces for batches of this size, made once.  A block serves one
-        stream at a time."""
-        key = (b, t, training)
-        if key not in self._buffers:
-            d, dev, bf = self.d, self.params[0].device, torch.bfloat16
-            new = lambda *s, dtype=bf: torch.empty(*s, dtype=dtype, device=dev)                      # noqa: E731
-            raw = lambda n: torch.empty(n, dtype=torch.uint8, device=dev)                            # noqa: E731
-            q = {"total": new(b, t, d), "n": new(b, t, d), "y": new(b, t, d), "workspace": raw(pb.recurrence_workspace_bytes(b, t, d))}
+        """Activations, their gradients and the operators' workspaces for batches of this size: views of the block's buffers, kept for
+        the last size.  A block serves one stream at a time."""
+        if self._views.get("size") != (b, t, training):
+            self._views = {}
+            d, new = self.d, self._buffer
+            raw = lambda name, n: new(name, n, dtype=torch.uint8)                                    # noqa: E731
+            q = {"size": (b, t, training), "total": new("total", b, t, d), "n": new("n", b, t, d), "y": new("y", b, t, d),
+                 "workspace": raw("workspace", pb.recurrence_workspace_bytes(b, t, d))}
             if training:
-                q.update(saved=raw(pb.recurrence_saved_bytes(b, t, d)), dz=new(b, t, 3 * d), dx=new(b, t, d),
-                         norm_workspace=raw(pb.rmsnorm_workspace_bytes(b * t, d)))
-            self._buffers[key] = q
-        return self._buffers[key]
+                q.update(saved=raw("saved", pb.recurrence_saved_bytes(b, t, d)), dz=new("dz", b, t, 3 * d), dx=new("dx", b, t, d),
+                         norm_workspace=raw("norm_workspace", pb.rmsnorm_workspace_bytes(b * t, d)))
+            self._views = q
+        return self._views
 
     def _columns(self, z):
         d = self.d

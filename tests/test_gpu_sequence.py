@@ -1031,3 +1031,27 @@ def test_adamw_is_refused_in_a_capture(gpu, bits):
         ref.step([g], 0.1, stream=s)
         torch.cuda.synchronize()
     assert opt.steps == 2 and torch.equal(p, ref.params[0])
+
+
+def test_sequence_block_keeps_no_more_than_the_largest_batch_takes(gpu):
+    """Batches of many sizes, in any order, take no more memory than the largest did, and answer as a new block does."""
+    torch, pb = gpu
+    from paper_2012_03096_amd import sequence
+    block = sequence.SequenceBlock(64, seed=5)
+    x = _randn(torch, 1, 6, 700, 64, dtype="bf16")
+    target, steps = torch.zeros_like(x), [(6, 700, True), (6, 700, False)] + [(b, t, k % 3 == 0) for k, (b, t) in enumerate((1 + k % 6, 1 + 37 * k % 699) for k in range(40))]
+    most = None
+    for b, t, training in steps:
+        cut = x[:b, :t].contiguous()
+        if training:
+            block.distill_step(cut, target[:b, :t].contiguous(), 0.0)
+        out = block.forward(cut)
+        if most is not None and b * t < 500:
+            assert torch.equal(out, sequence.SequenceBlock(64, seed=5).forward(cut)), (b, t)
+        torch.cuda.synchronize()
+        if t == 700:
+            del out, cut
+            most = torch.cuda.memory_allocated()
+            continue
+        del out, cut
+        assert torch.cuda.memory_allocated() <= most, (b, t)
