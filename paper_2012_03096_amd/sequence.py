@@ -54,10 +54,10 @@ class SequenceBlock:
             self._views = {}
             d, new = self.d, self._buffer
             raw = lambda name, n: new(name, n, dtype=torch.uint8)                                    # noqa: E731
-            q = {"size": (b, t, training), "total": new("total", b, t, d), "n": new("n", b, t, d), "y": new("y", b, t, d),
+            q = {"size": (b, t, training), "n": new("n", b, t, d), "y": new("y", b, t, d),
                  "workspace": raw("workspace", pb.recurrence_workspace_bytes(b, t, d))}
             if training:
-                q.update(saved=raw("saved", pb.recurrence_saved_bytes(b, t, d)), dz=new("dz", b, t, 3 * d), dx=new("dx", b, t, d),
+                q.update(saved=raw("saved", pb.recurrence_saved_bytes(b, t, d)), dz=new("dz", b, t, 3 * d), dx=new("dx", b, t, d), total=new("total", b, t, d),
                          norm_workspace=raw("norm_workspace", pb.rmsnorm_workspace_bytes(b * t, d)))
             self._views = q
         return self._views
@@ -69,7 +69,8 @@ class SequenceBlock:
     def _forward(self, x, residual, lengths, state, state_out, training: bool):
         b, t, d = x.shape
         q = self._sized(b, t, training)
-        pb.rmsnorm_forward(x, self.norm, q["n"], residual=residual, total=q["total"])
+        # the backward pass reads the sum, which is x itself where nothing is added; nobody else does
+        pb.rmsnorm_forward(x, self.norm, q["n"], residual=residual, total=q["total"] if training and residual is not None else None)
         z = (q["n"].view(-1, d) @ self.copies[1].t()).view(b, t, 3 * d)
         pb.recurrence_forward(**self._columns(z), y=q["y"], bias=self.bias, lengths=lengths, state=state, state_out=state_out,
                               saved=q.get("saved"), workspace=q["workspace"])

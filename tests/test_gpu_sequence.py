@@ -1055,3 +1055,18 @@ def test_sequence_block_keeps_no_more_than_the_largest_batch_takes(gpu):
             continue
         del out, cut
         assert torch.cuda.memory_allocated() <= most, (b, t)
+
+
+def test_sequence_block_writes_no_sum_that_nobody_reads(gpu, monkeypatch):
+    torch, pb = gpu
+    from paper_2012_03096_amd import sequence
+    seen = []
+    norm = pb.rmsnorm_forward
+    monkeypatch.setattr(pb, "rmsnorm_forward", lambda *a, **kw: (seen.append(kw.get("total")), norm(*a, **kw))[1])
+    block, x = sequence.SequenceBlock(64, seed=5), _randn(torch, 1, 2, 40, 64, dtype="bf16")
+    block.forward(x)
+    block.forward(x, residual=x)
+    block.distill_step(x, x, 1e-3)
+    assert seen == [None, None, None]
+    block.distill_step(x, x, 1e-3, residual=x)
+    assert seen[3] is not None and torch.equal(seen[3], x + x)
