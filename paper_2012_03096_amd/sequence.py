@@ -66,25 +66,27 @@ class SequenceBlock:
         d = self.d
         return {"u": z[..., :d], "gate": z[..., d:2 * d], "out_gate": z[..., 2 * d:]}
 
-    def _forward(self, x, residual, lengths, state, state_out, training: bool):
+    def _forward(self, x, residual, lengths, state, state_out, training: bool, total=None):
         b, t, d = x.shape
         q = self._sized(b, t, training)
-        # the backward pass reads the sum, which is x itself where nothing is added; nobody else does
-        pb.rmsnorm_forward(x, self.norm, q["n"], residual=residual, total=q["total"] if training and residual is not None else None)
+        # the backward pass reads the sum, which is x itself where nothing is added
+        pb.rmsnorm_forward(x, self.norm, q["n"], residual=residual, total=q["total"] if training and residual is not None else total)
         z = (q["n"].view(-1, d) @ self.copies[1].t()).view(b, t, 3 * d)
         pb.recurrence_forward(**self._columns(z), y=q["y"], bias=self.bias, lengths=lengths, state=state, state_out=state_out,
                               saved=q.get("saved"), workspace=q["workspace"])
         return (q["y"].view(-1, d) @ self.copies[3].t()).view(b, t, d), z, q
 
-    def forward(self, x, residual=None, lengths=None, state=None, state_out=None):
+    def forward(self, x, residual=None, lengths=None, state=None, state_out=None, total=None):
         """The block's output for x [batch, len, d] bf16 (plus residual); lengths: int32 [batch] of a padded batch; state and
-        state_out [batch, d] float32 carry a text on from piece to piece."""
-        return self._forward(x, residual, lengths, state, state_out, False)[0]
+        state_out [batch, d] float32 carry a text on from piece to piece.  total (like x) receives x + residual, the residual stream: blocks
+        follow each other as `out = a.forward(x, total=s); out = b.forward(out, residual=s, total=s)`, and out + s is what they give."""
+        return self._forward(x, residual, lengths, state, state_out, False, total)[0]
 
-    def step(self, x, state, active=None):
-        """The block's output for one token of each sequence, x [batch, d]; state is updated in place (rows with active 0 stay)."""
+    def step(self, x, state, active=None, residual=None, total=None):
+        """The block's output for one token of each sequence, x [batch, d] (plus residual); state is updated in place (rows with active 0
+        stay).  total receives x + residual, as in forward."""
         n, y = torch.empty_like(x), torch.empty_like(x)
-        pb.rmsnorm_forward(x, self.norm, n)
+        pb.rmsnorm_forward(x, self.norm, n, residual=residual, total=total)
         c = self._columns(n @ self.copies[1].t())
         pb.recurrence_step(c["u"], c["gate"], state, y, out_gate=c["out_gate"], bias=self.bias, active=active)
         return y @ self.copies[3].t()

@@ -1070,3 +1070,31 @@ def test_sequence_block_writes_no_sum_that_nobody_reads(gpu, monkeypatch):
     assert seen == [None, None, None]
     block.distill_step(x, x, 1e-3, residual=x)
     assert seen[3] is not None and torch.equal(seen[3], x + x)
+
+
+def test_sequence_blocks_in_a_chain_with_a_residual_stream(gpu):
+    """Two blocks behind each other: the stream is the sum of all that went before, and the answers token by token, residual and all, are
+    those of the pass over all tokens (up to the roundings of bf16, 2^-6 of the output's size)."""
+    torch, pb = gpu
+    from paper_2012_03096_amd import sequence
+    b, t, d = 3, 40, 64
+    one, two = sequence.SequenceBlock(d, seed=5), sequence.SequenceBlock(d, seed=6)
+    x, r = _randn(torch, 8, b, t, d, dtype="bf16"), _randn(torch, 9, b, t, d, dtype="bf16")
+    s = torch.empty_like(x)
+    first = one.forward(x, residual=r, total=s)
+    assert torch.equal(first, one.forward(x, residual=r)) and torch.equal(s, x + r)
+    was = s.clone()
+    second = two.forward(first, residual=s, total=s)                      # the stream in place
+    assert torch.equal(s, first + was) and torch.equal(second, two.forward(first, residual=was))
+    alone = torch.empty_like(x)
+    one.forward(x, total=alone)
+    assert torch.equal(alone, x)
+    states, out, stream = [torch.zeros(b, d, device="cuda") for _ in range(2)], torch.empty_like(x), torch.empty_like(x)
+    for i in range(t):
+        a = torch.empty(b, d, dtype=x.dtype, device="cuda")
+        h = one.step(x[:, i].contiguous(), states[0], residual=r[:, i].contiguous(), total=a)
+        assert torch.equal(a, was[:, i])
+        out[:, i] = two.step(h, states[1], residual=a, total=a)
+        stream[:, i] = a
+    for got, want in ((out, second), (stream, s)):
+        assert float((got.float() - want.float()).norm() / want.float().norm()) < 2.0 ** -6
