@@ -1098,3 +1098,33 @@ def test_sequence_blocks_in_a_chain_with_a_residual_stream(gpu):
         stream[:, i] = a
     for got, want in ((out, second), (stream, s)):
         assert float((got.float() - want.float()).norm() / want.float().norm()) < 2.0 ** -6
+
+
+# ------------------------------------------------------------------------------------------- paths by size and count
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("dtype,b,t,d", [("bf16", 9, 4163, 2048), ("f16", 9, 4163, 2048), ("f32", 4, 4321, 1312)])
+def test_recurrence_of_much_data_in_many_chains(gpu, dtype, b, t, d, gated):
+    """More than the last-level cache holds in tiles of four waves: 16-bit types in more than 128 chains, and fp32, its last slice half a
+    one.  The same bits as one sequence a call, which stays below the cache's size and takes the same tiles."""
+    torch, pb = gpu
+    size = 4 if dtype == "f32" else 2
+    assert b * t * d * size * 3 > 256e6 > t * d * size * 7 and d * size % 128 == 0 and (dtype == "f32" or b * -(-d // 64) > 128) and t < 8192
+    kind = _type(torch, dtype)
+    make = lambda: torch.randn(b, t, d, device="cuda").to(kind)                                     # noqa: E731
+    q = {"u": make(), "gate": make(), "out_gate": make() if gated else None, "bias": torch.rand(d, device="cuda") * 6, "state": torch.randn(b, d, device="cuda"),
+         "lengths": torch.tensor([t, 0, 1, t // 2, t - 1, 129, 64, 2049, t][:b], dtype=torch.int32).cuda()}
+    print("recurrence of much data", dtype, b, t, d, gated, flush=True)
+    f = _forward(torch, pb, q)
+    dy, dT = make(), torch.randn(b, d, device="cuda")
+    g = _backward(torch, pb, q, f, dy, dT)
+    part = torch.zeros(d, dtype=torch.float64, device="cuda")
+    for i in range(b):
+        one = {k: (v if k == "bias" else v[i:i + 1]) if v is not None else None for k, v in q.items()}
+        f1 = _forward(torch, pb, one)
+        g1 = _backward(torch, pb, one, f1, dy[i:i + 1], dT[i:i + 1])
+        assert torch.equal(f1["y"], f["y"][i:i + 1]) and torch.equal(f1["state"], f["state"][i:i + 1]), i
+        assert all(torch.equal(g1[k], g[k][i:i + 1]) for k in ("du", "dgate", "dstate") + (("dout_gate",) if gated else ())), i
+        part += g1["dbias"].double()
+    # each is a sum of at most 64 tokens in a thread, then of 4163 / 64 rows a sequence
+    size = g["dgate"].double().abs().sum((0, 1)) * (1 + 2 * HALF[dtype])
+    _within(_np(g["dbias"]), part.cpu().numpy(), (2 * (64 + b * t / 64) * E * size).cpu().numpy(), "dbias")
