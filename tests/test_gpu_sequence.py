@@ -1128,3 +1128,32 @@ def test_recurrence_of_much_data_in_many_chains(gpu, dtype, b, t, d, gated):
     # each is a sum of at most 64 tokens in a thread, then of 4163 / 64 rows a sequence
     size = g["dgate"].double().abs().sum((0, 1)) * (1 + 2 * HALF[dtype])
     _within(_np(g["dbias"]), part.cpu().numpy(), (2 * (64 + b * t / 64) * E * size).cpu().numpy(), "dbias")
+
+
+@pytest.mark.parametrize("bits,param,grad", [(8, "f32", "f32"), (8, "bf16", "bf16"), (32, "f32", "bf16"), (32, "bf16", "f32")])
+def test_adamw_of_more_tensors_than_one_launch_takes(gpu, bits, param, grad):
+    """A hundred tensors, some without elements, some without gradients, from nothing and under way: every parameter, state and scale, and
+    the random numbers by the elements' places across the launches."""
+    import types
+    torch, pb = gpu
+    sizes = [(37 * i) % 700 for i in range(100)]
+    absent = [i % 9 == 4 for i in range(100)]
+    assert sum(1 for n, a in zip(sizes, absent) if n and not a) > 80 and 0 in sizes
+    for start in (0, 41):
+        ps, gs, states = _adamw_setup(torch, sizes, param, grad, bits)
+        decays = [0.1 if i % 2 else 0.0 for i in range(100)]
+        opt = pb.AdamW(ps, state_bits=bits, states=states if start else None, weight_decay=decays, steps=start)
+        for _ in range(2):
+            before = [(p.clone(), tuple(x.clone() for x in s)) for p, s in zip(ps, opt.states)]
+            opt.step([None if a else g for a, g in zip(absent, gs)], 0.01)
+            torch.cuda.synchronize()
+            for i in range(100):
+                if absent[i]:
+                    assert torch.equal(before[i][0], ps[i]) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before[i][1], opt.states[i]))
+            # what had no gradient stands in the check as zeros that stay zeros, so that the elements behind it keep their numbers
+            zero = lambda t: torch.zeros_like(t.view(torch.uint8)).view(t.dtype)                    # noqa: E731
+            tiny = lambda s: tuple(zero(x) if k < 2 else torch.full_like(x, osq.TINY / 448.0) for k, x in enumerate(s))          # noqa: E731
+            told = types.SimpleNamespace(steps=opt.steps, params=[zero(p) if a else p for a, p in zip(absent, ps)],
+                                         states=[tiny(s) if a else s for a, s in zip(absent, opt.states)])
+            was = [(zero(p), tiny(s)) if a else (p, s) for a, (p, s) in zip(absent, before)]
+            _check_adamw(torch, was, [zero(g) if a else g for a, g in zip(absent, gs)], told, [np.float64(np.float32(x)) for x in decays], 0.01, bits, param)
