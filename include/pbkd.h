@@ -475,7 +475,8 @@ pbkd_status pbkd_recurrence_backward(const pbkd_recurrence_grad_desc *desc, void
  * scale for each 256 consecutive elements (m_scale_dev, v_scale_dev [ceil(n/256)]), scale = max(largest magnitude, 2^-100) / 448.
  * A NaN or an infinity is held as NaN in its own place and does not count for the scale: the elements beside it stay what they are.
  * m is rounded to nearest; sqrt(v) to one of its two neighbours at random, by their distances (to nearest, the small changes of
- * a beta2 near 1 would be lost in three bits of mantissa), and never from above zero to zero.  New states start as zeros
+ * a beta2 near 1 would be lost in three bits of mantissa), and never from above zero to zero; a v below 2^-126, fp32's normal
+ * range, counts as zero.  New states start as zeros
  * (codes and scales).  param_dtype PBKD_F32 or PBKD_BF16; a bf16 parameter is rounded at random too.  The random numbers are a
  * hash of `seed` and the element's number, first + its index in the tensor (modulo 2^32): the same call gives the same
  * bits.  copy_dev (nullable, with PBKD_F32 parameters): receives the new parameters in bf16, to nearest.

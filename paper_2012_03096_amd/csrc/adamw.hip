@@ -42,7 +42,9 @@ struct Launch {
 };
 static_assert(sizeof(Launch) <= 4000, "kernel arguments");
 
-// A random number for each element: multiplications and xor-shifts of its number and the seed.
+// A random number for each element: multiplications and xor-shifts of its number and the seed.  The shifts and the two factors of
+// element_hash are those published with C. Wellons' search for 32-bit mixing functions ("hash prospector"); kMul is a prime next to
+// 2^32 over the golden ratio.
 constexpr unsigned kMul = 0x9E3779B1u;
 __device__ __forceinline__ unsigned element_hash(unsigned x) {       // x = number * kMul + seed * 0x632BE5AB
   x = (x ^ (x >> 16)) * 0x21F0AAADu;

@@ -60,7 +60,9 @@ struct BwdArgs {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// sigmoid(x) and sigmoid(-x), each to a few units of its own last place: both from e = exp(-|x|)
+// sigmoid(x) and sigmoid(-x), both from e = exp(-|x|), so that neither is a difference from 1.  The larger is good to a few units of its last place;
+// the smaller one's relative error grows with |x|, whose product with log2 e is rounded before exp2: 4 units of the last place up to
+// |x| = 4, 15 up to 17, 62 at 80 (times 2^-24).
 __device__ __forceinline__ void sigmoids(float x, float &a, float &z) {
   const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
   a = x >= 0.f ? r : s;
@@ -205,9 +207,11 @@ __device__ __forceinline__ Chain chain_of(unsigned long long *work, int chain, i
 // knows the one in front: one addition and one product lie between them.  Only the chain's first tile reads the state in
 // front of the chain (`first`), and its pair is the constant map to the state behind it: the last tile, which may write over the
 // initial state, thereby has every reader of it behind itself.
-// EARLY of the pairs' words are read early.  Seven cost registers for as long as the tile's data are on their way, and tiles of eight waves,
-// which have the fewest, spill: with three 1x65536x1280 backward takes 237 us instead of 254, 1x65536x4096 728 instead of 778.
-// With four waves all of them are: 8x2048x2047 forward and backward 193 us, with three 197.
+// EARLY of the pairs' words are read early.  Seven cost registers for as long as the tile's data are on their way, and tiles of eight waves
+// have the fewest: with three 1x65536x1280 backward takes 237 us instead of 254, 1x65536x4096 728 instead of 778.
+// With four waves all of them are: 8x2048x2047 forward and backward 193 us, with three 197.  Neither choice keeps every kernel out of
+// scratch memory.  The compiler reports registers spilled in the gated kernels of 16-bit types: forward with four waves 18 past the caches and 30
+// (bf16) or 27 (f16) within, with eight 16, 25 and 29; backward with eight waves within the caches 32 and 18.  All others spill none.
 constexpr int early_words(int waves) { return waves == 8 ? 3 : kSeg - 1; }
 template <int EARLY>
 struct Words {
@@ -589,6 +593,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 4 : sizeof(T) == 4 ? 2 : 3) void r
 //   32x2048        -          6.8 /  9.0    8.5 /  8.9   11.9 / 10.1   15.6 / 11.3
 //   64x2048     5.5 / 15.0    7.3 / 15.4    9.3 / 16.1   15.7 / 20.3   19.9 / 22.8
 //   256x4096   21.6 / 97.5   30.6 / 98.3   40.3 /  131   84.5 /  161    113 /  172
+// All of these have channels in fours.  Otherwise the last thread of a sequence goes token by token, three reads after another, which was
+// not measured against tiles.
 constexpr int kFewChains = 128, kLongChain = 8192;
 constexpr int kFewSteps = 24, kManyThreads = 32768;
 constexpr int kAhead = 8;      // tokens on their way together (4: 5.0 against 4.7 us for 1x16x1280)
@@ -672,14 +678,15 @@ inline bool lines(const void *p, long long batch_stride, long long stride, int s
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(batch_stride * size) | (uintptr_t)(stride * size)) & 127) == 0;
 }
 
-// Whether tiles have eight waves.  A chain hands its state from segment to segment, about 1.8 us each; few long chains are bound by that, and tiles
-// of twice the tokens halve it.  Many chains hide it, and want small workgroups.  Measured in us, four / eight waves (bf16 with the output gate):
+// Whether tiles have eight waves.  A chain hands its state from segment to segment, about 0.75 us each (1x131072x64: 128 segments in 94 us, 64
+// in 53); few long chains are bound by that, and tiles of twice the tokens halve it.  Many chains hide it, and want small workgroups.  Measured in us, four / eight waves (bf16 with the output gate):
 //                     chains  forward     backward                           chains  forward     backward
 //   1x131072x64          1     94 /  53   156 /  88      8x8192x512            64     63 /  59   115 / 104
 //   1x65536x1280        20    147 / 128   282 / 237      4x16384x1280          80    137 / 127   264 / 237
 //   1x16384x1280        20   47.3 / 47.8 79.7 / 69.5     8x8192x1280          160    134 / 131   252 / 245
 //   1x65536x4096        64    428 / 396   799 / 724      8x8192x2048          256    193 / 200
-// fp32's registers leave a compute unit one workgroup of eight waves (1x65536x1280 forward 244 / 249).
+// fp32 stays with four: its registers leave a compute unit one workgroup of eight waves, 1x65536x1280 forward 244 / 249.  Fewer or shorter
+// chains would gain there too, 1x65536x320 79.5 / 73.4 and 1x1024x1280 16.8 / 15.8; no rule has been measured that parts the two.
 inline bool tall_tiles(int batch, long long len, int slices, int size) { return size == 2 && (long long)batch * slices <= kFewChains && len >= kLongChain; }
 
 template <typename T>
