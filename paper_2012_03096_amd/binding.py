@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
-from itertools import chain
+from itertools import accumulate, chain
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -611,25 +611,20 @@ class AdamW:
         self._table = t = np.zeros(n, _ADAMW_TENSOR)
         self._kind = kind = (torch.float32, torch.float32) if state_bits == 32 else (torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32)
         self._sizes, self._shapes, self._dtypes, made = [p.numel() for p in self.params], [p.shape for p in self.params], [p.dtype for p in self.params], []
-        first = 0
+        blocks, codes = [-(-k // 256) for k in self._sizes], [_CODES.get(y) for y in self._dtypes]
+        self._state_sizes = [(k, k, m, m)[:len(kind)] for k, m in zip(self._sizes, blocks)]
         for i, p in enumerate(self.params):
-            code = _CODES.get(p.dtype)
-            if code not in (F32, BF16):
+            if codes[i] not in (F32, BF16):
                 raise PbkdError(EINVAL, f"parameter {i} must be float32 or bfloat16, not {p.dtype}")
             if states is None:
-                made.append(tuple(torch.zeros(k, dtype=torch.uint8 if y == torch.float8_e4m3fn else y, device=p.device).view(y) for k, y in zip(self._state_sizes(i), kind)))
-            t[i]["first"], t[i]["param_dtype"], t[i]["weight_decay"] = first, code, decays[i]
-            first += -(-self._sizes[i] // 256) * 256
+                made.append(tuple(torch.zeros(k, dtype=torch.uint8 if y == torch.float8_e4m3fn else y, device=p.device).view(y) for k, y in zip(self._state_sizes[i], kind)))
+        t["first"], t["param_dtype"], t["weight_decay"] = [256 * k for k in accumulate([0, *blocks])][:n], codes, decays
         self.states = made if states is None else list(states)
         self._address = t.ctypes.data
         self._n, self._grad_dtype, self._grad, self._codes, self._at = t["n"], t["grad_dtype"], t["grad"], None, None
         self._take_addresses()
         if states is None and n:
             torch.cuda.current_stream().synchronize()
-
-    def _state_sizes(self, i: int):
-        n = self._sizes[i]
-        return (n, n, -(-n // 256), -(-n // 256))[:len(self._kind)]
 
     def _where(self):
         """Addresses of all parameters, states and copies, as one list."""
@@ -642,15 +637,14 @@ class AdamW:
         for name, given in (("parameters", self.params), ("states", self.states), ("copies", self.copies)):
             if given is not None and len(given) != n:
                 raise PbkdError(ESHAPE, f"{len(given)} {name}, {n} are needed")
-        at = {k: [] for k in ("param", "copy", *names[:len(self._kind)])}
+        dev, kind, rows = self._dev, self._kind, []
         for i, (p, s) in enumerate(zip(self.params, self.states)):
-            at["param"].append(_dense(p, self._shapes[i], self._dtypes[i], self._dev, f"parameter {i}"))
-            if len(s) != len(self._kind):
-                raise PbkdError(ESHAPE, f"parameter {i}: {len(s)} state tensors, {len(self._kind)} are needed")
-            for x, k, y, name in zip(s, self._state_sizes(i), self._kind, names):
-                at[name].append(_dense(x, (k,), y, self._dev, f"state of parameter {i}"))
-            at["copy"].append(_dense(self.copies[i], self._shapes[i], _torch.bfloat16, self._dev, f"copy of parameter {i}") if self.copies is not None else 0)
-        for k, v in at.items():
+            if len(s) != len(kind):
+                raise PbkdError(ESHAPE, f"parameter {i}: {len(s)} state tensors, {len(kind)} are needed")
+            name = f"state of parameter {i}"
+            rows.append((_dense(p, self._shapes[i], self._dtypes[i], dev, f"parameter {i}"), *[_dense(x, (k,), y, dev, name) for x, k, y in zip(s, self._state_sizes[i], kind)],
+                         _dense(self.copies[i], self._shapes[i], _torch.bfloat16, dev, f"copy of parameter {i}") if self.copies is not None else 0))
+        for k, v in zip(("param", *names[:len(kind)], "copy"), zip(*rows)):
             self._table[k] = v
         self._seen = self._where()
 
