@@ -9,6 +9,9 @@ other block.  The student takes the attention's place by a gated recurrence, who
 Norm, recurrence and update (AdamW, fp32 master weights, states in 8 or 32 bits) are the library's kernels; the projections are
 plain matrix products and torch's, in bf16.
 
+The block asks nothing of its teacher but activations: labels may come from attention or any other block.  Those of the demonstration below
+come from a frozen block of the student's own form, which it can match.
+
     python -m paper_2012_03096_amd.sequence          # trains a student on a frozen block's labels, then answers token by token
 """
 from __future__ import annotations
