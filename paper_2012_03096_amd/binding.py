@@ -621,7 +621,7 @@ class AdamW:
         t["first"], t["param_dtype"], t["weight_decay"] = [256 * k for k in accumulate([0, *blocks])][:n], codes, decays
         self.states = made if states is None else list(states)
         self._address = t.ctypes.data
-        self._n, self._grad_dtype, self._grad, self._codes, self._at = t["n"], t["grad_dtype"], t["grad"], None, None
+        self._n, self._grad_dtype, self._grad, self._types, self._at = t["n"], t["grad_dtype"], t["grad"], None, None
         self._take_addresses()
         if states is None and n:
             torch.cuda.current_stream().synchronize()
@@ -659,20 +659,23 @@ class AdamW:
             raise PbkdError(EINVAL, "the parameters must lie on the current GPU")
         if self._where() != self._seen:
             self._take_addresses()
-        t = _torch.Tensor
-        if not all(map(t.is_contiguous, self.params)):       # data may be viewed otherwise at the same place (a shorter view: its gradient tells)
-            raise PbkdError(ESHAPE, "a parameter is no longer contiguous")
-        live, want, counts = grads, sizes, sizes
-        if any([g is None for g in grads]):
+        t, live, want = _torch.Tensor, grads, sizes
+        try:
+            at = [*map(t.data_ptr, grads)]
+        except TypeError:                            # some are None
             live, want = [g for g in grads if g is not None], [n for g, n in zip(grads, sizes) if g is not None]
-            counts = [0 if g is None else n for g, n in zip(grads, sizes)]
-        codes, at = [_CODES.get(g.dtype) for g in live], [*map(t.data_ptr, live)]
-        if None in codes or [*map(t.numel, live)] != want or not all(map(t.is_contiguous, live)) or set(map(t.get_device, live)) - {dev}:
-            raise PbkdError(ESHAPE, "a gradient must be contiguous, float32, bfloat16 or float16, with its parameter's elements, on its GPU")
-        if live is not grads:
-            codes, at = ([next(x) if g is not None else 0 for g in grads] for x in (iter(codes), iter(at)))
-        if codes != self._codes or counts != self._counts:
-            self._n[:], self._grad_dtype[:], self._codes, self._counts = counts, codes, codes, counts
+            at = [0 if g is None else g.data_ptr() for g in grads]
+        # data of a parameter may be viewed otherwise at the same place (a shorter view: its gradient tells)
+        if [*map(t.numel, live)] != want or not all(map(t.is_contiguous, chain(live, self.params))) or set(map(t.get_device, live)) - {dev}:
+            raise PbkdError(ESHAPE, "gradients and parameters must be contiguous, a gradient with its parameter's elements, on its GPU")
+        types = [*map(t.dtype.__get__, live)]
+        if types != self._types or live is not grads:
+            if any(y not in _CODES for y in types):
+                raise PbkdError(ESHAPE, "a gradient must be float32, bfloat16 or float16")
+            codes = iter(types)
+            self._grad_dtype[:] = [F32 if g is None else _CODES[next(codes)] for g in grads]
+            self._n[:] = [0 if g is None else n for g, n in zip(grads, sizes)]
+            self._types = types if live is grads else None
         if at != self._at:
             self._grad[:] = self._at = at
         number = self.steps + 1

@@ -9,7 +9,7 @@
 //
 // Bound by memory: 67M fp32 parameters with 32-bit states 303 us, 6.2 TB/s; 201M fp32 parameters, bf16 gradients and copies,
 // 8-bit states 541 us, 6.0 TB/s.  Smaller calls are bound by the last-level cache and their arithmetic (6M bf16 parameters, 8-bit
-// states, 18.0 us), eight tensors of a convolutional block by the host (9.5 us, the kernel takes 5.0).
+// states, 18.0 us), eight tensors of a convolutional block by the host (9.2 us, the kernel takes 5.0).
 #include "seq_common.h"
 
 namespace pbkd {

@@ -297,3 +297,22 @@ def test_adamw_refuses_tensors_that_are_not_what_they_were(recorded, change):
     with pytest.raises(pb.PbkdError):
         opt.step(grads, 0.1, stream=_Stream)
     assert len(seen.tables) == 1 and opt.steps == 1
+
+
+def test_adamw_tells_the_library_each_steps_gradients(recorded):
+    """Their addresses, types and elements, step by step, as types change and gradients come and go."""
+    torch, seen = recorded
+    opt = _adamw_on_host(torch, 32, copies=False)
+    a, b, h = torch.zeros(6, 50), torch.zeros(300), torch.zeros(300, dtype=torch.bfloat16)
+    for grads in ([a, b], [a, h], (a, h), [None, h], [a, None], [None, None], [a, b], [a.half(), b.clone()], [a.half(), b]):
+        opt.step(grads, 0.1, stream=_Stream)
+        table = seen.tables[-1]
+        assert table["n"].tolist() == [0 if g is None else 300 for g in grads]
+        assert table["grad"].tolist() == [0 if g is None else g.data_ptr() for g in grads]
+        assert table["grad_dtype"].tolist() == [pb.F32 if g is None else pb._CODES[g.dtype] for g in grads]
+    for grads in ([a, b.double()], [a[:5], b], [a.t(), b], [a], [None, b.double()], [None, b[:299]]):
+        with pytest.raises(pb.PbkdError):
+            opt.step(grads, 0.1, stream=_Stream)
+    assert opt.steps == 9 == len(seen.tables)
+    opt.step([a, b], 0.1, stream=_Stream)
+    assert seen.tables[-1]["n"].tolist() == [300, 300] and seen.tables[-1]["grad_dtype"].tolist() == [pb.F32, pb.F32]
