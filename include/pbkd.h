@@ -502,6 +502,92 @@ typedef struct {
 } pbkd_adamw_args;
 pbkd_status pbkd_adamw_step(int n_tensors, const pbkd_adamw_tensor *tensors_host, const pbkd_adamw_args *args, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators of token students: what stands in front of a sequence model's first block and behind its last.
+ *
+ * The conventions are those of the sequence operators above.  Tokens, labels and places in the vocabulary are contiguous integers of
+ * 32 or 64 bits (index_dtype PBKD_I32 or PBKD_I64).  A number outside 0..vocab-1 names nothing: a padded token, a label to be
+ * ignored, a place that is not known; any such number may be used. */
+enum { PBKD_I32 = 8, PBKD_I64 = 9 };
+
+/* Lookup of tokens in a table, times a scale:  y_i = scale * weight[token_i]  (0 where token_i names nothing).
+ * rows >= 0, vocab >= 1, 1 <= d <= 65536; PBKD_EUNSUPPORTED for vocab above 2^22 or rows above 2^23. */
+typedef struct {
+  long long rows;
+  int vocab, d, dtype, index_dtype;
+  float scale;
+  const void *tokens_dev; /* [rows] */
+  const void *weight_dev; /* [vocab, d], rows strided */
+  void *y_dev;            /* [rows, d], rows strided */
+  long long weight_stride, y_stride;
+} pbkd_embed_desc;
+pbkd_status pbkd_embed_forward(const pbkd_embed_desc *desc, void *hip_stream);
+
+/* The table's gradient:  dweight_v = scale * (sum of dy_i over the rows with token_i == v), summed in fp32 in an order that only the
+ * tokens decide.  accumulate == 0: every row of dweight is written (0 for tokens that do not occur).  accumulate != 0: the sum is added to
+ * the row, and rows whose token does not occur stay as they are (a table that is the last product's weight too has two gradients).
+ * What dy holds where a token names nothing has no influence.  workspace: pbkd_embed_workspace_bytes(rows, vocab, d). */
+typedef struct {
+  long long rows;
+  int vocab, d, dtype, index_dtype;
+  float scale;
+  int accumulate;
+  const void *tokens_dev;
+  const void *dy_dev; /* [rows, d], rows strided */
+  void *dweight_dev;  /* [vocab, d], rows strided, of `dtype` too */
+  long long dy_stride, dweight_stride;
+  void *workspace_dev;
+  size_t workspace_bytes;
+} pbkd_embed_grad_desc;
+size_t pbkd_embed_workspace_bytes(long long rows, int vocab, int d); /* 0 for sizes the calls refuse */
+pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *desc, void *hip_stream);
+
+/* Softmax cross entropy over the whole vocabulary, from the activations in front of the last product, whose results (the
+ * logits) are formed in pieces and never kept.  Row n, with z_nv = h_n . weight_v:
+ *   lse_n = log(sum over v of exp(z_nv)),   loss_n = lse_n - z_{n,label_n}   (0 where label_n names nothing),
+ * and, if dh_dev and dweight_dev are given (both or neither), with dz_nv = row_weight_n (exp(z_nv - lse_n) - [v == label_n])
+ * (0 where label_n names nothing), the gradients of sum over n of row_weight_n loss_n:
+ *   dh_n = sum over v of dz_nv weight_v,   dweight_v = sum over n of dz_nv h_n   (both overwritten, of `dtype`).
+ * row_weight_dev nullable: 1.  lse_dev nullable.  What h holds in a row whose label names nothing has no influence on anything but that row's lse.
+ * Products of 16-bit types run on the matrix cores with fp32 sums, products of fp32 as sums of six products of bf16 terms; dz is
+ * rounded to `dtype` before it is multiplied (fp32: kept in three terms).
+ * workspace: pbkd_head_loss_workspace_bytes().  rows >= 0, vocab >= 1, d >= 1; PBKD_EUNSUPPORTED for rows above 2^21, vocab above 2^22, d above 65536. */
+typedef struct {
+  long long rows;
+  int vocab, d, dtype, index_dtype;
+  const void *h_dev;           /* [rows, d], rows strided */
+  const void *weight_dev;      /* [vocab, d], rows strided */
+  const void *labels_dev;      /* [rows] */
+  const float *row_weight_dev; /* [rows] */
+  float *loss_dev, *lse_dev;   /* [rows] */
+  void *dh_dev, *dweight_dev;  /* rows strided */
+  long long h_stride, weight_stride, dh_stride, dweight_stride;
+  void *workspace_dev;
+  size_t workspace_bytes;
+} pbkd_head_loss_desc;
+size_t pbkd_head_loss_workspace_bytes(long long rows, int vocab, int d, int dtype, int gradients); /* 0 for sizes the call refuses */
+pbkd_status pbkd_head_loss(const pbkd_head_loss_desc *desc, void *hip_stream);
+
+/* Distillation from a teacher of which the largest logits are known: row n has `top` pairs of a place in the vocabulary and the
+ * teacher's logit there.  Over the pairs whose place lies in the vocabulary and whose logit is above -infinity, with T = temperature,
+ *   q = softmax(teacher / T),   p = softmax(logits / T) over the whole vocabulary,   loss = T^2 * sum of q (log q - log p),
+ * and, if dlogits_dev is given, dlogits = row_weight * T * (p - q), the gradient of row_weight * loss.  A row without pairs has loss 0
+ * and gradient 0.  A place that occurs twice counts twice: its q are added.  row_weight_dev nullable: 1.  dlogits_dev may be logits_dev (same stride).
+ * The teacher's logits have a type of their own.  rows >= 0, vocab >= 1, 1 <= top <= 1024 (PBKD_EUNSUPPORTED beyond, and for rows above 2^21); temperature > 0. */
+typedef struct {
+  long long rows;
+  int vocab, top, dtype, teacher_dtype, index_dtype;
+  float temperature;
+  const void *logits_dev;  /* [rows, vocab], rows strided */
+  const void *teacher_dev; /* [rows, top], contiguous */
+  const void *at_dev;      /* [rows, top], contiguous */
+  const float *row_weight_dev; /* [rows] */
+  float *loss_dev;         /* [rows] */
+  void *dlogits_dev;       /* [rows, vocab], rows strided */
+  long long logits_stride, dlogits_stride;
+} pbkd_topk_distill_desc;
+pbkd_status pbkd_topk_distill(const pbkd_topk_distill_desc *desc, void *hip_stream);
+
 /* Message for the last error on the calling thread ("" if none). */
 const char *pbkd_last_error(void);
 

@@ -30,6 +30,7 @@ EXPORTS = [
     "pbkd_kernel_kinds", "pbkd_kernel_kind_name", "pbkd_block_profile_enable", "pbkd_block_profile_read",
     "pbkd_rmsnorm_forward", "pbkd_rmsnorm_backward", "pbkd_rmsnorm_workspace_bytes", "pbkd_recurrence_forward", "pbkd_recurrence_backward",
     "pbkd_recurrence_step", "pbkd_recurrence_saved_bytes", "pbkd_recurrence_workspace_bytes", "pbkd_adamw_step",
+    "pbkd_embed_forward", "pbkd_embed_backward", "pbkd_embed_workspace_bytes", "pbkd_head_loss", "pbkd_head_loss_workspace_bytes", "pbkd_topk_distill",
 ]
 
 
@@ -138,6 +139,12 @@ def lib():
         L.pbkd_rmsnorm_workspace_bytes.restype = ctypes.c_size_t
         for f in (L.pbkd_recurrence_saved_bytes, L.pbkd_recurrence_workspace_bytes):
             f.argtypes, f.restype = [ctypes.c_int, ctypes.c_longlong, ctypes.c_int], ctypes.c_size_t
+        for f in (L.pbkd_embed_forward, L.pbkd_embed_backward, L.pbkd_head_loss, L.pbkd_topk_distill):
+            f.argtypes, f.restype = [vp, vp], ctypes.c_int
+        L.pbkd_embed_workspace_bytes.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+        L.pbkd_embed_workspace_bytes.restype = ctypes.c_size_t
+        L.pbkd_head_loss_workspace_bytes.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]
+        L.pbkd_head_loss_workspace_bytes.restype = ctypes.c_size_t
         L.pbkd_adamw_step.argtypes = [ctypes.c_int, vp, vp, vp]
         L.pbkd_adamw_step.restype = ctypes.c_int
         _lib = L
@@ -400,26 +407,31 @@ def feature_mse_noalloc(a, b, stream=None, n: Optional[int] = None) -> float:
 
 
 # ------------------------------------------------------------------------------------------------ sequence operators
-# Root-mean-square norm, gated recurrence and AdamW (include/pbkd.h has the formulas).  All tensors are torch tensors on
+# Root-mean-square norm, gated recurrence, embedding, vocabulary loss, distillation from top logits and AdamW (include/pbkd.h has the formulas).  All tensors are torch tensors on
 # the current GPU, outputs too: nothing is allocated by a call.  A descriptor is packed with struct (native alignment, the C struct's
 # field order): a call of a few microseconds on the GPU should not wait for a ctypes structure's.
 F32, BF16, F16, E4M3 = range(4)
+I32, I64 = 8, 9
 _RMSNORM = struct.Struct("@q3if6P4q")
 _RMSNORM_GRAD = struct.Struct("@q2if6P4qPN")
 _RECURRENCE = struct.Struct("@2iqi8P8qPNPN")
 _RECURRENCE_GRAD = struct.Struct("@2iqi12P14qPNPN")
+_EMBED = struct.Struct("@q4if3P2q")
+_EMBED_GRAD = struct.Struct("@q4ifi3P2qPN")
+_HEAD_LOSS = struct.Struct("@q4i8P4qPN")
+_TOPK_DISTILL = struct.Struct("@q5if6P2q")
 _ADAMW_ARGS = struct.Struct("@5dqiI")
 _ADAMW_TENSOR = np.dtype([("n", "i8"), ("first", "i8"), ("param_dtype", "i4"), ("grad_dtype", "i4"), ("weight_decay", "f4"), ("param", "u8"), ("grad", "u8"),
                           ("m", "u8"), ("v", "u8"), ("m_scale", "u8"), ("v_scale", "u8"), ("copy", "u8")], align=True)
 _torch = _current_device = None       # set with the types by _types(), at the first call that needs them
-_CODES, _FP8, _FP32, _INT32 = {}, None, None, None
+_CODES, _INDEX, _FP8, _FP32, _INT32 = {}, {}, None, None, None
 
 
 def _types():
     """torch and its types by the library's numbers; the library is loaded (and torch with it) on the way."""
-    global _torch, _current_device, _CODES, _FP8, _FP32, _INT32
+    global _torch, _current_device, _CODES, _INDEX, _FP8, _FP32, _INT32
     import torch
-    _CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    _CODES, _INDEX = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}, {torch.int32: I32, torch.int64: I64}
     _FP8, _FP32, _INT32, _torch, _current_device = torch.float8_e4m3fn, torch.float32, torch.int32, torch, torch.cuda.current_device
     return lib()
 
@@ -584,6 +596,93 @@ def recurrence_step(u, gate, state, y, out_gate=None, bias=None, active=None, st
         _dense(bias, (d,), f32, dev, "bias"), _dense(active, (b,), _INT32, dev, "active"), sp, sp if state_out is None else _dense(state_out, (b, d), f32, dev, "state_out"),
         _same(y, dt, shape, dev, "y"), _row_stride(u, d, "u"), 0, _row_stride(gate, d, "gate"), 0, 0 if out_gate is None else _row_stride(out_gate, d, "out_gate"), 0,
         _row_stride(y, d, "y"), 0, 0, 0, 0, 0), _stream(stream)))
+
+
+def _indices(t, shape, dev: int, name: str):
+    """(address, type's number) of t, a contiguous tensor of 32- or 64-bit integers of this shape on GPU dev."""
+    code = _INDEX.get(t.dtype)
+    if code is None or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise PbkdError(ESHAPE, f"{name} must be a contiguous int32 or int64 tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), code
+
+
+def _table(shape, name: str):
+    """(rows, columns) of a matrix."""
+    if len(shape) != 2 or not shape[0] or not shape[1]:
+        raise PbkdError(ESHAPE, f"{name} must be a matrix with at least one row and column, not {tuple(shape)}")
+    return shape
+
+
+def embed_workspace_bytes(rows: int, vocab: int, d: int) -> int:
+    return lib().pbkd_embed_workspace_bytes(rows, vocab, d)
+
+
+def embed_forward(tokens, weight, y, scale: float = 1.0, stream=None) -> None:
+    """pbkd_embed_forward: y[..., :] <- scale * weight[tokens[...]] for tokens of any shape (int32 or int64), 0 for tokens outside
+    0..vocab-1.  weight [vocab, d], y [*tokens.shape, d] of weight's type."""
+    L, code, dt, shape, dev = _first(weight, "weight")
+    vocab, d = _table(shape, "weight")
+    tp, index = _indices(tokens, tokens.shape, dev, "tokens")
+    _check(L.pbkd_embed_forward(_EMBED.pack(tokens.numel(), vocab, d, code, index, scale, tp, weight.data_ptr(), _same(y, dt, (*tokens.shape, d), dev, "y"),
+                                            _row_stride(weight, d, "weight"), _row_stride(y, d, "y")), _stream(stream)))
+
+
+def embed_backward(tokens, dy, dweight, workspace, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """pbkd_embed_backward: dweight[v] <- scale * (sum of dy where tokens == v), added to what is there with accumulate (rows whose token
+    does not occur then stay as they are).  workspace: a tensor of embed_workspace_bytes(tokens.numel(), vocab, d) bytes."""
+    L, code, dt, shape, dev = _first(dweight, "dweight")
+    vocab, d = _table(shape, "dweight")
+    tp, index = _indices(tokens, tokens.shape, dev, "tokens")
+    wp, wn = _bytes(workspace, dev, "workspace")
+    _check(L.pbkd_embed_backward(_EMBED_GRAD.pack(tokens.numel(), vocab, d, code, index, scale, bool(accumulate), tp, _same(dy, dt, (*tokens.shape, d), dev, "dy"),
+                                                  dweight.data_ptr(), _row_stride(dy, d, "dy"), _row_stride(dweight, d, "dweight"), wp, wn), _stream(stream)))
+
+
+def head_loss_workspace_bytes(rows: int, vocab: int, d: int, dtype, gradients: bool) -> int:
+    """Bytes of workspace for head_loss on tensors of this torch type; with gradients or for losses only."""
+    L = lib() if _torch is not None else _types()
+    if dtype not in _CODES:
+        raise PbkdError(EINVAL, f"h must be float32, bfloat16 or float16, not {dtype}")
+    return L.pbkd_head_loss_workspace_bytes(rows, vocab, d, _CODES[dtype], bool(gradients))
+
+
+def head_loss(h, weight, labels, loss, workspace, lse=None, row_weight=None, dh=None, dweight=None, stream=None) -> None:
+    """pbkd_head_loss: loss [rows] float32 <- softmax cross entropy of h weight^T against labels, without keeping the logits; labels
+    outside 0..vocab-1 are ignored.  h [..., d], weight [vocab, d], labels [...] int32 or int64.  lse [rows]: the logits' log-sums.  dh and
+    dweight (like h and weight): the gradients of (row_weight * loss).sum().  workspace: a tensor of head_loss_workspace_bytes(...) bytes."""
+    L, code, dt, shape, dev = _first(h, "h")
+    vocab, d = _table(weight.shape, "weight")
+    if not shape or shape[-1] != d:
+        raise PbkdError(ESHAPE, f"rows of h must have weight's {d} elements, not {tuple(shape)}")
+    rows = h.numel() // d
+    lp, index = _indices(labels, shape[:-1], dev, "labels")
+    wp, wn = _bytes(workspace, dev, "workspace")
+    _check(L.pbkd_head_loss(_HEAD_LOSS.pack(
+        rows, vocab, d, code, index, h.data_ptr(), _same(weight, dt, weight.shape, dev, "weight"), lp, _dense(row_weight, (rows,), _FP32, dev, "row_weight"),
+        _dense(loss, (rows,), _FP32, dev, "loss"), _dense(lse, (rows,), _FP32, dev, "lse"), 0 if dh is None else _same(dh, dt, shape, dev, "dh"),
+        0 if dweight is None else _same(dweight, dt, weight.shape, dev, "dweight"), _row_stride(h, d, "h"), _row_stride(weight, d, "weight"),
+        0 if dh is None else _row_stride(dh, d, "dh"), 0 if dweight is None else _row_stride(dweight, d, "dweight"), wp, wn), _stream(stream)))
+
+
+def topk_distill(logits, teacher, at, loss, temperature: float = 1.0, row_weight=None, dlogits=None, stream=None) -> None:
+    """pbkd_topk_distill: loss [rows] float32 <- T^2 KL(softmax(teacher / T) || softmax(logits / T)), the teacher known at the places `at` only
+    (int32 or int64, like teacher [..., top]; a place outside 0..vocab-1 or a logit of -inf is not known).  logits [..., vocab].  dlogits
+    (like logits, or logits itself): the gradient of (row_weight * loss).sum()."""
+    L, code, dt, shape, dev = _first(logits, "logits")
+    vocab = shape[-1] if shape else 0
+    if vocab == 0:
+        raise PbkdError(ESHAPE, "logits has no elements in a row")
+    rows, known = logits.numel() // vocab, teacher.shape
+    if known[:-1] != shape[:-1] or not known[-1]:
+        raise PbkdError(ESHAPE, f"teacher must have logits' shape {tuple(shape)} but for the last dimension, not {tuple(known)}")
+    tcode = _CODES.get(teacher.dtype)
+    if tcode is None:
+        raise PbkdError(EINVAL, f"teacher must be float32, bfloat16 or float16, not {teacher.dtype}")
+    ap, index = _indices(at, known, dev, "at")
+    _check(L.pbkd_topk_distill(_TOPK_DISTILL.pack(
+        rows, vocab, known[-1], code, tcode, index, temperature, logits.data_ptr(), _dense(teacher, known, teacher.dtype, dev, "teacher"), ap,
+        _dense(row_weight, (rows,), _FP32, dev, "row_weight"), _dense(loss, (rows,), _FP32, dev, "loss"), 0 if dlogits is None else _same(dlogits, dt, shape, dev, "dlogits"),
+        _row_stride(logits, vocab, "logits"), 0 if dlogits is None else _row_stride(dlogits, vocab, "dlogits")), _stream(stream)))
 
 
 class AdamW:

@@ -1,0 +1,390 @@
+// Lookup of tokens in a table, times a scale, and the table's gradient.
+//
+//   forward    y_i = scale W[token_i]
+//   backward   dW_v = scale * sum over i with token_i = v of dy_i
+//
+// Both are bound by memory.  The gradient needs the rows of dy by token, and in an order that does not depend on timing.  Three launches:
+//   1. sort   A workgroup owns the tokens with one remainder modulo the number of workgroups, reads all tokens, counts its own and those
+//             before them, and lists its own rows by token, in their order (integers, read from the caches: no word from another
+//             workgroup is needed).
+//   2. sum    The list is cut into pieces of equal length; a piece adds its rows in registers and writes a token's sum when all its
+//             rows lie in the piece.  A sum that goes on in another piece is left as a partial one.  Other workgroups write
+//             the zeros of tokens that do not occur.
+//   3. join   Adds the partial sums of each token that crosses pieces, in order.
+#include "seq_common.h"
+
+namespace pbkd {
+namespace {
+
+constexpr int kMaxRows = 1 << 23, kMaxVocab = 1 << 22, kMaxD = 65536;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kMostBins = 512;       // tokens a workgroup of the sort owns: their counts for each wave fill 32 KB of LDS
+
+struct FwdArgs {
+  const void *tokens, *w;
+  void *y;
+  long long rows, ws, ys;
+  int v, d;
+  float scale;
+};
+
+// A group of TPR threads takes a row, eight elements a thread at a time.
+template <typename T, typename IT, int TPR, bool FAR>
+__global__ __launch_bounds__(256) void embed_fwd_kernel(FwdArgs A) {
+  constexpr int RPB = 256 / TPR;
+  const long long row = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
+  if (row >= A.rows) return;
+  const IT v = static_cast<const IT *>(A.tokens)[row];
+  const bool live = v >= 0 && v < A.v;
+  const T *w = static_cast<const T *>(A.w) + (live ? (long long)v : 0) * A.ws;
+  T *y = static_cast<T *>(A.y) + row * A.ys;
+  for (int c = threadIdx.x % TPR * 8; c < A.d; c += TPR * 8) {
+    float x[8];
+    load_n<T, 8>(w + c, live ? A.d - c : 0, x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] *= A.scale;
+    if (!live) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    store_n<T, 8, FAR>(y + c, A.d - c, x);
+  }
+}
+
+// The sorted list's layout in the workspace.  Token v belongs to workgroup v % groups, where it has bin v / groups.
+struct Plan {
+  int groups, bins;          // of the sort
+  int piece;                 // rows a piece of the list has
+  long long pieces;
+  size_t order, keys, counts, live, partial, bytes;   // offsets
+};
+
+inline Plan make_plan(long long rows, int vocab, int d) {
+  Plan p;
+  p.groups = 1;
+  while (p.groups < 256 && p.groups * 16 < vocab) p.groups *= 2;
+  while ((long long)p.groups * kMostBins < vocab) p.groups *= 2;
+  p.bins = (vocab + p.groups - 1) / p.groups;
+  p.piece = rows <= 16384 ? 8 : 32;
+  p.pieces = cdiv64(rows, p.piece);
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  p.order = 0;
+  p.keys = p.order + up(rows * 4);
+  p.counts = p.keys + up(rows * 4);
+  p.live = p.counts + up((size_t)p.groups * p.bins * 4);
+  p.partial = p.live + 256;
+  p.bytes = p.partial + up((size_t)p.pieces * 2 * d * 4) + 256;
+  return p;
+}
+
+struct SortArgs {
+  const void *tokens;
+  int *order, *keys, *counts, *live;
+  int rows, v, groups, bins;
+};
+
+// The lists of 16 waves, each of which reads a sixteenth of the tokens, follow each other within a token: rows stay in order.
+template <typename IT>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {
+  __shared__ int at[kSortWaves][kMostBins];   // first counts, then where the wave's next row of this token goes
+  __shared__ int wave_sum[kSortWaves], before_sum[kSortWaves];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, mine = blockIdx.x, mask = A.groups - 1;
+  const int shift = 31 - __builtin_clz(A.groups);
+  const IT *tokens = static_cast<const IT *>(A.tokens);
+  for (int i = tid; i < kSortWaves * kMostBins; i += kSortThreads) (&at[0][0])[i] = 0;
+  __syncthreads();
+  const int per = (A.rows + kSortThreads - 1) / kSortThreads * 64;
+  const long long lo = (long long)wave * per;
+  const int n = lo < A.rows ? (A.rows - lo < per ? (int)(A.rows - lo) : per) : 0;
+  constexpr int U = 8;
+  int before = 0;
+  for (int i = 0; i < n; i += 64 * U) {
+    IT w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) w[k] = i + k * 64 + lane < n ? tokens[lo + i + k * 64 + lane] : IT(-1);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool live = w[k] >= 0 && w[k] < A.v;
+      const int t = live ? (int)w[k] : 0, g = t & mask;
+      before += live && g < mine;
+      if (live && g == mine) atomicAdd(&at[wave][t >> shift], 1);
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) before += __shfl_xor(before, k, 64);
+  if (lane == 0) before_sum[wave] = before;
+  __syncthreads();
+  // a thread's bin: rows in all waves, and where they start
+  int total = 0;
+  if (tid < A.bins) {
+    for (int k = 0; k < kSortWaves; ++k) total += at[k][tid];
+    A.counts[mine * A.bins + tid] = total;
+  }
+  int scan = total;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const int x = __shfl_up(scan, k, 64);
+    if (lane >= k) scan += x;
+  }
+  if (lane == 63) wave_sum[wave] = scan;
+  __syncthreads();
+  int first = scan - total;
+  for (int k = 0; k < kSortWaves; ++k) first += before_sum[k] + (k < wave ? wave_sum[k] : 0);
+  if (tid < A.bins)
+    for (int k = 0; k < kSortWaves; ++k) {
+      const int x = at[k][tid];
+      at[k][tid] = first;
+      first += x;
+    }
+  if (mine == A.groups - 1 && tid == kSortThreads - 1) *A.live = first;   // bins behind the last are empty: the end of all
+  __syncthreads();
+  for (int i = 0; i < n; i += 64 * U) {
+    IT w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) w[k] = i + k * 64 + lane < n ? tokens[lo + i + k * 64 + lane] : IT(-1);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool live = w[k] >= 0 && w[k] < A.v;
+      const int t = live ? (int)w[k] : 0, bin = t >> shift;
+      const bool own = live && (t & mask) == mine;
+      unsigned long long todo = __ballot(own);
+      while (todo) {                             // one token after the other; mostly there is one
+        const int leader = __builtin_ctzll(todo), b = __shfl(bin, leader, 64);
+        const unsigned long long same = __ballot(own && bin == b);
+        if (own && bin == b) {
+          const int to = at[wave][b] + __popcll(same & ((1ull << lane) - 1));
+          A.order[to] = (int)(lo + i + k * 64 + lane);
+          A.keys[to] = t;
+        }
+        __builtin_amdgcn_wave_barrier();         // all lanes have read the place
+        if (lane == leader) at[wave][b] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        todo &= ~same;
+      }
+    }
+  }
+}
+
+struct SumArgs {
+  const int *order, *keys, *counts, *live;
+  const void *dy;
+  void *dw;
+  float *partial;
+  long long dys, dws, sum_blocks;
+  int v, d, groups, bins, piece, accumulate;
+  float scale;
+};
+
+template <typename T>
+__device__ __forceinline__ void put_row(const SumArgs &A, int key, int c, const float (&acc)[8]) {
+  T *p = static_cast<T *>(A.dw) + key * A.dws + c;
+  float x[8] = {};
+  if (A.accumulate) load_n<T, 8>(p, A.d - c, x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = A.accumulate ? x[k] + acc[k] * A.scale : acc[k] * A.scale;
+  store_n<T, 8>(p, A.d - c, x);
+}
+
+constexpr int kZeroRows = 16;        // rows of the table that a workgroup looks after for zeros
+
+template <typename T, int TPR>
+__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
+  const int sub = threadIdx.x / TPR, c = (blockIdx.y * TPR + threadIdx.x % TPR) * 8;
+  if (blockIdx.x >= A.sum_blocks) {
+    if (c >= A.d) return;
+    const int shift = 31 - __builtin_clz(A.groups);
+    const int v0 = (int)(blockIdx.x - A.sum_blocks) * kZeroRows;
+    for (int k = sub; k < kZeroRows && v0 + k < A.v; k += 256 / TPR) {
+      const int v = v0 + k;
+      if (A.counts[(v & (A.groups - 1)) * A.bins + (v >> shift)]) continue;
+      const float zero[8] = {};
+      store_n<T, 8>(static_cast<T *>(A.dw) + v * A.dws + c, A.d - c, zero);
+    }
+    return;
+  }
+  const int live = *A.live, piece = A.piece;
+  const long long p = (long long)blockIdx.x * (256 / TPR) + sub, first = p * piece;
+  if (first >= live || c >= A.d) return;
+  const int n = live - first < piece ? (int)(live - first) : piece;
+  const int *keys = A.keys + first, *order = A.order + first;
+  const bool from_before = first > 0 && keys[-1] == keys[0], goes_on = first + n < live && keys[n] == keys[n - 1];
+  float acc[8] = {};
+  bool head = true;                  // the sum is of the piece's first token
+  constexpr int U = 8;
+  const T *dy = static_cast<const T *>(A.dy);
+  for (int i = 0; i < n; i += U) {
+    float x[U][8];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool in = i + k < n;
+      load_n<T, 8>(dy + (in ? order[i + k] : 0) * A.dys + c, in ? A.d - c : 0, x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (i + k >= n) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += x[k][e];
+      const bool last = i + k == n - 1;
+      if (!last && keys[i + k + 1] == keys[i + k]) continue;
+      const bool open_front = head && from_before, open_back = last && goes_on;
+      if (open_front || open_back) store_n<float, 8>(A.partial + (p * 2 + (open_front ? 0 : 1)) * A.d + c, A.d - c, acc);
+      else put_row<T>(A, keys[i + k], c, acc);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+      head = false;
+    }
+  }
+}
+
+constexpr int kJoinPieces = 16;      // pieces a workgroup looks at for tokens that go on
+
+template <typename T>
+__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs A, long long pieces) {
+  __shared__ float part[4][64][8];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8;
+  const int live = *A.live, piece = A.piece;
+  const int shift = 31 - __builtin_clz(A.groups);
+  for (long long p = (long long)blockIdx.x * kJoinPieces; p < ((long long)blockIdx.x + 1) * kJoinPieces; ++p) {
+    const long long first = p * piece, next = first + piece;
+    if (p >= pieces || next >= live) return;
+    const int key = A.keys[next - 1];
+    if (A.keys[next] != key) continue;
+    int back = 1;                    // rows of this token in this piece
+    while (back < piece && A.keys[next - back - 1] == key) ++back;
+    if (back == piece && first > 0 && A.keys[first - 1] == key) continue;   // it began earlier
+    const int count = A.counts[(key & (A.groups - 1)) * A.bins + (key >> shift)];
+    const long long last = (next - back + count - 1) / piece;               // the piece that it ends in
+    float acc[8] = {};
+    if (c < A.d)
+      for (long long k = p + wave; k <= last; k += 4) {
+        float x[8];
+        load_n<float, 8>(A.partial + (k * 2 + (k == p ? 1 : 0)) * A.d + c, A.d - c, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += x[e];
+      }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[wave][lane][e] = acc[e];
+    __syncthreads();
+    if (wave == 0 && c < A.d) {
+#pragma unroll
+      for (int k = 1; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += part[k][lane][e];
+      put_row<T>(A, key, c, acc);
+    }
+    __syncthreads();
+  }
+}
+
+inline int row_threads(int d) {
+  int t = 8;
+  while (t < 256 && t * 8 < d) t *= 2;
+  return t;
+}
+
+template <typename T, typename IT>
+hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
+  const bool far = (double)A.rows * A.d * sizeof(T) > kLastLevelCache;
+  const int tpr = row_threads(A.d);
+  const unsigned grid = (unsigned)cdiv64(A.rows, 256 / tpr);
+#define FWD(N)                                                                      \
+  case N:                                                                           \
+    if (far) embed_fwd_kernel<T, IT, N, true><<<grid, 256, 0, st>>>(A);             \
+    else embed_fwd_kernel<T, IT, N, false><<<grid, 256, 0, st>>>(A);                \
+    break;
+  switch (tpr) { FWD(8) FWD(16) FWD(32) FWD(64) FWD(128) FWD(256) }
+#undef FWD
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_sum(SumArgs A, const Plan &p, hipStream_t st) {
+  const int tpr = row_threads(A.d);
+  A.sum_blocks = cdiv64(p.pieces, 256 / tpr);
+  const long long zero_blocks = A.accumulate ? 0 : cdiv64(A.v, kZeroRows);
+  const dim3 grid((unsigned)(A.sum_blocks + zero_blocks), (A.d + tpr * 8 - 1) / (tpr * 8));
+#define SUM(N) \
+  case N: embed_sum_kernel<T, N><<<grid, 256, 0, st>>>(A); break;
+  switch (tpr) { SUM(8) SUM(16) SUM(32) SUM(64) SUM(128) SUM(256) }
+#undef SUM
+  if (const hipError_t e = hipGetLastError()) return e;
+  if (p.pieces > 1) embed_join_kernel<T><<<dim3((unsigned)cdiv64(p.pieces, kJoinPieces), (A.d + 511) / 512), 256, 0, st>>>(A, p.pieces);
+  return hipGetLastError();
+}
+
+inline bool misaligned(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+
+pbkd_status check_embed(long long rows, int vocab, int d, int dtype, int index_dtype) {
+  if (rows < 0 || vocab < 1 || d < 1) return set_error(PBKD_ESHAPE, "embed: %lld tokens, a table of %d rows of %d", rows, vocab, d);
+  if (rows > kMaxRows || vocab > kMaxVocab || d > kMaxD)
+    return set_error(PBKD_EUNSUPPORTED, "embed: %lld tokens, a table of %d rows of %d, at most %d of %d", rows, vocab, d, kMaxVocab, kMaxD);
+  if (dtype != PBKD_F32 && dtype != PBKD_BF16 && dtype != PBKD_F16) return set_error(PBKD_EINVAL, "embed: dtype %d", dtype);
+  if (index_dtype != PBKD_I32 && index_dtype != PBKD_I64) return set_error(PBKD_EINVAL, "embed: index_dtype %d", index_dtype);
+  return PBKD_OK;
+}
+
+}  // namespace
+}  // namespace pbkd
+
+using namespace pbkd;
+
+extern "C" {
+
+pbkd_status pbkd_embed_forward(const pbkd_embed_desc *q, void *hip_stream) {
+  if (!q) return set_error(PBKD_EINVAL, "embed: null descriptor");
+  if (const pbkd_status s = check_embed(q->rows, q->vocab, q->d, q->dtype, q->index_dtype)) return s;
+  if (q->rows == 0) return PBKD_OK;
+  if (!q->tokens_dev || !q->weight_dev || !q->y_dev) return set_error(PBKD_EINVAL, "embed: null tensor");
+  const int size = q->dtype == PBKD_F32 ? 4 : 2;
+  if (misaligned(q->tokens_dev, q->index_dtype == PBKD_I64 ? 8 : 4) || misaligned(q->weight_dev, size) || misaligned(q->y_dev, size))
+    return set_error(PBKD_EINVAL, "embed: a tensor is not aligned to its elements");
+  if (q->weight_stride < 0) return set_error(PBKD_EINVAL, "embed: negative stride");
+  if (q->rows > 1 && q->y_stride < q->d) return set_error(PBKD_ESHAPE, "embed: rows of y overlap");
+  FwdArgs A{q->tokens_dev, q->weight_dev, q->y_dev, q->rows, q->weight_stride, q->y_stride, q->vocab, q->d, q->scale};
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const bool wide = q->index_dtype == PBKD_I64;
+  switch (q->dtype) {
+    case PBKD_F32: SEQ_HIPCHK((wide ? launch_fwd<float, long long>(A, st) : launch_fwd<float, int>(A, st))); break;
+    case PBKD_BF16: SEQ_HIPCHK((wide ? launch_fwd<bf16, long long>(A, st) : launch_fwd<bf16, int>(A, st))); break;
+    default: SEQ_HIPCHK((wide ? launch_fwd<f16, long long>(A, st) : launch_fwd<f16, int>(A, st))); break;
+  }
+  return PBKD_OK;
+}
+
+size_t pbkd_embed_workspace_bytes(long long rows, int vocab, int d) {
+  if (rows < 0 || vocab < 1 || d < 1 || rows > kMaxRows || vocab > kMaxVocab || d > kMaxD) return 0;
+  return make_plan(rows, vocab, d).bytes;
+}
+
+pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *q, void *hip_stream) {
+  if (!q) return set_error(PBKD_EINVAL, "embed: null descriptor");
+  if (const pbkd_status s = check_embed(q->rows, q->vocab, q->d, q->dtype, q->index_dtype)) return s;
+  if (!q->dweight_dev || (q->rows && (!q->tokens_dev || !q->dy_dev))) return set_error(PBKD_EINVAL, "embed: null tensor");
+  const int size = q->dtype == PBKD_F32 ? 4 : 2;
+  if (misaligned(q->tokens_dev, q->index_dtype == PBKD_I64 ? 8 : 4) || misaligned(q->dweight_dev, size) || misaligned(q->dy_dev, size))
+    return set_error(PBKD_EINVAL, "embed: a tensor is not aligned to its elements");
+  if (q->dy_stride < 0) return set_error(PBKD_EINVAL, "embed: negative stride");
+  if (q->vocab > 1 && q->dweight_stride < q->d) return set_error(PBKD_ESHAPE, "embed: rows of dweight overlap");
+  if (!q->workspace_dev || misaligned(q->workspace_dev, 256)) return set_error(PBKD_ENOMEM, "embed: the workspace must be 256-byte aligned");
+  const Plan p = make_plan(q->rows, q->vocab, q->d);
+  if (q->workspace_bytes < p.bytes) return set_error(PBKD_ENOMEM, "embed: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes, p.bytes);
+  if (q->rows == 0 && q->accumulate) return PBKD_OK;
+  char *ws = static_cast<char *>(q->workspace_dev);
+  int *order = reinterpret_cast<int *>(ws + p.order), *keys = reinterpret_cast<int *>(ws + p.keys), *counts = reinterpret_cast<int *>(ws + p.counts),
+      *live = reinterpret_cast<int *>(ws + p.live);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const SortArgs S{q->tokens_dev, order, keys, counts, live, (int)q->rows, q->vocab, p.groups, p.bins};
+  if (q->index_dtype == PBKD_I64) embed_sort_kernel<long long><<<p.groups, kSortThreads, 0, st>>>(S);
+  else embed_sort_kernel<int><<<p.groups, kSortThreads, 0, st>>>(S);
+  SEQ_HIPCHK(hipGetLastError());
+  const SumArgs A{order, keys, counts, live, q->dy_dev, q->dweight_dev, reinterpret_cast<float *>(ws + p.partial), q->dy_stride, q->dweight_stride, 0,
+                  q->vocab, q->d, p.groups, p.bins, p.piece, q->accumulate != 0, q->scale};
+  switch (q->dtype) {
+    case PBKD_F32: SEQ_HIPCHK(launch_sum<float>(A, p, st)); break;
+    case PBKD_BF16: SEQ_HIPCHK(launch_sum<bf16>(A, p, st)); break;
+    default: SEQ_HIPCHK(launch_sum<f16>(A, p, st)); break;
+  }
+  return PBKD_OK;
+}
+
+}  // extern "C"

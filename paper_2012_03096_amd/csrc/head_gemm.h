@@ -1,0 +1,253 @@
+// The matrix product under the vocabulary loss, and its three uses.
+//
+//   C[m][n] = sum over k of A[m][k] B[n][k],   A and B with k contiguous, k a multiple of 64, 16-bit types, fp32 sums
+//
+// A workgroup forms a tile of TM x TN.  Slices of 64 k of both operands go from memory straight into LDS (two stages: one on its way while
+// the other is multiplied).  A slice's row is 128 bytes, eight pieces of 16; a row's pieces are swapped by bits of its number, so that
+// the 16 rows that an MFMA's lanes read at once lie in different banks.  A wave's rows of A are dealt to its MFMA tiles so that
+// a lane ends with 4 * MT consecutive m of one n: results leave in wide stores, and a softmax over m needs two exchanges between lanes.
+//
+// fp32 operands come as three bf16 planes (x = x1 + x2 + x3 exactly); the product is the sum of the six plane products that matter
+// (what is left out is below 2^-24 of |a||b|), smallest first.
+#pragma once
+#include "seq_common.h"
+#include "split_bf16.h"
+
+namespace pbkd {
+namespace head {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+struct Operand {
+  const char *p;
+  long long ld, plane;     // bytes between rows, between planes
+  int rows;
+};
+
+enum { kStats, kDz, kOut, kSum };    // what becomes of a tile
+
+struct GemmArgs {
+  Operand a, b;
+  int kblocks, terms;              // slices of 64 in a plane, products of planes (1 or 6)
+  int tiles_m, tiles_n, splits;    // splits: parts of the sum over k, kSum only
+  // kStats, kDz: m is a place in the vocabulary, n a row of h
+  const int *label;                // -1: none
+  const float *lse, *g;            // g: 0 where there is no label
+  float *part, *at_label;          // kStats: [n][parts] pairs (maximum, sum)
+  int parts, part0, v0;            // v0: place of the piece's first row of A
+  char *dz, *dzt;                  // [n][m] and [m][n]
+  long long dz_ld, dz_plane, dzt_ld, dzt_plane;
+  int m_pad, n_pad;                // dz is written up to m_pad, dzt up to n_pad: zeros behind the ends
+  // kOut: out[n][m]; kSum: sum[split][n][m]
+  void *out;
+  long long out_ld;                // elements
+  const float *scale;
+  float *sum;
+  int add;
+};
+
+template <typename E>
+__device__ __forceinline__ floatx4 mma(uintx4 a, uintx4 b, floatx4 c) {
+  if constexpr (__is_same(E, f16)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kPlanesA = 0 << 0 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 2 << 10;   // six products, smallest first when read from the top
+constexpr int kPlanesB = 0 << 0 | 1 << 2 | 0 << 4 | 2 << 6 | 1 << 8 | 0 << 10;
+
+// OutT: the type of kOut's result.  PLANES: of dz (3: fp32 in three bf16 terms).
+template <typename E, typename OutT, int TM, int TN, int WM, int WN, int EPI, int PLANES>
+__global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
+  constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 16, NT = TN / WN / 16;
+  constexpr int RA = TM * 8 / THREADS, RB = TN * 8 / THREADS, ROWS = THREADS / 8;     // rounds of loads, rows a round
+  static_assert(RA * THREADS == TM * 8 && RB * THREADS == TN * 8, "whole rounds");
+  __shared__ __attribute__((aligned(1024))) char s0[(TM + TN) * 128];
+  __shared__ __attribute__((aligned(1024))) char s1[(TM + TN) * 128];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+
+  // neighbouring tiles meet in one die's L2: bands of 8 tiles of m, n inside a band
+  int tile = xcd_contiguous(blockIdx.x, G.tiles_m * G.tiles_n);
+  const int band = 8 * G.tiles_n, b0 = tile / band, in_band = G.tiles_m - b0 * 8 < 8 ? G.tiles_m - b0 * 8 : 8;
+  tile -= b0 * band;
+  const int m0 = (b0 * 8 + tile % in_band) * TM, n0 = tile / in_band * TN;
+
+  auto swz_a = [](int r) { return (r >> 1 & 1) | (r / (4 * MT) & 3) << 1; };
+  auto swz_b = [](int r) { return r >> 1 & 7; };
+  unsigned va[RA], vb[RB];
+  {
+    const int slot = tid & 7, r0 = tid >> 3;
+#pragma unroll
+    for (int i = 0; i < RA; ++i) {
+      const int r = i * ROWS + r0, row = m0 + r < G.a.rows ? r : G.a.rows - 1 - m0;      // rows behind the last: the last again
+      va[i] = (unsigned)(row * (int)G.a.ld + (slot ^ swz_a(r)) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const int r = i * ROWS + r0, row = n0 + r < G.b.rows ? r : G.b.rows - 1 - n0;
+      vb[i] = (unsigned)(row * (int)G.b.ld + (slot ^ swz_b(r)) * 16);
+    }
+  }
+  const char *pa = G.a.p + m0 * G.a.ld, *pb = G.b.p + n0 * G.b.ld;
+  const int rows_a = G.a.rows - m0 < TM ? G.a.rows - m0 : TM, rows_b = G.b.rows - n0 < TN ? G.b.rows - n0 : TN;
+  const int bytes_a = (rows_a - 1) * (int)G.a.ld + G.kblocks * 128, bytes_b = (rows_b - 1) * (int)G.b.ld + G.kblocks * 128;
+
+  // this workgroup's slices
+  const int total = G.kblocks * G.terms, per = (total + G.splits - 1) / G.splits;
+  const int first = blockIdx.y * per, last = first + per < total ? first + per : total;
+  int term = first / G.kblocks, kb = first - term * G.kblocks;
+  auto load = [&](char *s) {
+    const int t = G.terms - 1 - term, qa = kPlanesA >> 2 * t & 3, qb = kPlanesB >> 2 * t & 3;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pa + qa * G.a.plane), 0, bytes_a, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pb + qb * G.b.plane), 0, bytes_b, 0x00020000);
+    char *d = s + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], kb * 128);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], kb * 128);
+    if (++kb == G.kblocks) kb = 0, ++term;
+  };
+
+  floatx4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int r16 = lane & 15, q = lane >> 4;
+  const int row_a = wm * (MT * 16) + (r16 >> 2) * (4 * MT) + (r16 & 3), row_b = wn * (NT * 16) + r16;
+  // bits of the swizzle that do not depend on the MFMA tile: 4 i adds nothing to bit 1, and stays within 4 * MT rows
+  const int sa = swz_a(row_a), sb = swz_b(row_b);
+  auto compute = [&](const char *s) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      uintx4 fa[MT], fb[NT];
+      const int ca = (kk * 4 + q) ^ sa, cb = (kk * 4 + q) ^ sb;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fb[j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 16 * j) * 128 + cb * 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[i] = *reinterpret_cast<const uintx4 *>(s + (row_a + 4 * i) * 128 + ca * 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = mma<E>(fa[i], fb[j], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);      // or the next half's operands are read now, and registers spill
+    }
+  };
+
+  if (first < last) {
+    load(s0);
+    for (int k = first; k < last; k += 2) {
+      __syncthreads();
+      if (k + 1 < last) load(s1);
+      compute(s0);
+      if (k + 1 >= last) break;
+      __syncthreads();
+      if (k + 2 < last) load(s0);
+      compute(s1);
+    }
+  }
+
+  // a lane's results: n = n1 + 16 j, m = m1 .. m1 + 4 MT - 1 (tile i: four of them)
+  const int m1 = m0 + wm * (MT * 16) + q * (4 * MT), n1 = n0 + wn * (NT * 16) + r16;
+  if constexpr (EPI == kStats) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = n1 + 16 * j;
+      const bool in = n < G.b.rows;
+      const int at = in ? G.label[n] - G.v0 - m1 : -1;
+      float top = -__builtin_inff(), sum = 0.f, mine = 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (m1 + 4 * i + e >= G.a.rows) acc[i][j][e] = -__builtin_inff();
+          top = fmaxf(top, acc[i][j][e]);
+          if (at == 4 * i + e) mine = acc[i][j][e];
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float ref = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __expf(acc[i][j][e] - ref);
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      if (in) {
+        if (at >= 0 && at < 4 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
+        if (q == 0) {
+          float *p = G.part + ((long long)n * G.parts + G.part0 + m0 / TM * WM + wm) * 2;
+          p[0] = top, p[1] = sum;
+        }
+      }
+    }
+  } else if constexpr (EPI == kDz) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = n1 + 16 * j;
+      const bool in = n < G.b.rows;
+      const int label = in ? G.label[n] : -1, at = label - G.v0 - m1;
+      const float lse = in ? G.lse[n] : 0.f, g = in ? G.g[n] : 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[e] = label >= 0 && m1 + 4 * i + e < G.a.rows ? g * (__expf(acc[i][j][e] - lse) - (at == 4 * i + e ? 1.f : 0.f)) : 0.f;
+#pragma unroll
+        for (int k = 0; k < PLANES; ++k) {
+          E y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
+          if (in && m1 + 4 * i < G.m_pad) {
+            uintx2 w;
+            __builtin_memcpy(&w, y, 8);
+            *reinterpret_cast<uintx2 *>(G.dz + k * G.dz_plane + n * G.dz_ld + (m1 + 4 * i) * 2) = w;
+          }
+          if (n < G.n_pad) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (m1 + 4 * i + e < G.a.rows) *reinterpret_cast<E *>(G.dzt + k * G.dzt_plane + (m1 + 4 * i + e) * G.dzt_ld + n * 2) = y[e];
+          }
+        }
+      }
+    }
+  } else if constexpr (EPI == kOut) {
+    const float scale = *G.scale;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = n1 + 16 * j;
+      if (n >= G.b.rows) continue;
+      OutT *p = static_cast<OutT *>(G.out) + n * G.out_ld + m1;
+#pragma unroll
+      for (int i = 0; i < MT; i += 2) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = acc[i + e / 4][j][e % 4] * scale;
+        store_n<OutT, 8>(p + 4 * i, G.a.rows - m1 - 4 * i, x);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = n1 + 16 * j;
+      if (n >= G.b.rows) continue;
+      float *p = G.sum + ((long long)blockIdx.y * G.b.rows + n) * G.out_ld + m1;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        if (m1 + 4 * i >= G.a.rows) break;
+        float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]}, y[4];
+        if (G.add) {
+          load_n<float, 4>(p + 4 * i, G.a.rows - m1 - 4 * i, y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] += y[e];
+        }
+        store_n<float, 4>(p + 4 * i, G.a.rows - m1 - 4 * i, x);
+      }
+    }
+  }
+}
+
+}  // namespace head
+}  // namespace pbkd

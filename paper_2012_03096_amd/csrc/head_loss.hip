@@ -1,0 +1,386 @@
+// Softmax cross entropy over a large vocabulary from the activations in front of the last product, with the gradients of both.
+//
+//   z = h W^T,  lse_n = log sum_v exp z_nv,  loss_n = lse_n - z_{n,label},  dz_nv = g_n (exp(z_nv - lse_n) - [v = label_n]),  dh = dz W,  dW = dz^T h
+//
+// Bound by its products of matrices: 2 N V d operations for the losses, and 6 N V d for the gradients, because z is not kept but formed
+// again, piece of the vocabulary by piece.  The first pass leaves a maximum and a sum of every tile's rows; they give lse.  In the
+// second a piece's dz comes out of the product in both layouts, n by v for dh and v by n for dW, so that every product
+// reads both operands along k (head_gemm.h); W's and h's other layouts are copied first (a hundredth of the products' time).
+//
+// dz is rounded to the operands' type, which is an error of the size that rounding the gradients has anyway (half a step of a
+// value, averaged over the sum).  It is formed with row weights times a power of two that puts the largest near 2^15: fp16 keeps
+// probabilities down to 2^-24 / 2^15 of it.  fp32 is kept in three bf16 terms.
+#include "head_gemm.h"
+
+namespace pbkd {
+namespace {
+
+using namespace head;
+
+constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
+constexpr double kPieceBytes = 512e6;        // dz of a piece, both layouts
+
+inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
+
+// ------------------------------------------------------------------------------------------------------ small kernels
+struct RowArgs {
+  const void *labels;
+  const float *g;
+  int *label;
+  float *gs, *scale;       // scale[0] = 2^-s, what results are multiplied with; scale[1] = 1
+  int rows, v;
+};
+
+// Labels as 32-bit numbers (-1: none), row weights times 2^s (0 where there is no label).
+template <typename IT>
+__global__ __launch_bounds__(1024) void head_rows_kernel(RowArgs A) {
+  __shared__ float red[16];
+  const int tid = threadIdx.x;
+  const IT *labels = static_cast<const IT *>(A.labels);
+  float top = 0.f;
+  for (int i = tid; i < A.rows; i += 1024) {
+    const IT w = labels[i];
+    const bool live = w >= 0 && w < A.v;
+    A.label[i] = live ? (int)w : -1;
+    const float g = live ? (A.g ? A.g[i] : 1.f) : 0.f;
+    if (A.gs) A.gs[i] = g;
+    if (fabsf(g) < __builtin_inff()) top = fmaxf(top, fabsf(g));
+  }
+  if (!A.gs) return;
+  top = wave64_max(top);
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  for (int k = 0; k < 16; ++k) top = fmaxf(top, red[k]);
+  int e = top > 0.f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;       // top < 2^(14 - e): dz stays below 2^15
+  e = e < 100 ? e : 100;
+  const float s = ldexpf(1.f, e);
+  for (int i = tid; i < A.rows; i += 1024) A.gs[i] *= s;
+  if (tid == 0) A.scale[0] = ldexpf(1.f, -e), A.scale[1] = 1.f;
+}
+
+struct LayArgs {
+  const void *src;
+  char *dst;
+  long long stride;        // elements between the source's rows
+  long long ld, plane;     // bytes
+  const int *label;        // rows without a label become zeros; null: none do
+  int rows, cols;          // of the source
+  int fill;                // rows of the result's other dimension up to here are written: zeros behind the end
+};
+
+template <typename T, int PLANES, typename E>
+__device__ __forceinline__ void planes_of(float x, E (&y)[PLANES]) {
+#pragma unroll
+  for (int k = 0; k < PLANES; ++k) y[k] = static_cast<E>(x), x -= static_cast<float>(y[k]);
+}
+
+// dst[row][0..fill) = src[row][..], zeros behind cols.  Eight elements a thread.
+template <typename T, typename E, int PLANES>
+__global__ __launch_bounds__(256) void head_pack_kernel(LayArgs A) {
+  const int per = A.fill / 8;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)A.rows * per) return;
+  const long long row = i / per;
+  const int c = (int)(i - row * per) * 8;
+  float x[8];
+  load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c, A.cols - c, x);
+#pragma unroll
+  for (int k = 0; k < PLANES; ++k) {
+    E y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
+    uintx4 w;
+    __builtin_memcpy(&w, y, 16);
+    *reinterpret_cast<uintx4 *>(A.dst + k * A.plane + row * A.ld + c * 2) = w;
+  }
+}
+
+// dst[col][0..fill) = src[..][col], zeros behind rows.  Tiles of 64 x 64.
+template <typename T, typename E, int PLANES>
+__global__ __launch_bounds__(256) void head_transpose_kernel(LayArgs A) {
+  __shared__ E tile[PLANES][64][66];
+  const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int r = k * 32 + tid / 8, c = tid % 8 * 8, row = r0 + r;
+    float x[8] = {};
+    if (row < A.rows && (!A.label || A.label[row] >= 0)) load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c0 + c, A.cols - c0 - c, x);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const E y = static_cast<E>(x[e]);
+        x[e] -= static_cast<float>(y);
+        tile[p][c + e][r] = y;
+      }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = k * 32 + tid / 8, r = tid % 8 * 8;
+    if (c0 + c >= A.cols || r0 + r >= A.fill) continue;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) {
+      E y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = tile[p][c][r + e];
+      uintx4 w;
+      __builtin_memcpy(&w, y, 16);
+      *reinterpret_cast<uintx4 *>(A.dst + p * A.plane + (c0 + c) * A.ld + (r0 + r) * 2) = w;
+    }
+  }
+}
+
+// A wave joins a row's pairs in the order of the vocabulary's tiles.
+__global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int parts, int stride, const int *label, const float *at_label, float *lse, float *lse_out, float *loss,
+                                                       int rows) {
+  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (n >= rows) return;
+  const float *p = part + (long long)n * stride * 2;
+  float top = -__builtin_inff(), sum = 0.f;
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, p[2 * k]);
+  top = wave64_max(top);
+  const float ref = top == -__builtin_inff() ? 0.f : top;
+  for (int k = lane; k < parts; k += 64) sum += p[2 * k + 1] * expf(p[2 * k] - ref);
+  sum = wave64_sum(sum);
+  if (lane == 0) {
+    const float x = top + logf(sum);
+    lse[n] = x;
+    if (lse_out) lse_out[n] = x;
+    loss[n] = label[n] >= 0 ? x - at_label[n] : 0.f;
+  }
+}
+
+// out[n][m] = scale * sum over the splits, in order
+template <typename T>
+__global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int splits, int rows, int cols, const float *scale, T *out, long long stride) {
+  const int per = (cols + 7) / 8;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)rows * per) return;
+  const long long row = i / per;
+  const int c = (int)(i - row * per) * 8;
+  float x[8] = {};
+  for (int k = 0; k < splits; ++k) {
+    float y[8];
+    load_n<float, 8>(sum + ((long long)k * rows + row) * cols + c, cols - c, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += y[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= *scale;
+  store_n<T, 8>(out + row * stride + c, cols - c, x);
+}
+
+// ---------------------------------------------------------------------------------------------------------- the plan
+// Tiles of a product: large ones where they fill the chip, smaller ones where they would not, narrow ones for few rows of n.
+struct Shape {
+  int tm, tn, wm, wn;
+};
+constexpr Shape kShapes[3] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {128, 64, 4, 1}};
+
+inline int pick_shape(long long m, long long n, int splits) {
+  if (n <= 64) return 2;
+  return cdiv64(m, 256) * cdiv64(n, 256) * splits >= 192 ? 0 : 1;
+}
+
+struct Plan {
+  int d_pad, n_pad, piece, pieces, planes, terms, parts, first_shape, sum_shape, splits;
+  bool pack_h, pack_w;
+  size_t label, gs, scale, lse, at_label, part, h, ht, w, wt, dz, dzt, sum, bytes;
+};
+
+bool direct(const void *p, long long stride, int d, int dtype) {
+  return dtype != PBKD_F32 && d % 64 == 0 && stride % 8 == 0 && stride <= 1 << 20 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+}
+
+// pack_*: whether the operands have to be laid out (the workspace is counted as if they had)
+Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w) {
+  Plan p;
+  p.planes = dtype == PBKD_F32 ? 3 : 1, p.terms = dtype == PBKD_F32 ? 6 : 1;
+  p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
+  p.pack_h = pack_h, p.pack_w = pack_w;
+  double most = kPieceBytes / (4.0 * p.planes * p.n_pad);
+  if (!gradients) most = kPieceBytes / (2.0 * p.planes * p.d_pad);
+  long long piece = (long long)(most / 1024) * 1024;
+  piece = piece < 1024 ? 1024 : piece;
+  const int n = (int)cdiv64(vocab, piece);
+  p.piece = (int)(cdiv64(cdiv64(vocab, n), 256) * 256);
+  p.pieces = (int)cdiv64(vocab, p.piece);
+  if (!gradients && !pack_w) p.piece = vocab, p.pieces = 1;
+  p.first_shape = pick_shape(p.piece, rows, 1);
+  // dh: few tiles, a long sum
+  p.sum_shape = pick_shape(d, rows, 1);
+  const long long tiles = cdiv64(d, kShapes[p.sum_shape].tm) * cdiv64(rows, kShapes[p.sum_shape].tn);
+  const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.terms;
+  p.splits = (int)(256 / (tiles > 0 ? tiles : 1));
+  p.splits = p.splits > slices / 8 ? slices / 8 : p.splits;
+  p.splits = p.splits < 1 ? 1 : p.splits;
+  const Shape &s = kShapes[p.first_shape];
+  p.parts = (int)(cdiv64(vocab, s.tm) + p.pieces) * s.wm;
+  size_t at = 0;
+  auto put = [&](size_t n) {
+    const size_t here = at;
+    at += (n + 255) / 256 * 256;
+    return here;
+  };
+  const size_t R = rows, e = 2 * p.planes;
+  p.label = put(R * 4), p.gs = put(R * 4), p.scale = put(8), p.lse = put(R * 4), p.at_label = put(R * 4);
+  p.part = put(R * p.parts * 8);
+  p.h = put(pack_h ? R * p.d_pad * e : 0);
+  p.w = put(pack_w ? (size_t)p.piece * p.d_pad * e : 0);
+  if (gradients) {
+    p.ht = put((size_t)d * p.n_pad * e);
+    p.wt = put((size_t)d * p.piece * e);
+    p.dz = put(R * p.piece * e);
+    p.dzt = put((size_t)p.piece * p.n_pad * e);
+    p.sum = put((size_t)p.splits * R * d * 4);
+  }
+  p.bytes = at + 256;
+  return p;
+}
+
+// --------------------------------------------------------------------------------------------------------- the launches
+template <typename E, typename OutT, int EPI, int PLANES>
+hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
+  const Shape &s = kShapes[shape];
+  G.tiles_m = (int)cdiv64(G.a.rows, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
+  const dim3 grid(G.tiles_m * G.tiles_n, G.splits);
+  switch (shape) {
+    case 0: gemm_kernel<E, OutT, 256, 256, 2, 4, EPI, PLANES><<<grid, 512, 0, st>>>(G); break;
+    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
+    default: gemm_kernel<E, OutT, 128, 64, 4, 1, EPI, PLANES><<<grid, 256, 0, st>>>(G);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, typename E, int PLANES>
+hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
+  constexpr int es = sizeof(T);
+  char *ws = static_cast<char *>(q.workspace_dev);
+  const int rows = (int)q.rows, V = q.vocab, d = q.d;
+  const bool gradients = q.dh_dev != nullptr;
+  int *label = reinterpret_cast<int *>(ws + p.label);
+  auto floats = [&](size_t at) { return reinterpret_cast<float *>(ws + at); };
+  const RowArgs R{q.labels_dev, q.row_weight_dev, label, gradients ? floats(p.gs) : nullptr, floats(p.scale), rows, V};
+  if (q.index_dtype == PBKD_I64) head_rows_kernel<long long><<<1, 1024, 0, st>>>(R);
+  else head_rows_kernel<int><<<1, 1024, 0, st>>>(R);
+
+  Operand H{static_cast<const char *>(q.h_dev), q.h_stride * es, 0, rows};
+  if (p.pack_h) {
+    LayArgs L{q.h_dev, ws + p.h, q.h_stride, p.d_pad * 2, (long long)rows * p.d_pad * 2, nullptr, rows, d, p.d_pad};
+    head_pack_kernel<T, E, PLANES><<<(unsigned)cdiv64((long long)rows * p.d_pad / 8, 256), 256, 0, st>>>(L);
+    H = Operand{L.dst, L.ld, L.plane, rows};
+  }
+  if (gradients) {
+    LayArgs L{q.h_dev, ws + p.ht, q.h_stride, p.n_pad * 2, (long long)d * p.n_pad * 2, label, rows, d, p.n_pad};
+    head_transpose_kernel<T, E, PLANES><<<dim3(p.n_pad / 64, (d + 63) / 64), 256, 0, st>>>(L);
+  }
+  auto weight = [&](int v0, int n, bool lay) {       // rows v0 .. v0 + n of W along k
+    const T *w = static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride;
+    if (!p.pack_w) return Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n};
+    LayArgs L{w, ws + p.w, q.weight_stride, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, nullptr, n, d, p.d_pad};
+    if (lay) head_pack_kernel<T, E, PLANES><<<(unsigned)cdiv64((long long)n * p.d_pad / 8, 256), 256, 0, st>>>(L);
+    return Operand{L.dst, L.ld, L.plane, n};
+  };
+  GemmArgs G{};
+  G.b = H, G.kblocks = p.d_pad / 64, G.terms = p.terms, G.splits = 1;
+  G.label = label, G.lse = floats(p.lse), G.g = floats(p.gs), G.part = floats(p.part), G.at_label = floats(p.at_label);
+  G.m_pad = G.n_pad = 0;
+  int parts = 0;
+  const bool whole = !p.pack_w;                       // W as it lies: one product over the whole vocabulary
+  for (int v0 = 0; v0 < V; v0 += whole ? V : p.piece) {
+    const int n = whole || V - v0 < p.piece ? V - v0 : p.piece;
+    G.a = weight(v0, n, true), G.v0 = v0, G.parts = p.parts, G.part0 = parts;
+    if (const hipError_t e = launch_gemm<E, T, kStats, 1>(G, p.first_shape, st)) return e;
+    parts += (int)cdiv64(n, kShapes[p.first_shape].tm) * kShapes[p.first_shape].wm;
+  }
+  head_lse_kernel<<<(rows + 3) / 4, 256, 0, st>>>(floats(p.part), parts, p.parts, label, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev, rows);
+  if (!gradients) return hipGetLastError();
+
+  for (int v0 = 0; v0 < V; v0 += p.piece) {
+    const int n = V - v0 < p.piece ? V - v0 : p.piece, n64 = up64(n);
+    // dz of this piece, in both layouts
+    G.a = weight(v0, n, p.pieces > 1), G.v0 = v0;
+    G.dz = ws + p.dz, G.dz_ld = p.piece * 2, G.dz_plane = (long long)rows * p.piece * 2;
+    G.dzt = ws + p.dzt, G.dzt_ld = p.n_pad * 2, G.dzt_plane = (long long)p.piece * p.n_pad * 2;
+    G.m_pad = n64, G.n_pad = p.n_pad;
+    if (const hipError_t e = launch_gemm<E, T, kDz, PLANES>(G, p.first_shape, st)) return e;
+    LayArgs L{static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride, ws + p.wt, q.weight_stride, p.piece * 2, (long long)d * p.piece * 2, nullptr, n, d, n64};
+    head_transpose_kernel<T, E, PLANES><<<dim3(n64 / 64, (d + 63) / 64), 256, 0, st>>>(L);
+    GemmArgs D{};
+    D.terms = p.terms, D.scale = floats(p.scale);
+    D.a = Operand{ws + p.wt, L.ld, L.plane, d}, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
+    D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
+    if (const hipError_t e = launch_gemm<E, T, kSum, 1>(D, p.sum_shape, st)) return e;
+    D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
+    D.kblocks = p.n_pad / 64, D.splits = 1;
+    D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
+    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, pick_shape(d, n, 1), st)) return e;
+  }
+  head_finish_kernel<T><<<(unsigned)cdiv64((long long)rows * ((d + 7) / 8), 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale),
+                                                                                               static_cast<T *>(q.dh_dev), q.dh_stride);
+  return hipGetLastError();
+}
+
+inline bool misaligned(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+
+inline bool supported(long long rows, int vocab, int d) { return rows <= kMaxRows && vocab <= kMaxVocab && d <= kMaxD; }
+
+// dweight of a batch without rows
+template <typename T>
+__global__ __launch_bounds__(256) void head_zero_kernel(T *out, int rows, int cols, long long stride) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)rows * cols; i += (long long)gridDim.x * 256) out[i / cols * stride + i % cols] = T(0.f);
+}
+
+}  // namespace
+}  // namespace pbkd
+
+using namespace pbkd;
+
+extern "C" {
+
+size_t pbkd_head_loss_workspace_bytes(long long rows, int vocab, int d, int dtype, int gradients) {
+  if (rows < 0 || vocab < 1 || d < 1 || !supported(rows, vocab, d) || (dtype != PBKD_F32 && dtype != PBKD_BF16 && dtype != PBKD_F16)) return 0;
+  // laid out or not: what the addresses and strides of a call decide
+  const size_t a = make_plan((int)rows, vocab, d, dtype, gradients != 0, true, true).bytes, b = make_plan((int)rows, vocab, d, dtype, gradients != 0, true, false).bytes;
+  return a > b ? a : b;
+}
+
+pbkd_status pbkd_head_loss(const pbkd_head_loss_desc *q, void *hip_stream) {
+  if (!q) return set_error(PBKD_EINVAL, "head_loss: null descriptor");
+  if (q->rows < 0 || q->vocab < 1 || q->d < 1) return set_error(PBKD_ESHAPE, "head_loss: %lld rows, a weight of %d rows of %d", q->rows, q->vocab, q->d);
+  if (!supported(q->rows, q->vocab, q->d))
+    return set_error(PBKD_EUNSUPPORTED, "head_loss: %lld rows, a weight of %d rows of %d, at most %d, %d of %d", q->rows, q->vocab, q->d, kMaxRows, kMaxVocab, kMaxD);
+  if (q->dtype != PBKD_F32 && q->dtype != PBKD_BF16 && q->dtype != PBKD_F16) return set_error(PBKD_EINVAL, "head_loss: dtype %d", q->dtype);
+  if (q->index_dtype != PBKD_I32 && q->index_dtype != PBKD_I64) return set_error(PBKD_EINVAL, "head_loss: index_dtype %d", q->index_dtype);
+  if ((q->dh_dev != nullptr) != (q->dweight_dev != nullptr) && q->rows) return set_error(PBKD_EINVAL, "head_loss: dh and dweight come together");
+  if (q->rows && (!q->h_dev || !q->weight_dev || !q->labels_dev || !q->loss_dev)) return set_error(PBKD_EINVAL, "head_loss: null tensor");
+  const int size = q->dtype == PBKD_F32 ? 4 : 2;
+  if (misaligned(q->h_dev, size) || misaligned(q->weight_dev, size) || misaligned(q->dh_dev, size) || misaligned(q->dweight_dev, size) ||
+      misaligned(q->labels_dev, q->index_dtype == PBKD_I64 ? 8 : 4) || misaligned(q->row_weight_dev, 4) || misaligned(q->loss_dev, 4) || misaligned(q->lse_dev, 4))
+    return set_error(PBKD_EINVAL, "head_loss: a tensor is not aligned to its elements");
+  if (q->h_stride < 0 || q->weight_stride < 0) return set_error(PBKD_EINVAL, "head_loss: negative stride");
+  if (q->dh_dev && ((q->rows > 1 && q->dh_stride < q->d) || (q->vocab > 1 && q->dweight_stride < q->d)))
+    return set_error(PBKD_ESHAPE, "head_loss: rows of an output overlap");
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (q->rows == 0) {
+    if (!q->dweight_dev) return PBKD_OK;
+    if (size == 4) head_zero_kernel<float><<<1024, 256, 0, st>>>(static_cast<float *>(q->dweight_dev), q->vocab, q->d, q->dweight_stride);
+    else head_zero_kernel<bf16><<<1024, 256, 0, st>>>(static_cast<bf16 *>(q->dweight_dev), q->vocab, q->d, q->dweight_stride);
+    SEQ_HIPCHK(hipGetLastError());
+    return PBKD_OK;
+  }
+  if (!q->workspace_dev || misaligned(q->workspace_dev, 256)) return set_error(PBKD_ENOMEM, "head_loss: the workspace must be 256-byte aligned");
+  const size_t need = pbkd_head_loss_workspace_bytes(q->rows, q->vocab, q->d, q->dtype, q->dh_dev != nullptr);
+  if (q->workspace_bytes < need) return set_error(PBKD_ENOMEM, "head_loss: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes, need);
+  const Plan p = make_plan((int)q->rows, q->vocab, q->d, q->dtype, q->dh_dev != nullptr, !direct(q->h_dev, q->h_stride, q->d, q->dtype),
+                           !direct(q->weight_dev, q->weight_stride, q->d, q->dtype));
+  switch (q->dtype) {
+    case PBKD_F32: SEQ_HIPCHK((run<float, bf16, 3>(*q, p, st))); break;
+    case PBKD_BF16: SEQ_HIPCHK((run<bf16, bf16, 1>(*q, p, st))); break;
+    default: SEQ_HIPCHK((run<f16, f16, 1>(*q, p, st))); break;
+  }
+  return PBKD_OK;
+}
+
+}  // extern "C"
