@@ -17,7 +17,7 @@ namespace pbkd {
 namespace head {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 struct Operand {
   const char *p;
@@ -48,9 +48,9 @@ struct GemmArgs {
 };
 
 template <typename E>
-__device__ __forceinline__ floatx4 mma(uintx4 a, uintx4 b, floatx4 c) {
-  if constexpr (__is_same(E, f16)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+__device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
+  if constexpr (__is_same(E, f16)) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 constexpr int kPlanesA = 0 << 0 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 2 << 10;   // six products, smallest first when read from the top
@@ -59,7 +59,7 @@ constexpr int kPlanesB = 0 << 0 | 1 << 2 | 0 << 4 | 2 << 6 | 1 << 8 | 0 << 10;
 // OutT: the type of kOut's result.  PLANES: of dz (3: fp32 in three bf16 terms).
 template <typename E, typename OutT, int TM, int TN, int WM, int WN, int EPI, int PLANES>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
-  constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 16, NT = TN / WN / 16;
+  constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 32, NT = TN / WN / 32;
   constexpr int RA = TM * 8 / THREADS, RB = TN * 8 / THREADS, ROWS = THREADS / 8;     // rounds of loads, rows a round
   static_assert(RA * THREADS == TM * 8 && RB * THREADS == TN * 8, "whole rounds");
   __shared__ __attribute__((aligned(1024))) char s0[(TM + TN) * 128];
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   tile -= b0 * band;
   const int m0 = (b0 * 8 + tile % in_band) * TM, n0 = tile / in_band * TN;
 
-  auto swz_a = [](int r) { return (r >> 1 & 1) | (r / (4 * MT) & 3) << 1; };
+  auto swz_a = [](int r) { return (r >> 1 & 3) | (r / (16 * MT) & 1) << 2; };
   auto swz_b = [](int r) { return r >> 1 & 7; };
   unsigned va[RA], vb[RB];
   {
@@ -109,74 +109,115 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     if (++kb == G.kblocks) kb = 0, ++term;
   };
 
-  floatx4 acc[MT][NT];
+  floatx16 acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int r16 = lane & 15, q = lane >> 4;
-  const int row_a = wm * (MT * 16) + (r16 >> 2) * (4 * MT) + (r16 & 3), row_b = wn * (NT * 16) + r16;
-  // bits of the swizzle that do not depend on the MFMA tile: 4 i adds nothing to bit 1, and stays within 4 * MT rows
-  const int sa = swz_a(row_a), sb = swz_b(row_b);
-  auto compute = [&](const char *s) {
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      uintx4 fa[MT], fb[NT];
-      const int ca = (kk * 4 + q) ^ sa, cb = (kk * 4 + q) ^ sb;
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  const int r32 = lane & 31, h = lane >> 5;
+  // MFMA row 8 a + 4 b + c of tile i is the wave's row b * 16 MT + 16 i + 4 a + c: a lane then holds 16 MT rows in order
+  const int row_a = wm * (MT * 32) + (r32 >> 2 & 1) * (16 * MT) + (r32 >> 3) * 4 + (r32 & 3), row_b = wn * (NT * 32) + r32;
+  const int sa = swz_a(row_a), sb = swz_b(row_b);       // rows 16 i and 32 j further on are swapped alike
+
+  // Operands of half a slice (two MFMA steps) wait in registers while the half before is multiplied.
+  struct Half {
+    uintx4 a[2][MT], b[2][NT];
+  };
+  auto fetch = [&](Half &f, const char *s, int half) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) fb[j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 16 * j) * 128 + cb * 16);
+    for (int u = 0; u < 2; ++u) {
+      const int c = half * 4 + u * 2 + h;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) fa[i] = *reinterpret_cast<const uintx4 *>(s + (row_a + 4 * i) * 128 + ca * 16);
+      for (int j = 0; j < NT; ++j) f.b[u][j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 32 * j) * 128 + (c ^ sb) * 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) f.a[u][i] = *reinterpret_cast<const uintx4 *>(s + (row_a + 16 * i) * 128 + (c ^ sa) * 16);
+    }
+  };
+  auto multiply = [&](const Half &f) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mma<E>(fa[i], fb[j], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);      // or the next half's operands are read now, and registers spill
-    }
+        for (int j = 0; j < NT; ++j) acc[i][j] = mma<E>(f.a[u][i], f.b[u][j], acc[i][j]);
   };
-
+  // This wave's loads into LDS have landed, then everybody's.  The wait is written out: a barrier alone does not wait for them.
+  auto arrived = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The first half of a slice is in registers.  Behind the barrier the slice after it has arrived, and this one's place is free.
+  Half f0, f1;
+  auto step = [&](const char *now, const char *next, char *free, bool more, bool ahead) {
+    fetch(f1, now, 1);
+    multiply(f0);
+    // the reads first, one between two products, so that they are back before the barrier
+#pragma unroll
+    for (int i = 0; i < 2 * (MT + NT); ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    arrived();
+    if (ahead) load(free);
+    if (more) fetch(f0, next, 0);
+    multiply(f1);
+#pragma unroll
+    for (int i = 0; i < 2 * (MT + NT); ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
   if (first < last) {
     load(s0);
-    for (int k = first; k < last; k += 2) {
-      __syncthreads();
-      if (k + 1 < last) load(s1);
-      compute(s0);
-      if (k + 1 >= last) break;
-      __syncthreads();
-      if (k + 2 < last) load(s0);
-      compute(s1);
+    if (first + 1 < last) load(s1);
+    arrived();
+    fetch(f0, s0, 0);
+    int k = first;
+    for (; k + 3 < last; k += 2) {
+      step(s0, s1, s0, true, true);
+      step(s1, s0, s1, true, true);
+    }
+    for (; k < last; k += 2) {
+      step(s0, s1, s0, k + 1 < last, k + 2 < last);
+      if (k + 1 < last) step(s1, s0, s1, k + 2 < last, k + 3 < last);
     }
   }
 
-  // a lane's results: n = n1 + 16 j, m = m1 .. m1 + 4 MT - 1 (tile i: four of them)
-  const int m1 = m0 + wm * (MT * 16) + q * (4 * MT), n1 = n0 + wn * (NT * 16) + r16;
+  // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
+  const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
   if constexpr (EPI == kStats) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 16 * j;
+      const int n = n1 + 32 * j;
       const bool in = n < G.b.rows;
       const int at = in ? G.label[n] - G.v0 - m1 : -1;
       float top = -__builtin_inff(), sum = 0.f, mine = 0.f;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (m1 + 4 * i + e >= G.a.rows) acc[i][j][e] = -__builtin_inff();
-          top = fmaxf(top, acc[i][j][e]);
-          if (at == 4 * i + e) mine = acc[i][j][e];
+        for (int e = 0; e < 16; ++e) {
+          float x = acc[i][j][e];
+          if (at == 16 * i + e) mine = x;
+          x = m1 + 16 * i + e < G.a.rows ? x : -__builtin_inff();
+          acc[i][j][e] = x;
+          top = fmaxf(top, x);
         }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float ref = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __expf(acc[i][j][e] - ref);
-      sum += __shfl_xor(sum, 16, 64);
+        for (int e = 0; e < 16; ++e) sum += __expf(acc[i][j][e] - ref);
       sum += __shfl_xor(sum, 32, 64);
       if (in) {
-        if (at >= 0 && at < 4 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
-        if (q == 0) {
+        if (at >= 0 && at < 16 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
+        if (h == 0) {
           float *p = G.part + ((long long)n * G.parts + G.part0 + m0 / TM * WM + wm) * 2;
           p[0] = top, p[1] = sum;
         }
@@ -185,65 +226,60 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   } else if constexpr (EPI == kDz) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 16 * j;
+      const int n = n1 + 32 * j;
       const bool in = n < G.b.rows;
       const int label = in ? G.label[n] : -1, at = label - G.v0 - m1;
       const float lse = in ? G.lse[n] : 0.f, g = in ? G.g[n] : 0.f;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        float x[4];
+      for (int i = 0; i < 2 * MT; ++i) {
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[e] = label >= 0 && m1 + 4 * i + e < G.a.rows ? g * (__expf(acc[i][j][e] - lse) - (at == 4 * i + e ? 1.f : 0.f)) : 0.f;
+        for (int e = 0; e < 8; ++e)
+          x[e] = label >= 0 && m1 + 8 * i + e < G.a.rows ? g * (__expf(acc[i / 2][j][i % 2 * 8 + e] - lse) - (at == 8 * i + e ? 1.f : 0.f)) : 0.f;
 #pragma unroll
         for (int k = 0; k < PLANES; ++k) {
-          E y[4];
+          E y[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
-          if (in && m1 + 4 * i < G.m_pad) {
-            uintx2 w;
-            __builtin_memcpy(&w, y, 8);
-            *reinterpret_cast<uintx2 *>(G.dz + k * G.dz_plane + n * G.dz_ld + (m1 + 4 * i) * 2) = w;
+          for (int e = 0; e < 8; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
+          if (in && m1 + 8 * i < G.m_pad) {
+            uintx4 w;
+            __builtin_memcpy(&w, y, 16);
+            *reinterpret_cast<uintx4 *>(G.dz + k * G.dz_plane + n * G.dz_ld + (m1 + 8 * i) * 2) = w;
           }
           if (n < G.n_pad) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (m1 + 4 * i + e < G.a.rows) *reinterpret_cast<E *>(G.dzt + k * G.dzt_plane + (m1 + 4 * i + e) * G.dzt_ld + n * 2) = y[e];
+            for (int e = 0; e < 8; ++e)
+              if (m1 + 8 * i + e < G.a.rows) *reinterpret_cast<E *>(G.dzt + k * G.dzt_plane + (m1 + 8 * i + e) * G.dzt_ld + n * 2) = y[e];
           }
         }
       }
     }
-  } else if constexpr (EPI == kOut) {
-    const float scale = *G.scale;
+  } else {
+    float scale = 1.f;
+    if (EPI == kOut) scale = *G.scale;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 16 * j;
+      const int n = n1 + 32 * j;
       if (n >= G.b.rows) continue;
-      OutT *p = static_cast<OutT *>(G.out) + n * G.out_ld + m1;
 #pragma unroll
-      for (int i = 0; i < MT; i += 2) {
+      for (int i = 0; i < 2 * MT; ++i) {
+        const int m = m1 + 8 * i, left = G.a.rows - m;
+        if (left <= 0) break;
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = acc[i + e / 4][j][e % 4] * scale;
-        store_n<OutT, 8>(p + 4 * i, G.a.rows - m1 - 4 * i, x);
-      }
-    }
-  } else {
+        for (int e = 0; e < 8; ++e) x[e] = acc[i / 2][j][i % 2 * 8 + e] * scale;
+        if constexpr (EPI == kOut) {
+          store_n<OutT, 8>(static_cast<OutT *>(G.out) + n * G.out_ld + m, left, x);
+        } else {
+          float *p = G.sum + ((long long)blockIdx.y * G.b.rows + n) * G.out_ld + m;
+          if (G.add) {
+            float y[8];
+            load_n<float, 8>(p, left, y);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 16 * j;
-      if (n >= G.b.rows) continue;
-      float *p = G.sum + ((long long)blockIdx.y * G.b.rows + n) * G.out_ld + m1;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        if (m1 + 4 * i >= G.a.rows) break;
-        float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]}, y[4];
-        if (G.add) {
-          load_n<float, 4>(p + 4 * i, G.a.rows - m1 - 4 * i, y);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] += y[e];
+            for (int e = 0; e < 8; ++e) x[e] += y[e];
+          }
+          store_n<float, 8>(p, left, x);
         }
-        store_n<float, 4>(p + 4 * i, G.a.rows - m1 - 4 * i, x);
       }
     }
   }

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int 
 struct Shape {
   int tm, tn, wm, wn;
 };
-constexpr Shape kShapes[3] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {128, 64, 4, 1}};
+constexpr Shape kShapes[3] = {{256, 256, 2, 2}, {128, 128, 2, 2}, {128, 64, 4, 1}};
 
 inline int pick_shape(long long m, long long n, int splits) {
   if (n <= 64) return 2;
@@ -246,7 +246,7 @@ hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
   G.tiles_m = (int)cdiv64(G.a.rows, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
   const dim3 grid(G.tiles_m * G.tiles_n, G.splits);
   switch (shape) {
-    case 0: gemm_kernel<E, OutT, 256, 256, 2, 4, EPI, PLANES><<<grid, 512, 0, st>>>(G); break;
+    case 0: gemm_kernel<E, OutT, 256, 256, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
     case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
     default: gemm_kernel<E, OutT, 128, 64, 4, 1, EPI, PLANES><<<grid, 256, 0, st>>>(G);
   }
