@@ -28,26 +28,31 @@ struct FwdArgs {
   float scale;
 };
 
-// A group of TPR threads takes a row, eight elements a thread at a time.
-template <typename T, typename IT, int TPR, bool FAR>
+// A group of TPR threads takes ROWS rows, eight elements a thread at a time: their tokens, then their reads, are on their way together.
+template <typename T, typename IT, int TPR, int ROWS, bool FAR>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(FwdArgs A) {
-  constexpr int RPB = 256 / TPR;
-  const long long row = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
+  const long long row = ((long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR) * ROWS;
   if (row >= A.rows) return;
-  const IT v = static_cast<const IT *>(A.tokens)[row];
-  const bool live = v >= 0 && v < A.v;
-  const T *w = static_cast<const T *>(A.w) + (live ? (long long)v : 0) * A.ws;
+  bool live[ROWS], in[ROWS];
+  const T *w[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    in[r] = row + r < A.rows;
+    const IT v = in[r] ? static_cast<const IT *>(A.tokens)[row + r] : IT(-1);
+    live[r] = v >= 0 && v < A.v;
+    w[r] = static_cast<const T *>(A.w) + (live[r] ? (long long)v : 0) * A.ws;
+  }
   T *y = static_cast<T *>(A.y) + row * A.ys;
   for (int c = threadIdx.x % TPR * 8; c < A.d; c += TPR * 8) {
-    float x[8];
-    load_n<T, 8>(w + c, live ? A.d - c : 0, x);
+    float x[ROWS][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= A.scale;
-    if (!live) {
+    for (int r = 0; r < ROWS; ++r) load_n<T, 8>(w[r] + c, live[r] ? A.d - c : 0, x[r]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[r][k] = live[r] ? x[r][k] * A.scale : 0.f;
+      store_n<T, 8, FAR>(y + r * A.ys + c, in[r] ? A.d - c : 0, x[r]);
     }
-    store_n<T, 8, FAR>(y + c, A.d - c, x);
   }
 }
 
@@ -56,7 +61,7 @@ struct Plan {
   int groups, bins;          // of the sort
   int piece;                 // rows a piece of the list has
   long long pieces;
-  size_t order, keys, counts, live, partial, bytes;   // offsets
+  size_t order, keys, ranges, live, partial, bytes;   // offsets
 };
 
 inline Plan make_plan(long long rows, int vocab, int d) {
@@ -70,44 +75,68 @@ inline Plan make_plan(long long rows, int vocab, int d) {
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   p.order = 0;
   p.keys = p.order + up(rows * 4);
-  p.counts = p.keys + up(rows * 4);
-  p.live = p.counts + up((size_t)p.groups * p.bins * 4);
+  p.ranges = p.keys + up(rows * 4);
+  p.live = p.ranges + up((size_t)p.groups * p.bins * 8);
   p.partial = p.live + 256;
   p.bytes = p.partial + up((size_t)p.pieces * 2 * d * 4) + 256;
   return p;
 }
 
+struct Range {
+  int start, count;          // of a token in the list
+};
+
 struct SortArgs {
   const void *tokens;
-  int *order, *keys, *counts, *live;
+  int *order, *keys, *live;
+  Range *ranges;
   int rows, v, groups, bins;
 };
 
 // The lists of 16 waves, each of which reads a sixteenth of the tokens, follow each other within a token: rows stay in order.
+// A wave keeps its rows in LDS as it counts them; one that finds more than kQueue reads the tokens again.
+constexpr int kQueue = 1024;
+
 template <typename IT>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {
   __shared__ int at[kSortWaves][kMostBins];   // first counts, then where the wave's next row of this token goes
+  __shared__ int rows[kSortWaves][kQueue];
+  __shared__ unsigned short bins[kSortWaves][kQueue];
   __shared__ int wave_sum[kSortWaves], before_sum[kSortWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, mine = blockIdx.x, mask = A.groups - 1;
   const int shift = 31 - __builtin_clz(A.groups);
+  const unsigned long long below = (1ull << lane) - 1;
   const IT *tokens = static_cast<const IT *>(A.tokens);
-  for (int i = tid; i < kSortWaves * kMostBins; i += kSortThreads) (&at[0][0])[i] = 0;
-  __syncthreads();
   const int per = (A.rows + kSortThreads - 1) / kSortThreads * 64;
   const long long lo = (long long)wave * per;
   const int n = lo < A.rows ? (A.rows - lo < per ? (int)(A.rows - lo) : per) : 0;
-  constexpr int U = 8;
-  int before = 0;
-  for (int i = 0; i < n; i += 64 * U) {
-    IT w[U];
+  constexpr int U = 16;
+  auto read = [&](int i, IT (&w)[U]) {
 #pragma unroll
     for (int k = 0; k < U; ++k) w[k] = i + k * 64 + lane < n ? tokens[lo + i + k * 64 + lane] : IT(-1);
+  };
+  IT w[U], ahead[U];
+  read(0, ahead);
+  for (int i = lane; i < kMostBins; i += 64) at[wave][i] = 0;
+  int before = 0, found = 0;
+  for (int i = 0; i < n; i += 64 * U) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) w[k] = ahead[k];
+    if (i + 64 * U < n) read(i + 64 * U, ahead);
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const bool live = w[k] >= 0 && w[k] < A.v;
       const int t = live ? (int)w[k] : 0, g = t & mask;
+      const bool own = live && g == mine;
       before += live && g < mine;
-      if (live && g == mine) atomicAdd(&at[wave][t >> shift], 1);
+      const unsigned long long all = __ballot(own);
+      if (!all) continue;
+      if (own) {
+        atomicAdd(&at[wave][t >> shift], 1);
+        const int to = found + __popcll(all & below);
+        if (to < kQueue) rows[wave][to] = (int)(lo + i + k * 64 + lane), bins[wave][to] = (unsigned short)(t >> shift);
+      }
+      found += __popcll(all);
     }
   }
 #pragma unroll
@@ -116,10 +145,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {
   __syncthreads();
   // a thread's bin: rows in all waves, and where they start
   int total = 0;
-  if (tid < A.bins) {
+  if (tid < A.bins)
     for (int k = 0; k < kSortWaves; ++k) total += at[k][tid];
-    A.counts[mine * A.bins + tid] = total;
-  }
   int scan = total;
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
@@ -130,105 +157,161 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {
   __syncthreads();
   int first = scan - total;
   for (int k = 0; k < kSortWaves; ++k) first += before_sum[k] + (k < wave ? wave_sum[k] : 0);
-  if (tid < A.bins)
+  if (tid < A.bins) {
+    A.ranges[mine * A.bins + tid] = Range{first, total};
     for (int k = 0; k < kSortWaves; ++k) {
       const int x = at[k][tid];
       at[k][tid] = first;
       first += x;
     }
+  }
   if (mine == A.groups - 1 && tid == kSortThreads - 1) *A.live = first;   // bins behind the last are empty: the end of all
   __syncthreads();
+  // Lanes with the same bin find each other and take their places in the order of the lanes: bin by bin where there are few, which is
+  // how frequent tokens come, otherwise bit by bit.
+  const int bits = A.bins > 1 ? 32 - __builtin_clz(A.bins - 1) : 0;
+  auto place = [&](bool own, int bin, int row) {
+    const unsigned long long all = __ballot(own);
+    unsigned long long todo = all, same = 0;
+#pragma unroll 1
+    for (int k = 0; k < 4 && todo; ++k) {
+      const int b = __builtin_amdgcn_readlane(bin, __builtin_ctzll(todo));
+      const unsigned long long these = __ballot(own && bin == b);
+      if (bin == b) same = these;
+      todo &= ~these;
+    }
+    if (todo) {
+      same = all;
+#pragma unroll 1
+      for (int b = 0; b < bits; ++b) {
+        const unsigned long long ones = __ballot(bin >> b & 1);
+        same &= bin >> b & 1 ? ones : ~ones;
+      }
+    }
+    int to = 0;
+    if (own) to = at[wave][bin] + __popcll(same & below);
+    __builtin_amdgcn_wave_barrier();             // all lanes have read their place
+    if (own) {
+      if (!(same & below)) at[wave][bin] += __popcll(same);
+      A.order[to] = row;
+      A.keys[to] = bin << shift | mine;
+    }
+    __builtin_amdgcn_wave_barrier();
+  };
+  if (found <= kQueue) {
+    for (int i = 0; i < found; i += 64) {
+      const bool own = i + lane < found;
+      place(own, own ? bins[wave][i + lane] : 0, own ? rows[wave][i + lane] : 0);
+    }
+    return;
+  }
   for (int i = 0; i < n; i += 64 * U) {
-    IT w[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) w[k] = i + k * 64 + lane < n ? tokens[lo + i + k * 64 + lane] : IT(-1);
+    read(i, w);
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const bool live = w[k] >= 0 && w[k] < A.v;
-      const int t = live ? (int)w[k] : 0, bin = t >> shift;
+      const int t = live ? (int)w[k] : 0;
       const bool own = live && (t & mask) == mine;
-      unsigned long long todo = __ballot(own);
-      while (todo) {                             // one token after the other; mostly there is one
-        const int leader = __builtin_ctzll(todo), b = __shfl(bin, leader, 64);
-        const unsigned long long same = __ballot(own && bin == b);
-        if (own && bin == b) {
-          const int to = at[wave][b] + __popcll(same & ((1ull << lane) - 1));
-          A.order[to] = (int)(lo + i + k * 64 + lane);
-          A.keys[to] = t;
-        }
-        __builtin_amdgcn_wave_barrier();         // all lanes have read the place
-        if (lane == leader) at[wave][b] += __popcll(same);
-        __builtin_amdgcn_wave_barrier();
-        todo &= ~same;
-      }
+      if (__ballot(own)) place(own, t >> shift, (int)(lo + i + k * 64 + lane));
     }
   }
 }
 
 struct SumArgs {
-  const int *order, *keys, *counts, *live;
+  const int *order, *keys, *live;
+  const Range *ranges;
   const void *dy;
   void *dw;
   float *partial;
-  long long dys, dws, sum_blocks;
+  long long rows, dys, dws, sum_blocks;
   int v, d, groups, bins, piece, accumulate;
   float scale;
 };
 
-template <typename T>
+template <typename T, bool FAR>
 __device__ __forceinline__ void put_row(const SumArgs &A, int key, int c, const float (&acc)[8]) {
   T *p = static_cast<T *>(A.dw) + key * A.dws + c;
   float x[8] = {};
-  if (A.accumulate) load_n<T, 8>(p, A.d - c, x);
+  if (A.accumulate) load_n<T, 8, FAR>(p, A.d - c, x);
 #pragma unroll
   for (int k = 0; k < 8; ++k) x[k] = A.accumulate ? x[k] + acc[k] * A.scale : acc[k] * A.scale;
-  store_n<T, 8>(p, A.d - c, x);
+  store_n<T, 8, FAR>(p, A.d - c, x);
 }
 
 constexpr int kZeroRows = 16;        // rows of the table that a workgroup looks after for zeros
 
-template <typename T, int TPR>
+__device__ __forceinline__ Range range_of(const SumArgs &A, int key) {
+  const int shift = 31 - __builtin_clz(A.groups);
+  return A.ranges[(key & (A.groups - 1)) * A.bins + (key >> shift)];
+}
+
+// A piece takes the tokens that begin in it, to their ends: up to another piece's length behind its own.  Tokens with more rows than a
+// piece are cut where the pieces are, and leave partial sums: slot 0 of a piece is the token that began before it, slot 1 the one that goes on.
+template <typename T, int TPR, bool FAR>
 __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
   const int sub = threadIdx.x / TPR, c = (blockIdx.y * TPR + threadIdx.x % TPR) * 8;
   if (blockIdx.x >= A.sum_blocks) {
-    if (c >= A.d) return;
-    const int shift = 31 - __builtin_clz(A.groups);
+    __shared__ int counts[kZeroRows];
     const int v0 = (int)(blockIdx.x - A.sum_blocks) * kZeroRows;
-    for (int k = sub; k < kZeroRows && v0 + k < A.v; k += 256 / TPR) {
-      const int v = v0 + k;
-      if (A.counts[(v & (A.groups - 1)) * A.bins + (v >> shift)]) continue;
+    if (threadIdx.x < kZeroRows) counts[threadIdx.x] = v0 + (int)threadIdx.x < A.v ? range_of(A, v0 + threadIdx.x).count : 1;
+    __syncthreads();
+    if (c >= A.d) return;
+    for (int k = sub; k < kZeroRows; k += 256 / TPR) {
+      if (counts[k]) continue;
       const float zero[8] = {};
-      store_n<T, 8>(static_cast<T *>(A.dw) + v * A.dws + c, A.d - c, zero);
+      store_n<T, 8, FAR>(static_cast<T *>(A.dw) + (v0 + k) * A.dws + c, A.d - c, zero);
     }
     return;
   }
   const int live = *A.live, piece = A.piece;
   const long long p = (long long)blockIdx.x * (256 / TPR) + sub, first = p * piece;
   if (first >= live || c >= A.d) return;
-  const int n = live - first < piece ? (int)(live - first) : piece;
   const int *keys = A.keys + first, *order = A.order + first;
-  const bool from_before = first > 0 && keys[-1] == keys[0], goes_on = first + n < live && keys[n] == keys[n - 1];
+  const int left = live - first <= piece ? (int)(live - first) : piece + 1;
+  int n = left < piece ? left : piece, i = 0;
+  bool from_before = first > 0 && keys[-1] == keys[0], goes_on = n < left && keys[n] == keys[n - 1];
+  if (from_before) {
+    const Range r = range_of(A, keys[0]);
+    if (r.count <= piece) {          // the piece before takes it
+      i = (int)(r.start + r.count - first);
+      if (i >= n) return;
+      from_before = false;
+    }
+  }
+  if (goes_on) {
+    const Range r = range_of(A, keys[n - 1]);
+    if (r.count <= piece) n = (int)(r.start + r.count - first), goes_on = false;
+  }
   float acc[8] = {};
   bool head = true;                  // the sum is of the piece's first token
   constexpr int U = 8;
   const T *dy = static_cast<const T *>(A.dy);
-  for (int i = 0; i < n; i += U) {
-    float x[U][8];
+  for (; i < n; i += U) {
+    typename VecOf<T, 8>::type x[U];
+    int key[U + 1];
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const bool in = i + k < n;
-      load_n<T, 8>(dy + (in ? order[i + k] : 0) * A.dys + c, in ? A.d - c : 0, x[k]);
+    for (int k = 0; k <= U; ++k) key[k] = keys[i + k < n ? i + k : n - 1];
+    if (c + 8 <= A.d) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) x[k] = far_load<FAR, T, 8>(dy + order[i + k < n ? i + k : n - 1] * A.dys + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const T *row = dy + order[i + k < n ? i + k : n - 1] * A.dys + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[k][e] = c + e < A.d ? row[e] : T(0.f);
+      }
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (i + k >= n) break;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += x[k][e];
+      for (int e = 0; e < 8; ++e) acc[e] += static_cast<float>(x[k][e]);
       const bool last = i + k == n - 1;
-      if (!last && keys[i + k + 1] == keys[i + k]) continue;
+      if (!last && key[k + 1] == key[k]) continue;
       const bool open_front = head && from_before, open_back = last && goes_on;
       if (open_front || open_back) store_n<float, 8>(A.partial + (p * 2 + (open_front ? 0 : 1)) * A.d + c, A.d - c, acc);
-      else put_row<T>(A, keys[i + k], c, acc);
+      else put_row<T, FAR>(A, key[k], c, acc);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
       head = false;
@@ -236,41 +319,52 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
   }
 }
 
-constexpr int kJoinPieces = 16;      // pieces a workgroup looks at for tokens that go on
+constexpr int kJoinPieces = 4;       // pieces a workgroup looks at for tokens that go on
+constexpr int kJoinWaves = 8;
 
+// A wave adds every eighth partial sum of a token, then the eight are added in order.
 template <typename T>
-__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs A, long long pieces) {
-  __shared__ float part[4][64][8];
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs A, long long pieces) {
+  __shared__ float part[kJoinWaves][64][9];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8;
   const int live = *A.live, piece = A.piece;
-  const int shift = 31 - __builtin_clz(A.groups);
-  for (long long p = (long long)blockIdx.x * kJoinPieces; p < ((long long)blockIdx.x + 1) * kJoinPieces; ++p) {
-    const long long first = p * piece, next = first + piece;
-    if (p >= pieces || next >= live) return;
-    const int key = A.keys[next - 1];
-    if (A.keys[next] != key) continue;
-    int back = 1;                    // rows of this token in this piece
-    while (back < piece && A.keys[next - back - 1] == key) ++back;
-    if (back == piece && first > 0 && A.keys[first - 1] == key) continue;   // it began earlier
-    const int count = A.counts[(key & (A.groups - 1)) * A.bins + (key >> shift)];
-    const long long last = (next - back + count - 1) / piece;               // the piece that it ends in
+  // lane k looks at piece k: does a long token begin in it and go on?
+  const long long mine = (long long)blockIdx.x * kJoinPieces + lane, end = (mine + 1) * piece;
+  int key = 0;
+  Range r{0, 0};
+  if (lane < kJoinPieces && mine < pieces && end < live) key = A.keys[end - 1], r = range_of(A, key);
+  const bool head = r.count > piece && r.start >= end - piece && r.start + (long long)r.count > end;
+  unsigned long long heads = __ballot(head);
+  while (heads) {
+    const int k = __builtin_ctzll(heads);
+    heads &= heads - 1;
+    const int v = __shfl(key, k, 64), from = __shfl(r.start, k, 64);
+    const long long p = (long long)blockIdx.x * kJoinPieces + k, last = ((long long)from + __shfl(r.count, k, 64) - 1) / piece;   // the piece that it ends in
     float acc[8] = {};
-    if (c < A.d)
-      for (long long k = p + wave; k <= last; k += 4) {
-        float x[8];
-        load_n<float, 8>(A.partial + (k * 2 + (k == p ? 1 : 0)) * A.d + c, A.d - c, x);
+    if (c < A.d) {
+      constexpr int U = 4;
+      for (long long q = p + wave; q <= last; q += kJoinWaves * U) {
+        float x[U][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += x[e];
+        for (int u = 0; u < U; ++u) {
+          const long long r = q + u * kJoinWaves;
+          load_n<float, 8>(A.partial + (r * 2 + (r == p ? 1 : 0)) * A.d + c, r <= last ? A.d - c : 0, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
       }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) part[wave][lane][e] = acc[e];
     __syncthreads();
     if (wave == 0 && c < A.d) {
 #pragma unroll
-      for (int k = 1; k < 4; ++k)
+      for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += part[k][lane][e];
-      put_row<T>(A, key, c, acc);
+        for (int e = 0; e < 8; ++e) acc[e] += part[w][lane][e];
+      put_row<T, false>(A, v, c, acc);
     }
     __syncthreads();
   }
@@ -284,13 +378,16 @@ inline int row_threads(int d) {
 
 template <typename T, typename IT>
 hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
-  const bool far = (double)A.rows * A.d * sizeof(T) > kLastLevelCache;
   const int tpr = row_threads(A.d);
-  const unsigned grid = (unsigned)cdiv64(A.rows, 256 / tpr);
+  const int groups = 256 / tpr;
+  const bool many = cdiv64(A.rows, groups) >= 8192;      // four rows a group still fill the chip
+  const bool far = many && (double)A.rows * A.d * sizeof(T) > kLastLevelCache;
+  const unsigned grid = (unsigned)cdiv64(A.rows, groups * (many ? 4 : 1));
 #define FWD(N)                                                                      \
   case N:                                                                           \
-    if (far) embed_fwd_kernel<T, IT, N, true><<<grid, 256, 0, st>>>(A);             \
-    else embed_fwd_kernel<T, IT, N, false><<<grid, 256, 0, st>>>(A);                \
+    if (far) embed_fwd_kernel<T, IT, N, 4, true><<<grid, 256, 0, st>>>(A);          \
+    else if (many) embed_fwd_kernel<T, IT, N, 4, false><<<grid, 256, 0, st>>>(A);   \
+    else embed_fwd_kernel<T, IT, N, 1, false><<<grid, 256, 0, st>>>(A);             \
     break;
   switch (tpr) { FWD(8) FWD(16) FWD(32) FWD(64) FWD(128) FWD(256) }
 #undef FWD
@@ -303,12 +400,16 @@ hipError_t launch_sum(SumArgs A, const Plan &p, hipStream_t st) {
   A.sum_blocks = cdiv64(p.pieces, 256 / tpr);
   const long long zero_blocks = A.accumulate ? 0 : cdiv64(A.v, kZeroRows);
   const dim3 grid((unsigned)(A.sum_blocks + zero_blocks), (A.d + tpr * 8 - 1) / (tpr * 8));
-#define SUM(N) \
-  case N: embed_sum_kernel<T, N><<<grid, 256, 0, st>>>(A); break;
+  const bool far = ((double)A.rows + (A.accumulate ? 0 : A.v)) * A.d * sizeof(T) > kLastLevelCache;
+#define SUM(N)                                                          \
+  case N:                                                               \
+    if (far) embed_sum_kernel<T, N, true><<<grid, 256, 0, st>>>(A);     \
+    else embed_sum_kernel<T, N, false><<<grid, 256, 0, st>>>(A);        \
+    break;
   switch (tpr) { SUM(8) SUM(16) SUM(32) SUM(64) SUM(128) SUM(256) }
 #undef SUM
   if (const hipError_t e = hipGetLastError()) return e;
-  if (p.pieces > 1) embed_join_kernel<T><<<dim3((unsigned)cdiv64(p.pieces, kJoinPieces), (A.d + 511) / 512), 256, 0, st>>>(A, p.pieces);
+  if (p.pieces > 1) embed_join_kernel<T><<<dim3((unsigned)cdiv64(p.pieces, kJoinPieces), (A.d + 511) / 512), 64 * kJoinWaves, 0, st>>>(A, p.pieces);
   return hipGetLastError();
 }
 
@@ -370,14 +471,14 @@ pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *q, void *hip_stream)
   if (q->workspace_bytes < p.bytes) return set_error(PBKD_ENOMEM, "embed: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes, p.bytes);
   if (q->rows == 0 && q->accumulate) return PBKD_OK;
   char *ws = static_cast<char *>(q->workspace_dev);
-  int *order = reinterpret_cast<int *>(ws + p.order), *keys = reinterpret_cast<int *>(ws + p.keys), *counts = reinterpret_cast<int *>(ws + p.counts),
-      *live = reinterpret_cast<int *>(ws + p.live);
+  int *order = reinterpret_cast<int *>(ws + p.order), *keys = reinterpret_cast<int *>(ws + p.keys), *live = reinterpret_cast<int *>(ws + p.live);
+  Range *ranges = reinterpret_cast<Range *>(ws + p.ranges);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const SortArgs S{q->tokens_dev, order, keys, counts, live, (int)q->rows, q->vocab, p.groups, p.bins};
+  const SortArgs S{q->tokens_dev, order, keys, live, ranges, (int)q->rows, q->vocab, p.groups, p.bins};
   if (q->index_dtype == PBKD_I64) embed_sort_kernel<long long><<<p.groups, kSortThreads, 0, st>>>(S);
   else embed_sort_kernel<int><<<p.groups, kSortThreads, 0, st>>>(S);
   SEQ_HIPCHK(hipGetLastError());
-  const SumArgs A{order, keys, counts, live, q->dy_dev, q->dweight_dev, reinterpret_cast<float *>(ws + p.partial), q->dy_stride, q->dweight_stride, 0,
+  const SumArgs A{order, keys, live, ranges, q->dy_dev, q->dweight_dev, reinterpret_cast<float *>(ws + p.partial), q->rows, q->dy_stride, q->dweight_stride, 0,
                   q->vocab, q->d, p.groups, p.bins, p.piece, q->accumulate != 0, q->scale};
   switch (q->dtype) {
     case PBKD_F32: SEQ_HIPCHK(launch_sum<float>(A, p, st)); break;

@@ -4,7 +4,7 @@
 //   loss = T^2 sum_j q_j (log q_j - z_j / T + lse),  dz_v = g T (p_v - sum of the q_j whose place is v)
 //
 // Bound by memory: a workgroup takes a row, reads it once for its maximum and sum (one pass, the sum rescaled when the maximum
-// grows) and once more for the gradient, when it comes from the caches.  The pairs wait in LDS; their places' gradients
+// grows) and once more for the gradient: the first 64 KB from LDS, where they were left, the rest from the caches.  Their places' gradients
 // are written last, each by the first pair that names the place.
 #include "seq_common.h"
 
@@ -34,64 +34,134 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
   m = top;
 }
 
-template <typename T, typename TT, typename IT, int THREADS, bool FAR>
-__global__ __launch_bounds__(THREADS) void topk_distill_kernel(Args A) {
-  constexpr int W = THREADS / 64;
+// Vectors of 16 bytes a thread works on at a time, the next ones on their way.
+constexpr int kAhead = 4;
+
+template <typename T, typename TT, typename IT, int THREADS, bool GRADIENT, bool FAR>
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill_kernel(Args A) {
+  constexpr int W = THREADS / 64, PER = kMaxTop / THREADS, N = 16 / sizeof(T), HELD = kAhead, STEP = HELD * THREADS * N;
+  typedef typename VecOf<T, N>::type Vec;
   __shared__ int place[kMaxTop];
   __shared__ float share[kMaxTop];
   __shared__ float red[4][W];
+  __shared__ Vec kept[GRADIENT ? HELD : 1][GRADIENT ? THREADS : 1];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, v = A.v, top = A.top;
   const long long row = blockIdx.x;
-  const T *z = static_cast<const T *>(A.z) + row * A.zs;
+  const T *const z = static_cast<const T *>(A.z) + row * A.zs;
   const float c = A.inv_t * kLog2e;            // logits in units of log 2, over T
 
-  // the row's maximum and sum
-  float m = -__builtin_inff(), s = 0.f;
-  for (int i = tid * 8; i < v; i += THREADS * 8) {
-    float x[8];
-    if (i + 8 <= v) load_n<T, 8>(z + i, 8, x);
-    else {
+  // the pairs are read first, then the student's logits there: dz may be z, and nothing is written before
+  const TT *t = static_cast<const TT *>(A.t) + row * top;
+  const IT *at = static_cast<const IT *>(A.at) + row * top;
+  float mine[PER], logit[PER];
+  int w[PER];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = i + k < v ? static_cast<float>(z[i + k]) : -__builtin_inff();
-    }
+  for (int k = 0; k < PER; ++k) {
+    const int j = k * THREADS + tid;
+    const IT x = j < top ? at[j] : IT(-1);
+    logit[k] = j < top ? static_cast<float>(t[j]) * A.inv_t : -__builtin_inff();
+    w[k] = x >= 0 && x < v && logit[k] > -__builtin_inff() ? static_cast<int>(x) : -1;
+  }
+
+  Vec held[HELD];
+  // the row's maximum, in the logits' own units, and its sum relative to it: a batch's maximum first, one rescaling a batch
+  float m = -__builtin_inff(), s = 0.f;
+  auto take = [&](const Vec (&raw)[HELD]) {
     float most = m;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= c, most = fmaxf(most, x[k]);
-    const float ref = most == -__builtin_inff() ? 0.f : most;
-    s *= exp2_fast(m - ref);
+    for (int k = 0; k < HELD; ++k)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s += exp2_fast(x[k] - ref);
+      for (int e = 0; e < N; ++e) most = fmaxf(most, static_cast<float>(raw[k][e]));
+    const float ref = most == -__builtin_inff() ? 0.f : most * c;
+    s *= exp2_fast(fmaf(m, c, -ref));
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum += exp2_fast(fmaf(static_cast<float>(raw[k][e]), c, -ref));
+      s += sum;
+    }
+    m = most;
+  };
+  Vec next[HELD];
+  constexpr int ONE = THREADS * N;
+  const int full = v / STEP * STEP;              // the batches that the row fills
+  auto fetch = [&](int base) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) next[k] = far_load<FAR && !GRADIENT, T, N>(z + base + k * ONE + tid * N);
+  };
+  // What is left goes one vector a thread at a time.  A thread at the row's end, or behind it, reads the row's last logits, and those that
+  // are another thread's get no weight: reads behind branches, one after the other, cost 9 us a row.
+  auto fetch_one = [&](int base) {
+    const int i = base + tid * N;
+    if (v >= N) next[0] = far_load<FAR && !GRADIENT, T, N>(z + (i + N <= v ? i : v - N));
+    else
+#pragma unroll
+      for (int e = 0; e < N; ++e) next[0][e] = z[e < v ? e : v - 1];
+  };
+  auto mask = [&](int i, float (&x)[N]) {
+    const int at = i + N <= v ? i : v >= N ? v - N : 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (at + e < i || at + e >= v) x[e] = -__builtin_inff();
+  };
+  if (full) fetch(0);
+  else fetch_one(0);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) mine[k] = w[k] >= 0 ? static_cast<float>(z[w[k]]) : 0.f;
+  for (int base = 0; base < full; base += STEP) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) held[k] = next[k];
+    if (base + STEP < full) fetch(base + STEP);
+    else if (full < v) fetch_one(full);
+    if (GRADIENT && base == 0) {
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) kept[k][tid] = held[k];
+    }
+    take(held);
+  }
+  for (int base = full; base < v; base += ONE) {
+    float x[N], most = m, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = static_cast<float>(next[0][e]);
+    if (base + ONE < v) fetch_one(base + ONE);
+    mask(base + tid * N, x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = fmaxf(most, x[e]);
+    const float ref = most == -__builtin_inff() ? 0.f : most * c;
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum += exp2_fast(fmaf(x[e], c, -ref));
+    s = s * exp2_fast(fmaf(m, c, -ref)) + sum;
     m = most;
   }
+  m *= c;
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
     const float m2 = __shfl_xor(m, k, 64), s2 = __shfl_xor(s, k, 64);
     join(m, s, m2, s2);
   }
 
-  // the pairs: which are known, and their logits' maximum
-  const TT *t = static_cast<const TT *>(A.t) + row * top;
-  const IT *at = static_cast<const IT *>(A.at) + row * top;
   float tm = -__builtin_inff();
-  for (int j = tid; j < top; j += THREADS) {
-    const IT w = at[j];
-    float x = static_cast<float>(t[j]) * A.inv_t;
-    const bool known = w >= 0 && w < v && x > -__builtin_inff();
-    place[j] = known ? static_cast<int>(w) : -1;
-    share[j] = x = known ? x : -__builtin_inff();
-    tm = fmaxf(tm, x);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (w[k] < 0) logit[k] = -__builtin_inff();
+    tm = fmaxf(tm, logit[k]);
   }
   tm = wave64_max(tm);
   if (lane == 0) red[0][wave] = m, red[1][wave] = s, red[2][wave] = tm;
   __syncthreads();
-  m = red[0][0], s = red[1][0], tm = red[2][0];
+  m = red[0][0], s = 0.f, tm = red[2][0];
 #pragma unroll
-  for (int k = 1; k < W; ++k) join(m, s, red[0][k], red[1][k]), tm = fmaxf(tm, red[2][k]);
+  for (int k = 1; k < W; ++k) m = fmaxf(m, red[0][k]), tm = fmaxf(tm, red[2][k]);
+  const float base = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+  for (int k = 0; k < W; ++k) s += red[1][k] * exp2_fast(red[0][k] - base);
   const bool some = tm > -__builtin_inff();
   const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;
   float qs = 0.f;
-  for (int j = tid; j < top; j += THREADS)
-    if (place[j] >= 0) qs += expf(share[j] - tm);
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    if (w[k] >= 0) qs += expf(logit[k] - tm);
   qs = wave64_sum(qs);
   if (lane == 0) red[3][wave] = qs;
   __syncthreads();
@@ -100,71 +170,107 @@ __global__ __launch_bounds__(THREADS) void topk_distill_kernel(Args A) {
   for (int k = 1; k < W; ++k) qs += red[3][k];
   const float log_qs = logf(qs), inv_qs = 1.f / qs;
 
-  // loss, and each pair's share.  The student's logits there are read before anything is written: dz may be z
-  constexpr int PER = kMaxTop / THREADS;
-  float mine[PER];
+  // loss, and each pair's share
   float far = 0.f;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int j = k * THREADS + tid;
-    mine[k] = 0.f;
-    if (j < top) {
-      const int w = place[j];
-      float q = 0.f;
-      if (w >= 0) {
-        const float x = share[j] - tm;
-        q = expf(x) * inv_qs;
-        const float zj = static_cast<float>(z[w]);
-        mine[k] = zj * c;
-        if (q > 0.f) far += q * (x - log_qs - zj * A.inv_t + lse);
-      }
-      share[j] = q;
+    float q = 0.f;
+    if (w[k] >= 0) {
+      const float x = logit[k] - tm;
+      q = expf(x) * inv_qs;
+      if (q > 0.f) far += q * (x - log_qs - mine[k] * A.inv_t + lse);
     }
+    if (j < top) place[j] = w[k], share[j] = q;
   }
   far = wave64_sum(far);
-  __syncthreads();
-  if (lane == 0) red[0][wave] = far;
+  if (lane == 0) red[2][wave] = far;           // its readers of before are behind the barrier of qs
   __syncthreads();
   if (tid == 0) {
-    far = red[0][0];
-    for (int k = 1; k < W; ++k) far += red[0][k];
+    far = red[2][0];
+    for (int k = 1; k < W; ++k) far += red[2][k];
     A.loss[row] = some ? far * A.temperature * A.temperature : 0.f;
   }
-  if (!A.dz) return;
+  if (!GRADIENT) return;
 
-  T *dz = static_cast<T *>(A.dz) + row * A.ds;
+  T *const dz = static_cast<T *>(A.dz) + row * A.ds;
+  if (!some) {
+    const float zero[N] = {};
+    for (int i = tid * N; i < v; i += ONE) store_n<T, N>(dz + i, v - i, zero);
+    return;
+  }
   const float g = (A.g ? A.g[row] : 1.f) * A.temperature;
   const float shift = m == -__builtin_inff() ? __builtin_nanf("") : m, scale = g / s;
-  for (int i = tid * 8; i < v; i += THREADS * 8) {
-    float x[8];
-    load_n<T, 8>(z + i, v - i, x);
+  auto give = [&](const Vec &raw, int i) {
+    float x[N];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = some ? exp2_fast(x[k] * c - shift) * scale : 0.f;
-    store_n<T, 8, FAR>(dz + i, v - i, x);
+    for (int e = 0; e < N; ++e) x[e] = exp2_fast(fmaf(static_cast<float>(raw[e]), c, -shift)) * scale;
+    store_n<T, N, FAR>(dz + i, N, x);
+  };
+  if (STEP < full) fetch(STEP);
+  else if (full < v) fetch_one(full);
+  if (full) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) give(kept[k][tid], k * ONE + tid * N);
+  }
+  for (int base = STEP; base < full; base += STEP) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) held[k] = next[k];
+    if (base + STEP < full) fetch(base + STEP);
+    else if (full < v) fetch_one(full);
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) give(held[k], base + k * ONE + tid * N);
+  }
+  for (int base = full; base < v; base += ONE) {
+    const int i = base + tid * N;
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = exp2_fast(fmaf(static_cast<float>(next[0][e]), c, -shift)) * scale;
+    if (base + ONE < v) fetch_one(base + ONE);
+    if (i + N <= v) {
+      store_n<T, N, FAR>(dz + i, N, x);
+    } else {
+      const int at = v >= N ? v - N : 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (at + e >= i && at + e < v) dz[at + e] = static_cast<T>(x[e]);
+    }
   }
   __syncthreads();
-  if (!some) return;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
+    if (w[k] < 0) continue;
     const int j = k * THREADS + tid;
-    if (j >= top || place[j] < 0) continue;
-    const int w = place[j];
     float q = 0.f;
     bool first = true;
     for (int i = 0; i < top; ++i)
-      if (place[i] == w) q += share[i], first &= i >= j;
-    if (first) dz[w] = static_cast<T>(exp2_fast(mine[k] - shift) * scale - g * q);
+      if (place[i] == w[k]) q += share[i], first &= i >= j;
+    if (first) dz[w[k]] = static_cast<T>(exp2_fast(fmaf(mine[k], c, -shift)) * scale - g * q);
   }
 }
 
 template <typename T, typename TT, typename IT>
 hipError_t launch(const Args &A, hipStream_t st) {
-  const bool far = A.dz && (double)A.rows * A.v * sizeof(T) > kLastLevelCache;
   const unsigned grid = (unsigned)A.rows;
-  if (A.v <= 8192) topk_distill_kernel<T, TT, IT, 256, false><<<grid, 256, 0, st>>>(A);
-  else if (far) topk_distill_kernel<T, TT, IT, 1024, true><<<grid, 1024, 0, st>>>(A);
-  else topk_distill_kernel<T, TT, IT, 1024, false><<<grid, 1024, 0, st>>>(A);
-  return hipGetLastError();
+  const bool far = (double)A.rows * A.v * sizeof(T) > kLastLevelCache;      // of what nobody reads again
+#define DISTILL(THREADS, GRADIENT)                                                                       \
+  {                                                                                                      \
+    if (far) topk_distill_kernel<T, TT, IT, THREADS, GRADIENT, true><<<grid, THREADS, 0, st>>>(A);       \
+    else topk_distill_kernel<T, TT, IT, THREADS, GRADIENT, false><<<grid, THREADS, 0, st>>>(A);          \
+    return hipGetLastError();                                                                            \
+  }
+  if (A.v <= 8192) {
+    if (A.dz) DISTILL(256, true)
+    DISTILL(256, false)
+  }
+  if constexpr (sizeof(T) == 2)
+    if (A.v <= 16384) {
+      if (A.dz) DISTILL(512, true)
+      DISTILL(512, false)
+    }
+  if (A.dz) DISTILL(1024, true)
+  DISTILL(1024, false)
+#undef DISTILL
 }
 
 template <typename T, typename TT>

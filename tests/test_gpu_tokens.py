@@ -285,9 +285,10 @@ def _check_distill(torch, pb, z, t, at, g, temperature, dtype, what):
     loss, dz, only = torch.full((rows,), float("nan"), device="cuda"), torch.full_like(z, float("nan")), torch.full((rows,), float("nan"), device="cuda")
     pb.topk_distill(z, t, at, loss, temperature=temperature, row_weight=g, dlogits=dz)
     pb.topk_distill(z, t, at, only, temperature=temperature)
-    assert torch.equal(torch.nan_to_num(loss, 7.0), torch.nan_to_num(only, 7.0))
     r = otk.topk_distill(_np(z), _np(t), at.cpu().numpy(), temperature, None if g is None else _np(g))
+    # a call without a gradient sums a row in another order: either loss keeps the bound
     _within(_np(loss), r["loss"], r["loss_err"], "loss")
+    _within(_np(only), r["loss"], r["loss_err"], "loss alone")
     _within(_np(dz), r["dlogits"], _round(r["dlogits"], r["dlogits_err"], dtype), "dlogits")
     place, again = z.clone(), torch.empty_like(loss)
     pb.topk_distill(place, t, at, again, temperature=temperature, row_weight=g, dlogits=place)
