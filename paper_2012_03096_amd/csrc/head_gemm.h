@@ -2,14 +2,16 @@
 //
 //   C[m][n] = sum over k of A[m][k] B[n][k],   A and B with k contiguous, k a multiple of 64, 16-bit types, fp32 sums
 //
-// A workgroup forms a tile of TM x TN.  Slices of 64 k of both operands go from memory straight into LDS (two stages: one on its way while
-// the other is multiplied).  A slice's row is 128 bytes, eight pieces of 16; a row's pieces are swapped by bits of its number, so that
+// A workgroup forms a tile of TM x TN.  Slices of 64 k of both operands go from memory straight into LDS, STAGES of them at a time: one is
+// multiplied while the others are on their way.  A slice's row is 128 bytes, eight pieces of 16; a row's pieces are swapped by bits of its number, so that
 // the 16 rows that an MFMA's lanes read at once lie in different banks.  A wave's rows of A are dealt to its MFMA tiles so that
 // a lane ends with 4 * MT consecutive m of one n: results leave in wide stores, and a softmax over m needs two exchanges between lanes.
 //
 // fp32 operands come as three bf16 planes (x = x1 + x2 + x3 exactly); the product is the sum of the six plane products that matter
 // (what is left out is below 2^-24 of |a||b|), smallest first.
 #pragma once
+#include <type_traits>
+
 #include "seq_common.h"
 #include "split_bf16.h"
 
@@ -32,7 +34,8 @@ struct GemmArgs {
   int kblocks, terms;              // slices of 64 in a plane, products of planes (1 or 6)
   int tiles_m, tiles_n, splits;    // splits: parts of the sum over k, kSum only
   // kStats, kDz: m is a place in the vocabulary, n a row of h
-  const int *label;                // -1: none
+  const void *labels;              // of 32 or 64 bits; outside 0..vocab-1: none
+  int wide, vocab;
   const float *lse, *g;            // g: 0 where there is no label
   float *part, *at_label;          // kStats: [n][parts] pairs (maximum, sum)
   int parts, part0, v0;            // v0: place of the piece's first row of A
@@ -47,6 +50,12 @@ struct GemmArgs {
   int add;
 };
 
+// Row n's label, -1 for none.
+__device__ __forceinline__ int label_of(const void *labels, int wide, int vocab, long long n) {
+  const long long w = wide ? static_cast<const long long *>(labels)[n] : static_cast<const int *>(labels)[n];
+  return w >= 0 && w < vocab ? (int)w : -1;
+}
+
 template <typename E>
 __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
   if constexpr (__is_same(E, f16)) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -57,13 +66,15 @@ constexpr int kPlanesA = 0 << 0 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 2 << 10;  
 constexpr int kPlanesB = 0 << 0 | 1 << 2 | 0 << 4 | 2 << 6 | 1 << 8 | 0 << 10;
 
 // OutT: the type of kOut's result.  PLANES: of dz (3: fp32 in three bf16 terms).
-template <typename E, typename OutT, int TM, int TN, int WM, int WN, int EPI, int PLANES>
+template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 32, NT = TN / WN / 32;
   constexpr int RA = TM * 8 / THREADS, RB = TN * 8 / THREADS, ROWS = THREADS / 8;     // rounds of loads, rows a round
   static_assert(RA * THREADS == TM * 8 && RB * THREADS == TN * 8, "whole rounds");
-  __shared__ __attribute__((aligned(1024))) char s0[(TM + TN) * 128];
-  __shared__ __attribute__((aligned(1024))) char s1[(TM + TN) * 128];
+  // objects of their own: the compiler then knows that a read of one does not wait for loads into another
+  constexpr int SLICE = (TM + TN) * 128;
+  __shared__ __attribute__((aligned(1024))) char s0[SLICE], s1[SLICE], s2[STAGES > 2 ? SLICE : 16], s3[STAGES > 3 ? SLICE : 16];
+  char *const stage[4] = {s0, s1, s2, s3};
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
 
@@ -143,15 +154,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = mma<E>(f.a[u][i], f.b[u][j], acc[i][j]);
   };
-  // This wave's loads into LDS have landed, then everybody's.  The wait is written out: a barrier alone does not wait for them.
-  auto arrived = [&]() {
-    __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
-    __syncthreads();
+  // All but the last `later` slices that this wave loads have landed in LDS, and then everybody's; everybody has read what it needs of the
+  // slice before.  The waits are written out: a barrier alone does not wait for loads into LDS.
+  auto arrived = [&](auto later) {
+    constexpr int n = decltype(later)::value * (RA + RB);
+    static_assert(n < 64, "vmcnt has six bits");
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((n & 15) | 0x70 | (n >> 4) << 14);       // vmcnt(n), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
   };
   // The first half of a slice is in registers.  Behind the barrier the slice after it has arrived, and this one's place is free.
   Half f0, f1;
-  auto step = [&](const char *now, const char *next, char *free, bool more, bool ahead) {
+  auto step = [&](char *now, const char *next, bool more, bool ahead, auto later) {
     fetch(f1, now, 1);
     multiply(f0);
     // the reads first, one between two products, so that they are back before the barrier
@@ -160,9 +177,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    arrived();
-    if (ahead) load(free);
+    arrived(later);
+    if (ahead) load(now);
     if (more) fetch(f0, next, 0);
     multiply(f1);
 #pragma unroll
@@ -174,29 +190,34 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     __builtin_amdgcn_sched_barrier(0);
   };
   if (first < last) {
-    load(s0);
-    if (first + 1 < last) load(s1);
-    arrived();
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+      if (first + i < last) load(stage[i]);
+    if (first + STAGES <= last) arrived(std::integral_constant<int, STAGES - 1>());
+    else arrived(std::integral_constant<int, 0>());
     fetch(f0, s0, 0);
     int k = first;
-    for (; k + 3 < last; k += 2) {
-      step(s0, s1, s0, true, true);
-      step(s1, s0, s1, true, true);
+    for (; k + 2 * STAGES - 1 < last; k += STAGES) {
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) step(stage[i], stage[(i + 1) % STAGES], true, true, std::integral_constant<int, STAGES - 2>());
     }
-    for (; k < last; k += 2) {
-      step(s0, s1, s0, k + 1 < last, k + 2 < last);
-      if (k + 1 < last) step(s1, s0, s1, k + 2 < last, k + 3 < last);
+    for (; k < last; k += STAGES) {
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i)
+        if (k + i < last) step(stage[i], stage[(i + 1) % STAGES], k + i + 1 < last, k + i + STAGES < last, std::integral_constant<int, 0>());
     }
   }
 
   // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
   const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
   if constexpr (EPI == kStats) {
+    float *red = reinterpret_cast<float *>(s0);        // [WM][TN] pairs, once everybody is done with the slices
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int n = n1 + 32 * j;
       const bool in = n < G.b.rows;
-      const int at = in ? G.label[n] - G.v0 - m1 : -1;
+      const int at = in ? label_of(G.labels, G.wide, G.vocab, n) - G.v0 - m1 : -1;
       float top = -__builtin_inff(), sum = 0.f, mine = 0.f;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -215,20 +236,26 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum += __expf(acc[i][j][e] - ref);
       sum += __shfl_xor(sum, 32, 64);
-      if (in) {
-        if (at >= 0 && at < 16 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
-        if (h == 0) {
-          float *p = G.part + ((long long)n * G.parts + G.part0 + m0 / TM * WM + wm) * 2;
-          p[0] = top, p[1] = sum;
-        }
-      }
+      if (in && at >= 0 && at < 16 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
+      if (h == 0) red[(wm * TN + n - n0) * 2] = top, red[(wm * TN + n - n0) * 2 + 1] = sum;
+    }
+    __syncthreads();
+    for (int n = tid; n < TN && n0 + n < G.b.rows; n += THREADS) {
+      float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < WM; ++k) top = fmaxf(top, red[(k * TN + n) * 2]);
+      const float ref = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+      for (int k = 0; k < WM; ++k) sum += red[(k * TN + n) * 2 + 1] * __expf(red[(k * TN + n) * 2] - ref);
+      float *p = G.part + ((long long)(n0 + n) * G.parts + G.part0 + m0 / TM) * 2;
+      p[0] = top, p[1] = sum;
     }
   } else if constexpr (EPI == kDz) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int n = n1 + 32 * j;
       const bool in = n < G.b.rows;
-      const int label = in ? G.label[n] : -1, at = label - G.v0 - m1;
+      const int label = in ? label_of(G.labels, G.wide, G.vocab, n) : -1, at = label - G.v0 - m1;
       const float lse = in ? G.lse[n] : 0.f, g = in ? G.g[n] : 0.f;
 #pragma unroll
       for (int i = 0; i < 2 * MT; ++i) {

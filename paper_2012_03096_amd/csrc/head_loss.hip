@@ -18,7 +18,7 @@ namespace {
 using namespace head;
 
 constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
-constexpr double kPieceBytes = 512e6;        // dz of a piece, both layouts
+constexpr double kPieceBytes = 600e6;        // dz of a piece, both layouts
 
 inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
 
@@ -26,12 +26,11 @@ inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
 struct RowArgs {
   const void *labels;
   const float *g;
-  int *label;
-  float *gs, *scale;       // scale[0] = 2^-s, what results are multiplied with; scale[1] = 1
+  float *gs, *scale;       // scale: 2^-s, what results are multiplied with
   int rows, v;
 };
 
-// Labels as 32-bit numbers (-1: none), row weights times 2^s (0 where there is no label).
+// Row weights times 2^s, 0 where there is no label.
 template <typename IT>
 __global__ __launch_bounds__(1024) void head_rows_kernel(RowArgs A) {
   __shared__ float red[16];
@@ -40,13 +39,9 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(RowArgs A) {
   float top = 0.f;
   for (int i = tid; i < A.rows; i += 1024) {
     const IT w = labels[i];
-    const bool live = w >= 0 && w < A.v;
-    A.label[i] = live ? (int)w : -1;
-    const float g = live ? (A.g ? A.g[i] : 1.f) : 0.f;
-    if (A.gs) A.gs[i] = g;
+    const float g = w >= 0 && w < A.v ? (A.g ? A.g[i] : 1.f) : 0.f;
     if (fabsf(g) < __builtin_inff()) top = fmaxf(top, fabsf(g));
   }
-  if (!A.gs) return;
   top = wave64_max(top);
   if ((tid & 63) == 0) red[tid >> 6] = top;
   __syncthreads();
@@ -54,71 +49,54 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(RowArgs A) {
   int e = top > 0.f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;       // top < 2^(14 - e): dz stays below 2^15
   e = e < 100 ? e : 100;
   const float s = ldexpf(1.f, e);
-  for (int i = tid; i < A.rows; i += 1024) A.gs[i] *= s;
-  if (tid == 0) A.scale[0] = ldexpf(1.f, -e), A.scale[1] = 1.f;
+  for (int i = tid; i < A.rows; i += 1024) {
+    const IT w = labels[i];
+    A.gs[i] = w >= 0 && w < A.v ? (A.g ? A.g[i] : 1.f) * s : 0.f;
+  }
+  if (tid == 0) *A.scale = ldexpf(1.f, -e);
 }
 
 struct LayArgs {
   const void *src;
-  char *dst;
   long long stride;        // elements between the source's rows
-  long long ld, plane;     // bytes
-  const int *label;        // rows without a label become zeros; null: none do
-  int rows, cols;          // of the source
-  int fill;                // rows of the result's other dimension up to here are written: zeros behind the end
+  char *rows_dst, *cols_dst;                    // null: not wanted
+  long long rows_ld, rows_plane, cols_ld, cols_plane;    // bytes
+  const void *labels;      // rows without a label become zeros in cols_dst; null: none do
+  int wide, vocab;
+  int rows, cols, cols_fill, rows_fill;         // of the source; zeros behind the ends up to *_fill
 };
 
-template <typename T, int PLANES, typename E>
-__device__ __forceinline__ void planes_of(float x, E (&y)[PLANES]) {
-#pragma unroll
-  for (int k = 0; k < PLANES; ++k) y[k] = static_cast<E>(x), x -= static_cast<float>(y[k]);
-}
-
-// dst[row][0..fill) = src[row][..], zeros behind cols.  Eight elements a thread.
+// The two layouts that a product reads along k: rows_dst[row][..] = src[row][..] and cols_dst[col][..] = src[..][col], in planes.  Tiles of 64 x 64.
 template <typename T, typename E, int PLANES>
-__global__ __launch_bounds__(256) void head_pack_kernel(LayArgs A) {
-  const int per = A.fill / 8;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (long long)A.rows * per) return;
-  const long long row = i / per;
-  const int c = (int)(i - row * per) * 8;
-  float x[8];
-  load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c, A.cols - c, x);
-#pragma unroll
-  for (int k = 0; k < PLANES; ++k) {
-    E y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
-    uintx4 w;
-    __builtin_memcpy(&w, y, 16);
-    *reinterpret_cast<uintx4 *>(A.dst + k * A.plane + row * A.ld + c * 2) = w;
-  }
-}
-
-// dst[col][0..fill) = src[..][col], zeros behind rows.  Tiles of 64 x 64.
-template <typename T, typename E, int PLANES>
-__global__ __launch_bounds__(256) void head_transpose_kernel(LayArgs A) {
+__global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
   __shared__ E tile[PLANES][64][66];
   const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int r = k * 32 + tid / 8, c = tid % 8 * 8, row = r0 + r;
     float x[8] = {};
-    if (row < A.rows && (!A.label || A.label[row] >= 0)) load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c0 + c, A.cols - c0 - c, x);
+    if (row < A.rows) load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c0 + c, A.cols - c0 - c, x);
+    const bool live = row < A.rows && (!A.labels || label_of(A.labels, A.wide, A.vocab, row) >= 0);
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
+    for (int p = 0; p < PLANES; ++p) {
+      E y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const E y = static_cast<E>(x[e]);
-        x[e] -= static_cast<float>(y);
-        tile[p][c + e][r] = y;
+      for (int e = 0; e < 8; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
+      if (A.rows_dst && row < A.rows && c0 + c < A.cols_fill) {
+        uintx4 w;
+        __builtin_memcpy(&w, y, 16);
+        *reinterpret_cast<uintx4 *>(A.rows_dst + p * A.rows_plane + row * A.rows_ld + (c0 + c) * 2) = w;
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[p][c + e][r] = live ? y[e] : static_cast<E>(0.f);
+    }
   }
+  if (!A.cols_dst) return;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int c = k * 32 + tid / 8, r = tid % 8 * 8;
-    if (c0 + c >= A.cols || r0 + r >= A.fill) continue;
+    if (c0 + c >= A.cols || r0 + r >= A.rows_fill) continue;
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
       E y[8];
@@ -126,29 +104,37 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(LayArgs A) {
       for (int e = 0; e < 8; ++e) y[e] = tile[p][c][r + e];
       uintx4 w;
       __builtin_memcpy(&w, y, 16);
-      *reinterpret_cast<uintx4 *>(A.dst + p * A.plane + (c0 + c) * A.ld + (r0 + r) * 2) = w;
+      *reinterpret_cast<uintx4 *>(A.cols_dst + p * A.cols_plane + (c0 + c) * A.cols_ld + (r0 + r) * 2) = w;
     }
   }
 }
 
-// A wave joins a row's pairs in the order of the vocabulary's tiles.
-__global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int parts, int stride, const int *label, const float *at_label, float *lse, float *lse_out, float *loss,
-                                                       int rows) {
-  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (n >= rows) return;
+// A workgroup joins a row's pairs, in an order that only their number decides.
+__global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int parts, int stride, const void *labels, int wide, int vocab, const float *at_label, float *lse,
+                                                       float *lse_out, float *loss) {
+  __shared__ float red[2][4];
+  const int n = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
   const float *p = part + (long long)n * stride * 2;
   float top = -__builtin_inff(), sum = 0.f;
-  for (int k = lane; k < parts; k += 64) top = fmaxf(top, p[2 * k]);
-  top = wave64_max(top);
-  const float ref = top == -__builtin_inff() ? 0.f : top;
-  for (int k = lane; k < parts; k += 64) sum += p[2 * k + 1] * expf(p[2 * k] - ref);
-  sum = wave64_sum(sum);
-  if (lane == 0) {
-    const float x = top + logf(sum);
-    lse[n] = x;
-    if (lse_out) lse_out[n] = x;
-    loss[n] = label[n] >= 0 ? x - at_label[n] : 0.f;
+  for (int k = tid; k < parts; k += 256) {
+    const float m = p[2 * k], s = p[2 * k + 1], most = fmaxf(top, m), ref = most == -__builtin_inff() ? 0.f : most;
+    sum = sum * expf(top - ref) + s * expf(m - ref);
+    top = most;
   }
+  const float most = wave64_max(top), ref = most == -__builtin_inff() ? 0.f : most;
+  sum = wave64_sum(sum * expf(top - ref));
+  if ((tid & 63) == 0) red[0][wave] = most, red[1][wave] = sum;
+  __syncthreads();
+  if (tid) return;
+  const int label = label_of(labels, wide, vocab, n);
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  const float base = top == -__builtin_inff() ? 0.f : top;
+  sum = 0.f;
+  for (int k = 0; k < 4; ++k) sum += red[1][k] * expf(red[0][k] - base);
+  const float x = top + logf(sum);
+  lse[n] = x;
+  if (lse_out) lse_out[n] = x;
+  loss[n] = label >= 0 ? x - at_label[n] : 0.f;
 }
 
 // out[n][m] = scale * sum over the splits, in order
@@ -172,21 +158,34 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int 
 }
 
 // ---------------------------------------------------------------------------------------------------------- the plan
-// Tiles of a product: large ones where they fill the chip, smaller ones where they would not, narrow ones for few rows of n.
+// Tiles of a product: the largest of which there are enough for the chip's 256 compute units (with the sum over k in parts, where it
+// may be), narrow ones for few rows of n.
 struct Shape {
-  int tm, tn, wm, wn;
+  int tm, tn;
 };
-constexpr Shape kShapes[3] = {{256, 256, 2, 2}, {128, 128, 2, 2}, {128, 64, 4, 1}};
+constexpr Shape kShapes[4] = {{256, 256}, {128, 128}, {64, 64}, {128, 64}};
+constexpr int kFull = 192;           // tiles that count as enough
 
-inline int pick_shape(long long m, long long n, int splits) {
-  if (n <= 64) return 2;
-  return cdiv64(m, 256) * cdiv64(n, 256) * splits >= 192 ? 0 : 1;
+inline long long tiles_of(int shape, long long m, long long n) { return cdiv64(m, kShapes[shape].tm) * cdiv64(n, kShapes[shape].tn); }
+
+// slices: of the sum over k, 0 where it cannot be cut.  A part has eight slices at least.
+inline int splits_of(int shape, long long m, long long n, int slices) {
+  long long s = 256 / tiles_of(shape, m, n);
+  s = s > slices / 8 ? slices / 8 : s;
+  return s < 1 ? 1 : (int)s;
+}
+
+inline int pick_shape(long long m, long long n, int slices = 0) {
+  if (n <= 64 && m > 64 * kFull) return 3;
+  for (int shape = 0; shape < 2; ++shape)
+    if (tiles_of(shape, m, n) * splits_of(shape, m, n, slices) >= kFull) return shape;
+  return 2;
 }
 
 struct Plan {
   int d_pad, n_pad, piece, pieces, planes, terms, parts, first_shape, sum_shape, splits;
   bool pack_h, pack_w;
-  size_t label, gs, scale, lse, at_label, part, h, ht, w, wt, dz, dzt, sum, bytes;
+  size_t gs, scale, lse, at_label, part, h, ht, w, wt, dz, dzt, sum, bytes;
 };
 
 bool direct(const void *p, long long stride, int d, int dtype) {
@@ -199,24 +198,24 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   p.planes = dtype == PBKD_F32 ? 3 : 1, p.terms = dtype == PBKD_F32 ? 6 : 1;
   p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
   p.pack_h = pack_h, p.pack_w = pack_w;
-  double most = kPieceBytes / (4.0 * p.planes * p.n_pad);
-  if (!gradients) most = kPieceBytes / (2.0 * p.planes * p.d_pad);
-  long long piece = (long long)(most / 1024) * 1024;
+  // A piece's tiles of 256 x 256 fill whole rounds of the chip where that leaves pieces of a sensible size: 16 rows of tiles, 16 columns.
+  const double most = kPieceBytes / (gradients ? 4.0 * p.planes * p.n_pad : 2.0 * p.planes * p.d_pad);
+  long long unit = cdiv64(rows, 256);
+  unit = (unit & -unit) < 256 ? 256 / (unit & -unit) * 256 : 256;
+  if (unit > most / 2) unit = 256;
+  long long piece = (long long)(most / unit) * unit;
   piece = piece < 1024 ? 1024 : piece;
   const int n = (int)cdiv64(vocab, piece);
-  p.piece = (int)(cdiv64(cdiv64(vocab, n), 256) * 256);
+  p.piece = (int)(cdiv64(cdiv64(vocab, n), unit) * unit);
+  if (vocab <= p.piece) p.piece = (int)(cdiv64(vocab, 256) * 256);
+  if (!gradients && !pack_w) p.piece = vocab;
   p.pieces = (int)cdiv64(vocab, p.piece);
-  if (!gradients && !pack_w) p.piece = vocab, p.pieces = 1;
-  p.first_shape = pick_shape(p.piece, rows, 1);
+  p.first_shape = pick_shape(p.piece, rows);
   // dh: few tiles, a long sum
-  p.sum_shape = pick_shape(d, rows, 1);
-  const long long tiles = cdiv64(d, kShapes[p.sum_shape].tm) * cdiv64(rows, kShapes[p.sum_shape].tn);
   const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.terms;
-  p.splits = (int)(256 / (tiles > 0 ? tiles : 1));
-  p.splits = p.splits > slices / 8 ? slices / 8 : p.splits;
-  p.splits = p.splits < 1 ? 1 : p.splits;
-  const Shape &s = kShapes[p.first_shape];
-  p.parts = (int)(cdiv64(vocab, s.tm) + p.pieces) * s.wm;
+  p.sum_shape = pick_shape(d, rows, slices);
+  p.splits = splits_of(p.sum_shape, d, rows, slices);
+  p.parts = (int)cdiv64(vocab, kShapes[p.first_shape].tm) + p.pieces;
   size_t at = 0;
   auto put = [&](size_t n) {
     const size_t here = at;
@@ -224,7 +223,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
     return here;
   };
   const size_t R = rows, e = 2 * p.planes;
-  p.label = put(R * 4), p.gs = put(R * 4), p.scale = put(8), p.lse = put(R * 4), p.at_label = put(R * 4);
+  p.gs = put(R * 4), p.scale = put(4), p.lse = put(R * 4), p.at_label = put(R * 4);
   p.part = put(R * p.parts * 8);
   p.h = put(pack_h ? R * p.d_pad * e : 0);
   p.w = put(pack_w ? (size_t)p.piece * p.d_pad * e : 0);
@@ -246,9 +245,10 @@ hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
   G.tiles_m = (int)cdiv64(G.a.rows, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
   const dim3 grid(G.tiles_m * G.tiles_n, G.splits);
   switch (shape) {
-    case 0: gemm_kernel<E, OutT, 256, 256, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
-    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
-    default: gemm_kernel<E, OutT, 128, 64, 4, 1, EPI, PLANES><<<grid, 256, 0, st>>>(G);
+    case 0: gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
+    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
+    case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
+    default: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES><<<grid, 256, 0, st>>>(G);
   }
   return hipGetLastError();
 }
@@ -259,63 +259,65 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   char *ws = static_cast<char *>(q.workspace_dev);
   const int rows = (int)q.rows, V = q.vocab, d = q.d;
   const bool gradients = q.dh_dev != nullptr;
-  int *label = reinterpret_cast<int *>(ws + p.label);
   auto floats = [&](size_t at) { return reinterpret_cast<float *>(ws + at); };
-  const RowArgs R{q.labels_dev, q.row_weight_dev, label, gradients ? floats(p.gs) : nullptr, floats(p.scale), rows, V};
-  if (q.index_dtype == PBKD_I64) head_rows_kernel<long long><<<1, 1024, 0, st>>>(R);
-  else head_rows_kernel<int><<<1, 1024, 0, st>>>(R);
-
-  Operand H{static_cast<const char *>(q.h_dev), q.h_stride * es, 0, rows};
-  if (p.pack_h) {
-    LayArgs L{q.h_dev, ws + p.h, q.h_stride, p.d_pad * 2, (long long)rows * p.d_pad * 2, nullptr, rows, d, p.d_pad};
-    head_pack_kernel<T, E, PLANES><<<(unsigned)cdiv64((long long)rows * p.d_pad / 8, 256), 256, 0, st>>>(L);
-    H = Operand{L.dst, L.ld, L.plane, rows};
-  }
+  const int wide = q.index_dtype == PBKD_I64;
+  auto lay = [&](LayArgs L) {
+    L.wide = wide, L.vocab = V;
+    const int r = L.cols_dst ? L.rows_fill : L.rows, c = L.rows_dst ? L.cols_fill : L.cols;
+    head_lay_kernel<T, E, PLANES><<<dim3((r + 63) / 64, (c + 63) / 64), 256, 0, st>>>(L);
+  };
   if (gradients) {
-    LayArgs L{q.h_dev, ws + p.ht, q.h_stride, p.n_pad * 2, (long long)d * p.n_pad * 2, label, rows, d, p.n_pad};
-    head_transpose_kernel<T, E, PLANES><<<dim3(p.n_pad / 64, (d + 63) / 64), 256, 0, st>>>(L);
+    const RowArgs R{q.labels_dev, q.row_weight_dev, floats(p.gs), floats(p.scale), rows, V};
+    if (wide) head_rows_kernel<long long><<<1, 1024, 0, st>>>(R);
+    else head_rows_kernel<int><<<1, 1024, 0, st>>>(R);
   }
-  auto weight = [&](int v0, int n, bool lay) {       // rows v0 .. v0 + n of W along k
+  Operand H{static_cast<const char *>(q.h_dev), q.h_stride * es, 0, rows};
+  if (p.pack_h || gradients) {
+    LayArgs L{q.h_dev, q.h_stride, p.pack_h ? ws + p.h : nullptr, gradients ? ws + p.ht : nullptr, p.d_pad * 2, (long long)rows * p.d_pad * 2, p.n_pad * 2,
+              (long long)d * p.n_pad * 2, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
+    lay(L);
+    if (p.pack_h) H = Operand{L.rows_dst, L.rows_ld, L.rows_plane, rows};
+  }
+  // Rows v0 .. v0 + n of W along k, and (columns) along v: what of it is not there yet.  A piece that is the whole vocabulary is laid out once.
+  auto weight = [&](int v0, int n, bool rows_too, bool columns) {
     const T *w = static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride;
-    if (!p.pack_w) return Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n};
-    LayArgs L{w, ws + p.w, q.weight_stride, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, nullptr, n, d, p.d_pad};
-    if (lay) head_pack_kernel<T, E, PLANES><<<(unsigned)cdiv64((long long)n * p.d_pad / 8, 256), 256, 0, st>>>(L);
-    return Operand{L.dst, L.ld, L.plane, n};
+    LayArgs L{w, q.weight_stride, p.pack_w && rows_too ? ws + p.w : nullptr, columns ? ws + p.wt : nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, p.piece * 2,
+              (long long)d * p.piece * 2, nullptr, 0, 0, n, d, p.d_pad, up64(n)};
+    if (L.rows_dst || L.cols_dst) lay(L);
+    return p.pack_w ? Operand{ws + p.w, L.rows_ld, L.rows_plane, n} : Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n};
   };
   GemmArgs G{};
   G.b = H, G.kblocks = p.d_pad / 64, G.terms = p.terms, G.splits = 1;
-  G.label = label, G.lse = floats(p.lse), G.g = floats(p.gs), G.part = floats(p.part), G.at_label = floats(p.at_label);
+  G.labels = q.labels_dev, G.wide = wide, G.vocab = V, G.lse = floats(p.lse), G.g = floats(p.gs), G.part = floats(p.part), G.at_label = floats(p.at_label);
   G.m_pad = G.n_pad = 0;
   int parts = 0;
   const bool whole = !p.pack_w;                       // W as it lies: one product over the whole vocabulary
   for (int v0 = 0; v0 < V; v0 += whole ? V : p.piece) {
     const int n = whole || V - v0 < p.piece ? V - v0 : p.piece;
-    G.a = weight(v0, n, true), G.v0 = v0, G.parts = p.parts, G.part0 = parts;
+    G.a = weight(v0, n, true, gradients && p.pieces == 1), G.v0 = v0, G.parts = p.parts, G.part0 = parts;
     if (const hipError_t e = launch_gemm<E, T, kStats, 1>(G, p.first_shape, st)) return e;
-    parts += (int)cdiv64(n, kShapes[p.first_shape].tm) * kShapes[p.first_shape].wm;
+    parts += (int)cdiv64(n, kShapes[p.first_shape].tm);
   }
-  head_lse_kernel<<<(rows + 3) / 4, 256, 0, st>>>(floats(p.part), parts, p.parts, label, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev, rows);
+  head_lse_kernel<<<rows, 256, 0, st>>>(floats(p.part), parts, p.parts, q.labels_dev, wide, V, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev);
   if (!gradients) return hipGetLastError();
 
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = V - v0 < p.piece ? V - v0 : p.piece, n64 = up64(n);
     // dz of this piece, in both layouts
-    G.a = weight(v0, n, p.pieces > 1), G.v0 = v0;
+    G.a = weight(v0, n, p.pieces > 1, p.pieces > 1), G.v0 = v0;
     G.dz = ws + p.dz, G.dz_ld = p.piece * 2, G.dz_plane = (long long)rows * p.piece * 2;
     G.dzt = ws + p.dzt, G.dzt_ld = p.n_pad * 2, G.dzt_plane = (long long)p.piece * p.n_pad * 2;
     G.m_pad = n64, G.n_pad = p.n_pad;
     if (const hipError_t e = launch_gemm<E, T, kDz, PLANES>(G, p.first_shape, st)) return e;
-    LayArgs L{static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride, ws + p.wt, q.weight_stride, p.piece * 2, (long long)d * p.piece * 2, nullptr, n, d, n64};
-    head_transpose_kernel<T, E, PLANES><<<dim3(n64 / 64, (d + 63) / 64), 256, 0, st>>>(L);
     GemmArgs D{};
     D.terms = p.terms, D.scale = floats(p.scale);
-    D.a = Operand{ws + p.wt, L.ld, L.plane, d}, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
+    D.a = Operand{ws + p.wt, p.piece * 2, (long long)d * p.piece * 2, d}, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
     D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
     if (const hipError_t e = launch_gemm<E, T, kSum, 1>(D, p.sum_shape, st)) return e;
     D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
     D.kblocks = p.n_pad / 64, D.splits = 1;
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
-    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, pick_shape(d, n, 1), st)) return e;
+    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, pick_shape(d, n), st)) return e;
   }
   head_finish_kernel<T><<<(unsigned)cdiv64((long long)rows * ((d + 7) / 8), 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale),
                                                                                                static_cast<T *>(q.dh_dev), q.dh_stride);
