@@ -62,6 +62,8 @@ __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 constexpr int kPlanesA = 0 << 0 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 2 << 10;   // six products, smallest first when read from the top
 constexpr int kPlanesB = 0 << 0 | 1 << 2 | 0 << 4 | 2 << 6 | 1 << 8 | 0 << 10;
 
@@ -210,33 +212,58 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 
   // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
   const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
+  // what belongs to a lane's rows of n, read together: rows behind the end read the last one's
+  int label[NT];
+  if constexpr (EPI == kStats || EPI == kDz) {
+    if (G.wide) {
+      long long w[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j] = static_cast<const long long *>(G.labels)[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.b.rows ? (int)w[j] : -1;
+    } else {
+      int w[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j] = static_cast<const int *>(G.labels)[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.b.rows ? w[j] : -1;
+    }
+  }
+  const bool edge = m0 + TM > G.a.rows;                  // the vocabulary ends in this tile
   if constexpr (EPI == kStats) {
     float *red = reinterpret_cast<float *>(s0);        // [WM][TN] pairs, once everybody is done with the slices
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 32 * j;
-      const bool in = n < G.b.rows;
-      const int at = in ? label_of(G.labels, G.wide, G.vocab, n) - G.v0 - m1 : -1;
-      float top = -__builtin_inff(), sum = 0.f, mine = 0.f;
+      const int n = n1 + 32 * j, at = label[j] - G.v0 - m1;
+      if (at >= 0 && at < 16 * MT) {                     // few lanes have their label here
+        float mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (at == 16 * i + e) mine = acc[i][j][e];
+        G.at_label[n] = mine;
+      }
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (m1 + 16 * i + e >= G.a.rows) acc[i][j][e] = -__builtin_inff();
+      }
+      float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float x = acc[i][j][e];
-          if (at == 16 * i + e) mine = x;
-          x = m1 + 16 * i + e < G.a.rows ? x : -__builtin_inff();
-          acc[i][j][e] = x;
-          top = fmaxf(top, x);
-        }
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float ref = top == -__builtin_inff() ? 0.f : top;
+      const float ref = top == -__builtin_inff() ? 0.f : top * kLog2e;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum += __expf(acc[i][j][e] - ref);
+        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -ref));
       sum += __shfl_xor(sum, 32, 64);
-      if (in && at >= 0 && at < 16 * MT && m1 + at < G.a.rows) G.at_label[n] = mine;
       if (h == 0) red[(wm * TN + n - n0) * 2] = top, red[(wm * TN + n - n0) * 2 + 1] = sum;
     }
     __syncthreads();
@@ -251,35 +278,95 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       p[0] = top, p[1] = sum;
     }
   } else if constexpr (EPI == kDz) {
+    float lse[NT], g[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) lse[j] = G.lse[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1] * kLog2e, g[j] = G.g[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int n = n1 + 32 * j;
-      const bool in = n < G.b.rows;
-      const int label = in ? label_of(G.labels, G.wide, G.vocab, n) : -1, at = label - G.v0 - m1;
-      const float lse = in ? G.lse[n] : 0.f, g = in ? G.g[n] : 0.f;
+      const int at = label[j] - G.v0 - m1;
+      const bool live = label[j] >= 0, hit = live && at >= 0 && at < 16 * MT;
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) {
-        float x[8];
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x[e] = label >= 0 && m1 + 8 * i + e < G.a.rows ? g * (__expf(acc[i / 2][j][i % 2 * 8 + e] - lse) - (at == 8 * i + e ? 1.f : 0.f)) : 0.f;
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = g[j] * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -lse[j]));
+      if (__any(hit)) {
 #pragma unroll
-        for (int k = 0; k < PLANES; ++k) {
-          E y[8];
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = static_cast<E>(x[e]), x[e] -= static_cast<float>(y[e]);
-          if (in && m1 + 8 * i < G.m_pad) {
-            uintx4 w;
-            __builtin_memcpy(&w, y, 16);
-            *reinterpret_cast<uintx4 *>(G.dz + k * G.dz_plane + n * G.dz_ld + (m1 + 8 * i) * 2) = w;
-          }
-          if (n < G.n_pad) {
+          for (int e = 0; e < 16; ++e)
+            if (at == 16 * i + e) acc[i][j][e] -= g[j];
+      }
+      if (__any(!live) || edge) {                        // zeros, whatever the logits are
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (m1 + 8 * i + e < G.a.rows) *reinterpret_cast<E *>(G.dzt + k * G.dzt_plane + (m1 + 8 * i + e) * G.dzt_ld + n * 2) = y[e];
-          }
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!live || m1 + 16 * i + e >= G.a.rows) acc[i][j][e] = 0.f;
+      }
+    }
+    // Both layouts leave through the wave's own part of LDS, in whole rows: a lane's own results would go out in pieces of 16 and of 2 bytes.
+    constexpr int BYTES = 32 * MT * 32 * NT * 2, FIT = SLICE / BYTES;
+    static_assert(FIT * 2 >= WM * WN, "the waves' tiles fit into two stages");
+    char *own = (wave < FIT ? s0 : s1) + (wave < FIT ? wave : wave - FIT) * BYTES;
+    __syncthreads();
+    const int wave_m = m0 + wm * (MT * 32), wave_n = n0 + wn * (NT * 32);
+#pragma unroll 1
+    for (int k = 0; k < PLANES; ++k) {
+      // a word has two m of one n, in their order: word(j, 8 i + e) is of tile i
+      auto word_of = [&](int j, int w) {
+        const E y[2] = {static_cast<E>(acc[w / 8][j][w % 8 * 2]), static_cast<E>(acc[w / 8][j][w % 8 * 2 + 1])};
+        unsigned x;
+        __builtin_memcpy(&x, y, 4);
+        return x;
+      };
+      // rows of n: 4 MT pieces of 16 bytes, swapped by the row's number
+      constexpr int PM = 4 * MT, PN = 4 * NT;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (PLANES > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+          const int row = 32 * j + r32, piece = (h * 2 * MT + i) ^ (row & (PM - 1));
+          *reinterpret_cast<uintx4 *>(own + row * (PM * 16) + piece * 16) =
+              uintx4{word_of(j, 4 * i), word_of(j, 4 * i + 1), word_of(j, 4 * i + 2), word_of(j, 4 * i + 3)};
         }
       }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int t = 0; t < 32 * NT * PM / 64; ++t) {
+        const int row = t * (64 / PM) + lane / PM, piece = lane % PM;
+        const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PM * 16) + (piece ^ (row & (PM - 1))) * 16);
+        const int n = wave_n + row, m = wave_m + piece * 8;
+        if (n < G.b.rows && m < G.m_pad) *reinterpret_cast<uintx4 *>(G.dz + k * G.dz_plane + n * G.dz_ld + m * 2) = w;
+      }
+      asm volatile("" ::: "memory");
+      // rows of m: lanes of neighbouring n exchange halves, so that a word has two n of one m
+      const int odd = lane & 1;
+      const unsigned select = odd ? 0x03020706u : 0x05040100u;
+      auto swap_n = [](int m) { return NT == 4 ? ((m & 1) | (m / (16 * MT) & 1) << 1) << 2 : NT == 2 ? (m / (16 * MT) & 1) << 2 : 0; };
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (PLANES > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 8 * MT; ++e) {
+          if (PLANES > 1 && e % 8 == 0) asm volatile("" : "+a"(acc[e / 8][j]));      // rounded again, or the words of both passes are kept and spill
+          const unsigned mine = word_of(j, e), other = __builtin_amdgcn_update_dpp(0u, mine, 0xB1, 0xf, 0xf, true);
+          const int row = h * 16 * MT + 2 * e + odd, word = 16 * j + (r32 >> 1);
+          *reinterpret_cast<unsigned *>(own + row * (PN * 16) + ((word >> 2) ^ swap_n(row)) * 16 + (word & 3) * 4) = __builtin_amdgcn_perm(other, mine, select);
+          if (PLANES > 1)                                // what this plane leaves to the next
+#pragma unroll
+            for (int u = 0; u < 2; ++u) acc[e / 8][j][e % 8 * 2 + u] -= static_cast<float>(static_cast<E>(acc[e / 8][j][e % 8 * 2 + u]));
+        }
+      }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int t = 0; t < 32 * MT * PN / 64; ++t) {
+        const int row = t * (64 / PN) + lane / PN, piece = lane % PN;
+        const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PN * 16) + (piece ^ swap_n(row)) * 16);
+        const int m = wave_m + row, n = wave_n + piece * 8;
+        if (m < G.a.rows && n < G.n_pad) *reinterpret_cast<uintx4 *>(G.dzt + k * G.dzt_plane + m * G.dzt_ld + n * 2) = w;
+      }
+      asm volatile("" ::: "memory");
     }
   } else {
     float scale = 1.f;
