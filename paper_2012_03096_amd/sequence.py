@@ -94,6 +94,22 @@ class SequenceBlock:
         pb.recurrence_step(c["u"], c["gate"], state, y, out_gate=c["out_gate"], bias=self.bias, active=active)
         return y @ self.copies[3].t()
 
+    def _backward(self, x, residual, dout, z, q, lengths=None, dtotal=None):
+        """Gradients of the block's parameters (into self.grads) and of x + residual (returned, a buffer of the block) from dout, what the
+        training forward pass left (z, q), and the gradient that arrives at the residual stream."""
+        b, t, d = x.shape
+        dnorm, dw_in, dbias, dw_out = self.grads
+        torch.mm(dout.t(), q["y"].view(-1, d), out=dw_out)
+        dy = (dout @ self.copies[3]).view(b, t, d)
+        c, g = self._columns(z), self._columns(q["dz"])
+        pb.recurrence_backward(**c, dy=dy, saved=q["saved"], du=g["u"], dgate=g["gate"], dout_gate=g["out_gate"], bias=self.bias, dbias=dbias,
+                               lengths=lengths, workspace=q["workspace"])
+        dz = q["dz"].view(-1, 3 * d)
+        torch.mm(dz.t(), q["n"].view(-1, d), out=dw_in)
+        dn = (dz @ self.copies[1]).view(b, t, d)
+        pb.rmsnorm_backward(q["total"] if residual is not None else x, self.norm, dn, q["dx"], dnorm, q["norm_workspace"], dtotal=dtotal)
+        return q["dx"]
+
     def distill_step(self, x, target, lr: float, residual=None, lengths=None):
         """One distillation step: forward, mean squared difference from target over the real tokens (Eq. 3), backward through this block
         only, AdamW.  What x, residual and target hold behind a sequence has no influence.  Returns the loss of the forward pass as a
@@ -112,16 +128,7 @@ class SequenceBlock:
             count = live.sum().clamp_min(1) * d
         loss = diff.square().sum() / count
         dout = (diff * (2.0 / count)).to(torch.bfloat16).view(-1, d)
-        dnorm, dw_in, dbias, dw_out = self.grads
-        torch.mm(dout.t(), q["y"].view(-1, d), out=dw_out)
-        dy = (dout @ self.copies[3]).view(b, t, d)
-        c, g = self._columns(z), self._columns(q["dz"])
-        pb.recurrence_backward(**c, dy=dy, saved=q["saved"], du=g["u"], dgate=g["gate"], dout_gate=g["out_gate"], bias=self.bias, dbias=dbias,
-                               lengths=lengths, workspace=q["workspace"])
-        dz = q["dz"].view(-1, 3 * d)
-        torch.mm(dz.t(), q["n"].view(-1, d), out=dw_in)
-        dn = (dz @ self.copies[1]).view(b, t, d)
-        pb.rmsnorm_backward(q["total"] if residual is not None else x, self.norm, dn, q["dx"], dnorm, q["norm_workspace"])
+        self._backward(x, residual, dout, z, q, lengths)
         self.optimizer.step(self.grads, lr)
         return loss
 

@@ -473,3 +473,89 @@ def test_binding_refuses_wrong_tensors(gpu):
             print("not refused:", i)
     with pytest.raises(pb.PbkdError):
         pb.head_loss_workspace_bytes(4, 10, 8, torch.float64, False)
+
+
+# ---------------------------------------------------------------------------------------------------- the token student
+def _reference_student(torch, student, tokens, dtype):
+    """The student's formulas in torch operations, differentiable: (leaves in the order of the student's gradients, h)."""
+    table, norm = student.table.to(dtype).requires_grad_(), student.norm.to(dtype).clone().requires_grad_()
+    leaves = [table, norm]
+
+    def rms(x, w):
+        return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6) * w
+    live = ((tokens >= 0) & (tokens < student.vocab))[..., None]
+    out, stream = torch.where(live, table[tokens.clamp(0, student.vocab - 1)], torch.zeros((), dtype=dtype, device="cuda")) * student.scale, None
+    for block in student.blocks:
+        w = [block.norm.to(dtype).clone(), block.copies[1].to(dtype), block.bias.to(dtype).clone(), block.copies[3].to(dtype)]
+        w = [t.requires_grad_() for t in w]
+        leaves += w
+        s = out if stream is None else out + stream
+        u, gate, o = (rms(s, w[0]) @ w[1].t()).split(student.d, -1)
+        a, state, ys = torch.sigmoid(gate + w[2]), torch.zeros_like(u[:, 0]), []
+        for i in range(u.shape[1]):
+            state = a[:, i] * state + torch.sigmoid(-(gate[:, i] + w[2])) * u[:, i]
+            ys.append(state)
+        stream, out = s, (torch.stack(ys, 1) * o * torch.sigmoid(o)) @ w[3].t()
+    return leaves, rms(out + stream, norm).view(-1, student.d)
+
+
+@pytest.mark.parametrize("blocks", [1, 2])
+@pytest.mark.parametrize("way", ["learn", "imitate"])
+def test_token_student_gradients(gpu, blocks, way):
+    """All operators in a training step, against automatic differentiation of the same formulas in float64.  Between the table and a gradient lie at most
+    30 bf16 tensors (15 of a block and its backward pass, twice), each off by at most 2^-8 of its norm, and no step here makes a
+    relative error larger than it was by more than its share of the sum it enters: 30 * 2^-8 = 0.12 of a gradient's norm."""
+    torch, pb = gpu
+    from paper_2012_03096_amd.tokens import TokenStudent
+    student = TokenStudent(300, 64, blocks=blocks, seed=3)
+    tokens, labels = _ints(torch, 1, 0, 300, 4, 25), _ints(torch, 2, 0, 300, 4, 25)
+    tokens[0, 20:], labels[0, 19:], labels[2, 3] = -1, -100, 300
+    leaves, h = _reference_student(torch, student, tokens, torch.float64)
+    logits = h @ leaves[0].t()
+    if way == "learn":
+        mean = student.learn_gradients(tokens, labels)
+        want = torch.nn.functional.cross_entropy(logits, torch.where((labels >= 0) & (labels < 300), labels, -100).view(-1), ignore_index=-100)
+    else:
+        teacher, at = _randn(torch, 4, 4, 25, 8, scale=3.0), torch.stack([torch.randperm(300)[:8] for _ in range(100)]).view(4, 25, 8).cuda()
+        at[1, 2] = -1
+        mean = student.imitate_gradients(tokens, teacher, at, temperature=2.0)
+        some = (at >= 0).all(-1).view(-1)
+        q = torch.softmax(teacher.view(-1, 8).double() / 2, 1)
+        log_p = torch.log_softmax(logits / 2, 1).gather(1, at.view(-1, 8).clamp_min(0))
+        want = (4 * (q * (torch.log(q) - log_p)).sum(1) * some).sum() / some.sum()
+    want.backward()
+    want = want.detach()
+    got = student.grads + [g for block in student.blocks for g in block.grads]
+    assert len(got) == len(leaves)
+    assert abs(float(mean) - float(want)) < 0.12 * float(want)
+    for i, (g, leaf) in enumerate(zip(got, leaves)):
+        off = float((g.double() - leaf.grad).norm() / leaf.grad.norm())
+        print(way, blocks, i, f"{off:.4f}", flush=True)
+        assert off < 0.12, (i, off)
+
+
+def test_token_student_steps_scores_and_answers(gpu):
+    torch, pb = gpu
+    from paper_2012_03096_amd.tokens import TokenStudent
+    student, other = TokenStudent(500, 64, blocks=2, seed=1), TokenStudent(500, 64, seed=2)
+    x, y = _ints(torch, 1, 0, 500, 3, 17), _ints(torch, 2, 0, 500, 3, 17)
+    before = [p.clone() for p in student.params + student.blocks[1].params]
+    student.learn(x, y, 1e-3)
+    assert all(bool((a != b).any()) for a, b in zip(before, student.params + student.blocks[1].params))
+    values, at = student.top_logits(x, 5)
+    assert torch.isfinite(other.imitate(x, values, at, 1e-3)) and at.dtype == torch.int32
+    score = student.score(x, y)
+    logits = (student._forward(x, False) @ student.table.t()).float()
+    # the logits themselves were rounded to bf16 here: half a step of the largest, twice
+    want = torch.nn.functional.cross_entropy(logits, y.view(-1), reduction="none")
+    assert float((score.view(-1) - want).abs().max()) < 2 * 2.0 ** -8 * float(logits.abs().max()) + 1e-4
+    state = student.new_state(3)
+    alone = torch.stack([student.answer(x[:, t].contiguous(), state) for t in range(17)], 1)
+    # 12 bf16 tensors up to the logits, each off by at most 2^-8 of its norm
+    assert float((alone.view(-1, 500).float() - logits).norm() / logits.norm()) < 12 * 2.0 ** -8
+
+
+def test_token_student_demonstration_runs(gpu):
+    from paper_2012_03096_amd import tokens
+    losses, off = tokens.demo(vocab=300, d=64, batch=4, length=20, steps=4, report=2)
+    assert len(losses) == 6 and np.isfinite(losses).all() and off < 12 * 2.0 ** -8
