@@ -1,14 +1,16 @@
 // The matrix product under the vocabulary loss, and its three uses.
 //
-//   C[m][n] = sum over k of A[m][k] B[n][k],   A and B with k contiguous, k a multiple of 64, 16-bit types, fp32 sums
+//   C[m][n] = sum over k of A[m][k] B[n][k],   k contiguous (of A, as it suits: m contiguous), k a multiple of 64, 16-bit types, fp32 sums
 //
 // A workgroup forms a tile of TM x TN.  Slices of 64 k of both operands go from memory straight into LDS, STAGES of them at a time: one is
 // multiplied while the others are on their way.  A slice's row is 128 bytes, eight pieces of 16; a row's pieces are swapped by bits of its number, so that
 // the 16 rows that an MFMA's lanes read at once lie in different banks.  A wave's rows of A are dealt to its MFMA tiles so that
-// a lane ends with 4 * MT consecutive m of one n: results leave in wide stores, and a softmax over m needs two exchanges between lanes.
+// a lane ends with 16 * MT consecutive m of one n: results leave in wide stores, and a softmax over m needs one exchange between lanes.
+// An operand A with m contiguous is staged row of k by row of k and read by the transposing LDS read: in each group of 16 lanes, lane s gives
+// the address of four m of the k that is s / 4 from the first, and lane i receives the four k of the i-th m.
 //
 // fp32 operands come as three bf16 planes (x = x1 + x2 + x3 exactly); the product is the sum of the six plane products that matter
-// (what is left out is below 2^-24 of |a||b|), smallest first.
+// (what is left out is below 2^-24 of |a||b|).  A slice's plane products follow each other: each plane is read from the caches but once.
 #pragma once
 #include <type_traits>
 
@@ -25,13 +27,15 @@ struct Operand {
   const char *p;
   long long ld, plane;     // bytes between rows, between planes
   int rows;
+  int cols;                // A with m contiguous: numbers that a row (of one k) has
 };
 
 enum { kStats, kDz, kOut, kSum };    // what becomes of a tile
 
 struct GemmArgs {
   Operand a, b;
-  int kblocks, terms;              // slices of 64 in a plane, products of planes (1 or 6)
+  int m;                           // of the result; n is b.rows
+  int kblocks, terms;              // slices of 64 in a plane, products of planes: 1, 2 (B has two) or 6 (both have three)
   int tiles_m, tiles_n, splits;    // splits: parts of the sum over k, kSum only
   // kStats, kDz: m is a place in the vocabulary, n a row of h
   const void *labels;              // of 32 or 64 bits; outside 0..vocab-1: none
@@ -56,6 +60,16 @@ __device__ __forceinline__ int label_of(const void *labels, int wide, int vocab,
   return w >= 0 && w < vocab ? (int)w : -1;
 }
 
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uintx2 read_turned(const char *p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4 *)p));
+#else
+  return uintx2{};
+#endif
+}
+
 template <typename E>
 __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
   if constexpr (__is_same(E, f16)) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -64,11 +78,11 @@ __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-constexpr int kPlanesA = 0 << 0 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 2 << 10;   // six products, smallest first when read from the top
-constexpr int kPlanesB = 0 << 0 | 1 << 2 | 0 << 4 | 2 << 6 | 1 << 8 | 0 << 10;
+constexpr int kPlanesA = 0 << 0 | 0 << 2 | 0 << 4 | 1 << 6 | 1 << 8 | 2 << 10;   // of the products, two bits each; the first two are those of a single plane A
+constexpr int kPlanesB = 0 << 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
 
-// OutT: the type of kOut's result.  PLANES: of dz (3: fp32 in three bf16 terms).
-template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES>
+// OutT: the type of kOut's result.  PLANES: of dz (2: 16-bit types in two terms; 3: fp32 in three bf16 terms).  TURN: A has m contiguous.
+template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES, bool TURN>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 32, NT = TN / WN / 32;
   constexpr int RA = TM * 8 / THREADS, RB = TN * 8 / THREADS, ROWS = THREADS / 8;     // rounds of loads, rows a round
@@ -88,13 +102,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 
   auto swz_a = [](int r) { return (r >> 1 & 3) | (r / (16 * MT) & 1) << 2; };
   auto swz_b = [](int r) { return r >> 1 & 7; };
+  // of a row of k: the four that a group of lanes reads at once lie in different banks
+  auto swz_t = [](int r) { return MT == 4 ? (r & 3) << 1 : MT == 2 ? (r & 1) << 1 | (r & 2) << 2 : TM == 64 ? (r & 2) << 1 : (r & 3) << 2; };
   unsigned va[RA], vb[RB];
   {
     const int slot = tid & 7, r0 = tid >> 3;
 #pragma unroll
     for (int i = 0; i < RA; ++i) {
-      const int r = i * ROWS + r0, row = m0 + r < G.a.rows ? r : G.a.rows - 1 - m0;      // rows behind the last: the last again
-      va[i] = (unsigned)(row * (int)G.a.ld + (slot ^ swz_a(r)) * 16);
+      if constexpr (TURN) {
+        const int at = (i * THREADS + tid) * 16, r = at / (TM * 2), left = G.a.cols / 8 - 1 - m0 / 8;
+        const int piece = (at % (TM * 2) / 16) ^ swz_t(r);
+        va[i] = (unsigned)(r * (int)G.a.ld + (piece < left ? piece : left) * 16);          // m behind the end: the last again
+      } else {
+        const int r = i * ROWS + r0, row = m0 + r < G.a.rows ? r : G.a.rows - 1 - m0;      // rows behind the last: the last again
+        va[i] = (unsigned)(row * (int)G.a.ld + (slot ^ swz_a(r)) * 16);
+      }
     }
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
@@ -102,24 +124,27 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       vb[i] = (unsigned)(row * (int)G.b.ld + (slot ^ swz_b(r)) * 16);
     }
   }
-  const char *pa = G.a.p + m0 * G.a.ld, *pb = G.b.p + n0 * G.b.ld;
+  const char *pa = TURN ? G.a.p + m0 * 2 : G.a.p + m0 * G.a.ld, *pb = G.b.p + n0 * G.b.ld;
   const int rows_a = G.a.rows - m0 < TM ? G.a.rows - m0 : TM, rows_b = G.b.rows - n0 < TN ? G.b.rows - n0 : TN;
-  const int bytes_a = (rows_a - 1) * (int)G.a.ld + G.kblocks * 128, bytes_b = (rows_b - 1) * (int)G.b.ld + G.kblocks * 128;
+  const int bytes_a = (rows_a - 1) * (int)G.a.ld + G.kblocks * 128;
+  const int bytes_b = (rows_b - 1) * (int)G.b.ld + G.kblocks * 128;
 
   // this workgroup's slices
   const int total = G.kblocks * G.terms, per = (total + G.splits - 1) / G.splits;
   const int first = blockIdx.y * per, last = first + per < total ? first + per : total;
-  int term = first / G.kblocks, kb = first - term * G.kblocks;
+  int kb = first / G.terms, term = first - kb * G.terms;
   auto load = [&](char *s) {
-    const int t = G.terms - 1 - term, qa = kPlanesA >> 2 * t & 3, qb = kPlanesB >> 2 * t & 3;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pa + qa * G.a.plane), 0, bytes_a, 0x00020000);
+    const int qa = kPlanesA >> 2 * term & 3, qb = kPlanesB >> 2 * term & 3;
+    const int here = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64;      // rows of k that A has; what lies behind them reads as zeros
+    const char *from = pa + qa * G.a.plane + (TURN ? kb * 64 * G.a.ld : 0);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, TURN ? (here - 1) * (int)G.a.ld + (G.a.cols - m0) * 2 : bytes_a, 0x00020000);
     const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pb + qb * G.b.plane), 0, bytes_b, 0x00020000);
     char *d = s + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], kb * 128);
+    for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], TURN ? 0 : kb * 128);
 #pragma unroll
     for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], kb * 128);
-    if (++kb == G.kblocks) kb = 0, ++term;
+    if (++term == G.terms) term = 0, ++kb;
   };
 
   floatx16 acc[MT][NT];
@@ -134,6 +159,12 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   const int row_a = wm * (MT * 32) + (r32 >> 2 & 1) * (16 * MT) + (r32 >> 3) * 4 + (r32 & 3), row_b = wn * (NT * 32) + r32;
   const int sa = swz_a(row_a), sb = swz_b(row_b);       // rows 16 i and 32 j further on are swapped alike
 
+  // where a lane's four m of tile i begin, of the k that is lane % 16 / 4 behind k (8 more for the upper half of the lanes)
+  const int turn_k = (lane >> 2 & 3) + 8 * h, turn_m = wm * (MT * 32) + (lane & 1) * (16 * MT) + (lane >> 4 & 1) * 8 + (lane >> 1 & 1) * 4;
+  auto turned = [&](int k, int i) {
+    const int r = k + turn_k, m = turn_m + 16 * i;
+    return r * (TM * 2) + ((m >> 3) ^ swz_t(turn_k)) * 16 + (m & 7) * 2;         // k is a multiple of four: it does not change the swap
+  };
   // Operands of half a slice (two MFMA steps) wait in registers while the half before is multiplied.
   struct Half {
     uintx4 a[2][MT], b[2][NT];
@@ -144,10 +175,19 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       const int c = half * 4 + u * 2 + h;
 #pragma unroll
       for (int j = 0; j < NT; ++j) f.b[u][j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 32 * j) * 128 + (c ^ sb) * 16);
+      if constexpr (TURN) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) f.a[u][i] = *reinterpret_cast<const uintx4 *>(s + (row_a + 16 * i) * 128 + (c ^ sa) * 16);
+        for (int i = 0; i < MT; ++i) {
+          const uintx2 lo = read_turned(s + turned(half * 32 + u * 16, i)), hi = read_turned(s + turned(half * 32 + u * 16 + 4, i));
+          f.a[u][i] = uintx4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) f.a[u][i] = *reinterpret_cast<const uintx4 *>(s + (row_a + 16 * i) * 128 + (c ^ sa) * 16);
+      }
     }
   };
+  constexpr int READS = 2 * ((TURN ? 2 : 1) * MT + NT);
   auto multiply = [&](const Half &f) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -175,7 +215,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     multiply(f0);
     // the reads first, one between two products, so that they are back before the barrier
 #pragma unroll
-    for (int i = 0; i < 2 * (MT + NT); ++i) {
+    for (int i = 0; i < READS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     }
@@ -184,7 +224,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     if (more) fetch(f0, next, 0);
     multiply(f1);
 #pragma unroll
-    for (int i = 0; i < 2 * (MT + NT); ++i) {
+    for (int i = 0; i < READS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -229,7 +269,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.b.rows ? w[j] : -1;
     }
   }
-  const bool edge = m0 + TM > G.a.rows;                  // the vocabulary ends in this tile
+  const bool edge = m0 + TM > G.m;                  // the vocabulary ends in this tile
   if constexpr (EPI == kStats) {
     float *red = reinterpret_cast<float *>(s0);        // [WM][TN] pairs, once everybody is done with the slices
     __syncthreads();
@@ -250,7 +290,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (m1 + 16 * i + e >= G.a.rows) acc[i][j][e] = -__builtin_inff();
+            if (m1 + 16 * i + e >= G.m) acc[i][j][e] = -__builtin_inff();
       }
       float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
@@ -301,7 +341,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (!live || m1 + 16 * i + e >= G.a.rows) acc[i][j][e] = 0.f;
+            if (!live || m1 + 16 * i + e >= G.m) acc[i][j][e] = 0.f;
       }
     }
     // Both layouts leave through the wave's own part of LDS, in whole rows: a lane's own results would go out in pieces of 16 and of 2 bytes.
@@ -364,7 +404,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         const int row = t * (64 / PN) + lane / PN, piece = lane % PN;
         const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PN * 16) + (piece ^ swap_n(row)) * 16);
         const int m = wave_m + row, n = wave_n + piece * 8;
-        if (m < G.a.rows && n < G.n_pad) *reinterpret_cast<uintx4 *>(G.dzt + k * G.dzt_plane + m * G.dzt_ld + n * 2) = w;
+        if (m < G.m && n < G.n_pad) *reinterpret_cast<uintx4 *>(G.dzt + k * G.dzt_plane + m * G.dzt_ld + n * 2) = w;
       }
       asm volatile("" ::: "memory");
     }
@@ -377,7 +417,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       if (n >= G.b.rows) continue;
 #pragma unroll
       for (int i = 0; i < 2 * MT; ++i) {
-        const int m = m1 + 8 * i, left = G.a.rows - m;
+        const int m = m1 + 8 * i, left = G.m - m;
         if (left <= 0) break;
         float x[8];
 #pragma unroll

@@ -4,11 +4,11 @@
 //
 // Bound by its products of matrices: 2 N V d operations for the losses, and 6 N V d for the gradients, because z is not kept but formed
 // again, piece of the vocabulary by piece.  The first pass leaves a maximum and a sum of every tile's rows; they give lse.  In the
-// second a piece's dz comes out of the product in both layouts, n by v for dh and v by n for dW, so that every product
-// reads both operands along k (head_gemm.h); W's and h's other layouts are copied first (a hundredth of the products' time).
+// second a piece's dz comes out of the product in both layouts, n by v for dh and v by n for dW; W serves dh as it lies, by transposing
+// reads, and h's other layout is copied first (head_gemm.h).
 //
 // dz is rounded to the operands' type, which is an error of the size that rounding the gradients has anyway (half a step of a
-// value, averaged over the sum).  It is formed with row weights times a power of two that puts the largest near 2^15: fp16 keeps
+// value, averaged over the sum); for few rows it is kept in two terms.  It is formed with row weights times a power of two that puts the largest near 2^15: fp16 keeps
 // probabilities down to 2^-24 / 2^15 of it.  fp32 is kept in three bf16 terms.
 #include "head_gemm.h"
 
@@ -18,6 +18,8 @@ namespace {
 using namespace head;
 
 constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
+// Up to here dz is kept in two terms: a few rows' rounding errors do not average out, and the products wait for W anyway.
+constexpr int kFewRows = 64;
 constexpr double kPieceBytes = 600e6;        // dz of a piece, both layouts
 
 inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
@@ -183,9 +185,9 @@ inline int pick_shape(long long m, long long n, int slices = 0) {
 }
 
 struct Plan {
-  int d_pad, n_pad, piece, pieces, planes, terms, parts, first_shape, sum_shape, splits;
+  int d_pad, n_pad, piece, pieces, planes, terms, dz_planes, dz_terms, parts, first_shape, sum_shape, splits;
   bool pack_h, pack_w;
-  size_t gs, scale, lse, at_label, part, h, ht, w, wt, dz, dzt, sum, bytes;
+  size_t gs, scale, lse, at_label, part, h, ht, w, dz, dzt, sum, bytes;
 };
 
 bool direct(const void *p, long long stride, int d, int dtype) {
@@ -196,10 +198,11 @@ bool direct(const void *p, long long stride, int d, int dtype) {
 Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w) {
   Plan p;
   p.planes = dtype == PBKD_F32 ? 3 : 1, p.terms = dtype == PBKD_F32 ? 6 : 1;
+  p.dz_planes = dtype == PBKD_F32 ? 3 : rows <= kFewRows ? 2 : 1, p.dz_terms = dtype == PBKD_F32 ? 6 : p.dz_planes;
   p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
   p.pack_h = pack_h, p.pack_w = pack_w;
   // A piece's tiles of 256 x 256 fill whole rounds of the chip where that leaves pieces of a sensible size: 16 rows of tiles, 16 columns.
-  const double most = kPieceBytes / (gradients ? 4.0 * p.planes * p.n_pad : 2.0 * p.planes * p.d_pad);
+  const double most = kPieceBytes / (gradients ? 4.0 * p.dz_planes * p.n_pad : 2.0 * p.planes * p.d_pad);
   long long unit = cdiv64(rows, 256);
   unit = (unit & -unit) < 256 ? 256 / (unit & -unit) * 256 : 256;
   if (unit > most / 2) unit = 256;
@@ -212,7 +215,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   p.pieces = (int)cdiv64(vocab, p.piece);
   p.first_shape = pick_shape(p.piece, rows);
   // dh: few tiles, a long sum
-  const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.terms;
+  const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.dz_terms;
   p.sum_shape = pick_shape(d, rows, slices);
   p.splits = splits_of(p.sum_shape, d, rows, slices);
   p.parts = (int)cdiv64(vocab, kShapes[p.first_shape].tm) + p.pieces;
@@ -229,9 +232,8 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   p.w = put(pack_w ? (size_t)p.piece * p.d_pad * e : 0);
   if (gradients) {
     p.ht = put((size_t)d * p.n_pad * e);
-    p.wt = put((size_t)d * p.piece * e);
-    p.dz = put(R * p.piece * e);
-    p.dzt = put((size_t)p.piece * p.n_pad * e);
+    p.dz = put(R * p.piece * 2 * p.dz_planes);
+    p.dzt = put((size_t)p.piece * p.n_pad * 2 * p.dz_planes);
     p.sum = put((size_t)p.splits * R * d * 4);
   }
   p.bytes = at + 256;
@@ -239,16 +241,18 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
 }
 
 // --------------------------------------------------------------------------------------------------------- the launches
-template <typename E, typename OutT, int EPI, int PLANES>
+template <typename E, typename OutT, int EPI, int PLANES, bool TURN = false>
 hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
   const Shape &s = kShapes[shape];
-  G.tiles_m = (int)cdiv64(G.a.rows, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
+  G.tiles_m = (int)cdiv64(G.m, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
   const dim3 grid(G.tiles_m * G.tiles_n, G.splits);
   switch (shape) {
-    case 0: gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
-    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
-    case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES><<<grid, 256, 0, st>>>(G); break;
-    default: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES><<<grid, 256, 0, st>>>(G);
+    case 0:
+      if constexpr (PLANES != 2) gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
+      break;                         // kFewRows rows never have so many tiles
+    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
+    case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
+    default: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
   }
   return hipGetLastError();
 }
@@ -278,13 +282,13 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     lay(L);
     if (p.pack_h) H = Operand{L.rows_dst, L.rows_ld, L.rows_plane, rows};
   }
-  // Rows v0 .. v0 + n of W along k, and (columns) along v: what of it is not there yet.  A piece that is the whole vocabulary is laid out once.
-  auto weight = [&](int v0, int n, bool rows_too, bool columns) {
+  // Rows v0 .. v0 + n of W, as they lie or laid out (a piece that is the whole vocabulary is laid out once).
+  auto weight = [&](int v0, int n, bool now) {
     const T *w = static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride;
-    LayArgs L{w, q.weight_stride, p.pack_w && rows_too ? ws + p.w : nullptr, columns ? ws + p.wt : nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, p.piece * 2,
-              (long long)d * p.piece * 2, nullptr, 0, 0, n, d, p.d_pad, up64(n)};
-    if (L.rows_dst || L.cols_dst) lay(L);
-    return p.pack_w ? Operand{ws + p.w, L.rows_ld, L.rows_plane, n} : Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n};
+    if (!p.pack_w) return Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n, d};
+    LayArgs L{w, q.weight_stride, ws + p.w, nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, 0, 0, nullptr, 0, 0, n, d, p.d_pad, 0};
+    if (now) lay(L);
+    return Operand{ws + p.w, L.rows_ld, L.rows_plane, n, p.d_pad};
   };
   GemmArgs G{};
   G.b = H, G.kblocks = p.d_pad / 64, G.terms = p.terms, G.splits = 1;
@@ -294,7 +298,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   const bool whole = !p.pack_w;                       // W as it lies: one product over the whole vocabulary
   for (int v0 = 0; v0 < V; v0 += whole ? V : p.piece) {
     const int n = whole || V - v0 < p.piece ? V - v0 : p.piece;
-    G.a = weight(v0, n, true, gradients && p.pieces == 1), G.v0 = v0, G.parts = p.parts, G.part0 = parts;
+    G.a = weight(v0, n, true), G.m = n, G.v0 = v0, G.parts = p.parts, G.part0 = parts;
     if (const hipError_t e = launch_gemm<E, T, kStats, 1>(G, p.first_shape, st)) return e;
     parts += (int)cdiv64(n, kShapes[p.first_shape].tm);
   }
@@ -304,17 +308,17 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = V - v0 < p.piece ? V - v0 : p.piece, n64 = up64(n);
     // dz of this piece, in both layouts
-    G.a = weight(v0, n, p.pieces > 1, p.pieces > 1), G.v0 = v0;
+    G.a = weight(v0, n, p.pieces > 1), G.m = n, G.v0 = v0;
     G.dz = ws + p.dz, G.dz_ld = p.piece * 2, G.dz_plane = (long long)rows * p.piece * 2;
     G.dzt = ws + p.dzt, G.dzt_ld = p.n_pad * 2, G.dzt_plane = (long long)p.piece * p.n_pad * 2;
     G.m_pad = n64, G.n_pad = p.n_pad;
-    if (const hipError_t e = launch_gemm<E, T, kDz, PLANES>(G, p.first_shape, st)) return e;
+    if (const hipError_t e = PLANES == 1 && p.dz_planes == 2 ? launch_gemm<E, T, kDz, 2>(G, p.first_shape, st) : launch_gemm<E, T, kDz, PLANES>(G, p.first_shape, st)) return e;
     GemmArgs D{};
-    D.terms = p.terms, D.scale = floats(p.scale);
-    D.a = Operand{ws + p.wt, p.piece * 2, (long long)d * p.piece * 2, d}, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
+    D.terms = p.dz_terms, D.scale = floats(p.scale);
+    D.a = G.a, D.m = d, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
     D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
-    if (const hipError_t e = launch_gemm<E, T, kSum, 1>(D, p.sum_shape, st)) return e;
-    D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
+    if (const hipError_t e = launch_gemm<E, T, kSum, 1, true>(D, p.sum_shape, st)) return e;
+    D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
     D.kblocks = p.n_pad / 64, D.splits = 1;
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
     if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, pick_shape(d, n), st)) return e;
