@@ -49,6 +49,7 @@ struct GemmArgs {
   // kOut: out[n][m]; kSum: sum[split][n][m]
   void *out;
   long long out_ld;                // elements
+  int whole_rows;                  // kOut: m is a multiple of 8, rows begin at multiples of 16 bytes
   const float *scale;
   float *sum;
   int add;
@@ -133,6 +134,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   const int total = G.kblocks * G.terms, per = (total + G.splits - 1) / G.splits;
   const int first = blockIdx.y * per, last = first + per < total ? first + per : total;
   int kb = first / G.terms, term = first - kb * G.terms;
+  // Narrow tiles read A, once, from memory: each begins at another k, or all would ask the few channels that hold one k of rows a power of two apart.
+  if (TN <= 64 && !TURN && G.splits == 1) kb = (int)((unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks);
   auto load = [&](char *s) {
     const int qa = kPlanesA >> 2 * term & 3, qb = kPlanesB >> 2 * term & 3;
     const int here = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64;      // rows of k that A has; what lies behind them reads as zeros
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], TURN ? 0 : kb * 128);
 #pragma unroll
     for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], kb * 128);
-    if (++term == G.terms) term = 0, ++kb;
+    if (++term == G.terms) term = 0, kb = kb + 1 == G.kblocks ? 0 : kb + 1;
   };
 
   floatx16 acc[MT][NT];
@@ -411,6 +414,34 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   } else {
     float scale = 1.f;
     if (EPI == kOut) scale = *G.scale;
+    if constexpr (EPI == kOut && sizeof(OutT) == 2) {
+      if (G.whole_rows) {              // 16-byte steps: the results leave in whole rows, as dz does
+        constexpr int BYTES = 32 * MT * 32 * NT * 2, FIT = SLICE / BYTES, PM = 4 * MT;
+        char *own = (wave < FIT ? s0 : s1) + (wave < FIT ? wave : wave - FIT) * BYTES;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 2 * MT; ++i) {
+            const int row = 32 * j + r32, piece = (h * 2 * MT + i) ^ (row & (PM - 1));
+            OutT y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = static_cast<OutT>(acc[i / 2][j][i % 2 * 8 + e] * scale);
+            uintx4 w;
+            __builtin_memcpy(&w, y, 16);
+            *reinterpret_cast<uintx4 *>(own + row * (PM * 16) + piece * 16) = w;
+          }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 32 * NT * PM / 64; ++t) {
+          const int row = t * (64 / PM) + lane / PM, piece = lane % PM;
+          const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PM * 16) + (piece ^ (row & (PM - 1))) * 16);
+          const int n = n0 + wn * (NT * 32) + row, m = m0 + wm * (MT * 32) + piece * 8;
+          if (n < G.b.rows && m < G.m) *reinterpret_cast<uintx4 *>(static_cast<char *>(G.out) + (n * G.out_ld + m) * 2) = w;
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int n = n1 + 32 * j;

@@ -139,24 +139,34 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int pa
   loss[n] = label >= 0 ? x - at_label[n] : 0.f;
 }
 
-// out[n][m] = scale * sum over the splits, in order
-template <typename T>
+// out[n][m] = scale * sum over the splits: eight numbers a thread.  With many splits GROUPS threads share them, and their sums are added in order.
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int splits, int rows, int cols, const float *scale, T *out, long long stride) {
-  const int per = (cols + 7) / 8;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (long long)rows * per) return;
-  const long long row = i / per;
-  const int c = (int)(i - row * per) * 8;
+  constexpr int LANES = 256 / GROUPS;
+  __shared__ float part[GROUPS][LANES][9];
+  const int per = (cols + 7) / 8, lane = threadIdx.x % LANES, g = threadIdx.x / LANES;
+  const long long i = (long long)blockIdx.x * LANES + lane, row = i / per;
+  const int c = (int)(i - row * per) * 8, left = i < (long long)rows * per ? cols - c : 0;
   float x[8] = {};
-  for (int k = 0; k < splits; ++k) {
+  for (int k = g; k < splits; k += GROUPS) {
     float y[8];
-    load_n<float, 8>(sum + ((long long)k * rows + row) * cols + c, cols - c, y);
+    load_n<float, 8>(sum + ((long long)k * rows + row) * cols + c, left, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
+  if constexpr (GROUPS > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[g][lane][e] = x[e];
+    __syncthreads();
+    if (g) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += part[k][lane][e];
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= *scale;
-  store_n<T, 8>(out + row * stride + c, cols - c, x);
+  store_n<T, 8>(out + row * stride + c, left, x);
 }
 
 // ---------------------------------------------------------------------------------------------------------- the plan
@@ -165,8 +175,9 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int 
 struct Shape {
   int tm, tn;
 };
-constexpr Shape kShapes[4] = {{256, 256}, {128, 128}, {64, 64}, {128, 64}};
+constexpr Shape kShapes[6] = {{256, 256}, {128, 128}, {64, 64}, {128, 64}, {128, 32}, {128, 128}};
 constexpr int kFull = 192;           // tiles that count as enough
+constexpr int kShortSum = 4;         // slices of a sum that is over before the next tile's operands are there
 
 inline long long tiles_of(int shape, long long m, long long n) { return cdiv64(m, kShapes[shape].tm) * cdiv64(n, kShapes[shape].tn); }
 
@@ -178,7 +189,8 @@ inline int splits_of(int shape, long long m, long long n, int slices) {
 }
 
 inline int pick_shape(long long m, long long n, int slices = 0) {
-  if (n <= 64 && m > 64 * kFull) return 3;
+  const int narrow = n <= 32 ? 4 : n <= 64 ? 3 : 0;
+  if (narrow) return tiles_of(narrow, m, n) * splits_of(narrow, m, n, slices) >= kFull ? narrow : 2;
   for (int shape = 0; shape < 2; ++shape)
     if (tiles_of(shape, m, n) * splits_of(shape, m, n, slices) >= kFull) return shape;
   return 2;
@@ -252,7 +264,10 @@ hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
       break;                         // kFewRows rows never have so many tiles
     case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
     case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
-    default: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
+    case 3: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
+    case 4: gemm_kernel<E, OutT, 128, 32, 4, 1, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
+    default:                         // a short sum: two workgroups to a compute unit, one stores while the other begins
+      if constexpr (EPI == kOut) gemm_kernel<E, OutT, 128, 128, 2, 2, 2, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
   }
   return hipGetLastError();
 }
@@ -321,10 +336,14 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
     D.kblocks = p.n_pad / 64, D.splits = 1;
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
-    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, pick_shape(d, n), st)) return e;
+    D.whole_rows = es == 2 && d % 8 == 0 && q.dweight_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(q.dweight_dev) & 15) == 0;
+    const int shape = pick_shape(d, n);
+    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, shape == 0 && D.kblocks * D.terms <= kShortSum ? 5 : shape, st)) return e;
   }
-  head_finish_kernel<T><<<(unsigned)cdiv64((long long)rows * ((d + 7) / 8), 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale),
-                                                                                               static_cast<T *>(q.dh_dev), q.dh_stride);
+  const long long eights = (long long)rows * ((d + 7) / 8);
+  T *dh = static_cast<T *>(q.dh_dev);
+  if (p.splits >= 8) head_finish_kernel<T, 8><<<(unsigned)cdiv64(eights, 32), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride);
+  else head_finish_kernel<T, 1><<<(unsigned)cdiv64(eights, 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride);
   return hipGetLastError();
 }
 
