@@ -135,7 +135,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   const int first = blockIdx.y * per, last = first + per < total ? first + per : total;
   int kb = first / G.terms, term = first - kb * G.terms;
   // Narrow tiles read A, once, from memory: each begins at another k, or all would ask the few channels that hold one k of rows a power of two apart.
-  if (TN <= 64 && !TURN && G.splits == 1) kb = (int)((unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks);
+  // Large tiles share what they read with the others on their die: the dies begin at different k.
+  if (!TURN && G.splits == 1) kb = (int)(TN <= 64 ? (unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks : (blockIdx.x & 7) * (unsigned)G.kblocks >> 3);
   auto load = [&](char *s) {
     const int qa = kPlanesA >> 2 * term & 3, qb = kPlanesB >> 2 * term & 3;
     const int here = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64;      // rows of k that A has; what lies behind them reads as zeros
