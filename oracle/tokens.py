@@ -41,9 +41,11 @@ def _softmax(z):
         return e / s, (top + np.log(s))[:, 0]
 
 
-def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0):
+def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0, pairs=False):
     """A dict: loss, lse, dh, dweight and their bounds.  half: what rounding dz to its type is off by at most, relative to the value; least: and absolutely, in units of the
-    largest row weight (a type without small numbers)."""
+    largest row weight (a type without small numbers).  pairs: the logits are products of pairs of fp16 terms: a number scaled to at most 2^14 is the sum of
+    its terms up to 2^-22 of itself (two roundings of 2^-11) and 2^-25 (half fp16's smallest step; the largest lies above 2^13: 2^-38 of it), and of
+    a product the terms' smallest part, 2^-22, is left out; three products are summed for each."""
     h, w, labels = np.asarray(h, np.float64), np.asarray(weight, np.float64), np.asarray(labels, np.int64)
     n, d = h.shape
     v = w.shape[0]
@@ -51,6 +53,10 @@ def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0):
     g = np.where(live, 1.0 if row_weight is None else np.asarray(row_weight, np.float64), 0.0)
     z = h @ w.T
     zerr = (2 * d + 32) * EPS32 * (np.abs(h) @ np.abs(w).T)
+    if pairs:
+        finite = lambda x: np.where(np.isfinite(x), np.abs(x), 0.0)                                  # noqa: E731
+        zerr = 3 * zerr + 3 * 2.0 ** -22 * (np.abs(h) @ np.abs(w).T)
+        zerr = zerr + 2.0 ** -38 * 1.01 * (finite(h).max() * np.abs(w).sum(1)[None] + finite(w).max() * np.abs(h).sum(1)[:, None])
     p, lse = _softmax(z)
     # the sum over v: a tile's lane adds up to 128 terms, then the tiles are joined; arguments are rounded, as are the exponentials
     spread = np.abs(z - lse[:, None])

@@ -9,8 +9,11 @@
 // An operand A with m contiguous is staged row of k by row of k and read by the transposing LDS read: in each group of 16 lanes, lane s gives
 // the address of four m of the k that is s / 4 from the first, and lane i receives the four k of the i-th m.
 //
-// fp32 operands come as three bf16 planes (x = x1 + x2 + x3 exactly); the product is the sum of the six plane products that matter
-// (what is left out is below 2^-24 of |a||b|).  A slice's plane products follow each other: each plane is read from the caches but once.
+// fp32 operands come in planes of 16-bit terms, and the product is the sum of the plane products that matter.  Where the numbers' relative size to the
+// tensor's largest is all that counts (logits), two fp16 terms of x 2^s, s such that the largest lies near 2^14: what is left out is below
+// 2^-20 of |a||b| and 2^-38 of the largest; three products.  Where small numbers count by themselves (gradients of rare tokens), three
+// bf16 terms (x = x1 + x2 + x3 exactly, left out: 2^-24 of |a||b|); six products.  A slice's plane products follow each other: each plane is read from
+// memory but once.
 #pragma once
 #include <type_traits>
 
@@ -32,10 +35,19 @@ struct Operand {
 
 enum { kStats, kDz, kOut, kSum };    // what becomes of a tile
 
+// Planes of A and B in each product, two bits each from the lowest on.
+struct Planes {
+  int terms, a, b;
+};
+constexpr Planes kOne = {1, 0, 0}, kTwoOfB = {2, 0, 0 | 1 << 2}, kPairs = {3, 0 | 0 << 2 | 1 << 4, 0 | 1 << 2 | 0 << 4},
+                 kTriples = {6, 0 << 0 | 0 << 2 | 0 << 4 | 1 << 6 | 1 << 8 | 2 << 10, 0 << 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10};
+
 struct GemmArgs {
   Operand a, b;
   int m;                           // of the result; n is b.rows
-  int kblocks, terms;              // slices of 64 in a plane, products of planes: 1, 2 (B has two) or 6 (both have three)
+  int kblocks;                     // slices of 64 in a plane
+  Planes planes;
+  const unsigned *tops;            // kStats, kDz: bits of the largest numbers that A and B were scaled by; null: they were not
   int tiles_m, tiles_n, splits;    // splits: parts of the sum over k, kSum only
   // kStats, kDz: m is a place in the vocabulary, n a row of h
   const void *labels;              // of 32 or 64 bits; outside 0..vocab-1: none
@@ -79,10 +91,14 @@ __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-constexpr int kPlanesA = 0 << 0 | 0 << 2 | 0 << 4 | 1 << 6 | 1 << 8 | 2 << 10;   // of the products, two bits each; the first two are those of a single plane A
-constexpr int kPlanesB = 0 << 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+// The power of two that brings numbers of at most `top` (its bits) below 2^14.
+__device__ __forceinline__ float scale_of(unsigned bits) {
+  const float top = __builtin_bit_cast(float, bits);
+  const int e = top > 0.f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+  return ldexpf(1.f, e < 126 ? e > -126 ? e : -126 : 126);
+}
 
-// OutT: the type of kOut's result.  PLANES: of dz (2: 16-bit types in two terms; 3: fp32 in three bf16 terms).  TURN: A has m contiguous.
+// OutT: the type of kOut's result, and of dz.  PLANES: of dz (2: 16-bit types in two terms; 3: fp32 in three bf16 terms).  TURN: A has m contiguous.
 template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES, bool TURN>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 32, NT = TN / WN / 32;
@@ -131,14 +147,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   const int bytes_b = (rows_b - 1) * (int)G.b.ld + G.kblocks * 128;
 
   // this workgroup's slices
-  const int total = G.kblocks * G.terms, per = (total + G.splits - 1) / G.splits;
+  const int total = G.kblocks * G.planes.terms, per = (total + G.splits - 1) / G.splits;
   const int first = blockIdx.y * per, last = first + per < total ? first + per : total;
-  int kb = first / G.terms, term = first - kb * G.terms;
+  int kb = first / G.planes.terms, term = first - kb * G.planes.terms;
   // Narrow tiles read A, once, from memory: each begins at another k, or all would ask the few channels that hold one k of rows a power of two apart.
   // Large tiles share what they read with the others on their die: the dies begin at different k.
   if (!TURN && G.splits == 1) kb = (int)(TN <= 64 ? (unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks : (blockIdx.x & 7) * (unsigned)G.kblocks >> 3);
   auto load = [&](char *s) {
-    const int qa = kPlanesA >> 2 * term & 3, qb = kPlanesB >> 2 * term & 3;
+    const int qa = G.planes.a >> 2 * term & 3, qb = G.planes.b >> 2 * term & 3;
     const int here = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64;      // rows of k that A has; what lies behind them reads as zeros
     const char *from = pa + qa * G.a.plane + (TURN ? kb * 64 * G.a.ld : 0);
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, TURN ? (here - 1) * (int)G.a.ld + (G.a.cols - m0) * 2 : bytes_a, 0x00020000);
@@ -148,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], TURN ? 0 : kb * 128);
 #pragma unroll
     for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], kb * 128);
-    if (++term == G.terms) term = 0, kb = kb + 1 == G.kblocks ? 0 : kb + 1;
+    if (++term == G.planes.terms) term = 0, kb = kb + 1 == G.kblocks ? 0 : kb + 1;
   };
 
   floatx16 acc[MT][NT];
@@ -274,6 +290,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     }
   }
   const bool edge = m0 + TM > G.m;                  // the vocabulary ends in this tile
+  float unit = 1.f;                                 // of the results
+  if constexpr (EPI == kStats || EPI == kDz) unit = G.tops ? 1.f / (scale_of(G.tops[0]) * scale_of(G.tops[1])) : 1.f;
+  const float unit2 = unit * kLog2e;
   if constexpr (EPI == kStats) {
     float *red = reinterpret_cast<float *>(s0);        // [WM][TN] pairs, once everybody is done with the slices
     __syncthreads();
@@ -287,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (at == 16 * i + e) mine = acc[i][j][e];
-        G.at_label[n] = mine;
+        G.at_label[n] = mine * unit;
       }
       if (edge) {
 #pragma unroll
@@ -302,13 +321,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float ref = top == -__builtin_inff() ? 0.f : top * kLog2e;
+      const float ref = top == -__builtin_inff() ? 0.f : top * unit2;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -ref));
+        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], unit2, -ref));
       sum += __shfl_xor(sum, 32, 64);
-      if (h == 0) red[(wm * TN + n - n0) * 2] = top, red[(wm * TN + n - n0) * 2 + 1] = sum;
+      if (h == 0) red[(wm * TN + n - n0) * 2] = top * unit, red[(wm * TN + n - n0) * 2 + 1] = sum;
     }
     __syncthreads();
     for (int n = tid; n < TN && n0 + n < G.b.rows; n += THREADS) {
@@ -332,7 +351,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = g[j] * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -lse[j]));
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = g[j] * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], unit2, -lse[j]));
       if (__any(hit)) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -358,7 +377,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     for (int k = 0; k < PLANES; ++k) {
       // a word has two m of one n, in their order: word(j, 8 i + e) is of tile i
       auto word_of = [&](int j, int w) {
-        const E y[2] = {static_cast<E>(acc[w / 8][j][w % 8 * 2]), static_cast<E>(acc[w / 8][j][w % 8 * 2 + 1])};
+        const OutT y[2] = {static_cast<OutT>(acc[w / 8][j][w % 8 * 2]), static_cast<OutT>(acc[w / 8][j][w % 8 * 2 + 1])};
         unsigned x;
         __builtin_memcpy(&x, y, 4);
         return x;
@@ -399,7 +418,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
           *reinterpret_cast<unsigned *>(own + row * (PN * 16) + ((word >> 2) ^ swap_n(row)) * 16 + (word & 3) * 4) = __builtin_amdgcn_perm(other, mine, select);
           if (PLANES > 1)                                // what this plane leaves to the next
 #pragma unroll
-            for (int u = 0; u < 2; ++u) acc[e / 8][j][e % 8 * 2 + u] -= static_cast<float>(static_cast<E>(acc[e / 8][j][e % 8 * 2 + u]));
+            for (int u = 0; u < 2; ++u) acc[e / 8][j][e % 8 * 2 + u] -= static_cast<float>(static_cast<OutT>(acc[e / 8][j][e % 8 * 2 + u]));
         }
       }
       asm volatile("" ::: "memory");

@@ -10,6 +10,8 @@
 // dz is rounded to the operands' type, which is an error of the size that rounding the gradients has anyway (half a step of a
 // value, averaged over the sum); for few rows it is kept in two terms.  It is formed with row weights times a power of two that puts the largest near 2^15: fp16 keeps
 // probabilities down to 2^-24 / 2^15 of it.  fp32 is kept in three bf16 terms.
+#include <type_traits>
+
 #include "head_gemm.h"
 
 namespace pbkd {
@@ -20,6 +22,9 @@ using namespace head;
 constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
 // Up to here dz is kept in two terms: a few rows' rounding errors do not average out, and the products wait for W anyway.
 constexpr int kFewRows = 64;
+// From here on (rows x vocabulary x width) fp32 logits come from pairs of fp16 terms, three products instead of six of triples: 4096 x 32768 x 1024 with
+// gradients 7.10 -> 6.16 ms, losses alone 1.46 -> 0.93 ms.  Below, looking for the largest numbers costs more than it saves: 500 x 1013 x 515 73 -> 90 us.
+constexpr double kPairsFrom = 1e10;
 constexpr double kPieceBytes = 600e6;        // dz of a piece, both layouts
 
 inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
@@ -63,6 +68,8 @@ struct LayArgs {
   long long stride;        // elements between the source's rows
   char *rows_dst, *cols_dst;                    // null: not wanted
   long long rows_ld, rows_plane, cols_ld, cols_plane;    // bytes
+  char *pairs_dst;         // of fp32: like rows_dst, in two fp16 terms of the number times scale_of(*top)
+  const unsigned *top;
   const void *labels;      // rows without a label become zeros in cols_dst; null: none do
   int wide, vocab;
   int rows, cols, cols_fill, rows_fill;         // of the source; zeros behind the ends up to *_fill
@@ -78,6 +85,21 @@ __global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
     const int r = k * 32 + tid / 8, c = tid % 8 * 8, row = r0 + r;
     float x[8] = {};
     if (row < A.rows) load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c0 + c, A.cols - c0 - c, x);
+    if constexpr (sizeof(T) == 4) {
+      if (A.pairs_dst && row < A.rows && c0 + c < A.cols_fill) {
+        const float scale = scale_of(*A.top);
+        f16 y[2][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[0][e] = static_cast<f16>(x[e] * scale), y[1][e] = static_cast<f16>(x[e] * scale - static_cast<float>(y[0][e]));
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          uintx4 w;
+          __builtin_memcpy(&w, y[p], 16);
+          *reinterpret_cast<uintx4 *>(A.pairs_dst + p * A.rows_plane + row * A.rows_ld + (c0 + c) * 2) = w;
+        }
+      }
+      if (!A.rows_dst && !A.cols_dst) continue;
+    }
     const bool live = row < A.rows && (!A.labels || label_of(A.labels, A.wide, A.vocab, row) >= 0);
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
@@ -109,6 +131,27 @@ __global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
       *reinterpret_cast<uintx4 *>(A.cols_dst + p * A.cols_plane + (c0 + c) * A.cols_ld + (r0 + r) * 2) = w;
     }
   }
+}
+
+// tops[at] = bits of the largest finite magnitude: as integers they compare like the numbers.
+__global__ void head_clear_kernel(unsigned *tops) {
+  if (threadIdx.x < 2) tops[threadIdx.x] = 0;
+}
+
+__global__ __launch_bounds__(256) void head_top_kernel(const float *src, long long stride, int rows, int cols, unsigned *top) {
+  __shared__ float red[4];
+  float most = 0.f;
+  for (int r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
+      float x[8];
+      load_n<float, 8>(src + r * stride + c, cols - c, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fabsf(x[e]) < __builtin_inff() ? fmaxf(most, fabsf(x[e])) : most;
+    }
+  most = wave64_max(most);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) atomicMax(top, __builtin_bit_cast(unsigned, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]))));
 }
 
 // A workgroup joins a row's pairs, in an order that only their number decides.
@@ -197,9 +240,10 @@ inline int pick_shape(long long m, long long n, int slices = 0) {
 }
 
 struct Plan {
-  int d_pad, n_pad, piece, pieces, planes, terms, dz_planes, dz_terms, parts, first_shape, sum_shape, splits;
-  bool pack_h, pack_w;
-  size_t gs, scale, lse, at_label, part, h, ht, w, dz, dzt, sum, bytes;
+  int d_pad, n_pad, piece, pieces, planes, dz_planes, parts, first_shape, sum_shape, splits;
+  bool pack_h, pack_w, pairs;
+  Planes logits, grads;
+  size_t gs, scale, tops, lse, at_label, part, h, ht, w, wpairs, dz, dzt, sum, bytes;
 };
 
 bool direct(const void *p, long long stride, int d, int dtype) {
@@ -209,12 +253,15 @@ bool direct(const void *p, long long stride, int d, int dtype) {
 // pack_*: whether the operands have to be laid out (the workspace is counted as if they had)
 Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w) {
   Plan p;
-  p.planes = dtype == PBKD_F32 ? 3 : 1, p.terms = dtype == PBKD_F32 ? 6 : 1;
-  p.dz_planes = dtype == PBKD_F32 ? 3 : rows <= kFewRows ? 2 : 1, p.dz_terms = dtype == PBKD_F32 ? 6 : p.dz_planes;
+  const bool f32 = dtype == PBKD_F32;
+  p.pairs = f32 && (double)rows * vocab * d >= kPairsFrom;
+  p.logits = p.pairs ? kPairs : f32 ? kTriples : kOne;         // products of planes for the logits, and for the gradients
+  p.planes = f32 ? 3 : 1, p.dz_planes = f32 ? 3 : rows <= kFewRows ? 2 : 1;
+  p.grads = f32 ? kTriples : rows <= kFewRows ? kTwoOfB : kOne;
   p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
   p.pack_h = pack_h, p.pack_w = pack_w;
   // A piece's tiles of 256 x 256 fill whole rounds of the chip where that leaves pieces of a sensible size: 16 rows of tiles, 16 columns.
-  const double most = kPieceBytes / (gradients ? 4.0 * p.dz_planes * p.n_pad : 2.0 * p.planes * p.d_pad);
+  const double most = kPieceBytes / (gradients ? 4.0 * p.dz_planes * p.n_pad : 4.0 * p.d_pad);
   long long unit = cdiv64(rows, 256);
   unit = (unit & -unit) < 256 ? 256 / (unit & -unit) * 256 : 256;
   if (unit > most / 2) unit = 256;
@@ -227,7 +274,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   p.pieces = (int)cdiv64(vocab, p.piece);
   p.first_shape = pick_shape(p.piece, rows);
   // dh: few tiles, a long sum
-  const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.dz_terms;
+  const int slices = up64(p.piece < vocab ? p.piece : vocab) / 64 * p.grads.terms;
   p.sum_shape = pick_shape(d, rows, slices);
   p.splits = splits_of(p.sum_shape, d, rows, slices);
   p.parts = (int)cdiv64(vocab, kShapes[p.first_shape].tm) + p.pieces;
@@ -238,10 +285,12 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
     return here;
   };
   const size_t R = rows, e = 2 * p.planes;
-  p.gs = put(R * 4), p.scale = put(4), p.lse = put(R * 4), p.at_label = put(R * 4);
+  p.gs = put(R * 4), p.scale = put(4), p.tops = put(8), p.lse = put(R * 4), p.at_label = put(R * 4);
   p.part = put(R * p.parts * 8);
-  p.h = put(pack_h ? R * p.d_pad * e : 0);
-  p.w = put(pack_w ? (size_t)p.piece * p.d_pad * e : 0);
+  // pairs: h as pairs only, W both ways
+  p.h = put(pack_h ? R * p.d_pad * (p.pairs ? 4 : e) : 0);
+  p.w = put(pack_w && (gradients || !p.pairs) ? (size_t)p.piece * p.d_pad * e : 0);
+  p.wpairs = put(p.pairs ? (size_t)p.piece * p.d_pad * 4 : 0);
   if (gradients) {
     p.ht = put((size_t)d * p.n_pad * e);
     p.dz = put(R * p.piece * 2 * p.dz_planes);
@@ -282,7 +331,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   const int wide = q.index_dtype == PBKD_I64;
   auto lay = [&](LayArgs L) {
     L.wide = wide, L.vocab = V;
-    const int r = L.cols_dst ? L.rows_fill : L.rows, c = L.rows_dst ? L.cols_fill : L.cols;
+    const int r = L.cols_dst ? L.rows_fill : L.rows, c = L.rows_dst || L.pairs_dst ? L.cols_fill : L.cols;
     head_lay_kernel<T, E, PLANES><<<dim3((r + 63) / 64, (c + 63) / 64), 256, 0, st>>>(L);
   };
   if (gradients) {
@@ -290,23 +339,31 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     if (wide) head_rows_kernel<long long><<<1, 1024, 0, st>>>(R);
     else head_rows_kernel<int><<<1, 1024, 0, st>>>(R);
   }
+  constexpr bool F32 = es == 4;
+  unsigned *tops = reinterpret_cast<unsigned *>(ws + p.tops);         // W's, h's
+  if constexpr (F32) if (p.pairs) {
+    head_clear_kernel<<<1, 64, 0, st>>>(tops);
+    head_top_kernel<<<V < 2048 ? V : 2048, 256, 0, st>>>(static_cast<const float *>(q.weight_dev), q.weight_stride, V, d, tops);
+    head_top_kernel<<<rows < 2048 ? rows : 2048, 256, 0, st>>>(static_cast<const float *>(q.h_dev), q.h_stride, rows, d, tops + 1);
+  }
   Operand H{static_cast<const char *>(q.h_dev), q.h_stride * es, 0, rows};
   if (p.pack_h || gradients) {
-    LayArgs L{q.h_dev, q.h_stride, p.pack_h ? ws + p.h : nullptr, gradients ? ws + p.ht : nullptr, p.d_pad * 2, (long long)rows * p.d_pad * 2, p.n_pad * 2,
-              (long long)d * p.n_pad * 2, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
+    LayArgs L{q.h_dev, q.h_stride, p.pack_h && !p.pairs ? ws + p.h : nullptr, gradients ? ws + p.ht : nullptr, p.d_pad * 2, (long long)rows * p.d_pad * 2, p.n_pad * 2,
+              (long long)d * p.n_pad * 2, p.pairs ? ws + p.h : nullptr, tops + 1, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
     lay(L);
-    if (p.pack_h) H = Operand{L.rows_dst, L.rows_ld, L.rows_plane, rows};
+    if (p.pack_h) H = Operand{ws + p.h, L.rows_ld, L.rows_plane, rows};
   }
-  // Rows v0 .. v0 + n of W, as they lie or laid out (a piece that is the whole vocabulary is laid out once).
+  // Rows v0 .. v0 + n of W for the logits, as they lie or laid out (a piece that is the whole vocabulary is laid out once); fp32: and for h's gradient.
   auto weight = [&](int v0, int n, bool now) {
     const T *w = static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride;
     if (!p.pack_w) return Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n, d};
-    LayArgs L{w, q.weight_stride, ws + p.w, nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, 0, 0, nullptr, 0, 0, n, d, p.d_pad, 0};
+    LayArgs L{w, q.weight_stride, gradients || !p.pairs ? ws + p.w : nullptr, nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, 0, 0, p.pairs ? ws + p.wpairs : nullptr, tops,
+              nullptr, 0, 0, n, d, p.d_pad, 0};
     if (now) lay(L);
-    return Operand{ws + p.w, L.rows_ld, L.rows_plane, n, p.d_pad};
+    return Operand{ws + (p.pairs ? p.wpairs : p.w), L.rows_ld, L.rows_plane, n, p.d_pad};
   };
   GemmArgs G{};
-  G.b = H, G.kblocks = p.d_pad / 64, G.terms = p.terms, G.splits = 1;
+  G.b = H, G.kblocks = p.d_pad / 64, G.planes = p.logits, G.tops = p.pairs ? tops : nullptr, G.splits = 1;
   G.labels = q.labels_dev, G.wide = wide, G.vocab = V, G.lse = floats(p.lse), G.g = floats(p.gs), G.part = floats(p.part), G.at_label = floats(p.at_label);
   G.m_pad = G.n_pad = 0;
   int parts = 0;
@@ -314,7 +371,10 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   for (int v0 = 0; v0 < V; v0 += whole ? V : p.piece) {
     const int n = whole || V - v0 < p.piece ? V - v0 : p.piece;
     G.a = weight(v0, n, true), G.m = n, G.v0 = v0, G.parts = p.parts, G.part0 = parts;
-    if (const hipError_t e = launch_gemm<E, T, kStats, 1>(G, p.first_shape, st)) return e;
+    hipError_t e = hipSuccess;
+    if constexpr (F32) e = p.pairs ? launch_gemm<f16, E, kStats, 1>(G, p.first_shape, st) : launch_gemm<E, E, kStats, 1>(G, p.first_shape, st);
+    else e = launch_gemm<E, E, kStats, 1>(G, p.first_shape, st);
+    if (e) return e;
     parts += (int)cdiv64(n, kShapes[p.first_shape].tm);
   }
   head_lse_kernel<<<rows, 256, 0, st>>>(floats(p.part), parts, p.parts, q.labels_dev, wide, V, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev);
@@ -327,10 +387,15 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     G.dz = ws + p.dz, G.dz_ld = p.piece * 2, G.dz_plane = (long long)rows * p.piece * 2;
     G.dzt = ws + p.dzt, G.dzt_ld = p.n_pad * 2, G.dzt_plane = (long long)p.piece * p.n_pad * 2;
     G.m_pad = n64, G.n_pad = p.n_pad;
-    if (const hipError_t e = PLANES == 1 && p.dz_planes == 2 ? launch_gemm<E, T, kDz, 2>(G, p.first_shape, st) : launch_gemm<E, T, kDz, PLANES>(G, p.first_shape, st)) return e;
+    hipError_t e = hipSuccess;
+    if constexpr (F32) e = p.pairs ? launch_gemm<f16, E, kDz, PLANES>(G, p.first_shape, st) : launch_gemm<E, E, kDz, PLANES>(G, p.first_shape, st);
+    else e = p.dz_planes == 2 ? launch_gemm<E, E, kDz, 2>(G, p.first_shape, st) : launch_gemm<E, E, kDz, 1>(G, p.first_shape, st);
+    if (e) return e;
     GemmArgs D{};
-    D.terms = p.dz_terms, D.scale = floats(p.scale);
-    D.a = G.a, D.m = d, D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
+    D.planes = p.grads, D.scale = floats(p.scale);
+    D.a = G.a, D.m = d;
+    if (p.pairs) D.a.p = ws + p.w;                       // laid out alike, in three terms
+    D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
     D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
     if (const hipError_t e = launch_gemm<E, T, kSum, 1, true>(D, p.sum_shape, st)) return e;
     D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
@@ -338,7 +403,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
     D.whole_rows = es == 2 && d % 8 == 0 && q.dweight_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(q.dweight_dev) & 15) == 0;
     const int shape = pick_shape(d, n);
-    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, shape == 0 && D.kblocks * D.terms <= kShortSum ? 5 : shape, st)) return e;
+    if (const hipError_t e = launch_gemm<E, T, kOut, 1>(D, shape == 0 && D.kblocks * D.planes.terms <= kShortSum ? 5 : shape, st)) return e;
   }
   const long long eights = (long long)rows * ((d + 7) / 8);
   T *dh = static_cast<T *>(q.dh_dev);

@@ -163,7 +163,7 @@ def _check_head(torch, pb, h, w, labels, g, dtype, what, gradients=True, out=Non
     for a, b in zip(*results):
         assert a is None or torch.equal(a, b), "the same bits again"
     loss, lse, dh, dw = results[0]
-    r = otk.head_loss(_np(h), _np(w), labels.cpu().numpy(), None if g is None else _np(g), HALF[dtype], 2.0 ** -38 if dtype == "f16" else 0.0)
+    r = otk.head_loss(_np(h), _np(w), labels.cpu().numpy(), None if g is None else _np(g), HALF[dtype], 2.0 ** -38 if dtype == "f16" else 0.0, pairs=dtype == "f32" and rows * vocab * d >= 1e10)
     _within(_np(loss), r["loss"], r["loss_err"], "loss")
     _within(_np(lse), r["lse"], r["lse_err"], "lse")
     if gradients:
@@ -224,6 +224,21 @@ def test_head_loss_far_logits(gpu):
     h *= 100.0
     labels[:20] = (h[:20] @ w.t()).argmax(1)
     _check_head(torch, pb, h, w, labels, None, "f32", "far logits")
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e12, 1e18])
+def test_head_loss_numbers_of_any_size(gpu, size):
+    """fp32 operands of large calls are scaled for the logits: tiny and huge ones whose products are ordinary, rows of far smaller numbers beside
+    them, zeros; small calls do without."""
+    torch, pb = gpu
+    for rows, vocab, d in ((40, 500, 96), (1210, 2730, 3040)):
+        h, w, labels, g = _head_inputs(torch, rows, vocab, d, "f32")
+        h, w = h * size, w / size
+        h[:10] *= 2.0 ** -20
+        h[10], w[3] = 0.0, 0.0
+        _check_head(torch, pb, h, w, labels, g, "f32", ("sizes", size, rows))
+        if rows == 40 or size == 1e12:
+            _check_head(torch, pb, torch.zeros_like(h), w, labels, g, "f32", "zeros")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
