@@ -574,7 +574,7 @@ pbkd_status pbkd_head_loss(const pbkd_head_loss_desc *desc, void *hip_stream);
  *   q = softmax(teacher / T),   p = softmax(logits / T) over the whole vocabulary,   loss = T^2 * sum of q (log q - log p),
  * and, if dlogits_dev is given, dlogits = row_weight * T * (p - q), the gradient of row_weight * loss.  A row without pairs has loss 0
  * and gradient 0.  A place that occurs twice counts twice: its q are added.  row_weight_dev nullable: 1.  dlogits_dev may be logits_dev (same stride).
- * The teacher's logits have a type of their own.  rows >= 0, vocab >= 1, 1 <= top <= 1024 (PBKD_EUNSUPPORTED beyond, and for rows above 2^21); temperature > 0. */
+ * The teacher's logits have a type of their own.  rows >= 0, vocab >= 1, 1 <= top <= 1024 (PBKD_EUNSUPPORTED beyond, for rows above 2^21 and vocab above 2^30); temperature > 0. */
 typedef struct {
   long long rows;
   int vocab, top, dtype, teacher_dtype, index_dtype;

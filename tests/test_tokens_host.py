@@ -129,6 +129,7 @@ def test_library_refuses_bad_distillations():
     assert f(**{**ok, "_0": 0}) == pb.OK
     assert f(**{**ok, "_0": -1}) == pb.ESHAPE and f(**{**ok, "_1": 0}) == pb.ESHAPE and f(**{**ok, "_2": 0}) == pb.ESHAPE
     assert f(**{**ok, "_2": 1025}) == pb.EUNSUPPORTED and f(**{**ok, "_0": (1 << 21) + 1}) == pb.EUNSUPPORTED
+    assert f(**{**ok, "_1": (1 << 30) + 1, "_13": 1 << 31, "_14": 1 << 31}) == pb.EUNSUPPORTED
     assert f(**{**ok, "_3": 3}) == pb.EINVAL and f(**{**ok, "_4": 3}) == pb.EINVAL and f(**{**ok, "_5": 3}) == pb.EINVAL
     for bad in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
         assert f(**{**ok, "_6": bad}) == pb.EINVAL
