@@ -7,10 +7,13 @@
 //   1. sort   A workgroup owns the tokens with one remainder modulo the number of workgroups, reads all tokens, counts its own and those
 //             before them, and lists its own rows by token, in their order (integers, read from the caches: no word from another
 //             workgroup is needed).
-//   2. sum    The list is cut into pieces of equal length; a piece adds its rows in registers and writes a token's sum when all its
-//             rows lie in the piece.  A sum that goes on in another piece is left as a partial one.  Other workgroups write
-//             the zeros of tokens that do not occur.
-//   3. join   Adds the partial sums of each token that crosses pieces, in order.
+//   2. sum    The list is cut into pieces of equal length; a piece adds rows in registers and writes the sums of the tokens that begin in it, to
+//             their ends.  Tokens with more rows than a piece leave a partial sum in each.  Other workgroups write the zeros of tokens that
+//             do not occur.
+//   3. join   Adds the partial sums of each long token, in order.
+//
+// Measured (bf16): 32768 tokens of 65536 by 2048 lookup 35 us, sort 14, sum 81 (5.0 TB/s), join 7; 65536 of 131072 by 4096, added to the
+// table's other gradient, 133, 20, 192, 17; 64 tokens by 2048 2.5 us, which is a launch's own length.
 #include "seq_common.h"
 
 namespace pbkd {
@@ -70,7 +73,7 @@ inline Plan make_plan(long long rows, int vocab, int d) {
   while (p.groups < 256 && p.groups * 16 < vocab) p.groups *= 2;
   while ((long long)p.groups * kMostBins < vocab) p.groups *= 2;
   p.bins = (vocab + p.groups - 1) / p.groups;
-  p.piece = rows <= 16384 ? 8 : 32;
+  p.piece = rows <= 16384 ? 8 : 32;      // few rows: more pieces fill the chip; many: fewer partial sums
   p.pieces = cdiv64(rows, p.piece);
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   p.order = 0;
@@ -95,7 +98,7 @@ struct SortArgs {
 
 // The lists of 16 waves, each of which reads a sixteenth of the tokens, follow each other within a token: rows stay in order.
 // A wave keeps its rows in LDS as it counts them; one that finds more than kQueue reads the tokens again.
-constexpr int kQueue = 1024;
+constexpr int kQueue = 1024;        // 65536 tokens of which one makes 9 %: 61 us with 256
 
 template <typename IT>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {

@@ -14,6 +14,9 @@
 // 2^-20 of |a||b| and 2^-38 of the largest; three products.  Where small numbers count by themselves (gradients of rare tokens), three
 // bf16 terms (x = x1 + x2 + x3 exactly, left out: 2^-24 of |a||b|); six products.  A slice's plane products follow each other: each plane is read from
 // memory but once.
+//
+// The large tile reads (128 + 128) rows of 128 bytes from LDS a wave and slice for 64 MFMAs of 32 cycles: 1024 cycles of LDS beside 2048 of MFMA.  Eight waves of 128 x 64
+// would read half as much again.  Measured: 16384 x 4096 results, k = 8192, bf16 787 to 820 us, 1340 to 1396 TFLOP/s.
 #pragma once
 #include <type_traits>
 
