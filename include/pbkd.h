@@ -551,7 +551,7 @@ pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *desc, void *hip_stre
  * row_weight_dev nullable: 1.  lse_dev nullable.  What h holds in a row whose label names nothing has no influence on anything but that row's lse.
  * Products of 16-bit types run on the matrix cores with fp32 sums; dz is rounded to `dtype` before it is multiplied (up to 64 rows: kept in two
  * terms).  fp32 products are sums of six products of bf16 terms, off by 2^-24 of the products' magnitudes; the logits of calls with rows * vocab * d of 1e10 or
- * more are sums of three products of fp16 terms, off by 2^-20 and by 2^-38 of the tensors' largest numbers.
+ * more are sums of three products of fp16 terms, off by 2^-20 and by 2^-38 of the largest numbers of weight and of h's row.
  * workspace: pbkd_head_loss_workspace_bytes().  rows >= 0, vocab >= 1, d >= 1; PBKD_EUNSUPPORTED for rows above 2^21, vocab above 2^22, d above 65536. */
 typedef struct {
   long long rows;

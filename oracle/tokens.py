@@ -56,7 +56,7 @@ def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0, pairs=F
     if pairs:
         finite = lambda x: np.where(np.isfinite(x), np.abs(x), 0.0)                                  # noqa: E731
         zerr = 3 * zerr + 3 * 2.0 ** -22 * (np.abs(h) @ np.abs(w).T)
-        zerr = zerr + 2.0 ** -38 * 1.01 * (finite(h).max() * np.abs(w).sum(1)[None] + finite(w).max() * np.abs(h).sum(1)[:, None])
+        zerr = zerr + 2.0 ** -38 * 1.01 * (finite(h).max(1, keepdims=True) * np.abs(w).sum(1)[None] + finite(w).max() * np.abs(h).sum(1)[:, None])
     p, lse = _softmax(z)
     # the sum over v: a tile's lane adds up to 128 terms, then the tiles are joined; arguments are rounded, as are the exponentials
     spread = np.abs(z - lse[:, None])

@@ -50,7 +50,7 @@ struct GemmArgs {
   int m;                           // of the result; n is b.rows
   int kblocks;                     // slices of 64 in a plane
   Planes planes;
-  const unsigned *tops;            // kStats, kDz: bits of the largest numbers that A and B were scaled by; null: they were not
+  const unsigned *tops;            // kStats, kDz: bits of the largest numbers by which A, and each row of B, was scaled; null: they were not
   int tiles_m, tiles_n, splits;    // splits: parts of the sum over k, kSum only
   // kStats, kDz: m is a place in the vocabulary, n a row of h
   const void *labels;              // of 32 or 64 bits; outside 0..vocab-1: none
@@ -293,9 +293,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     }
   }
   const bool edge = m0 + TM > G.m;                  // the vocabulary ends in this tile
-  float unit = 1.f;                                 // of the results
-  if constexpr (EPI == kStats || EPI == kDz) unit = G.tops ? 1.f / (scale_of(G.tops[0]) * scale_of(G.tops[1])) : 1.f;
-  const float unit2 = unit * kLog2e;
+  float unit[NT];                                   // of the results
+  if constexpr (EPI == kStats || EPI == kDz) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) unit[j] = 1.f;
+    if (G.tops) {
+      const float a = scale_of(G.tops[0]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) unit[j] = 1.f / (a * scale_of(G.tops[1 + (n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1)]));
+    }
+  }
   if constexpr (EPI == kStats) {
     float *red = reinterpret_cast<float *>(s0);        // [WM][TN] pairs, once everybody is done with the slices
     __syncthreads();
@@ -309,7 +316,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (at == 16 * i + e) mine = acc[i][j][e];
-        G.at_label[n] = mine * unit;
+        G.at_label[n] = mine * unit[j];
       }
       if (edge) {
 #pragma unroll
@@ -318,6 +325,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
           for (int e = 0; e < 16; ++e)
             if (m1 + 16 * i + e >= G.m) acc[i][j][e] = -__builtin_inff();
       }
+      const float unit2 = unit[j] * kLog2e;
       float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -330,7 +338,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], unit2, -ref));
       sum += __shfl_xor(sum, 32, 64);
-      if (h == 0) red[(wm * TN + n - n0) * 2] = top * unit, red[(wm * TN + n - n0) * 2 + 1] = sum;
+      if (h == 0) red[(wm * TN + n - n0) * 2] = top * unit[j], red[(wm * TN + n - n0) * 2 + 1] = sum;
     }
     __syncthreads();
     for (int n = tid; n < TN && n0 + n < G.b.rows; n += THREADS) {
@@ -350,6 +358,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int at = label[j] - G.v0 - m1;
+      const float unit2 = unit[j] * kLog2e;
       const bool live = label[j] >= 0, hit = live && at >= 0 && at < 16 * MT;
 #pragma unroll
       for (int i = 0; i < MT; ++i)

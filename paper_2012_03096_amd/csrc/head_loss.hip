@@ -71,8 +71,9 @@ struct LayArgs {
   long long stride;        // elements between the source's rows
   char *rows_dst, *cols_dst;                    // null: not wanted
   long long rows_ld, rows_plane, cols_ld, cols_plane;    // bytes
-  char *pairs_dst;         // of fp32: like rows_dst, in two fp16 terms of the number times scale_of(*top)
+  char *pairs_dst;         // of fp32: like rows_dst, in two fp16 terms of the number times scale_of(top)
   const unsigned *top;
+  int top_step;            // 1: a scale for each row
   const void *labels;      // rows without a label become zeros in cols_dst; null: none do
   int wide, vocab;
   int rows, cols, cols_fill, rows_fill;         // of the source; zeros behind the ends up to *_fill
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
     if (row < A.rows) load_n<T, 8>(static_cast<const T *>(A.src) + row * A.stride + c0 + c, A.cols - c0 - c, x);
     if constexpr (sizeof(T) == 4) {
       if (A.pairs_dst && row < A.rows && c0 + c < A.cols_fill) {
-        const float scale = scale_of(*A.top);
+        const float scale = scale_of(A.top[row * A.top_step]);
         f16 y[2][8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[0][e] = static_cast<f16>(x[e] * scale), y[1][e] = static_cast<f16>(x[e] * scale - static_cast<float>(y[0][e]));
@@ -136,11 +137,13 @@ __global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
   }
 }
 
-// tops[at] = bits of the largest finite magnitude: as integers they compare like the numbers.
-__global__ void head_clear_kernel(unsigned *tops) {
-  if (threadIdx.x < 2) tops[threadIdx.x] = 0;
+// Bits of the largest finite magnitude of a matrix, or of each of its rows: as integers they compare like the numbers.  h is scaled row by row, so that no
+// row has to do with another.
+__global__ void head_clear_kernel(unsigned *top) {
+  if (threadIdx.x == 0) *top = 0;
 }
 
+template <bool ROWS>
 __global__ __launch_bounds__(256) void head_top_kernel(const float *src, long long stride, int rows, int cols, unsigned *top) {
   __shared__ float red[4];
   float most = 0.f;
@@ -154,7 +157,10 @@ __global__ __launch_bounds__(256) void head_top_kernel(const float *src, long lo
   most = wave64_max(most);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
   __syncthreads();
-  if (threadIdx.x == 0) atomicMax(top, __builtin_bit_cast(unsigned, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]))));
+  if (threadIdx.x) return;
+  const unsigned bits = __builtin_bit_cast(unsigned, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  if (ROWS) top[blockIdx.x] = bits;
+  else atomicMax(top, bits);
 }
 
 // A workgroup joins a row's pairs, in an order that only their number decides.
@@ -288,7 +294,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
     return here;
   };
   const size_t R = rows, e = 2 * p.planes;
-  p.gs = put(R * 4), p.scale = put(4), p.tops = put(8), p.lse = put(R * 4), p.at_label = put(R * 4);
+  p.gs = put(R * 4), p.scale = put(4), p.tops = put(p.pairs ? (R + 1) * 4 : 0), p.lse = put(R * 4), p.at_label = put(R * 4);
   p.part = put(R * p.parts * 8);
   // pairs: h as pairs only, W both ways
   p.h = put(pack_h ? R * p.d_pad * (p.pairs ? 4 : e) : 0);
@@ -343,16 +349,16 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     else head_rows_kernel<int><<<1, 1024, 0, st>>>(R);
   }
   constexpr bool F32 = es == 4;
-  unsigned *tops = reinterpret_cast<unsigned *>(ws + p.tops);         // W's, h's
+  unsigned *tops = reinterpret_cast<unsigned *>(ws + p.tops);         // W's, and each row's of h
   if constexpr (F32) if (p.pairs) {
     head_clear_kernel<<<1, 64, 0, st>>>(tops);
-    head_top_kernel<<<V < 2048 ? V : 2048, 256, 0, st>>>(static_cast<const float *>(q.weight_dev), q.weight_stride, V, d, tops);
-    head_top_kernel<<<rows < 2048 ? rows : 2048, 256, 0, st>>>(static_cast<const float *>(q.h_dev), q.h_stride, rows, d, tops + 1);
+    head_top_kernel<false><<<V < 2048 ? V : 2048, 256, 0, st>>>(static_cast<const float *>(q.weight_dev), q.weight_stride, V, d, tops);
+    head_top_kernel<true><<<rows, 256, 0, st>>>(static_cast<const float *>(q.h_dev), q.h_stride, rows, d, tops + 1);
   }
   Operand H{static_cast<const char *>(q.h_dev), q.h_stride * es, 0, rows};
   if (p.pack_h || gradients) {
     LayArgs L{q.h_dev, q.h_stride, p.pack_h && !p.pairs ? ws + p.h : nullptr, gradients ? ws + p.ht : nullptr, p.d_pad * 2, (long long)rows * p.d_pad * 2, p.n_pad * 2,
-              (long long)d * p.n_pad * 2, p.pairs ? ws + p.h : nullptr, tops + 1, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
+              (long long)d * p.n_pad * 2, p.pairs ? ws + p.h : nullptr, tops + 1, 1, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
     lay(L);
     if (p.pack_h) H = Operand{ws + p.h, L.rows_ld, L.rows_plane, rows};
   }
@@ -360,7 +366,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   auto weight = [&](int v0, int n, bool now) {
     const T *w = static_cast<const T *>(q.weight_dev) + v0 * q.weight_stride;
     if (!p.pack_w) return Operand{reinterpret_cast<const char *>(w), q.weight_stride * es, 0, n, d};
-    LayArgs L{w, q.weight_stride, gradients || !p.pairs ? ws + p.w : nullptr, nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, 0, 0, p.pairs ? ws + p.wpairs : nullptr, tops,
+    LayArgs L{w, q.weight_stride, gradients || !p.pairs ? ws + p.w : nullptr, nullptr, p.d_pad * 2, (long long)p.piece * p.d_pad * 2, 0, 0, p.pairs ? ws + p.wpairs : nullptr, tops, 0,
               nullptr, 0, 0, n, d, p.d_pad, 0};
     if (now) lay(L);
     return Operand{ws + (p.pairs ? p.wpairs : p.w), L.rows_ld, L.rows_plane, n, p.d_pad};

@@ -226,6 +226,23 @@ def test_head_loss_far_logits(gpu):
     _check_head(torch, pb, h, w, labels, None, "f32", "far logits")
 
 
+def test_head_loss_rows_do_not_scale_each_other(gpu):
+    """A large fp32 call: rows to be ignored hold NaN, infinities or numbers of 1e30; the others' results are those without them, bit for bit."""
+    torch, pb = gpu
+    rows, vocab, d = 1210, 2730, 3040
+    h, w, labels, g = _head_inputs(torch, rows, vocab, d, "f32")
+    labels[:40] = -1
+    results = []
+    for junk in (0.0, float("nan"), float("inf"), 1e30):
+        h[:40] = junk
+        out = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(w)
+        pb.head_loss(h, w, labels, out[0], _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, h.dtype, True)), lse=out[1], row_weight=g, dh=out[2], dweight=out[3])
+        results.append(out)
+    for out in results[1:]:
+        assert torch.equal(out[0], results[0][0]) and torch.equal(out[1][40:], results[0][1][40:]) and torch.equal(out[2], results[0][2]) and torch.equal(out[3], results[0][3])
+    assert bool((results[0][0][:40] == 0).all()) and bool((results[0][2][:40] == 0).all())
+
+
 @pytest.mark.parametrize("size", [1e-30, 1e-12, 1e12, 1e18])
 def test_head_loss_numbers_of_any_size(gpu, size):
     """fp32 operands of large calls are scaled for the logits: tiny and huge ones whose products are ordinary, rows of far smaller numbers beside
