@@ -33,7 +33,7 @@ struct Operand {
   const char *p;
   long long ld, plane;     // bytes between rows, between planes
   int rows;
-  int cols;                // A with m contiguous: numbers that a row (of one k) has
+  int cols;                // where k is not contiguous: numbers that a row (of one k) has
 };
 
 enum { kStats, kDz, kOut, kSum };    // what becomes of a tile
@@ -47,7 +47,7 @@ constexpr Planes kOne = {1, 0, 0}, kTwoOfB = {2, 0, 0 | 1 << 2}, kPairs = {3, 0 
 
 struct GemmArgs {
   Operand a, b;
-  int m;                           // of the result; n is b.rows
+  int m, n;                        // of the result
   int kblocks;                     // slices of 64 in a plane
   Planes planes;
   const unsigned *tops;            // kStats, kDz: bits of the largest numbers by which A, and each row of B, was scaled; null: they were not
@@ -58,9 +58,9 @@ struct GemmArgs {
   const float *lse, *g;            // g: 0 where there is no label
   float *part, *at_label;          // kStats: [n][parts] pairs (maximum, sum)
   int parts, part0, v0;            // v0: place of the piece's first row of A
-  char *dz, *dzt;                  // [n][m] and [m][n]
-  long long dz_ld, dz_plane, dzt_ld, dzt_plane;
-  int m_pad, n_pad;                // dz is written up to m_pad, dzt up to n_pad: zeros behind the ends
+  char *dz;                        // [n][m]
+  long long dz_ld, dz_plane;
+  int m_pad;                       // dz is written up to here: zeros behind the end
   // kOut: out[n][m]; kSum: sum[split][n][m]
   void *out;
   long long out_ld;                // elements
@@ -101,8 +101,8 @@ __device__ __forceinline__ float scale_of(unsigned bits) {
   return ldexpf(1.f, e < 126 ? e > -126 ? e : -126 : 126);
 }
 
-// OutT: the type of kOut's result, and of dz.  PLANES: of dz (2: 16-bit types in two terms; 3: fp32 in three bf16 terms).  TURN: A has m contiguous.
-template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES, bool TURN>
+// OutT: the type of kOut's result, and of dz.  PLANES: of dz (2: 16-bit types in two terms; 3: fp32 in three bf16 terms).  TURN_A: A has m contiguous; TURN_B: B has n contiguous.
+template <typename E, typename OutT, int TM, int TN, int WM, int WN, int STAGES, int EPI, int PLANES, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   constexpr int THREADS = 64 * WM * WN, MT = TM / WM / 32, NT = TN / WN / 32;
   constexpr int RA = TM * 8 / THREADS, RB = TN * 8 / THREADS, ROWS = THREADS / 8;     // rounds of loads, rows a round
@@ -123,13 +123,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   auto swz_a = [](int r) { return (r >> 1 & 3) | (r / (16 * MT) & 1) << 2; };
   auto swz_b = [](int r) { return r >> 1 & 7; };
   // of a row of k: the four that a group of lanes reads at once lie in different banks
+  auto swz_tb = [](int r) { return TN >= 128 ? (r & 3) << 2 : TN == 64 ? (r & 2) << 1 : 0; };
   auto swz_t = [](int r) { return MT == 4 ? (r & 3) << 1 : MT == 2 ? (r & 1) << 1 | (r & 2) << 2 : TM == 64 ? (r & 2) << 1 : (r & 3) << 2; };
   unsigned va[RA], vb[RB];
   {
     const int slot = tid & 7, r0 = tid >> 3;
 #pragma unroll
     for (int i = 0; i < RA; ++i) {
-      if constexpr (TURN) {
+      if constexpr (TURN_A) {
         const int at = (i * THREADS + tid) * 16, r = at / (TM * 2), left = G.a.cols / 8 - 1 - m0 / 8;
         const int piece = (at % (TM * 2) / 16) ^ swz_t(r);
         va[i] = (unsigned)(r * (int)G.a.ld + (piece < left ? piece : left) * 16);          // m behind the end: the last again
@@ -140,11 +141,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     }
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
-      const int r = i * ROWS + r0, row = n0 + r < G.b.rows ? r : G.b.rows - 1 - n0;
-      vb[i] = (unsigned)(row * (int)G.b.ld + (slot ^ swz_b(r)) * 16);
+      if constexpr (TURN_B) {
+        const int at = (i * THREADS + tid) * 16, r = at / (TN * 2), left = G.b.cols / 8 - 1 - n0 / 8;
+        const int piece = (at % (TN * 2) / 16) ^ swz_tb(r);
+        vb[i] = (unsigned)(r * (int)G.b.ld + (piece < left ? piece : left) * 16);
+      } else {
+        const int r = i * ROWS + r0, row = n0 + r < G.b.rows ? r : G.b.rows - 1 - n0;
+        vb[i] = (unsigned)(row * (int)G.b.ld + (slot ^ swz_b(r)) * 16);
+      }
     }
   }
-  const char *pa = TURN ? G.a.p + m0 * 2 : G.a.p + m0 * G.a.ld, *pb = G.b.p + n0 * G.b.ld;
+  const char *pa = G.a.p + (TURN_A ? m0 * 2 : m0 * G.a.ld), *pb = G.b.p + (TURN_B ? n0 * 2 : n0 * G.b.ld);
   const int rows_a = G.a.rows - m0 < TM ? G.a.rows - m0 : TM, rows_b = G.b.rows - n0 < TN ? G.b.rows - n0 : TN;
   const int bytes_a = (rows_a - 1) * (int)G.a.ld + G.kblocks * 128;
   const int bytes_b = (rows_b - 1) * (int)G.b.ld + G.kblocks * 128;
@@ -155,18 +162,19 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   int kb = first / G.planes.terms, term = first - kb * G.planes.terms;
   // Narrow tiles read A, once, from memory: each begins at another k, or all would ask the few channels that hold one k of rows a power of two apart.
   // Large tiles share what they read with the others on their die: the dies begin at different k.
-  if (!TURN && G.splits == 1) kb = (int)(TN <= 64 ? (unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks : (blockIdx.x & 7) * (unsigned)G.kblocks >> 3);
+  if (!TURN_A && G.splits == 1) kb = (int)(TN <= 64 ? (unsigned)(m0 / TM) * 7u % (unsigned)G.kblocks : (blockIdx.x & 7) * (unsigned)G.kblocks >> 3);
   auto load = [&](char *s) {
     const int qa = G.planes.a >> 2 * term & 3, qb = G.planes.b >> 2 * term & 3;
-    const int here = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64;      // rows of k that A has; what lies behind them reads as zeros
-    const char *from = pa + qa * G.a.plane + (TURN ? kb * 64 * G.a.ld : 0);
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, TURN ? (here - 1) * (int)G.a.ld + (G.a.cols - m0) * 2 : bytes_a, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pb + qb * G.b.plane), 0, bytes_b, 0x00020000);
+    // rows of k that an operand has here; what lies behind them reads as zeros
+    const int ka = G.a.rows - kb * 64 < 64 ? G.a.rows - kb * 64 : 64, kbb = G.b.rows - kb * 64 < 64 ? G.b.rows - kb * 64 : 64;
+    const char *fa = pa + qa * G.a.plane + (TURN_A ? kb * 64 * G.a.ld : 0), *fb = pb + qb * G.b.plane + (TURN_B ? kb * 64 * G.b.ld : 0);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(fa), 0, TURN_A ? (ka - 1) * (int)G.a.ld + (G.a.cols - m0) * 2 : bytes_a, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(fb), 0, TURN_B ? (kbb - 1) * (int)G.b.ld + (G.b.cols - n0) * 2 : bytes_b, 0x00020000);
     char *d = s + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], TURN ? 0 : kb * 128);
+    for (int i = 0; i < RA; ++i) load16_to_lds(ra, d + i * THREADS * 16, va[i], TURN_A ? 0 : kb * 128);
 #pragma unroll
-    for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], kb * 128);
+    for (int i = 0; i < RB; ++i) load16_to_lds(rb, d + TM * 128 + i * THREADS * 16, vb[i], TURN_B ? 0 : kb * 128);
     if (++term == G.planes.terms) term = 0, kb = kb + 1 == G.kblocks ? 0 : kb + 1;
   };
 
@@ -188,6 +196,11 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     const int r = k + turn_k, m = turn_m + 16 * i;
     return r * (TM * 2) + ((m >> 3) ^ swz_t(turn_k)) * 16 + (m & 7) * 2;         // k is a multiple of four: it does not change the swap
   };
+  // and its four n of tile j
+  auto turned_b = [&](int k, int j) {
+    const int r = k + turn_k, n = wn * (NT * 32) + (lane >> 4 & 1) * 16 + (lane & 3) * 4 + 32 * j;
+    return TM * 128 + r * (TN * 2) + ((n >> 3) ^ swz_tb(turn_k)) * 16 + (n & 7) * 2;
+  };
   // Operands of half a slice (two MFMA steps) wait in registers while the half before is multiplied.
   struct Half {
     uintx4 a[2][MT], b[2][NT];
@@ -196,9 +209,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int c = half * 4 + u * 2 + h;
+      if constexpr (TURN_B) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) f.b[u][j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 32 * j) * 128 + (c ^ sb) * 16);
-      if constexpr (TURN) {
+        for (int j = 0; j < NT; ++j) {
+          const uintx2 lo = read_turned(s + turned_b(half * 32 + u * 16, j)), hi = read_turned(s + turned_b(half * 32 + u * 16 + 4, j));
+          f.b[u][j] = uintx4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) f.b[u][j] = *reinterpret_cast<const uintx4 *>(s + TM * 128 + (row_b + 32 * j) * 128 + (c ^ sb) * 16);
+      }
+      if constexpr (TURN_A) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const uintx2 lo = read_turned(s + turned(half * 32 + u * 16, i)), hi = read_turned(s + turned(half * 32 + u * 16 + 4, i));
@@ -210,7 +231,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       }
     }
   };
-  constexpr int READS = 2 * ((TURN ? 2 : 1) * MT + NT);
+  constexpr int READS = 2 * ((TURN_A ? 2 : 1) * MT + (TURN_B ? 2 : 1) * NT);
   auto multiply = [&](const Half &f) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -281,15 +302,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     if (G.wide) {
       long long w[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[j] = static_cast<const long long *>(G.labels)[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
+      for (int j = 0; j < NT; ++j) w[j] = static_cast<const long long *>(G.labels)[n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.b.rows ? (int)w[j] : -1;
+      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.n ? (int)w[j] : -1;
     } else {
       int w[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[j] = static_cast<const int *>(G.labels)[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
+      for (int j = 0; j < NT; ++j) w[j] = static_cast<const int *>(G.labels)[n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.b.rows ? w[j] : -1;
+      for (int j = 0; j < NT; ++j) label[j] = w[j] >= 0 && w[j] < G.vocab && n1 + 32 * j < G.n ? w[j] : -1;
     }
   }
   const bool edge = m0 + TM > G.m;                  // the vocabulary ends in this tile
@@ -300,7 +321,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     if (G.tops) {
       const float a = scale_of(G.tops[0]);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) unit[j] = 1.f / (a * scale_of(G.tops[1 + (n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1)]));
+      for (int j = 0; j < NT; ++j) unit[j] = 1.f / (a * scale_of(G.tops[1 + (n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1)]));
     }
   }
   if constexpr (EPI == kStats) {
@@ -341,7 +362,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       if (h == 0) red[(wm * TN + n - n0) * 2] = top * unit[j], red[(wm * TN + n - n0) * 2 + 1] = sum;
     }
     __syncthreads();
-    for (int n = tid; n < TN && n0 + n < G.b.rows; n += THREADS) {
+    for (int n = tid; n < TN && n0 + n < G.n; n += THREADS) {
       float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
       for (int k = 0; k < WM; ++k) top = fmaxf(top, red[(k * TN + n) * 2]);
@@ -354,7 +375,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   } else if constexpr (EPI == kDz) {
     float lse[NT], g[NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) lse[j] = G.lse[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1] * kLog2e, g[j] = G.g[n1 + 32 * j < G.b.rows ? n1 + 32 * j : G.b.rows - 1];
+    for (int j = 0; j < NT; ++j) lse[j] = G.lse[n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1] * kLog2e, g[j] = G.g[n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int at = label[j] - G.v0 - m1;
@@ -379,7 +400,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
             if (!live || m1 + 16 * i + e >= G.m) acc[i][j][e] = 0.f;
       }
     }
-    // Both layouts leave through the wave's own part of LDS, in whole rows: a lane's own results would go out in pieces of 16 and of 2 bytes.
+    // dz leaves through the wave's own part of LDS, in whole rows: a lane's own results would go out in pieces of 16 bytes.
     constexpr int BYTES = 32 * MT * 32 * NT * 2, FIT = SLICE / BYTES;
     static_assert(FIT * 2 >= WM * WN, "the waves' tiles fit into two stages");
     char *own = (wave < FIT ? s0 : s1) + (wave < FIT ? wave : wave - FIT) * BYTES;
@@ -395,7 +416,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         return x;
       };
       // rows of n: 4 MT pieces of 16 bytes, swapped by the row's number
-      constexpr int PM = 4 * MT, PN = 4 * NT;
+      constexpr int PM = 4 * MT;
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         if (PLANES > 1) __builtin_amdgcn_sched_barrier(0);
@@ -405,6 +426,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
           *reinterpret_cast<uintx4 *>(own + row * (PM * 16) + piece * 16) =
               uintx4{word_of(j, 4 * i), word_of(j, 4 * i + 1), word_of(j, 4 * i + 2), word_of(j, 4 * i + 3)};
         }
+        if (PLANES > 1)                // what this plane leaves to the next
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+a"(acc[i][j]));          // rounded once more, or all the rounded values are kept and spill
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] -= static_cast<float>(static_cast<OutT>(acc[i][j][e]));
+          }
       }
       asm volatile("" ::: "memory");
 #pragma unroll
@@ -412,34 +441,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         const int row = t * (64 / PM) + lane / PM, piece = lane % PM;
         const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PM * 16) + (piece ^ (row & (PM - 1))) * 16);
         const int n = wave_n + row, m = wave_m + piece * 8;
-        if (n < G.b.rows && m < G.m_pad) *reinterpret_cast<uintx4 *>(G.dz + k * G.dz_plane + n * G.dz_ld + m * 2) = w;
-      }
-      asm volatile("" ::: "memory");
-      // rows of m: lanes of neighbouring n exchange halves, so that a word has two n of one m
-      const int odd = lane & 1;
-      const unsigned select = odd ? 0x03020706u : 0x05040100u;
-      auto swap_n = [](int m) { return NT == 4 ? ((m & 1) | (m / (16 * MT) & 1) << 1) << 2 : NT == 2 ? (m / (16 * MT) & 1) << 2 : 0; };
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if (PLANES > 1) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int e = 0; e < 8 * MT; ++e) {
-          if (PLANES > 1 && e % 8 == 0) asm volatile("" : "+a"(acc[e / 8][j]));      // rounded again, or the words of both passes are kept and spill
-          const unsigned mine = word_of(j, e), other = __builtin_amdgcn_update_dpp(0u, mine, 0xB1, 0xf, 0xf, true);
-          const int row = h * 16 * MT + 2 * e + odd, word = 16 * j + (r32 >> 1);
-          *reinterpret_cast<unsigned *>(own + row * (PN * 16) + ((word >> 2) ^ swap_n(row)) * 16 + (word & 3) * 4) = __builtin_amdgcn_perm(other, mine, select);
-          if (PLANES > 1)                                // what this plane leaves to the next
-#pragma unroll
-            for (int u = 0; u < 2; ++u) acc[e / 8][j][e % 8 * 2 + u] -= static_cast<float>(static_cast<OutT>(acc[e / 8][j][e % 8 * 2 + u]));
-        }
-      }
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int t = 0; t < 32 * MT * PN / 64; ++t) {
-        const int row = t * (64 / PN) + lane / PN, piece = lane % PN;
-        const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PN * 16) + (piece ^ swap_n(row)) * 16);
-        const int m = wave_m + row, n = wave_n + piece * 8;
-        if (m < G.m && n < G.n_pad) *reinterpret_cast<uintx4 *>(G.dzt + k * G.dzt_plane + m * G.dzt_ld + n * 2) = w;
+        if (n < G.n && m < G.m_pad) *reinterpret_cast<uintx4 *>(G.dz + k * G.dz_plane + n * G.dz_ld + m * 2) = w;
       }
       asm volatile("" ::: "memory");
     }
@@ -469,7 +471,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
           const int row = t * (64 / PM) + lane / PM, piece = lane % PM;
           const uintx4 w = *reinterpret_cast<const uintx4 *>(own + row * (PM * 16) + (piece ^ (row & (PM - 1))) * 16);
           const int n = n0 + wn * (NT * 32) + row, m = m0 + wm * (MT * 32) + piece * 8;
-          if (n < G.b.rows && m < G.m) *reinterpret_cast<uintx4 *>(static_cast<char *>(G.out) + (n * G.out_ld + m) * 2) = w;
+          if (n < G.n && m < G.m) *reinterpret_cast<uintx4 *>(static_cast<char *>(G.out) + (n * G.out_ld + m) * 2) = w;
         }
         return;
       }
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int n = n1 + 32 * j;
-      if (n >= G.b.rows) continue;
+      if (n >= G.n) continue;
 #pragma unroll
       for (int i = 0; i < 2 * MT; ++i) {
         const int m = m1 + 8 * i, left = G.m - m;
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         if constexpr (EPI == kOut) {
           store_n<OutT, 8>(static_cast<OutT *>(G.out) + n * G.out_ld + m, left, x);
         } else {
-          float *p = G.sum + ((long long)blockIdx.y * G.b.rows + n) * G.out_ld + m;
+          float *p = G.sum + ((long long)blockIdx.y * G.n + n) * G.out_ld + m;
           if (G.add) {
             float y[8];
             load_n<float, 8>(p, left, y);

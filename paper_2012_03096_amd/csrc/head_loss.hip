@@ -4,8 +4,8 @@
 //
 // Bound by its products of matrices: 2 N V d operations for the losses, and 6 N V d for the gradients, because z is not kept but formed
 // again, piece of the vocabulary by piece.  The first pass leaves a maximum and a sum of every tile's rows; they give lse.  In the
-// second a piece's dz comes out of the product in both layouts, n by v for dh and v by n for dW; W serves dh as it lies, by transposing
-// reads, and h's other layout is copied first (head_gemm.h).
+// second a piece's dz comes out of the product once, n by v: dh reads it along v with W as it lies, dW along n with a copy of h's other layout, by the
+// transposing reads of head_gemm.h.
 //
 // Measured (bf16): 8192 rows by 4096 over 131072 27.6 to 28.6 ms, 1230 to 1275 TFLOP/s over the four products (losses 6.9, dz 7.7, dh 7.3, dW 6.5); 4096 by 2048 over 65536 3.9
 // ms; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 74 us in eight launches.
@@ -28,7 +28,7 @@ constexpr int kFewRows = 64;
 // From here on (rows x vocabulary x width) fp32 logits come from pairs of fp16 terms, three products instead of six of triples: 4096 x 32768 x 1024 with
 // gradients 7.10 -> 6.16 ms, losses alone 1.46 -> 0.93 ms.  Below, looking for the largest numbers costs more than it saves: 500 x 1013 x 515 73 -> 90 us.
 constexpr double kPairsFrom = 1e10;
-constexpr double kPieceBytes = 600e6;        // dz of a piece, both layouts
+constexpr double kPieceBytes = 300e6;        // dz of a piece
 
 inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
 
@@ -252,7 +252,7 @@ struct Plan {
   int d_pad, n_pad, piece, pieces, planes, dz_planes, parts, first_shape, sum_shape, splits;
   bool pack_h, pack_w, pairs;
   Planes logits, grads;
-  size_t gs, scale, tops, lse, at_label, part, h, ht, w, wpairs, dz, dzt, sum, bytes;
+  size_t gs, scale, tops, lse, at_label, part, h, ht, w, wpairs, dz, sum, bytes;
 };
 
 bool direct(const void *p, long long stride, int d, int dtype) {
@@ -270,7 +270,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
   p.pack_h = pack_h, p.pack_w = pack_w;
   // A piece's tiles of 256 x 256 fill whole rounds of the chip where that leaves pieces of a sensible size: 16 rows of tiles, 16 columns.
-  const double most = kPieceBytes / (gradients ? 4.0 * p.dz_planes * p.n_pad : 4.0 * p.d_pad);
+  const double most = kPieceBytes / (gradients ? 2.0 * p.dz_planes * p.n_pad : 2.0 * p.d_pad);
   long long unit = cdiv64(rows, 256);
   unit = (unit & -unit) < 256 ? 256 / (unit & -unit) * 256 : 256;
   if (unit > most / 2) unit = 256;
@@ -303,7 +303,6 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
   if (gradients) {
     p.ht = put((size_t)d * p.n_pad * e);
     p.dz = put(R * p.piece * 2 * p.dz_planes);
-    p.dzt = put((size_t)p.piece * p.n_pad * 2 * p.dz_planes);
     p.sum = put((size_t)p.splits * R * d * 4);
   }
   p.bytes = at + 256;
@@ -311,21 +310,22 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
 }
 
 // --------------------------------------------------------------------------------------------------------- the launches
-template <typename E, typename OutT, int EPI, int PLANES, bool TURN = false>
+template <typename E, typename OutT, int EPI, int PLANES>
 hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
   const Shape &s = kShapes[shape];
-  G.tiles_m = (int)cdiv64(G.m, s.tm), G.tiles_n = (int)cdiv64(G.b.rows, s.tn);
+  constexpr bool TA = EPI == kSum, TB = EPI == kOut;       // dh reads W as it lies, dW reads dz
+  G.tiles_m = (int)cdiv64(G.m, s.tm), G.tiles_n = (int)cdiv64(G.n, s.tn);
   const dim3 grid(G.tiles_m * G.tiles_n, G.splits);
   switch (shape) {
     case 0:
-      if constexpr (PLANES != 2) gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
+      if constexpr (PLANES != 2) gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G);
       break;                         // kFewRows rows never have so many tiles
-    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
-    case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
-    case 3: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
-    case 4: gemm_kernel<E, OutT, 128, 32, 4, 1, 4, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G); break;
+    case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
+    case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
+    case 3: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
+    case 4: gemm_kernel<E, OutT, 128, 32, 4, 1, 4, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
     default:                         // a short sum: two workgroups to a compute unit, one stores while the other begins
-      if constexpr (EPI == kOut) gemm_kernel<E, OutT, 128, 128, 2, 2, 2, EPI, PLANES, TURN><<<grid, 256, 0, st>>>(G);
+      if constexpr (EPI == kOut) gemm_kernel<E, OutT, 128, 128, 2, 2, 2, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G);
   }
   return hipGetLastError();
 }
@@ -374,7 +374,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   GemmArgs G{};
   G.b = H, G.kblocks = p.d_pad / 64, G.planes = p.logits, G.tops = p.pairs ? tops : nullptr, G.splits = 1;
   G.labels = q.labels_dev, G.wide = wide, G.vocab = V, G.lse = floats(p.lse), G.g = floats(p.gs), G.part = floats(p.part), G.at_label = floats(p.at_label);
-  G.m_pad = G.n_pad = 0;
+  G.n = rows;
   int parts = 0;
   const bool whole = !p.pack_w;                       // W as it lies: one product over the whole vocabulary
   for (int v0 = 0; v0 < V; v0 += whole ? V : p.piece) {
@@ -391,23 +391,22 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
 
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = V - v0 < p.piece ? V - v0 : p.piece, n64 = up64(n);
-    // dz of this piece, in both layouts
+    // dz of this piece
     G.a = weight(v0, n, p.pieces > 1), G.m = n, G.v0 = v0;
     G.dz = ws + p.dz, G.dz_ld = p.piece * 2, G.dz_plane = (long long)rows * p.piece * 2;
-    G.dzt = ws + p.dzt, G.dzt_ld = p.n_pad * 2, G.dzt_plane = (long long)p.piece * p.n_pad * 2;
-    G.m_pad = n64, G.n_pad = p.n_pad;
+    G.m_pad = n64;
     hipError_t e = hipSuccess;
     if constexpr (F32) e = p.pairs ? launch_gemm<f16, E, kDz, PLANES>(G, p.first_shape, st) : launch_gemm<E, E, kDz, PLANES>(G, p.first_shape, st);
     else e = p.dz_planes == 2 ? launch_gemm<E, E, kDz, 2>(G, p.first_shape, st) : launch_gemm<E, E, kDz, 1>(G, p.first_shape, st);
     if (e) return e;
     GemmArgs D{};
     D.planes = p.grads, D.scale = floats(p.scale);
-    D.a = G.a, D.m = d;
+    D.a = G.a, D.m = d, D.n = rows;
     if (p.pairs) D.a.p = ws + p.w;                       // laid out alike, in three terms
-    D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows};
+    D.b = Operand{G.dz, G.dz_ld, G.dz_plane, rows, n64};
     D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
-    if (const hipError_t e = launch_gemm<E, T, kSum, 1, true>(D, p.sum_shape, st)) return e;
-    D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.b = Operand{G.dzt, G.dzt_ld, G.dzt_plane, n};
+    if (const hipError_t e = launch_gemm<E, T, kSum, 1>(D, p.sum_shape, st)) return e;
+    D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.n = n;      // and dz as it lies
     D.kblocks = p.n_pad / 64, D.splits = 1;
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
     D.whole_rows = es == 2 && d % 8 == 0 && q.dweight_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(q.dweight_dev) & 15) == 0;
