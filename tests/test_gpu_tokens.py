@@ -196,6 +196,22 @@ def test_head_loss_of_large_tiles_and_pieces(gpu, rows, vocab, d, dtype):
     _check_head(torch, pb, h, w, labels, g, dtype, (rows, vocab, d, dtype))
 
 
+def test_head_loss_vocabulary_in_pieces(gpu):
+    """16000 rows of fp32: dz of 6500 places takes two pieces, the second one not a multiple of a slice."""
+    torch, pb = gpu
+    h, w, labels, g = _head_inputs(torch, 16000, 6500, 24, "f32")
+    _check_head(torch, pb, h, w, labels, g, "f32", "two pieces")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 2990), ("f32", 2990)])
+def test_head_loss_losses_in_pieces(gpu, dtype, d):
+    """A weight that is laid out for the losses, in two pieces."""
+    torch, pb = gpu
+    h, w, labels, g = _head_inputs(torch, 5, 100500, d, dtype)
+    labels[0] = 100499
+    _check_head(torch, pb, h, w, labels, g, dtype, ("losses in pieces", dtype), gradients=False)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_head_loss_ignored_labels(gpu, dtype):
     """No label at all; labels at the ends; rows to be ignored that hold NaN; weights of very different sizes, and none."""
@@ -457,6 +473,21 @@ def test_token_operators_on_another_stream(gpu):
         run()
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+def test_token_operators_on_two_streams_at_once(gpu):
+    torch, pb = gpu
+    calls = [_all_calls(torch, pb) for _ in range(2)]          # each with a workspace of its own
+    calls[0][0]()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in calls[0][1]]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for (run, _), stream in zip(calls, streams):
+            run(stream)
+    torch.cuda.synchronize()
+    for _, out in calls:
+        assert all(torch.equal(a, b) for a, b in zip(want, out))
 
 
 def test_token_operators_in_a_graph(gpu):
