@@ -185,6 +185,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  floatx16 second = acc[0][0];       // of a wave with one MFMA tile: products into one sum alone would wait for each other
   const int r32 = lane & 31, h = lane >> 5;
   // MFMA row 8 a + 4 b + c of tile i is the wave's row b * 16 MT + 16 i + 4 a + c: a lane then holds 16 MT rows in order
   const int row_a = wm * (MT * 32) + (r32 >> 2 & 1) * (16 * MT) + (r32 >> 3) * 4 + (r32 & 3), row_b = wn * (NT * 32) + r32;
@@ -238,7 +239,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mma<E>(f.a[u][i], f.b[u][j], acc[i][j]);
+        for (int j = 0; j < NT; ++j) {
+          floatx16 &to = MT * NT == 1 && u ? second : acc[i][j];
+          to = mma<E>(f.a[u][i], f.b[u][j], to);
+        }
   };
   // All but the last `later` slices that this wave loads have landed in LDS, and then everybody's; everybody has read what it needs of the
   // slice before.  The waits are written out: a barrier alone does not wait for loads into LDS.
@@ -275,23 +279,61 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     }
     __builtin_amdgcn_sched_barrier(0);
   };
+  // Small tiles have too few products in half a slice to hide a read behind: a whole slice waits in registers (500 x 1013 x 515 fp32 75.5 -> 72.5 us, 2113 x 192 x
+  // 888 116 -> 109; narrow tiles wait for memory and gain nothing).
+  auto step_whole = [&](Half (&now)[2], Half (&then)[2], char *place, const char *next, bool more, bool ahead, auto later) {
+    if (more) arrived(later);
+    if (ahead) load(place);
+    if (more) fetch(then[0], next, 0), fetch(then[1], next, 1);
+    multiply(now[0]);
+    multiply(now[1]);
+    constexpr int PRODUCTS = 4 * MT * NT;
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x010, (RA + RB + PRODUCTS - 1) / PRODUCTS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, (2 * READS + PRODUCTS - 1) / PRODUCTS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
   if (first < last) {
 #pragma unroll
     for (int i = 0; i < STAGES; ++i)
       if (first + i < last) load(stage[i]);
     if (first + STAGES <= last) arrived(std::integral_constant<int, STAGES - 1>());
     else arrived(std::integral_constant<int, 0>());
-    fetch(f0, s0, 0);
     int k = first;
-    for (; k + 2 * STAGES - 1 < last; k += STAGES) {
+    if constexpr (STAGES == 4 && TM == TN) {
+      constexpr int U = STAGES;
+      Half r[2][2];
+      fetch(r[0][0], s0, 0), fetch(r[0][1], s0, 1);
+      for (; k + U + STAGES - 1 < last; k += U) {
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i) step(stage[i], stage[(i + 1) % STAGES], true, true, std::integral_constant<int, STAGES - 2>());
-    }
-    for (; k < last; k += STAGES) {
+        for (int i = 0; i < U; ++i) step_whole(r[i & 1], r[~i & 1], stage[i % STAGES], stage[(i + 1) % STAGES], true, true, std::integral_constant<int, STAGES - 2>());
+      }
+      for (; k < last; k += U) {
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i)
-        if (k + i < last) step(stage[i], stage[(i + 1) % STAGES], k + i + 1 < last, k + i + STAGES < last, std::integral_constant<int, 0>());
+        for (int i = 0; i < U; ++i)
+          if (k + i < last)
+            step_whole(r[i & 1], r[~i & 1], stage[i % STAGES], stage[(i + 1) % STAGES], k + i + 1 < last, k + i + STAGES < last, std::integral_constant<int, 0>());
+      }
+    } else {
+      fetch(f0, s0, 0);
+      for (; k + 2 * STAGES - 1 < last; k += STAGES) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) step(stage[i], stage[(i + 1) % STAGES], true, true, std::integral_constant<int, STAGES - 2>());
+      }
+      for (; k < last; k += STAGES) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i)
+          if (k + i < last) step(stage[i], stage[(i + 1) % STAGES], k + i + 1 < last, k + i + STAGES < last, std::integral_constant<int, 0>());
+      }
     }
+  }
+
+  if (MT * NT == 1) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][0][e] += second[e];
   }
 
   // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
