@@ -35,7 +35,7 @@ def _workspace(torch, n):
 
 # ------------------------------------------------------------------------------------------------------- embedding
 EMBED = [(1, 1, 1), (1, 300, 16), (7, 5, 33), (64, 1000, 129), (33, 3, 2048), (700, 40, 515), (3000, 5000, 64), (5000, 700, 72), (2500, 20000, 100), (40, 9, 5000),
-         (20000, 30, 24), (18000, 9000, 520)]
+         (255, 4, 100), (256, 300, 40), (257, 300, 40), (256, 20000, 2100), (20000, 30, 24), (18000, 9000, 520)]
 
 
 @pytest.mark.parametrize("rows,vocab,d", EMBED)
@@ -65,7 +65,7 @@ def test_embed(gpu, rows, vocab, d, dtype, index, accumulate):
     assert torch.equal(dw, again)
 
 
-@pytest.mark.parametrize("rows,vocab", [(4096, 1), (4096, 4096), (20000, 70000), (3000, 1 << 20)])
+@pytest.mark.parametrize("rows,vocab", [(200, 1), (256, 70000), (4096, 1), (4096, 4096), (20000, 70000), (3000, 1 << 20)])
 @pytest.mark.parametrize("kind", ["one", "two in turn", "multiples", "falling", "none"])
 def test_embed_backward_orders_of_tokens(gpu, rows, vocab, kind):
     """One token everywhere, tokens of one workgroup's share only, tokens in falling order, padding only."""
