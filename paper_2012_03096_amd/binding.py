@@ -622,8 +622,13 @@ def embed_forward(tokens, weight, y, scale: float = 1.0, stream=None) -> None:
     0..vocab-1.  weight [vocab, d], y [*tokens.shape, d] of weight's type."""
     L, code, dt, shape, dev = _first(weight, "weight")
     vocab, d = _table(shape, "weight")
-    tp, index = _indices(tokens, tokens.shape, dev, "tokens")
-    _check(L.pbkd_embed_forward(_EMBED.pack(tokens.numel(), vocab, d, code, index, scale, tp, weight.data_ptr(), _same(y, dt, (*tokens.shape, d), dev, "y"),
+    index, at, out = _INDEX.get(tokens.dtype), tokens.shape, y.shape
+    if index is None or tokens.get_device() != dev or not tokens.is_contiguous():
+        _indices(tokens, at, dev, "tokens")
+    # shapes number by number where they are the usual ones: this call is made for one token at a time
+    if y.dtype is not dt or y.get_device() != dev or not (len(out) == 2 and len(at) == 1 and out[1] == d and out[0] == at[0] or out == (*at, d)):
+        raise PbkdError(ESHAPE, f"y must be a {dt} tensor of {(*at, d)} on the same GPU, not {y.dtype} {tuple(out)} on {y.device}")
+    _check(L.pbkd_embed_forward(_EMBED.pack(at[0] if len(at) == 1 else tokens.numel(), vocab, d, code, index, scale, tokens.data_ptr(), weight.data_ptr(), y.data_ptr(),
                                             _row_stride(weight, d, "weight"), _row_stride(y, d, "y")), _stream(stream)))
 
 
@@ -672,16 +677,18 @@ def topk_distill(logits, teacher, at, loss, temperature: float = 1.0, row_weight
     vocab = shape[-1] if shape else 0
     if vocab == 0:
         raise PbkdError(ESHAPE, "logits has no elements in a row")
-    rows, known = logits.numel() // vocab, teacher.shape
-    if known[:-1] != shape[:-1] or not known[-1]:
+    known, flat = teacher.shape, len(shape) == 2
+    rows = shape[0] if flat else logits.numel() // vocab
+    if not known or not (flat and len(known) == 2 and known[0] == rows or known[:-1] == shape[:-1]) or not known[-1]:
         raise PbkdError(ESHAPE, f"teacher must have logits' shape {tuple(shape)} but for the last dimension, not {tuple(known)}")
     tcode = _CODES.get(teacher.dtype)
     if tcode is None:
         raise PbkdError(EINVAL, f"teacher must be float32, bfloat16 or float16, not {teacher.dtype}")
     ap, index = _indices(at, known, dev, "at")
+    each = (rows,)
     _check(L.pbkd_topk_distill(_TOPK_DISTILL.pack(
         rows, vocab, known[-1], code, tcode, index, temperature, logits.data_ptr(), _dense(teacher, known, teacher.dtype, dev, "teacher"), ap,
-        _dense(row_weight, (rows,), _FP32, dev, "row_weight"), _dense(loss, (rows,), _FP32, dev, "loss"), 0 if dlogits is None else _same(dlogits, dt, shape, dev, "dlogits"),
+        0 if row_weight is None else _dense(row_weight, each, _FP32, dev, "row_weight"), _dense(loss, each, _FP32, dev, "loss"), 0 if dlogits is None else _same(dlogits, dt, shape, dev, "dlogits"),
         _row_stride(logits, vocab, "logits"), 0 if dlogits is None else _row_stride(dlogits, vocab, "dlogits")), _stream(stream)))
 
 

@@ -528,7 +528,7 @@ def test_binding_refuses_wrong_tensors(gpu):
         lambda: pb.topk_distill(z, t, at.float(), loss), lambda: pb.topk_distill(z, t, at[:, :1], loss), lambda: pb.topk_distill(z, t[:3], at[:3], loss),
         lambda: pb.topk_distill(z, t.double(), at, loss), lambda: pb.topk_distill(z, t, at, loss[:3]), lambda: pb.topk_distill(z, t, at, loss, dlogits=z.half()),
         lambda: pb.topk_distill(z, t, at, loss, temperature=0.0), lambda: pb.topk_distill(z[:, :0], t, at, loss), lambda: pb.topk_distill(z, t[:, :0], at[:, :0], loss),
-        lambda: pb.topk_distill(z.double(), t, at, loss), lambda: pb.topk_distill(z, t.cpu(), at, loss),
+        lambda: pb.topk_distill(z.double(), t, at, loss), lambda: pb.topk_distill(z[0], t[0, 0], at[0, 0], loss[:1]), lambda: pb.embed_forward(tok.view(2, 2), w, y), lambda: pb.topk_distill(z, t.cpu(), at, loss),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(pb.PbkdError):
