@@ -48,6 +48,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
   __shared__ int place[kMaxTop];
   __shared__ float share[kMaxTop];
   __shared__ float red[4][W];
+  __shared__ unsigned seen[256];               // a bit for each place that a pair names
+  __shared__ int twice;
   __shared__ Vec kept[GRADIENT ? HELD : 1][GRADIENT ? THREADS : 1];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, v = A.v, top = A.top;
   const long long row = blockIdx.x;
@@ -58,6 +60,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
   const T *const zz = z - par;
   const float c = A.inv_t * kLog2e;            // logits in units of log 2, over T
 
+  // whether a place is named twice is looked up where rows are short (in long ones it hides, and 28 registers would spill)
+  constexpr bool LOOK = GRADIENT && THREADS < 1024;
+  if (LOOK && tid < 256) seen[tid] = 0;
+  if (LOOK && tid == 0) twice = 0;
   // the pairs are read first, then the student's logits there: dz may be z, and nothing is written before
   const TT *t = static_cast<const TT *>(A.t) + row * top;
   const IT *at = static_cast<const IT *>(A.at) + row * top;
@@ -174,6 +180,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
   for (int k = 0; k < W; ++k) s += red[1][k] * exp2_fast(red[0][k] - base);
   const bool some = tm > -__builtin_inff();
   const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;
+  // Places beyond 8192 may share a bit and count as named twice: looking through all pairs for each pair costs 2 us of a row with 235 (12149 rows of 744 fp16
+  // 172 us, so 50).
+  if (LOOK) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (w[k] >= 0) {
+        const int bit = (w[k] ^ w[k] >> 13) & 8191;
+        if (atomicOr(&seen[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) twice = 1;
+      }
+  }
   float qs = 0.f;
 #pragma unroll
   for (int k = 0; k < PER; ++k)
@@ -264,8 +280,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
     const int j = k * THREADS + tid;
     float q = 0.f;
     bool first = true;
-    for (int i = 0; i < top; ++i)
-      if (place[i] == w[k]) q += share[i], first &= i >= j;
+    if (LOOK && !twice) q = share[j];
+    else
+      for (int i = 0; i < top; ++i)
+        if (place[i] == w[k]) q += share[i], first &= i >= j;
     if (first) dz[w[k]] = static_cast<T>(exp2_fast(fmaf(mine[k], c, -shift)) * scale - g * q);
   }
 }

@@ -353,6 +353,19 @@ def test_topk_distill(gpu, rows, vocab, top, dtype, teacher, index, temperature)
     _check_distill(torch, pb, z, t, at, g, temperature, dtype, (rows, vocab, top, dtype, teacher, temperature))
 
 
+@pytest.mark.parametrize("vocab,dtype", [(8192, "f32"), (700, "f16"), (16384, "bf16")])
+def test_topk_distill_one_repeated_place_among_many(gpu, vocab, dtype):
+    torch, pb = gpu
+    rows, top = 4, 301
+    z, t, _, g = _distill_inputs(torch, rows, vocab, top, dtype, "f32")
+    at = torch.stack([torch.randperm(vocab, generator=torch.Generator().manual_seed(r))[:top] for r in range(rows)]).cuda()
+    at[1, 300] = at[1, 0]                          # the first and the last pair
+    at[2, 257] = at[2, 256]                        # neighbours
+    at[3, :150] = torch.arange(150, device="cuda")
+    at[3, 150:300] = (torch.arange(150, device="cuda") + 8192) % vocab ^ (1 if vocab > 8192 else 0)
+    _check_distill(torch, pb, z, t, at, g, 1.5, dtype, ("one place twice", vocab, dtype))
+
+
 @pytest.mark.parametrize("vocab", [300, 20000])
 def test_topk_distill_rows_without_pairs_and_repeated_places(gpu, vocab):
     torch, pb = gpu
