@@ -94,10 +94,19 @@ __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// The power of two that brings numbers of at most `top` (its bits) below 2^14.
-__device__ __forceinline__ float scale_of(unsigned bits) {
+// The power of two that brings numbers of at most `top` (its bits) below 2^14: its exponent, and itself.
+__device__ __forceinline__ int exponent_of(unsigned bits) {
   const float top = __builtin_bit_cast(float, bits);
   const int e = top > 0.f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+  return e < 126 ? e : 126;          // e >= 14 - 128
+}
+__device__ __forceinline__ float scale_of(unsigned bits) { return ldexpf(1.f, exponent_of(bits)); }
+
+// What sums of products of numbers scaled by two such powers are multiplied with.  The two together may pass fp32's range (0.3 beside 1e-32: 2^133).  The
+// unit stays a number that sums, minus infinity and zero can be multiplied with, also times log2 e: below 2^-126 no logit is above d 2^-97, which
+// is zero to a softmax; above 2^126 products of the largest numbers pass fp32, and logits of zero stay zero.
+__device__ __forceinline__ float unit_of(int a, int b) {
+  const int e = -(a + b);
   return ldexpf(1.f, e < 126 ? e > -126 ? e : -126 : 126);
 }
 
@@ -361,9 +370,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) unit[j] = 1.f;
     if (G.tops) {
-      const float a = scale_of(G.tops[0]);
+      const int a = exponent_of(G.tops[0]);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) unit[j] = 1.f / (a * scale_of(G.tops[1 + (n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1)]));
+      for (int j = 0; j < NT; ++j) unit[j] = unit_of(a, exponent_of(G.tops[1 + (n1 + 32 * j < G.n ? n1 + 32 * j : G.n - 1)]));
     }
   }
   if constexpr (EPI == kStats) {
