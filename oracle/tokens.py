@@ -95,9 +95,9 @@ def topk_distill(logits, teacher, at, temperature=1.0, row_weight=None):
         log_q = t - tm - np.log(share)
         zj = np.take_along_axis(z, np.where(known, at, 0), 1)
         loss = np.where(q > 0, q * (log_q - zj + lse[:, None]), 0.0).sum(1) * temperature ** 2
-        # a row is summed in runs of v / 256 (one thread's) and a tree
+        # at least 256 threads sum a row, each in groups of at least four that are added one after the other, then a tree
         top = np.where(np.isfinite(z), np.abs(z), 0.0).max(1)
-        lse_err = (32 + v / 256 + 4 * top) * EPS32
+        lse_err = (32 + v / 1024 + 4 * top) * EPS32
         far = np.where(known, np.abs(t), 0.0)
         qerr = (16 + at.shape[1] / 64 + 6 * far.max(1, keepdims=True)) * EPS32
         size = np.where(q > 0, q * (np.abs(log_q) + np.abs(zj) + np.abs(lse)[:, None]), 0.0)

@@ -78,16 +78,24 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
   }
 
   Vec held[HELD];
-  // the row's maximum, in the logits' own units, and its sum relative to it: a batch's maximum first, one rescaling a batch
+  // the row's maximum, times c and rounded, and its sum relative to just that number: a batch's maximum first, one rescaling a batch, by exactly 1
+  // where the maximum stays.  (From the exact product, a rescaling would be off by what the product was rounded by, every batch: rows of 2^21 with one
+  // logit of 500 had a log-sum off by 2e-3.)
   float m = -__builtin_inff(), s = 0.f;
+  auto raise = [&](float most) {
+    const float before = m;
+    m = fmaxf(m, most * c);
+    const float ref = m == -__builtin_inff() ? 0.f : m;
+    s *= exp2_fast(before - ref);
+    return ref;
+  };
   auto take = [&](const Vec (&raw)[HELD]) {
-    float most = m;
+    float most = -__builtin_inff();
 #pragma unroll
     for (int k = 0; k < HELD; ++k)
 #pragma unroll
       for (int e = 0; e < N; ++e) most = fmaxf(most, static_cast<float>(raw[k][e]));
-    const float ref = most == -__builtin_inff() ? 0.f : most * c;
-    s *= exp2_fast(fmaf(m, c, -ref));
+    const float ref = raise(most);
 #pragma unroll
     for (int k = 0; k < HELD; ++k) {
       float sum = 0.f;
@@ -95,7 +103,6 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
       for (int e = 0; e < N; ++e) sum += exp2_fast(fmaf(static_cast<float>(raw[k][e]), c, -ref));
       s += sum;
     }
-    m = most;
   };
   Vec next[HELD];
   constexpr int ONE = THREADS * N;
@@ -143,20 +150,19 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void topk_distill
     take(held);
   }
   for (int base = full; base < n; base += ONE) {
-    float x[N], most = m, sum = 0.f;
+    float x[N], most = -__builtin_inff();
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = static_cast<float>(next[0][e]);
     if (base + ONE < n) fetch_one(base + ONE);
     mask(base + tid * N, x);
 #pragma unroll
     for (int e = 0; e < N; ++e) most = fmaxf(most, x[e]);
-    const float ref = most == -__builtin_inff() ? 0.f : most * c;
+    const float ref = raise(most);
+    float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) sum += exp2_fast(fmaf(x[e], c, -ref));
-    s = s * exp2_fast(fmaf(m, c, -ref)) + sum;
-    m = most;
+    s += sum;
   }
-  m *= c;
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
     const float m2 = __shfl_xor(m, k, 64), s2 = __shfl_xor(s, k, 64);

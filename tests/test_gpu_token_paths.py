@@ -45,3 +45,33 @@ def test_head_loss_large_numbers_that_never_meet(gpu):
     _within(_np(loss), r["loss"], r["loss_err"], "loss")
     _within(_np(dh), r["dh"], _round(r["dh"], r["dh_err"], "f32"), "dh")
     _within(_np(dw), r["dweight"], _round(r["dweight"], r["dweight_err"], "f32"), "dweight")
+
+
+# -------------------------------------------------------------------------------------- distillation from top logits
+@pytest.mark.parametrize("vocab,dtype", [(9000, "f32"), (50021, "f32"), (262144, "f32"), (1 << 21, "f32"), (131072, "bf16"), (1 << 21, "bf16"), ((1 << 21) + 1, "f16")])
+@pytest.mark.parametrize("temperature", [1.0, 2.0])
+def test_topk_distill_of_confident_rows(gpu, vocab, dtype, temperature):
+    """One logit, or two equal ones, far above the rest: the sum of exponentials stays that of the first batch through all later ones.
+
+    lse = (m + log2 s) ln 2 with m the maximum in units of log 2: rounded when the two are added and when they are multiplied, by 2^-24 of lse each, the two
+    constants are off by half of that together, a pair's logit is subtracted and added to (two more), its share multiplied and summed: at most 8
+    times 2^-24 of lse, and 64 for what does not grow with it (the hardware's logarithm near 1, joining 16 waves of 64 threads).  A probability's exponent
+    has no errors but those of lse.  How long the row is does not matter."""
+    torch, pb = gpu
+    tops = torch.tensor([100.0, 117.5, 251.0, 500.0, 100.0, 117.5, 251.0, 500.0])
+    rows = len(tops)
+    z = _randn(torch, 1, rows, vocab, dtype=dtype)
+    z[:, 3] = tops.to(z.dtype).cuda()
+    z[4:, vocab - 5] = z[4:, 3]                    # two
+    at, t = torch.tensor([[3, vocab // 2]] * rows, device="cuda"), torch.tensor([[5.0, float("-inf")]] * rows, device="cuda")
+    t[::2, 1] = 5.0
+    g = torch.ones(rows, device="cuda")
+    loss, only, dz = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(z)
+    print("topk_distill confident", vocab, dtype, temperature, flush=True)
+    pb.topk_distill(z, t, at, loss, temperature=temperature, row_weight=g, dlogits=dz)
+    pb.topk_distill(z, t, at, only, temperature=temperature)
+    r = otk.topk_distill(_np(z), _np(t), at.cpu().numpy(), temperature)
+    off = (8 * tops.numpy() / temperature + 64) * E
+    _within(_np(loss), r["loss"], temperature ** 2 * off, "loss")
+    _within(_np(only), r["loss"], temperature ** 2 * off, "loss alone")
+    _within(_np(dz), r["dlogits"], _round(r["dlogits"], temperature * (off[:, None] + 2 * otk.LEAST), dtype), "dlogits")
