@@ -436,10 +436,16 @@ def _types():
     return lib()
 
 
+def _missing(name: str):
+    raise PbkdError(EINVAL, f"{name} is missing")
+
+
 def _first(t, name: str):
     """(library, type's number, type, shape, GPU) of a call's first tensor, which must lie on the current GPU: the kernels are launched
     there."""
     L = _lib if _torch is not None and _lib is not None else _types()
+    if t is None:
+        _missing(name)
     dtype, dev = t.dtype, t.get_device()
     code = _CODES.get(dtype)
     if code is None:
@@ -455,6 +461,8 @@ def _stream(stream) -> int:
 
 def _same(t, dtype, shape, dev: int, name: str) -> int:
     """Address of t, a tensor of this type and shape on GPU dev."""
+    if t is None:
+        _missing(name)
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         raise PbkdError(ESHAPE, f"{name} must be a {dtype} tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -500,6 +508,8 @@ def rmsnorm_forward(x, weight, y, residual=None, total=None, scale=None, eps: fl
     if d == 0:
         raise PbkdError(ESHAPE, "x has no elements in a row")
     rows = x.numel() // d
+    if y is None:
+        _missing("y")
     eight = y.dtype is _FP8
     if eight and (y.shape != shape or y.get_device() != dev):
         raise PbkdError(ESHAPE, f"y must have x's shape {tuple(x.shape)} and lie on its GPU")
@@ -600,6 +610,8 @@ def recurrence_step(u, gate, state, y, out_gate=None, bias=None, active=None, st
 
 def _indices(t, shape, dev: int, name: str):
     """(address, type's number) of t, a contiguous tensor of 32- or 64-bit integers of this shape on GPU dev."""
+    if t is None:
+        _missing(name)
     code = _INDEX.get(t.dtype)
     if code is None or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         raise PbkdError(ESHAPE, f"{name} must be a contiguous int32 or int64 tensor of {tuple(shape)} on the same GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -622,6 +634,8 @@ def embed_forward(tokens, weight, y, scale: float = 1.0, stream=None) -> None:
     0..vocab-1.  weight [vocab, d], y [*tokens.shape, d] of weight's type."""
     L, code, dt, shape, dev = _first(weight, "weight")
     vocab, d = _table(shape, "weight")
+    if tokens is None or y is None:
+        _missing("tokens" if tokens is None else "y")
     index, at, out = _INDEX.get(tokens.dtype), tokens.shape, y.shape
     if index is None or tokens.get_device() != dev or not tokens.is_contiguous():
         _indices(tokens, at, dev, "tokens")
@@ -637,6 +651,8 @@ def embed_backward(tokens, dy, dweight, workspace, scale: float = 1.0, accumulat
     does not occur then stay as they are).  workspace: a tensor of embed_workspace_bytes(tokens.numel(), vocab, d) bytes."""
     L, code, dt, shape, dev = _first(dweight, "dweight")
     vocab, d = _table(shape, "dweight")
+    if tokens is None:
+        _missing("tokens")
     tp, index = _indices(tokens, tokens.shape, dev, "tokens")
     wp, wn = _bytes(workspace, dev, "workspace")
     _check(L.pbkd_embed_backward(_EMBED_GRAD.pack(tokens.numel(), vocab, d, code, index, scale, bool(accumulate), tp, _same(dy, dt, (*tokens.shape, d), dev, "dy"),
@@ -656,6 +672,8 @@ def head_loss(h, weight, labels, loss, workspace, lse=None, row_weight=None, dh=
     outside 0..vocab-1 are ignored.  h [..., d], weight [vocab, d], labels [...] int32 or int64.  lse [rows]: the logits' log-sums.  dh and
     dweight (like h and weight): the gradients of (row_weight * loss).sum().  workspace: a tensor of head_loss_workspace_bytes(...) bytes."""
     L, code, dt, shape, dev = _first(h, "h")
+    if weight is None:
+        _missing("weight")
     vocab, d = _table(weight.shape, "weight")
     if not shape or shape[-1] != d:
         raise PbkdError(ESHAPE, f"rows of h must have weight's {d} elements, not {tuple(shape)}")
@@ -677,6 +695,8 @@ def topk_distill(logits, teacher, at, loss, temperature: float = 1.0, row_weight
     vocab = shape[-1] if shape else 0
     if vocab == 0:
         raise PbkdError(ESHAPE, "logits has no elements in a row")
+    if teacher is None:
+        _missing("teacher")
     known, flat = teacher.shape, len(shape) == 2
     rows = shape[0] if flat else logits.numel() // vocab
     if not known or not (flat and len(known) == 2 and known[0] == rows or known[:-1] == shape[:-1]) or not known[-1]:

@@ -75,3 +75,17 @@ def test_topk_distill_of_confident_rows(gpu, vocab, dtype, temperature):
     _within(_np(loss), r["loss"], temperature ** 2 * off, "loss")
     _within(_np(only), r["loss"], temperature ** 2 * off, "loss alone")
     _within(_np(dz), r["dlogits"], _round(r["dlogits"], temperature * (off[:, None] + 2 * otk.LEAST), dtype), "dlogits")
+
+
+# ------------------------------------------------------------------------------------------------------------ refusals
+def test_binding_refuses_missing_tensors(gpu):
+    torch, pb = gpu
+    w, y, tok = torch.zeros(10, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    ws, loss = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"), torch.zeros(4, device="cuda")
+    z, t, at = torch.zeros(4, 10, device="cuda"), torch.zeros(4, 2, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    calls = [(pb.embed_forward, (tok, w, y)), (pb.embed_backward, (tok, y, w, ws)), (pb.head_loss, (y, w, tok, loss, ws)), (pb.topk_distill, (z, t, at, loss)), (pb.rmsnorm_forward, (y, loss.new_zeros(8), torch.empty_like(y)))]
+    for call, args in calls:
+        for i in range(len(args)):
+            with pytest.raises(pb.PbkdError):
+                call(*args[:i], None, *args[i + 1:])
+                print("not refused:", call.__name__, i)

@@ -148,3 +148,12 @@ def test_binding_refuses_tensors_on_the_host():
                  lambda: pb.topk_distill(y, y[:, :2].contiguous(), t[:, None].expand(4, 2).contiguous(), loss), lambda: pb.embed_forward(t, w.double(), y.double())):
         with pytest.raises(pb.PbkdError):
             call()
+
+
+def test_binding_refuses_missing_tensors_without_a_gpu():
+    torch = pytest.importorskip("torch")
+    y, t = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: pb.embed_forward(t, None, y), lambda: pb.embed_backward(t, y, None, None), lambda: pb.head_loss(None, y, t, y[:, 0], None),
+                 lambda: pb.topk_distill(None, y, t, y[:, 0]), lambda: pb.rmsnorm_forward(None, y[0], y)):
+        with pytest.raises(pb.PbkdError, match="missing"):
+            call()
