@@ -25,7 +25,8 @@ from .sequence import SequenceBlock
 
 
 class TokenStudent:
-    """A model of `blocks` recurrent blocks of width d over `vocab` tokens.  A token or label outside 0..vocab-1 is padding."""
+    """A model of `blocks` recurrent blocks of width d over `vocab` tokens.  A token or label outside 0..vocab-1 is padding.  Tokens,
+    labels and a teacher's logits may have any strides."""
 
     def __init__(self, vocab: int, d: int, blocks: int = 1, seed: int = 0, device: str = "cuda", state_bits: int = 8, weight_decay: float = 0.01):
         gen = torch.Generator().manual_seed(seed)
@@ -54,7 +55,7 @@ class TokenStudent:
         """h [batch * len, d] for tokens [batch, len]; a training pass keeps what the backward pass needs."""
         b, t = tokens.shape
         out, stream, saved = self._buffer("x", b, t, self.d), None, []
-        pb.embed_forward(tokens, self.table, out, scale=self.scale)
+        pb.embed_forward(tokens.contiguous(), self.table, out, scale=self.scale)
         for k, block in enumerate(self.blocks):
             total = None if stream is None else torch.empty_like(out)
             y, z, q = block._forward(out, stream, None, None, None, training, total=total)
@@ -76,7 +77,7 @@ class TokenStudent:
         for block, (x, stream, z, q) in zip(reversed(self.blocks), reversed(saved)):
             # what arrives at the sum behind the block reaches its output and, past it, the stream in front of it
             g = block._backward(x, stream, g.view(-1, self.d), z, q, dtotal=g)
-        pb.embed_backward(tokens, g, self.grads[0], self._bytes("embed_workspace", pb.embed_workspace_bytes(rows, self.vocab, self.d)), scale=self.scale,
+        pb.embed_backward(tokens.contiguous(), g, self.grads[0], self._bytes("embed_workspace", pb.embed_workspace_bytes(rows, self.vocab, self.d)), scale=self.scale,
                           accumulate=True)
         self._saved = None
 
@@ -94,7 +95,7 @@ class TokenStudent:
         weight = (live / live.sum().clamp_min(1)).view(-1).float()
         loss, dh = self._buffer("loss", rows, dtype=torch.float32), self._buffer("dh", rows, self.d)
         workspace = self._bytes("head_workspace", pb.head_loss_workspace_bytes(rows, self.vocab, self.d, h.dtype, gradients=True))
-        pb.head_loss(h, self.table, labels.reshape(-1), loss, workspace, row_weight=weight, dh=dh, dweight=self.grads[0])
+        pb.head_loss(h, self.table, labels.reshape(-1).contiguous(), loss, workspace, row_weight=weight, dh=dh, dweight=self.grads[0])
         mean = (loss * weight).sum()
         self._backward(tokens, dh)
         return mean
@@ -108,7 +109,7 @@ class TokenStudent:
         weight = some / some.sum().clamp_min(1).float()
         logits = h @ self.table.t()
         loss = self._buffer("loss", h.shape[0], dtype=torch.float32)
-        pb.topk_distill(logits, teacher.view(-1, top), at.view(-1, top), loss, temperature=temperature, row_weight=weight, dlogits=logits)
+        pb.topk_distill(logits, teacher.reshape(-1, top).contiguous(), at.reshape(-1, top).contiguous(), loss, temperature=temperature, row_weight=weight, dlogits=logits)
         torch.mm(logits.t(), h, out=self.grads[0])
         mean = (loss * weight).sum()
         self._backward(tokens, logits @ self.table)
@@ -131,7 +132,7 @@ class TokenStudent:
         h = self._forward(tokens, False)
         loss = torch.empty(h.shape[0], device=h.device)
         workspace = self._bytes("head_workspace", pb.head_loss_workspace_bytes(h.shape[0], self.vocab, self.d, h.dtype, gradients=False))
-        pb.head_loss(h, self.table, labels.reshape(-1), loss, workspace)
+        pb.head_loss(h, self.table, labels.reshape(-1).contiguous(), loss, workspace)
         return loss.view(labels.shape)
 
     def top_logits(self, tokens, top: int):
@@ -146,7 +147,7 @@ class TokenStudent:
     def answer(self, token, state):
         """Logits [batch, vocab] for the next token after `token` [batch]; state (of new_state) is updated in place."""
         out, stream = torch.empty(token.shape[0], self.d, dtype=torch.bfloat16, device=token.device), None
-        pb.embed_forward(token, self.table, out, scale=self.scale)
+        pb.embed_forward(token.contiguous(), self.table, out, scale=self.scale)
         for block, s in zip(self.blocks, state):
             total = None if stream is None else torch.empty_like(out)
             y = block.step(out, s, residual=stream, total=total)

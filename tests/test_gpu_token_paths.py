@@ -89,3 +89,36 @@ def test_binding_refuses_missing_tensors(gpu):
             with pytest.raises(pb.PbkdError):
                 call(*args[:i], None, *args[i + 1:])
                 print("not refused:", call.__name__, i)
+
+
+# ---------------------------------------------------------------------------------------------------- the token student
+def test_token_student_imitates_from_strided_tensors(gpu):
+    """The teacher's logits as slices of longer lists, and stored token by token: the gradients of contiguous ones."""
+    torch, pb = gpu
+    from paper_2012_03096_amd.tokens import TokenStudent
+    student = TokenStudent(300, 64, seed=3)
+    tokens, teacher = _ints(torch, 1, 0, 300, 3, 11), _randn(torch, 2, 3, 11, 8, scale=3.0)
+    at = torch.stack([torch.randperm(300, generator=torch.Generator().manual_seed(k))[:8] for k in range(33)]).view(3, 11, 8).cuda()
+    at[1, 2] = -1
+    mean = student.imitate_gradients(tokens, teacher[..., :5].contiguous(), at[..., :5].contiguous())
+    want = [mean] + [g.clone() for g in student.grads + student.blocks[0].grads]
+    turned = [t[..., :5].transpose(0, 1).contiguous().transpose(0, 1) for t in (teacher, at)]
+    for given in ((teacher[..., :5], at[..., :5]), turned):
+        mean = student.imitate_gradients(tokens, *given)
+        assert all(torch.equal(a, b) for a, b in zip(want, [mean] + student.grads + student.blocks[0].grads))
+
+
+def test_token_student_takes_slices_of_a_text(gpu):
+    """Tokens and labels as neighbouring slices of one tensor, and single columns of it."""
+    torch, pb = gpu
+    from paper_2012_03096_amd.tokens import TokenStudent
+    student, text = TokenStudent(300, 64, seed=3), _ints(torch, 1, 0, 300, 3, 12)
+
+    def results(x, y, one, label):
+        state = student.new_state(3)
+        mean = student.learn_gradients(x, y)
+        out = [mean] + [g.clone() for g in student.grads + student.blocks[0].grads]
+        return out + [student.score(x, y), student.score(one, label), *student.top_logits(x, 4), student.answer(one[:, 0], state), *state]
+    strided = results(text[:, :-1], text[:, 1:], text[:, 3:4], text[:, 4:5])
+    dense = results(*(t.contiguous() for t in (text[:, :-1], text[:, 1:], text[:, 3:4], text[:, 4:5])))
+    assert all(torch.equal(a, b) for a, b in zip(strided, dense))
