@@ -57,7 +57,7 @@ class TokenStudent:
         out, stream, saved = self._buffer("x", b, t, self.d), None, []
         pb.embed_forward(tokens.contiguous(), self.table, out, scale=self.scale)
         for k, block in enumerate(self.blocks):
-            total = None if stream is None else torch.empty_like(out)
+            total = None if stream is None or training else torch.empty_like(out)
             y, z, q = block._forward(out, stream, None, None, None, training, total=total)
             saved.append((out, stream, z, q))
             # the stream behind the first sum is the sum itself; a training pass keeps it in the block's buffer

@@ -122,3 +122,18 @@ def test_token_student_takes_slices_of_a_text(gpu):
     strided = results(text[:, :-1], text[:, 1:], text[:, 3:4], text[:, 4:5])
     dense = results(*(t.contiguous() for t in (text[:, :-1], text[:, 1:], text[:, 3:4], text[:, 4:5])))
     assert all(torch.equal(a, b) for a, b in zip(strided, dense))
+
+
+def test_token_student_keeps_a_training_pass_sums_in_its_blocks(gpu, monkeypatch):
+    """A training pass stores each residual sum in the block that reads it again, and asks for no other room."""
+    torch, pb = gpu
+    from paper_2012_03096_amd import tokens as module
+    student, totals, forward = module.TokenStudent(300, 64, blocks=3, seed=3), [], module.SequenceBlock._forward
+
+    def spy(self, x, residual, lengths, state, state_out, training, total=None):
+        totals.append(total)
+        return forward(self, x, residual, lengths, state, state_out, training, total=total)
+    monkeypatch.setattr(module.SequenceBlock, "_forward", spy)
+    x = _ints(torch, 1, 0, 300, 2, 9)
+    student.learn_gradients(x, x)
+    assert totals == [None] * 3
