@@ -13,6 +13,129 @@ from tests.test_gpu_tokens import _check_head, _head_inputs, _ints, _words, _wor
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------------------------------------------- embedding
+# Up to 256 tokens take one launch for the gradient, more are sorted first: what follows is about the latter.
+def _embed_gradient(torch, tokens, dy, vocab, scale, before=None):
+    """(dweight, bound, tokens that occur) on the GPU, in 64 bits; the bound is the oracle's."""
+    live = (tokens >= 0) & (tokens < vocab)
+    at, rows = tokens[live].long(), dy[live].double()
+    dw, size = (torch.zeros(vocab, dy.shape[1], dtype=torch.float64, device="cuda").index_add_(0, at, r) for r in (rows, rows.abs()))
+    count = torch.bincount(at, minlength=vocab)
+    dw, err = dw * scale, (count[:, None] + 2) * E * size * abs(scale)
+    if before is not None:
+        dw = dw + before.double()
+        err = err + E * (dw.abs() + before.double().abs())
+    return dw, err, count
+
+
+def _near(torch, got, ref, bound, dtype, what):
+    """got, of this type, is ref to within bound and its rounding, everywhere."""
+    bound = bound + (ref.abs() + bound) * HALF[dtype] * 1.001 + (2.0 ** -25 if dtype == "f16" else 0.0)
+    bad = ~((got.double() - ref).abs() <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:3].tolist(), got[bad][:3], ref[bad][:3], bound[bad][:3])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [600, 20000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_sorted_gradient_strides(gpu, dtype, rows, accumulate):
+    """Some tokens are longer than a piece, some of a dy's and a gradient's rows lie inside wider ones."""
+    torch, pb = gpu
+    vocab, d = 133, 77
+    tokens, dy, first = _words(torch, 1, rows, vocab), _randn(torch, 2, rows, d, dtype=dtype), _randn(torch, 3, vocab, d, dtype=dtype)
+    ws = _workspace(torch, pb.embed_workspace_bytes(rows, vocab, d))
+    dense, strided = first.clone(), _strided(torch, first, 9, 1)
+    print("embed_backward strides", dtype, rows, accumulate, flush=True)
+    pb.embed_backward(tokens, dy, dense, ws, scale=0.75, accumulate=accumulate)
+    pb.embed_backward(tokens, _strided(torch, dy, 1, 2), strided, ws, scale=0.75, accumulate=accumulate)
+    ref, err, count = _embed_gradient(torch, tokens, dy, vocab, 0.75, first if accumulate else None)
+    _near(torch, dense, ref, err, dtype, "dweight")
+    assert torch.equal(strided, dense) and torch.isnan(strided._base[:, :1]).all() and torch.isnan(strided._base[:, 1 + d:]).all()
+    # one row of dy for all tokens, as the gradient of a sum has it
+    same = dy[:1].expand(rows, d)
+    pb.embed_backward(tokens, same, dense, ws)
+    pb.embed_backward(tokens, same.contiguous(), strided, ws)
+    assert same.stride(0) == 0 and torch.equal(strided, dense)
+
+
+def test_embed_sorted_gradient_is_the_slope_of_the_loss(gpu):
+    torch, pb = gpu
+    tokens, w, dy = _words(torch, 1, 300, 6), _randn(torch, 2, 6, 5), _randn(torch, 3, 300, 5)
+    y, dw = torch.empty(300, 5, device="cuda"), torch.empty(6, 5, device="cuda")
+    pb.embed_backward(tokens, dy, dw, _workspace(torch, pb.embed_workspace_bytes(300, 6, 5)), scale=2.0)
+
+    def loss(x):
+        pb.embed_forward(tokens, x, y, scale=2.0)
+        return float((y.double() * dy.double()).sum())
+    for i in range(30):
+        a, b = w.clone(), w.clone()
+        a.view(-1)[i] += 0.5
+        b.view(-1)[i] -= 0.5
+        # the loss is linear; of its terms 300 at most have this number, each rounded to 2^-24 of at most 2 * 4 * 4 when it is formed and when it is added
+        assert abs(float(dw.view(-1)[i]) - (loss(a) - loss(b))) < 300 * 2 * 4 * 4 * 2 * E
+
+
+def test_embed_sorted_gradient_offsets_beyond_32_bits(gpu):
+    """A table of 2.2G elements, written in its first and last rows; one token is longer than a piece."""
+    torch, pb = gpu
+    vocab, d, rows = 1 << 20, 2112, 300
+    dw = torch.full((vocab, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    tokens = torch.randint(vocab - 9, vocab - 1, (rows,), generator=torch.Generator().manual_seed(1))
+    tokens[::3], tokens[1], tokens[2] = vocab - 1, 0, vocab
+    dy = _randn(torch, 2, rows, d, dtype="bf16")
+    print("embed_backward far table", flush=True)
+    pb.embed_backward(tokens.cuda(), dy, dw, _workspace(torch, pb.embed_workspace_bytes(rows, vocab, d)))
+    at = torch.where(tokens == 0, 0, tokens - (vocab - 10)).cuda()                     # tokens by their place among the first and the last nine rows
+    ref, err, count = _embed_gradient(torch, torch.where(tokens.cuda() < vocab, at, -1), dy, 10, 1.0)
+    assert int(count[9]) == 100 and int(count[0]) == 1
+    _near(torch, torch.cat([dw[:1], dw[-9:]]), ref, err, "bf16", "dweight")
+    assert bool((dw[1:-9] == 0).all())
+
+
+def test_embed_activations_beyond_32_bits(gpu):
+    """2.2G elements of y and dy, padding but for tokens at the ends and between."""
+    torch, pb = gpu
+    rows, vocab, d = (1 << 20) + 700, 50, 2112
+    tokens = torch.full((rows,), -1, dtype=torch.int32)
+    places = torch.cat([torch.arange(200), torch.arange(rows // 2, rows // 2 + 9), torch.arange(rows - 400, rows)])
+    tokens[places] = _words(torch, 1, len(places), vocab, "i32").cpu()
+    tokens[-1] = 49
+    w, tokens = _randn(torch, 2, vocab, d, dtype="bf16"), tokens.cuda()
+    y, dw = torch.full((rows, d), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.empty_like(w)
+    print("embed far activations", flush=True)
+    pb.embed_forward(tokens, w, y)
+    live = (tokens >= 0) & (tokens < vocab)
+    # every row: the table's own numbers where there is a token, zeros elsewhere
+    assert bool((y[~live] == 0).all()) and torch.equal(y[live], w[tokens[live].long()])
+    y[live] = _randn(torch, 3, int(live.sum()), d, dtype="bf16")
+    pb.embed_backward(tokens, y, dw, _workspace(torch, pb.embed_workspace_bytes(rows, vocab, d)))
+    ref, err, _ = _embed_gradient(torch, tokens[live], y[live], vocab, 1.0)
+    _near(torch, dw, ref, err, "bf16", "dweight")
+
+
+# past the caches: wide rows with a tail, narrow rows of which four go to a thread
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(33000, 40000, 4100, "bf16"), (33000, 40000, 4096, "f16"), (33000, 9000, 2050, "f32"), (2200000, 1000, 64, "bf16"), (600000, 70001, 250, "f32")])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_beyond_the_last_level_cache(gpu, rows, vocab, d, dtype, accumulate):
+    torch, pb = gpu
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda n: torch.randn(n, d, generator=gen, device="cuda").to({"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype])     # noqa: E731
+    tokens, w, dy, dw = _words(torch, 1, rows, vocab), new(vocab), new(rows), new(vocab)
+    y = torch.full_like(dy, float("nan"))
+    assert y.nbytes > 256e6
+    print("embed beyond the cache", rows, vocab, d, dtype, accumulate, flush=True)
+    pb.embed_forward(tokens, w, y, scale=1.25)
+    live = ((tokens >= 0) & (tokens < vocab))[:, None]
+    # 1.25 times a 16-bit number is exact in 32 bits and rounded once to the type; of an fp32 number it is the one rounding
+    assert torch.equal(y, torch.where(live, (w[tokens.clamp(0, vocab - 1)].float() * 1.25).to(w.dtype), 0.0))
+    ref, err, count = _embed_gradient(torch, tokens, dy, vocab, 1.25, dw if accumulate else None)
+    before = dw.clone()
+    pb.embed_backward(tokens, dy, dw, _workspace(torch, pb.embed_workspace_bytes(rows, vocab, d)), scale=1.25, accumulate=accumulate)
+    _near(torch, dw, ref, err, dtype, "dweight")
+    if accumulate:
+        assert torch.equal(dw[count == 0], before[count == 0])
+
+
 # ------------------------------------------------------------------------------------------------- vocabulary loss
 LARGE = (1210, 2730, 3040)           # fp32 logits from pairs of fp16 terms, the vocabulary ends inside a tile
 
