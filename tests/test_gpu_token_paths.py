@@ -170,6 +170,116 @@ def test_head_loss_large_numbers_that_never_meet(gpu):
     _within(_np(dw), r["dweight"], _round(r["dweight"], r["dweight_err"], "f32"), "dweight")
 
 
+# few rows: tiles of 128 x 32 and 128 x 64, dz in two terms (three of fp32)
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(16, 25000, 256, "bf16"), (48, 25000, 256, "bf16"), (32, 24700, 256, "f16"), (64, 25100, 200, "f16"), (17, 25000, 70, "f32"),
+                                                (33, 25003, 100, "f32"), (1, 25000, 64, "bf16"), (30, 24700, 2100, "f16")])
+@pytest.mark.parametrize("gradients", [False, True])
+def test_head_loss_of_few_rows_of_a_large_vocabulary(gpu, rows, vocab, d, dtype, gradients):
+    torch, pb = gpu
+    h, w, labels, g = _head_inputs(torch, rows, vocab, d, dtype)
+    labels[-1] = vocab - 1
+    _check_head(torch, pb, h, w, labels, g, dtype, (rows, vocab, d, dtype, gradients), gradients)
+
+
+def _head_reference(torch, h, w, labels, g, dtype, gradients):
+    """The oracle's values and bounds (oracle.tokens.head_loss has their derivation) on the GPU, in 64 bits, a range of rows at a time."""
+    (n, d), v = h.shape, w.shape[0]
+    half, least, pairs = HALF[dtype], 2.0 ** -38 if dtype == "f16" else 0.0, dtype == "f32" and n * v * d >= 1e10
+    w = w.double()
+    aw, wt = w.abs(), w.t().contiguous()
+    awt = aw.t().contiguous()
+    live = (labels >= 0) & (labels < v)
+    at, g = torch.where(live, labels, 0).long()[:, None], torch.where(live, g.double(), 0.0)[:, None]
+    parts = {k: [] for k in ("loss", "loss_err", "lse", "lse_err", "dh", "dh_err")}
+    dw, dw_err = (torch.zeros_like(w), torch.zeros_like(w)) if gradients else (None, None)
+    step = max(1, (1 << 26) // v)
+    for i in range(0, n, step):
+        s = slice(i, i + step)
+        x, a, gi, on = h[s].double(), at[s], g[s], live[s][:, None]
+        ax = x.abs()
+        z, size = x @ wt, ax @ awt
+        zerr = (2 * d + 32) * E * size
+        if pairs:
+            zerr = 3 * zerr + 3 * 2.0 ** -22 * size + 2.0 ** -38 * 1.01 * (ax.amax(1, keepdim=True) * aw.sum(1)[None] + aw.max() * ax.sum(1, keepdim=True))
+        lse = torch.logsumexp(z, 1, keepdim=True)
+        p = torch.exp(z - lse)
+        perr = zerr + (8 + 2 * (z - lse).abs()) * E
+        lse_err = (p * perr).sum(1, keepdim=True) + (160 + v / 2048) * E + 2 * E * lse.abs()
+        label = z.gather(1, a)
+        parts["lse"].append(lse[:, 0])
+        parts["lse_err"].append(lse_err[:, 0])
+        parts["loss"].append(torch.where(on, lse - label, 0.0)[:, 0])
+        parts["loss_err"].append(torch.where(on, lse_err + zerr.gather(1, a) + 2 * E * (lse.abs() + label.abs()), 0.0)[:, 0])
+        if not gradients:
+            continue
+        hot = torch.zeros_like(p).scatter_(1, a, on.double())
+        dz = gi * (p - hot)
+        off = gi.abs() * (p * (perr + lse_err) + 2 * E * (p + hot))
+        off = off + (dz.abs() + off) * half + torch.where(gi != 0, least * float(g.abs().max()), 0.0) + 2 * otk.LEAST * gi.abs()
+        x, ax = torch.where(on, x, 0.0), torch.where(on, ax, 0.0)
+        parts["dh"].append(dz @ w)
+        parts["dh_err"].append(off @ aw + (2 * v + 64) * E * (dz.abs() @ aw) + v * otk.LEAST)
+        dw += dz.t().contiguous() @ x
+        dw_err += off.t().contiguous() @ ax + (2 * n + 64) * E * (dz.abs().t().contiguous() @ ax)
+    r = {k: torch.cat(t) for k, t in parts.items() if t}
+    return {**r, "dweight": dw, "dweight_err": dw_err + n * otk.LEAST} if gradients else r
+
+
+def _check_head_on_gpu(torch, pb, rows, vocab, d, dtype, gradients, stride=None):
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    h = torch.randn(rows, d, generator=gen, device="cuda").to(dt)
+    w = torch.full((vocab, stride or d), float("nan"), dtype=dt, device="cuda")[:, :d]
+    w.copy_(torch.randn(vocab, d, generator=gen, device="cuda") * 2.0 * d ** -0.5)
+    g = (0.5 + torch.rand(rows, generator=gen, device="cuda")) / rows
+    labels = _words(torch, 3, rows, vocab)
+    # a vocabulary is cut at multiples of 256: labels on both sides of each
+    cuts = torch.arange(256, vocab, 256, device="cuda")
+    sides = torch.cat([cuts, cuts - 1, torch.tensor([vocab - 1], device="cuda")])[-rows:]
+    labels[:len(sides)] = sides
+    out = [torch.full((rows,), float("nan"), device="cuda"), torch.full((rows,), float("nan"), device="cuda")] + [torch.full_like(t, float("nan")) for t in (h, w)]
+    ws = torch.full((pb.head_loss_workspace_bytes(rows, vocab, d, dt, gradients),), 255, device="cuda", dtype=torch.uint8)
+    print("head_loss", rows, vocab, d, dtype, gradients, flush=True)
+    more = dict(dh=out[2], dweight=out[3]) if gradients else {}
+    pb.head_loss(h, w, labels, out[0], ws, lse=out[1], row_weight=g, **more)
+    r = _head_reference(torch, h, w, labels, g, dtype, gradients)
+    for name, got in zip(("loss", "lse") + (("dh", "dweight") if gradients else ()), out):
+        if got.dtype is torch.float32:
+            bad = ~((got.double() - r[name]).abs() <= r[name + "_err"] + (got.double().abs() * 2 * E if name[0] == "d" else 0.0))
+            assert not bool(bad.any()), (name, int(bad.sum()), bad.nonzero()[:3].tolist(), got[bad][:3], r[name][bad][:3])
+        else:
+            _near(torch, got, r[name], r[name + "_err"], dtype, name)
+    ws.fill_(0)
+    again = [torch.empty_like(t) for t in out]
+    more = dict(dh=again[2], dweight=again[3]) if gradients else {}
+    pb.head_loss(h, w, labels, again[0], ws, lse=again[1], row_weight=g, **more)
+    assert all(torch.equal(a, b) for a, b in zip(out[:4 if gradients else 2], again))
+
+
+# dz of the whole vocabulary would pass its share of the workspace: two or three pieces, the last one shorter and no multiple of a slice.  W as it lies,
+# in rows with gaps, laid out; sums of dh in parts and in one; fp32 in triples and in pairs, whose tiles are 256 x 256 here
+@pytest.mark.parametrize("rows,vocab,d,dtype,stride", [(16000, 20000, 128, "bf16", None), (16001, 20011, 64, "f16", None), (16000, 20011, 128, "bf16", 144), (16000, 20011, 72, "f16", None),
+                                                       (15999, 40007, 64, "bf16", 67), (16000, 19999, 1100, "bf16", None), (16000, 6500, 100, "f32", None), (16000, 12511, 24, "f32", None),
+                                                       (4097, 30011, 90, "f32", None), (5000, 20003, 1030, "f32", None)])
+def test_head_loss_gradients_in_pieces(gpu, rows, vocab, d, dtype, stride):
+    torch, pb = gpu
+    _check_head_on_gpu(torch, pb, rows, vocab, d, dtype, True, stride)
+
+
+# a weight that is laid out for the losses alone: 128 x 64 and 256 x 256 tiles, pairs of fp16 terms and 16-bit numbers, in pieces
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(40, 100501, 2990, "f32"), (300, 120003, 2560, "f32"), (300, 120003, 2565, "bf16"), (2000, 32771, 1024, "f32")])
+def test_head_loss_losses_of_large_calls(gpu, rows, vocab, d, dtype):
+    torch, pb = gpu
+    _check_head_on_gpu(torch, pb, rows, vocab, d, dtype, False)
+
+
+# W as it lies, in one piece: 256 x 256, 128 x 128 and 64 x 64 tiles, dh in parts, sums of dW short and long
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(256, 24700, 2112, "bf16"), (4096, 12000, 256, "f16"), (2500, 12300, 1024, "bf16"), (1210, 2731, 3008, "bf16"), (700, 50001, 512, "f16")])
+def test_head_loss_gradients_of_large_tiles(gpu, rows, vocab, d, dtype):
+    torch, pb = gpu
+    _check_head_on_gpu(torch, pb, rows, vocab, d, dtype, True)
+
+
 # -------------------------------------------------------------------------------------- distillation from top logits
 @pytest.mark.parametrize("vocab,dtype", [(9000, "f32"), (50021, "f32"), (262144, "f32"), (1 << 21, "f32"), (131072, "bf16"), (1 << 21, "bf16"), ((1 << 21) + 1, "f16")])
 @pytest.mark.parametrize("temperature", [1.0, 2.0])
