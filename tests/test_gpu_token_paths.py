@@ -310,6 +310,58 @@ def test_topk_distill_of_confident_rows(gpu, vocab, dtype, temperature):
     _within(_np(dz), r["dlogits"], _round(r["dlogits"], temperature * (off[:, None] + 2 * otk.LEAST), dtype), "dlogits")
 
 
+def _distill_reference(torch, z, t, at, temperature, g):
+    """The oracle's values and bounds (oracle.tokens.topk_distill) on the GPU, in 64 bits, a range of rows at a time: losses, dlogits in ranges."""
+    n, v = z.shape
+    top, step = at.shape[1], max(1, (1 << 26) // v)
+    for i in range(0, n, step):
+        s = slice(i, i + step)
+        x, c, a = z[s].double() / temperature, t[s].double() / temperature, at[s].long()
+        known = (a >= 0) & (a < v)
+        a = torch.where(known, a, 0)
+        some = known.any(1)
+        lse = torch.logsumexp(x, 1)
+        lse_err = (32 + v / 1024 + 4 * x.abs().amax(1)) * E
+        log_q = torch.where(known, c, -torch.inf)
+        log_q = log_q - torch.where(some, torch.logsumexp(log_q, 1), 0.0)[:, None]
+        q = torch.exp(log_q)
+        xj = x.gather(1, a)
+        qerr = ((16 + top / 64 + 6 * torch.where(known, c.abs(), 0.0).amax(1)) * E)[:, None]
+        loss = torch.where(known, q * (log_q - xj + lse[:, None]), 0.0).sum(1) * temperature ** 2
+        size = torch.where(known, q * (log_q.abs() + xj.abs() + lse.abs()[:, None]), 0.0)
+        loss_err = torch.where(some, temperature ** 2 * ((size * ((top / 64 + 16) * E + qerr)).sum(1) + lse_err), 0.0)
+        p = torch.exp(x - lse[:, None])
+        c = torch.where(some, g[s].double() * temperature, 0.0)[:, None]
+        derr = (p * (lse_err[:, None] + (8 + 4 * x.abs()) * E)).scatter_add_(1, a, q * (qerr + top * E))
+        dz = p.scatter_add_(1, a, -q) * c
+        yield s, loss, loss_err, dz, (derr + 2 * otk.LEAST) * c.abs() + 4 * E * dz.abs()
+
+
+# past the caches, in each number of threads a row; rows that begin between two words
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(40000, 4096, 33, "bf16"), (9000, 8191, 40, "f32"), (9001, 15001, 100, "f16"), (1100, 131071, 64, "f16"), (1001, 131072, 300, "bf16"),
+                                                  (700, 100003, 7, "f32")])
+def test_topk_distill_beyond_the_last_level_cache(gpu, rows, vocab, top, dtype):
+    torch, pb = gpu
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    z = (torch.randn(rows, vocab, generator=gen, device="cuda") * 3.0).to({"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype])
+    assert z.nbytes > 256e6
+    t, at = torch.randn(rows, top, generator=gen, device="cuda") * 3.0, torch.randint(-1, vocab + 1, (rows, top), generator=gen, device="cuda", dtype=torch.int32)
+    at[rows // 2] = -1
+    g = 0.5 + torch.rand(rows, generator=gen, device="cuda")
+    loss, only, dz = torch.full((rows,), float("nan"), device="cuda"), torch.full((rows,), float("nan"), device="cuda"), torch.full_like(z, float("nan"))
+    print("topk_distill beyond the cache", rows, vocab, top, dtype, flush=True)
+    pb.topk_distill(z, t, at, loss, temperature=2.0, row_weight=g, dlogits=dz)
+    pb.topk_distill(z, t, at, only, temperature=2.0)
+    seen = 0
+    for s, ref, err, dref, derr in _distill_reference(torch, z, t, at, 2.0, g):
+        for got in (loss, only):
+            bad = ~((got[s].double() - ref).abs() <= err)
+            assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:3].tolist(), got[s][bad][:3], ref[bad][:3], err[bad][:3])
+        _near(torch, dz[s], dref, derr, dtype, "dlogits")
+        seen += len(ref)
+    assert seen == rows
+
+
 # ------------------------------------------------------------------------------------------------------------ refusals
 def test_binding_refuses_missing_tensors(gpu):
     torch, pb = gpu
