@@ -13,8 +13,8 @@
 //             do not occur.
 //   3. join   Adds the partial sums of each long token, in order.
 //
-// Measured (bf16): 32768 tokens of 65536 by 2048 lookup 35 us, sort 14, sum 81 (5.0 TB/s), join 7; 65536 of 131072 by 4096, added to the
-// table's other gradient, 133, 20, 192, 17; 64 tokens by 2048 2.5 us, which is a launch's own length.
+// Measured (bf16): 32768 tokens of 65536 by 2048 lookup 41 us (4.3 TB/s), sort 14, sum 82 (4.9 TB/s), join 7; 65536 of 131072 by 4096, added to the
+// table's other gradient, 145, 20, 193, 17; 64 tokens by 2048 2.4 us, which is a launch's own length.
 #include "seq_common.h"
 
 namespace pbkd {

@@ -7,11 +7,11 @@
 // second a piece's dz comes out of the product once, n by v: dh reads it along v with W as it lies, dW along n with a copy of h's other layout, by the
 // transposing reads of head_gemm.h.
 //
-// Measured (bf16): 8192 rows by 4096 over 131072 27.8 ms, 1270 TFLOP/s over the four products; 4096 by 2048 over 65536 3.79 ms, 1160; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 74 us in eight launches.
+// Measured (bf16): 8192 rows by 4096 over 131072 27.8 to 28.1 ms, 1250 to 1270 TFLOP/s over the four products; 4096 by 2048 over 65536 3.79 ms, 1160; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 71 us in nine launches.
 //
 // dz is rounded to the operands' type, which is an error of the size that rounding the gradients has anyway (half a step of a
-// value, averaged over the sum); for few rows it is kept in two terms.  It is formed with row weights times a power of two that puts the largest near 2^15: fp16 keeps
-// probabilities down to 2^-24 / 2^15 of it.  fp32 is kept in three bf16 terms.
+// value, averaged over the sum); for few rows it is kept in two terms.  It is formed with row weights times a power of two that puts the largest between 2^13 and 2^14: fp16 keeps
+// probabilities in steps of 2^-24 / 2^13 of it.  fp32 is kept in three bf16 terms.
 #include <type_traits>
 
 #include "head_gemm.h"
@@ -25,7 +25,7 @@ constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
 // Up to here dz is kept in two terms: a few rows' rounding errors do not average out, and the products wait for W anyway.
 constexpr int kFewRows = 64;
 // From here on (rows x vocabulary x width) fp32 logits come from pairs of fp16 terms, three products instead of six of triples: 4096 x 32768 x 1024 with
-// gradients 7.10 -> 6.16 ms (4.7 since dz is written once), losses alone 1.46 -> 0.82 ms.  Below, looking for the largest numbers costs more than it saves: 500 x 1013 x 515 73 -> 90 us.
+// gradients 7.10 -> 6.16 ms (4.7 since dz is written once), losses alone 1.46 -> 0.93 ms (0.79 since).  Below, looking for the largest numbers costs more than it saves: 500 x 1013 x 515 73 -> 90 us.
 constexpr double kPairsFrom = 1e10;
 constexpr double kPieceBytes = 600e6;        // dz of a piece: with 300 MB 8192 x 131072 x 4096 27.9 instead of 27.8 ms, with 150 28.4
 

@@ -4,7 +4,8 @@ What stands in front of a sequence model's first block and behind its last, with
 
     x = scale * table[token],  s <- x + block_1(x) + ...,  h = norm(s),  logits = h table^T
 
-The table is the last product's weight too, so it has two gradients: the loss writes one, the embedding's is added to it.  Blocks that were distilled
+The table is the last product's weight too, so it has two gradients: the loss writes one, the embedding's is added to it (each time
+in fp32 and rounded to bf16: two roundings, of which the second is what a sum of two bf16 gradients has anyway).  Blocks that were distilled
 one by one against a teacher's can be put between, and the whole then learns on text: `learn` from labels (softmax cross entropy over
 the whole vocabulary, whose logits are never kept), `imitate` from the teacher's largest logits, stored beforehand.
 

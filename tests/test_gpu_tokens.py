@@ -187,7 +187,7 @@ def test_head_loss(gpu, rows, vocab, d, dtype, index, gradients):
     _check_head(torch, pb, h, w, labels, g, dtype, (rows, vocab, d, dtype, gradients), gradients)
 
 
-# large tiles for the losses, for the weight's gradient, for h's gradient; a vocabulary in pieces
+# large tiles for the losses, for the weight's gradient, for h's gradient
 @pytest.mark.parametrize("rows,vocab,d,dtype", [(1600, 8200, 128, "bf16"), (1500, 8300, 70, "f16"), (70, 8200, 1600, "bf16"), (3100, 700, 4100, "bf16"), (8000, 6000, 40, "f32"),
                                                 (1300, 10000, 64, "f32")])
 def test_head_loss_of_large_tiles_and_pieces(gpu, rows, vocab, d, dtype):
