@@ -549,8 +549,9 @@ pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *desc, void *hip_stre
  * (0 where label_n names nothing), the gradients of sum over n of row_weight_n loss_n:
  *   dh_n = sum over v of dz_nv weight_v,   dweight_v = sum over n of dz_nv h_n   (both overwritten, of `dtype`).
  * row_weight_dev nullable: 1.  lse_dev nullable.  What h holds in a row whose label names nothing has no influence on anything but that row's lse.
- * Products of 16-bit types run on the matrix cores with fp32 sums; dz is rounded to `dtype` before it is multiplied (up to 64 rows: kept in two
- * terms).  fp32 products are sums of six products of bf16 terms, off by 2^-24 of the products' magnitudes; the logits of calls with rows * vocab * d of 1e10 or
+ * Products of 16-bit types run on the matrix cores with fp32 sums; dz is rounded to `dtype` before it is multiplied, but for dz_{n,label_n}, most of both
+ * gradients, which stays in fp32 (small calls: all of dz is kept in two terms).  dh_dev may be h_dev and dweight_dev weight_dev, with the same strides (dz is then kept in
+ * two terms too, which takes more time).  fp32 products are sums of six products of bf16 terms, off by 2^-24 of the products' magnitudes; the logits of calls with rows * vocab * d of 1e10 or
  * more are sums of three products of fp16 terms, off by 2^-20 and by 2^-38 of the largest numbers of weight and of h's row.
  * workspace: pbkd_head_loss_workspace_bytes().  rows >= 0, vocab >= 1, d >= 1; PBKD_EUNSUPPORTED for rows above 2^21, vocab above 2^22, d above 65536. */
 typedef struct {

@@ -42,7 +42,7 @@ def _softmax(z):
 
 
 def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0, pairs=False):
-    """A dict: loss, lse, dh, dweight and their bounds.  half: what rounding dz to its type is off by at most, relative to the value; least: and absolutely, in units of the
+    """A dict: loss, lse, dh, dweight and their bounds.  half: what rounding dz to its type is off by at most, relative to the value, where v is not the row's label; least: and absolutely, in units of the
     largest row weight (a type without small numbers).  pairs: the logits are products of pairs of fp16 terms: a number scaled to at most 2^14 is the sum of
     its terms up to 2^-22 of itself (two roundings of 2^-11) and 2^-25 (half fp16's smallest step; the largest lies above 2^13: 2^-38 of it), and of
     a product the terms' smallest part, 2^-22, is left out; three products are summed for each."""
@@ -70,7 +70,8 @@ def head_loss(h, weight, labels, row_weight=None, half=EPS32, least=0.0, pairs=F
     hot[rows[live], labels[live]] = 1.0
     dz = g[:, None] * (p - hot)
     off = np.abs(g)[:, None] * (p * (perr + lse_err[:, None]) + 2 * EPS32 * (p + hot))
-    off = off + (np.abs(dz) + off) * half + np.where(g[:, None] != 0, least * np.abs(g).max(initial=0.0), 0.0) + 2 * LEAST * np.abs(g)[:, None]
+    # a row's own label is most of its gradient: it is kept in two terms at least (what rounding leaves is rounded once more)
+    off = off + (np.abs(dz) + off) * np.where(hot > 0, max(half * half, EPS32), half) + np.where(g[:, None] != 0, least * np.abs(g).max(initial=0.0), 0.0) + 2 * LEAST * np.abs(g)[:, None]
     hl = np.where(live[:, None], h, 0.0)
     dh, dw = dz @ w, dz.T @ hl
     dh_err = off @ np.abs(w) + (2 * v + 64) * EPS32 * (np.abs(dz) @ np.abs(w)) + v * LEAST

@@ -15,6 +15,7 @@
 //
 // Measured (bf16): 32768 tokens of 65536 by 2048 lookup 41 us (4.3 TB/s), sort 14, sum 82 (4.9 TB/s), join 7; 65536 of 131072 by 4096, added to the
 // table's other gradient, 145, 20, 193, 17; 64 tokens by 2048 2.4 us, which is a launch's own length.
+#include "label_sums.h"
 #include "seq_common.h"
 
 namespace pbkd {
@@ -95,6 +96,7 @@ struct SortArgs {
   int *order, *keys, *live;
   Range *ranges;
   int rows, v, groups, bins;
+  int *slot;                 // null, or [v]: where a token's rows begin in the list, -1 for none
 };
 
 // The lists of 16 waves, each of which reads a sixteenth of the tokens, follow each other within a token: rows stay in order.
@@ -163,6 +165,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs A) {
   for (int k = 0; k < kSortWaves; ++k) first += before_sum[k] + (k < wave ? wave_sum[k] : 0);
   if (tid < A.bins) {
     A.ranges[mine * A.bins + tid] = Range{first, total};
+    if (A.slot && (tid << shift | mine) < A.v) A.slot[tid << shift | mine] = total ? first : -1;
     for (int k = 0; k < kSortWaves; ++k) {
       const int x = at[k][tid];
       at[k][tid] = first;
@@ -230,12 +233,25 @@ struct SumArgs {
   long long rows, dys, dws, sum_blocks;
   int v, d, groups, bins, piece, accumulate;
   float scale;
+  // LABELS (label_sums.h): of the rows; what each sum is added to; the scale's place
+  const float *weights, *base, *scale_at;
+  const int *slot;
+  long long base_ld;
 };
 
-template <typename T, bool FAR>
-__device__ __forceinline__ void put_row(const SumArgs &A, int key, int c, const float (&acc)[8]) {
+// slot: of the token in base
+template <typename T, bool FAR, bool LABELS = false>
+__device__ __forceinline__ void put_row(const SumArgs &A, int key, long long slot, int c, const float (&acc)[8]) {
   T *p = static_cast<T *>(A.dw) + key * A.dws + c;
   float x[8] = {};
+  if constexpr (LABELS) {
+    load_n<float, 8>(A.base + slot * A.base_ld + c, A.d - c, x);
+    const float scale = *A.scale_at;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = (x[k] + acc[k]) * scale;
+    store_n<T, 8>(p, A.d - c, x);
+    return;
+  }
   if (A.accumulate) load_n<T, 8, FAR>(p, A.d - c, x);
 #pragma unroll
   for (int k = 0; k < 8; ++k) x[k] = A.accumulate ? x[k] + acc[k] * A.scale : acc[k] * A.scale;
@@ -251,7 +267,7 @@ __device__ __forceinline__ Range range_of(const SumArgs &A, int key) {
 
 // A piece takes the tokens that begin in it, to their ends: up to another piece's length behind its own.  Tokens with more rows than a
 // piece are cut where the pieces are, and leave partial sums: slot 0 of a piece is the token that began before it, slot 1 the one that goes on.
-template <typename T, int TPR, bool FAR>
+template <typename T, int TPR, bool FAR, bool LABELS>
 __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
   const int sub = threadIdx.x / TPR, c = (blockIdx.y * TPR + threadIdx.x % TPR) * 8;
   if (blockIdx.x >= A.sum_blocks) {
@@ -288,6 +304,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
   }
   float acc[8] = {};
   bool head = true;                  // the sum is of the piece's first token
+  int begin = i;                     // where the sum's token begins, if it does in this piece
   constexpr int U = 8;
   const T *dy = static_cast<const T *>(A.dy);
   for (; i < n; i += U) {
@@ -295,6 +312,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
     int key[U + 1];
 #pragma unroll
     for (int k = 0; k <= U; ++k) key[k] = keys[i + k < n ? i + k : n - 1];
+    float weight[U];
+    if constexpr (LABELS) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) weight[k] = A.weights[order[i + k < n ? i + k : n - 1]];
+    }
     if (c + 8 <= A.d) {
 #pragma unroll
       for (int k = 0; k < U; ++k) x[k] = far_load<FAR, T, 8>(dy + order[i + k < n ? i + k : n - 1] * A.dys + c);
@@ -310,15 +332,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
     for (int k = 0; k < U; ++k) {
       if (i + k >= n) break;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += static_cast<float>(x[k][e]);
+      for (int e = 0; e < 8; ++e) acc[e] += LABELS ? weight[k] * static_cast<float>(x[k][e]) : static_cast<float>(x[k][e]);
       const bool last = i + k == n - 1;
       if (!last && key[k + 1] == key[k]) continue;
       const bool open_front = head && from_before, open_back = last && goes_on;
       if (open_front || open_back) store_n<float, 8>(A.partial + (p * 2 + (open_front ? 0 : 1)) * A.d + c, A.d - c, acc);
-      else put_row<T, FAR>(A, key[k], c, acc);
+      else put_row<T, FAR, LABELS>(A, key[k], first + begin, c, acc);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
       head = false;
+      begin = i + k + 1;
     }
   }
 }
@@ -327,7 +350,7 @@ constexpr int kJoinPieces = 4;       // pieces a workgroup looks at for tokens t
 constexpr int kJoinWaves = 8;
 
 // A wave adds every eighth partial sum of a token, then the eight are added in order.
-template <typename T>
+template <typename T, bool LABELS>
 __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs A, long long pieces) {
   __shared__ float part[kJoinWaves][64][9];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8;
@@ -368,7 +391,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs A, 
       for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += part[w][lane][e];
-      put_row<T, false>(A, v, c, acc);
+      put_row<T, false, LABELS>(A, v, from, c, acc);
     }
     __syncthreads();
   }
@@ -436,7 +459,76 @@ __global__ __launch_bounds__(256) void embed_few_kernel(SumArgs A, const IT *tok
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += i + k < n ? static_cast<float>(y[k][e]) : 0.f;
   }
-  put_row<T, false>(A, (int)x, c, acc);
+  put_row<T, false>(A, (int)x, 0, c, acc);
+}
+
+// Sums by label of up to kFewLabels rows, in one launch: a workgroup for each row and 512 columns; the first row of a label adds all of its rows, each wave every eighth.
+constexpr int kLabelWaves = 8;
+
+template <typename T, typename IT>
+__global__ __launch_bounds__(64 * kLabelWaves) void label_few_kernel(SumArgs A, const IT *labels) {
+  constexpr int W = kLabelWaves, STEPS = kFewLabels / (64 * W), U = 8;
+  __shared__ int list[kFewLabels], count[W];
+  __shared__ float part[W][64][9];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rows = (int)A.rows, row = blockIdx.x, c = (blockIdx.y * 64 + lane) * 8;
+  const IT x = labels[row];
+  if (!(x >= 0 && x < A.v) || A.slot[x] != row) return;
+  // a wave looks through its share of the labels, from this row's on
+  const int steps = (rows - row + 64 * W - 1) / (64 * W), from = row + wave * steps * 64;
+  unsigned long long same[STEPS];
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int i = from + k * 64 + lane;
+    same[k] = __ballot(k < steps && i < rows && labels[i < rows ? i : rows - 1] == x);
+    mine += __popcll(same[k]);
+  }
+  if (lane == 0) count[wave] = mine;
+  __syncthreads();
+  int at = 0, n = 0;
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    if (k < wave) at += count[k];
+    n += count[k];
+  }
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    if (same[k] >> lane & 1) list[at + __popcll(same[k] & ((1ull << lane) - 1))] = from + k * 64 + lane;
+    at += __popcll(same[k]);
+  }
+  __syncthreads();
+  float acc[8] = {};
+  const T *h = static_cast<const T *>(A.dy);
+  for (int i = wave; i < n && c < A.d; i += W * U) {
+    typename VecOf<T, 8>::type y[U];
+    float weight[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) weight[k] = A.weights[list[i + W * k < n ? i + W * k : n - 1]];
+    if (c + 8 <= A.d) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) y[k] = far_load<false, T, 8>(h + list[i + W * k < n ? i + W * k : n - 1] * A.dys + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const T *r = h + list[i + W * k < n ? i + W * k : n - 1] * A.dys + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[k][e] = c + e < A.d ? r[e] : T(0.f);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += i + W * k < n ? weight[k] * static_cast<float>(y[k][e]) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) part[wave][lane][e] = acc[e];
+  __syncthreads();
+  if (wave || c >= A.d) return;
+  const int most = n < W ? n : W;
+  for (int k = 1; k < most; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += part[k][lane][e];
+  put_row<T, false, true>(A, (int)x, row, c, acc);
 }
 
 inline int row_threads(int d) {
@@ -463,22 +555,22 @@ hipError_t launch_fwd(const FwdArgs &A, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool LABELS = false>
 hipError_t launch_sum(SumArgs A, const Plan &p, hipStream_t st) {
   const int tpr = row_threads(A.d);
   A.sum_blocks = cdiv64(p.pieces, 256 / tpr);
   const long long zero_blocks = A.accumulate ? 0 : cdiv64(A.v, kZeroRows);
   const dim3 grid((unsigned)(A.sum_blocks + zero_blocks), (A.d + tpr * 8 - 1) / (tpr * 8));
   const bool far = ((double)A.rows + (A.accumulate ? 0 : A.v)) * A.d * sizeof(T) > kLastLevelCache;
-#define SUM(N)                                                          \
-  case N:                                                               \
-    if (far) embed_sum_kernel<T, N, true><<<grid, 256, 0, st>>>(A);     \
-    else embed_sum_kernel<T, N, false><<<grid, 256, 0, st>>>(A);        \
+#define SUM(N)                                                                  \
+  case N:                                                                       \
+    if (far) embed_sum_kernel<T, N, true, LABELS><<<grid, 256, 0, st>>>(A);     \
+    else embed_sum_kernel<T, N, false, LABELS><<<grid, 256, 0, st>>>(A);        \
     break;
   switch (tpr) { SUM(8) SUM(16) SUM(32) SUM(64) SUM(128) SUM(256) }
 #undef SUM
   if (const hipError_t e = hipGetLastError()) return e;
-  if (p.pieces > 1) embed_join_kernel<T><<<dim3((unsigned)cdiv64(p.pieces, kJoinPieces), (A.d + 511) / 512), 64 * kJoinWaves, 0, st>>>(A, p.pieces);
+  if (p.pieces > 1) embed_join_kernel<T, LABELS><<<dim3((unsigned)cdiv64(p.pieces, kJoinPieces), (A.d + 511) / 512), 64 * kJoinWaves, 0, st>>>(A, p.pieces);
   return hipGetLastError();
 }
 
@@ -502,6 +594,38 @@ pbkd_status check_embed(long long rows, int vocab, int d, int dtype, int index_d
 }
 
 }  // namespace
+
+size_t label_sums_bytes(int n, int vocab, int d) { return n <= kFewLabels ? 0 : make_plan(n, vocab, d).bytes; }
+
+hipError_t launch_label_sort(const LabelSums &q, char *workspace, hipStream_t st) {
+  const Plan p = make_plan(q.n, q.vocab, q.d);
+  const SortArgs S{q.labels, reinterpret_cast<int *>(workspace + p.order), reinterpret_cast<int *>(workspace + p.keys), reinterpret_cast<int *>(workspace + p.live),
+                   reinterpret_cast<Range *>(workspace + p.ranges), q.n, q.vocab, p.groups, p.bins, q.slot};
+  if (q.wide) embed_sort_kernel<long long><<<p.groups, kSortThreads, 0, st>>>(S);
+  else embed_sort_kernel<int><<<p.groups, kSortThreads, 0, st>>>(S);
+  return hipGetLastError();
+}
+
+hipError_t launch_label_sums(const LabelSums &q, char *workspace, hipStream_t st) {
+  const Plan p = make_plan(q.n, q.vocab, q.d);
+  // as with a gradient that is added to another, no zeros are written
+  const SumArgs A{reinterpret_cast<int *>(workspace + p.order), reinterpret_cast<int *>(workspace + p.keys), reinterpret_cast<int *>(workspace + p.live),
+                  reinterpret_cast<Range *>(workspace + p.ranges), q.rows, q.out, reinterpret_cast<float *>(workspace + p.partial), q.n, q.stride, q.out_stride, 0,
+                  q.vocab, q.d, p.groups, p.bins, p.piece, 1, 1.f, q.weights, q.base, q.scale, q.slot, q.base_ld};
+  if (q.n > kFewLabels) return q.dtype == PBKD_BF16 ? launch_sum<bf16, true>(A, p, st) : launch_sum<f16, true>(A, p, st);
+  const dim3 grid(q.n, (q.d + 511) / 512);
+  const int *narrow = static_cast<const int *>(q.labels);
+  const long long *wide = static_cast<const long long *>(q.labels);
+  if (q.dtype == PBKD_BF16) {
+    if (q.wide) label_few_kernel<bf16><<<grid, 64 * kLabelWaves, 0, st>>>(A, wide);
+    else label_few_kernel<bf16><<<grid, 64 * kLabelWaves, 0, st>>>(A, narrow);
+  } else {
+    if (q.wide) label_few_kernel<f16><<<grid, 64 * kLabelWaves, 0, st>>>(A, wide);
+    else label_few_kernel<f16><<<grid, 64 * kLabelWaves, 0, st>>>(A, narrow);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace pbkd
 
 using namespace pbkd;
@@ -552,7 +676,7 @@ pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *q, void *hip_stream)
   Range *ranges = reinterpret_cast<Range *>(ws + p.ranges);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const SumArgs A{order, keys, live, ranges, q->dy_dev, q->dweight_dev, reinterpret_cast<float *>(ws + p.partial), q->rows, q->dy_stride, q->dweight_stride, 0,
-                  q->vocab, q->d, p.groups, p.bins, p.piece, q->accumulate != 0, q->scale};
+                  q->vocab, q->d, p.groups, p.bins, p.piece, q->accumulate != 0, q->scale, nullptr, nullptr, nullptr, nullptr, 0};
   if (q->rows <= kFewRows) {
     const bool wide = q->index_dtype == PBKD_I64;
     switch (q->dtype) {
@@ -562,7 +686,7 @@ pbkd_status pbkd_embed_backward(const pbkd_embed_grad_desc *q, void *hip_stream)
     }
     return PBKD_OK;
   }
-  const SortArgs S{q->tokens_dev, order, keys, live, ranges, (int)q->rows, q->vocab, p.groups, p.bins};
+  const SortArgs S{q->tokens_dev, order, keys, live, ranges, (int)q->rows, q->vocab, p.groups, p.bins, nullptr};
   if (q->index_dtype == PBKD_I64) embed_sort_kernel<long long><<<p.groups, kSortThreads, 0, st>>>(S);
   else embed_sort_kernel<int><<<p.groups, kSortThreads, 0, st>>>(S);
   SEQ_HIPCHK(hipGetLastError());

@@ -28,6 +28,7 @@ namespace head {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 struct Operand {
   const char *p;
@@ -61,6 +62,11 @@ struct GemmArgs {
   char *dz;                        // [n][m]
   long long dz_ld, dz_plane;
   int m_pad;                       // dz is written up to here: zeros behind the end
+  // null, or by place a row of base, -1 where no row has the place as its label.  kDz: dz is zero where a row has its label.  kOut: n is a place too, from v0 on; the results of
+  // those with a slot go to base [slot][m] as well, neither scaled nor rounded
+  const int *slot;
+  float *base;
+  long long base_ld;
   // kOut: out[n][m]; kSum: sum[split][n][m]
   void *out;
   long long out_ld;                // elements
@@ -196,6 +202,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   floatx16 second = acc[0][0];       // of a wave with one MFMA tile: products into one sum alone would wait for each other
   const int r32 = lane & 31, h = lane >> 5;
+  // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
+  const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
+  // Read ahead of the sum, which may be short (128 x 131072 x 8192: dW 790 us without).  The largest tile has no registers for that, and no short sums.
+  constexpr bool EARLY = EPI == kOut && MT * NT < 16;
+  int slot[NT];
+  auto read_slots = [&] {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) slot[j] = G.slot && n1 + 32 * j < G.n ? G.slot[G.v0 + n1 + 32 * j] : -1;
+  };
+  if (EARLY) read_slots();
   // MFMA row 8 a + 4 b + c of tile i is the wave's row b * 16 MT + 16 i + 4 a + c: a lane then holds 16 MT rows in order
   const int row_a = wm * (MT * 32) + (r32 >> 2 & 1) * (16 * MT) + (r32 >> 3) * 4 + (r32 & 3), row_b = wn * (NT * 32) + r32;
   const int sa = swz_a(row_a), sb = swz_b(row_b);       // rows 16 i and 32 j further on are swapped alike
@@ -345,8 +361,6 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     for (int e = 0; e < 16; ++e) acc[0][0][e] += second[e];
   }
 
-  // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
-  const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
   // what belongs to a lane's rows of n, read together: rows behind the end read the last one's
   int label[NT];
   if constexpr (EPI == kStats || EPI == kDz) {
@@ -441,7 +455,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (at == 16 * i + e) acc[i][j][e] -= g[j];
+            if (at == 16 * i + e) acc[i][j][e] = G.slot ? 0.f : acc[i][j][e] - g[j];
       }
       if (__any(!live) || edge) {                        // zeros, whatever the logits are
 #pragma unroll
@@ -500,6 +514,24 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
     float scale = 1.f;
     if (EPI == kOut) scale = *G.scale;
     if constexpr (EPI == kOut && sizeof(OutT) == 2) {
+      if (G.slot) {
+        if (!EARLY) read_slots();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (slot[j] >= 0) {          // up to the row's end in steps of 16 bytes: base's rows are that long
+            float *p = G.base + slot[j] * G.base_ld + m1;
+#pragma unroll
+            for (int i = 0; i < 4 * MT; ++i) {
+              const floatx16 &x = acc[i / 4][j];
+              const int e = i % 4 * 4;
+              if (m1 + 4 * i < G.m) *reinterpret_cast<floatx4 *>(p + 4 * i) = floatx4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < MT; ++i) asm volatile("" : "+a"(acc[i][j]));      // stays where it is, or the copies spill
+        }
+      }
       if (G.whole_rows) {              // 16-byte steps: the results leave in whole rows, as dz does
         constexpr int BYTES = 32 * MT * 32 * NT * 2, FIT = SLICE / BYTES, PM = 4 * MT;
         char *own = (wave < FIT ? s0 : s1) + (wave < FIT ? wave : wave - FIT) * BYTES;

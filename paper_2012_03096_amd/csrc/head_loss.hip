@@ -9,12 +9,15 @@
 //
 // Measured (bf16): 8192 rows by 4096 over 131072 27.8 to 28.1 ms, 1250 to 1270 TFLOP/s over the four products; 4096 by 2048 over 65536 3.79 ms, 1160; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 71 us in nine launches.
 //
-// dz is rounded to the operands' type, which is an error of the size that rounding the gradients has anyway (half a step of a
-// value, averaged over the sum); for few rows it is kept in two terms.  It is formed with row weights times a power of two that puts the largest between 2^13 and 2^14: fp16 keeps
-// probabilities in steps of 2^-24 / 2^13 of it.  fp32 is kept in three bf16 terms.
+// dz is rounded to the operands' type, but not where a row has its label: there it is nearly the row's weight, most of both gradients, and rounding it would be
+// an error of the size that rounding the gradients has anyway (against 64 bits 0.0024 instead of 0.0017).  These numbers, one a row, stay in fp32, and dz is zero there: head_finish
+// adds the label's row of W to dh, and the dW of places that are labels is kept in fp32 until label_sums.h has added their rows of h.  Small calls keep all of dz in two
+// terms.  dz is formed with row weights times a power of two that puts the largest between 2^13 and 2^14: fp16 keeps probabilities in steps of 2^-24 / 2^13 of it.  fp32 is kept
+// in three bf16 terms.
 #include <type_traits>
 
 #include "head_gemm.h"
+#include "label_sums.h"
 
 namespace pbkd {
 namespace {
@@ -22,14 +25,17 @@ namespace {
 using namespace head;
 
 constexpr int kMaxRows = 1 << 21, kMaxVocab = 1 << 22, kMaxD = 65536;
-// Up to here dz is kept in two terms: a few rows' rounding errors do not average out, and the products wait for W anyway.
+// dz is kept in two terms for so few rows, whose products wait for W anyway, and for calls of up to so many products (rows x vocabulary x width), where two more terms
+// take less than another launch: 1000 x 1000 x 512 bf16 43 instead of 50 us, 80 x 20000 x 512 68 instead of 66, 2000 x 8192 x 1024 285 instead of 235.
 constexpr int kFewRows = 64;
+constexpr double kTwoTermsUpTo = 8e8;
 // From here on (rows x vocabulary x width) fp32 logits come from pairs of fp16 terms, three products instead of six of triples: 4096 x 32768 x 1024 with
 // gradients 7.10 -> 6.16 ms (4.7 since dz is written once), losses alone 1.46 -> 0.93 ms (0.79 since).  Below, looking for the largest numbers costs more than it saves: 500 x 1013 x 515 73 -> 90 us.
 constexpr double kPairsFrom = 1e10;
 constexpr double kPieceBytes = 600e6;        // dz of a piece: with 300 MB 8192 x 131072 x 4096 27.9 instead of 27.8 ms, with 150 28.4
 
 inline int up64(long long n) { return (int)((n + 63) / 64 * 64); }
+inline long long up4(int n) { return ((long long)n + 3) / 4 * 4; }        // rows of fp32 that begin at multiples of 16 bytes
 
 // ------------------------------------------------------------------------------------------------------ small kernels
 struct RowArgs {
@@ -78,10 +84,18 @@ struct LayArgs {
   int rows, cols, cols_fill, rows_fill;         // of the source; zeros behind the ends up to *_fill
 };
 
+// slot[0 .. vocab-1] <- -1.
+struct ClearArgs {
+  int *slot;               // null: none
+  int vocab;
+};
+
 // The two layouts that a product reads along k: rows_dst[row][..] = src[row][..] and cols_dst[col][..] = src[..][col], in planes.  Tiles of 64 x 64.
 template <typename T, typename E, int PLANES>
-__global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A) {
+__global__ __launch_bounds__(256) void head_lay_kernel(LayArgs A, ClearArgs C) {
   __shared__ E tile[PLANES][64][66];
+  if (C.slot)
+    for (int v = (blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x; v < C.vocab; v += gridDim.x * gridDim.y * 256) C.slot[v] = -1;
   const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -162,11 +176,16 @@ __global__ __launch_bounds__(256) void head_top_kernel(const float *src, long lo
   else atomicMax(top, bits);
 }
 
-// A workgroup joins a row's pairs, in an order that only their number decides.
+// A workgroup joins a row's pairs, in an order that only their number decides.  at_place, if wanted: dz where the row has its label; slot: the first row with a label.
 __global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int parts, int stride, const void *labels, int wide, int vocab, const float *at_label, float *lse,
-                                                       float *lse_out, float *loss) {
+                                                       float *lse_out, float *loss, const float *g, float *at_place, int *slot) {
   __shared__ float red[2][4];
   const int n = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+  const int label = label_of(labels, wide, vocab, n);
+  const float z = at_label[n], weight = at_place ? g[n] : 0.f;
+  int before = 0;
+  if (slot && label >= 0)
+    for (int k = tid; k < n; k += 256) before |= label_of(labels, wide, vocab, k) == label;
   const float *p = part + (long long)n * stride * 2;
   float top = -__builtin_inff(), sum = 0.f;
   for (int k = tid; k < parts; k += 256) {
@@ -177,9 +196,9 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int pa
   const float most = wave64_max(top), ref = most == -__builtin_inff() ? 0.f : most;
   sum = wave64_sum(sum * expf(top - ref));
   if ((tid & 63) == 0) red[0][wave] = most, red[1][wave] = sum;
-  __syncthreads();
+  if (slot) before = __syncthreads_or(before);
+  else __syncthreads();
   if (tid) return;
-  const int label = label_of(labels, wide, vocab, n);
   top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   const float base = top == -__builtin_inff() ? 0.f : top;
   sum = 0.f;
@@ -187,12 +206,25 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float *part, int pa
   const float x = top + logf(sum);
   lse[n] = x;
   if (lse_out) lse_out[n] = x;
-  loss[n] = label >= 0 ? x - at_label[n] : 0.f;
+  loss[n] = label >= 0 ? x - z : 0.f;
+  if (!at_place) return;
+  at_place[n] = label >= 0 ? weight * expm1f(z - x) : 0.f;
+  if (slot && label >= 0 && !before) slot[label] = n;
 }
 
-// out[n][m] = scale * sum over the splits: eight numbers a thread.  With many splits GROUPS threads share them, and their sums are added in order.
+// What dz is at the rows' labels, where that is not among the products: null, or a number for each row.
+template <typename T>
+struct AtLabel {
+  const float *dz;
+  const T *weight;
+  long long stride;
+  const void *labels;
+  int wide, vocab;
+};
+
+// out[n][m] = scale * (sum over the splits, and the label's part): eight numbers a thread.  With many splits GROUPS threads share them, and their sums are added in order.
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int splits, int rows, int cols, const float *scale, T *out, long long stride) {
+__global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int splits, int rows, int cols, const float *scale, T *out, long long stride, AtLabel<T> at) {
   constexpr int LANES = 256 / GROUPS;
   __shared__ float part[GROUPS][LANES][9];
   const int per = (cols + 7) / 8, lane = threadIdx.x % LANES, g = threadIdx.x / LANES;
@@ -214,6 +246,16 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const float *sum, int 
     for (int k = 1; k < GROUPS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] += part[k][lane][e];
+  }
+  if (at.dz && left > 0) {
+    const int label = label_of(at.labels, at.wide, at.vocab, row);
+    if (label >= 0) {
+      const float dz = at.dz[row];
+      float y[8];
+      load_n<T, 8>(at.weight + label * at.stride + c, left, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += dz * y[e];
+    }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= *scale;
@@ -249,23 +291,25 @@ inline int pick_shape(long long m, long long n, int slices = 0) {
 
 struct Plan {
   int d_pad, n_pad, piece, pieces, planes, dz_planes, parts, first_shape, sum_shape, splits;
-  bool pack_h, pack_w, pairs;
+  bool pack_h, pack_w, pairs, by_label;
   Planes logits, grads;
-  size_t gs, scale, tops, lse, at_label, part, h, ht, w, wpairs, dz, sum, bytes;
+  size_t gs, scale, tops, lse, at_label, part, h, ht, w, wpairs, dz, sum, at_place, slot, base, labels, bytes;
 };
 
 bool direct(const void *p, long long stride, int d, int dtype) {
   return dtype != PBKD_F32 && d % 64 == 0 && stride % 8 == 0 && stride <= 1 << 20 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
-// pack_*: whether the operands have to be laid out (the workspace is counted as if they had)
-Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w) {
+// pack_*: whether the operands have to be laid out (the workspace is counted as if they had).  in_place: a gradient lies where its tensor does, which the last
+// launches read where dz is not zero at the labels.
+Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w, bool in_place) {
   Plan p;
   const bool f32 = dtype == PBKD_F32;
   p.pairs = f32 && (double)rows * vocab * d >= kPairsFrom;
   p.logits = p.pairs ? kPairs : f32 ? kTriples : kOne;         // products of planes for the logits, and for the gradients
-  p.planes = f32 ? 3 : 1, p.dz_planes = f32 ? 3 : rows <= kFewRows ? 2 : 1;
-  p.grads = f32 ? kTriples : rows <= kFewRows ? kTwoOfB : kOne;
+  p.planes = f32 ? 3 : 1, p.dz_planes = f32 ? 3 : rows <= kFewRows || (double)rows * vocab * d <= kTwoTermsUpTo || in_place ? 2 : 1;
+  p.grads = f32 ? kTriples : p.dz_planes == 2 ? kTwoOfB : kOne;
+  p.by_label = gradients && p.dz_planes == 1;
   p.d_pad = up64(d), p.n_pad = up64(rows > 0 ? rows : 1);
   p.pack_h = pack_h, p.pack_w = pack_w;
   // A piece's tiles of 256 x 256 fill whole rounds of the chip where that leaves pieces of a sensible size: 16 rows of tiles, 16 columns.
@@ -303,6 +347,7 @@ Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_
     p.ht = put((size_t)d * p.n_pad * e);
     p.dz = put(R * p.piece * 2 * p.dz_planes);
     p.sum = put((size_t)p.splits * R * d * 4);
+    if (p.by_label) p.at_place = put(R * 4), p.slot = put((size_t)vocab * 4), p.base = put(R * up4(d) * 4), p.labels = put(label_sums_bytes(rows, vocab, d));
   }
   p.bytes = at + 256;
   return p;
@@ -318,7 +363,7 @@ hipError_t launch_gemm(GemmArgs G, int shape, hipStream_t st) {
   switch (shape) {
     case 0:
       if constexpr (PLANES != 2) gemm_kernel<E, OutT, 256, 256, 2, 2, 2, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G);
-      break;                         // kFewRows rows never have so many tiles
+      break;                         // dz in two planes takes smaller tiles
     case 1: gemm_kernel<E, OutT, 128, 128, 2, 2, 4, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
     case 2: gemm_kernel<E, OutT, 64, 64, 2, 2, 4, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
     case 3: gemm_kernel<E, OutT, 128, 64, 4, 1, 3, EPI, PLANES, TA, TB><<<grid, 256, 0, st>>>(G); break;
@@ -337,11 +382,14 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   const bool gradients = q.dh_dev != nullptr;
   auto floats = [&](size_t at) { return reinterpret_cast<float *>(ws + at); };
   const int wide = q.index_dtype == PBKD_I64;
-  auto lay = [&](LayArgs L) {
+  auto lay = [&](LayArgs L, ClearArgs clear = {}) {
     L.wide = wide, L.vocab = V;
     const int r = L.cols_dst ? L.rows_fill : L.rows, c = L.rows_dst || L.pairs_dst ? L.cols_fill : L.cols;
-    head_lay_kernel<T, E, PLANES><<<dim3((r + 63) / 64, (c + 63) / 64), 256, 0, st>>>(L);
+    head_lay_kernel<T, E, PLANES><<<dim3((r + 63) / 64, (c + 63) / 64), 256, 0, st>>>(L, clear);
   };
+  const bool sorted = rows > kFewLabels;
+  const LabelSums sums{q.h_dev, q.h_stride, q.labels_dev, wide != 0, q.dtype, rows, V, d, floats(p.at_place), p.by_label ? reinterpret_cast<int *>(ws + p.slot) : nullptr,
+                       floats(p.base), up4(d), floats(p.scale), q.dweight_dev, q.dweight_stride};
   if (gradients) {
     const RowArgs R{q.labels_dev, q.row_weight_dev, floats(p.gs), floats(p.scale), rows, V};
     if (wide) head_rows_kernel<long long><<<1, 1024, 0, st>>>(R);
@@ -358,7 +406,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   if (p.pack_h || gradients) {
     LayArgs L{q.h_dev, q.h_stride, p.pack_h && !p.pairs ? ws + p.h : nullptr, gradients ? ws + p.ht : nullptr, p.d_pad * 2, (long long)rows * p.d_pad * 2, p.n_pad * 2,
               (long long)d * p.n_pad * 2, p.pairs ? ws + p.h : nullptr, tops + 1, 1, q.labels_dev, 0, 0, rows, d, p.d_pad, p.n_pad};
-    lay(L);
+    lay(L, ClearArgs{sorted ? nullptr : sums.slot, V});
     if (p.pack_h) H = Operand{ws + p.h, L.rows_ld, L.rows_plane, rows};
   }
   // Rows v0 .. v0 + n of W for the logits, as they lie or laid out (a piece that is the whole vocabulary is laid out once); fp32: and for h's gradient.
@@ -385,8 +433,12 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     if (e) return e;
     parts += (int)cdiv64(n, kShapes[p.first_shape].tm);
   }
-  head_lse_kernel<<<rows, 256, 0, st>>>(floats(p.part), parts, p.parts, q.labels_dev, wide, V, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev);
+  head_lse_kernel<<<rows, 256, 0, st>>>(floats(p.part), parts, p.parts, q.labels_dev, wide, V, floats(p.at_label), floats(p.lse), q.lse_dev, q.loss_dev,
+                                        floats(p.gs), p.by_label ? floats(p.at_place) : nullptr, sorted ? nullptr : sums.slot);
   if (!gradients) return hipGetLastError();
+  if (p.by_label && sorted)
+    if (const hipError_t e = launch_label_sort(sums, ws + p.labels, st)) return e;
+  G.slot = sums.slot;
 
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = V - v0 < p.piece ? V - v0 : p.piece, n64 = up64(n);
@@ -396,7 +448,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     G.m_pad = n64;
     hipError_t e = hipSuccess;
     if constexpr (F32) e = p.pairs ? launch_gemm<f16, E, kDz, PLANES>(G, p.first_shape, st) : launch_gemm<E, E, kDz, PLANES>(G, p.first_shape, st);
-    else e = p.dz_planes == 2 ? launch_gemm<E, E, kDz, 2>(G, p.first_shape, st) : launch_gemm<E, E, kDz, 1>(G, p.first_shape, st);
+    else e = p.dz_planes == 2 ? launch_gemm<E, E, kDz, 2>(G, p.first_shape == 0 ? 1 : p.first_shape, st) : launch_gemm<E, E, kDz, 1>(G, p.first_shape, st);
     if (e) return e;
     GemmArgs D{};
     D.planes = p.grads, D.scale = floats(p.scale);
@@ -406,7 +458,7 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
     D.kblocks = n64 / 64, D.splits = p.splits, D.sum = floats(p.sum), D.out_ld = d, D.add = v0 > 0;
     if (const hipError_t e = launch_gemm<E, T, kSum, 1>(D, p.sum_shape, st)) return e;
     D.a = Operand{ws + p.ht, p.n_pad * 2, (long long)d * p.n_pad * 2, d, 0}, D.n = n;      // and dz as it lies
-    D.kblocks = p.n_pad / 64, D.splits = 1;
+    D.kblocks = p.n_pad / 64, D.splits = 1, D.v0 = v0, D.slot = sums.slot, D.base = floats(p.base), D.base_ld = sums.base_ld;
     D.out = static_cast<T *>(q.dweight_dev) + v0 * q.dweight_stride, D.out_ld = q.dweight_stride;
     D.whole_rows = es == 2 && d % 8 == 0 && q.dweight_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(q.dweight_dev) & 15) == 0;
     const int shape = pick_shape(d, n);
@@ -414,12 +466,20 @@ hipError_t run(const pbkd_head_loss_desc &q, const Plan &p, hipStream_t st) {
   }
   const long long eights = (long long)rows * ((d + 7) / 8);
   T *dh = static_cast<T *>(q.dh_dev);
-  if (p.splits >= 8) head_finish_kernel<T, 8><<<(unsigned)cdiv64(eights, 32), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride);
-  else head_finish_kernel<T, 1><<<(unsigned)cdiv64(eights, 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride);
-  return hipGetLastError();
+  const AtLabel<T> at{p.by_label ? floats(p.at_place) : nullptr, static_cast<const T *>(q.weight_dev), q.weight_stride, q.labels_dev, wide, V};
+  if (p.splits >= 8) head_finish_kernel<T, 8><<<(unsigned)cdiv64(eights, 32), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride, at);
+  else head_finish_kernel<T, 1><<<(unsigned)cdiv64(eights, 256), 256, 0, st>>>(floats(p.sum), p.splits, rows, d, floats(p.scale), dh, q.dh_stride, at);
+  if (const hipError_t e = hipGetLastError()) return e;
+  return p.by_label ? launch_label_sums(sums, ws + p.labels, st) : hipSuccess;
 }
 
 inline bool misaligned(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+
+// Whether two matrices of rows x d share memory.
+inline bool meet(const void *a, long long a_stride, const void *b, long long b_stride, long long rows, int d, int size) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + ((rows - 1) * b_stride + d) * size && y < x + ((rows - 1) * a_stride + d) * size;
+}
 
 inline bool supported(long long rows, int vocab, int d) { return rows <= kMaxRows && vocab <= kMaxVocab && d <= kMaxD; }
 
@@ -438,9 +498,13 @@ extern "C" {
 
 size_t pbkd_head_loss_workspace_bytes(long long rows, int vocab, int d, int dtype, int gradients) {
   if (rows < 0 || vocab < 1 || d < 1 || !supported(rows, vocab, d) || (dtype != PBKD_F32 && dtype != PBKD_BF16 && dtype != PBKD_F16)) return 0;
-  // laid out or not: what the addresses and strides of a call decide
-  const size_t a = make_plan((int)rows, vocab, d, dtype, gradients != 0, true, true).bytes, b = make_plan((int)rows, vocab, d, dtype, gradients != 0, true, false).bytes;
-  return a > b ? a : b;
+  // laid out or not, in place or not: what the addresses and strides of a call decide
+  size_t most = 0;
+  for (int k = 0; k < 4; ++k) {
+    const size_t n = make_plan((int)rows, vocab, d, dtype, gradients != 0, true, k & 1, k & 2).bytes;
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 pbkd_status pbkd_head_loss(const pbkd_head_loss_desc *q, void *hip_stream) {
@@ -471,7 +535,9 @@ pbkd_status pbkd_head_loss(const pbkd_head_loss_desc *q, void *hip_stream) {
   const size_t need = pbkd_head_loss_workspace_bytes(q->rows, q->vocab, q->d, q->dtype, q->dh_dev != nullptr);
   if (q->workspace_bytes < need) return set_error(PBKD_ENOMEM, "head_loss: workspace of %zu bytes is smaller than the %zu needed", q->workspace_bytes, need);
   const Plan p = make_plan((int)q->rows, q->vocab, q->d, q->dtype, q->dh_dev != nullptr, !direct(q->h_dev, q->h_stride, q->d, q->dtype),
-                           !direct(q->weight_dev, q->weight_stride, q->d, q->dtype));
+                           !direct(q->weight_dev, q->weight_stride, q->d, q->dtype),
+                           q->dh_dev && (meet(q->h_dev, q->h_stride, q->dh_dev, q->dh_stride, q->rows, q->d, size) ||
+                                         meet(q->weight_dev, q->weight_stride, q->dweight_dev, q->dweight_stride, q->vocab, q->d, size)));
   switch (q->dtype) {
     case PBKD_F32: SEQ_HIPCHK((run<float, bf16, 3>(*q, p, st))); break;
     case PBKD_BF16: SEQ_HIPCHK((run<bf16, bf16, 1>(*q, p, st))); break;

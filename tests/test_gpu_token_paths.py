@@ -215,7 +215,7 @@ def _head_reference(torch, h, w, labels, g, dtype, gradients):
         hot = torch.zeros_like(p).scatter_(1, a, on.double())
         dz = gi * (p - hot)
         off = gi.abs() * (p * (perr + lse_err) + 2 * E * (p + hot))
-        off = off + (dz.abs() + off) * half + torch.where(gi != 0, least * float(g.abs().max()), 0.0) + 2 * otk.LEAST * gi.abs()
+        off = off + (dz.abs() + off) * torch.where(hot > 0, max(half * half, E), half) + torch.where(gi != 0, least * float(g.abs().max()), 0.0) + 2 * otk.LEAST * gi.abs()
         x, ax = torch.where(on, x, 0.0), torch.where(on, ax, 0.0)
         parts["dh"].append(dz @ w)
         parts["dh_err"].append(off @ aw + (2 * v + 64) * E * (dz.abs() @ aw) + v * otk.LEAST)
@@ -278,6 +278,130 @@ def test_head_loss_losses_of_large_calls(gpu, rows, vocab, d, dtype):
 def test_head_loss_gradients_of_large_tiles(gpu, rows, vocab, d, dtype):
     torch, pb = gpu
     _check_head_on_gpu(torch, pb, rows, vocab, d, dtype, True)
+
+
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(65, 300, 64, "bf16"), (130, 1000, 100, "f16"), (700, 2500, 512, "bf16"), (4096, 20000, 512, "bf16"), (3000, 33000, 1030, "f16"), (2048, 9000, 2048, "bf16"), (1000, 10000, 300, "f16")])
+@pytest.mark.parametrize("weights", ["means", "of all sizes"])
+def test_head_loss_gradients_are_off_by_their_own_rounding(gpu, rows, vocab, d, dtype, weights):
+    """16-bit gradients against those in 64 bits, in the 2-norm: hardly more off than the exact ones rounded once to the type.
+
+    Rounding leaves r = |round(x) - x| / |x|.  dz is rounded where v is not the label, which leaves at most half a step of each such number: random signs in sums over rows (columns) make
+    that at most 2 half / sqrt(12) of the norm of those numbers' part, which is sqrt(sum over v of p^2) of g |h| beside the label's 1 - p.  Here no probability is above a
+    quarter but for the label's own, so that the part is below sqrt(1 / 4) of what the label gives, and the whole below sqrt(r^2 + (r / 2)^2) = 1.12 r up to how roundings are distributed: 1.15 r."""
+    torch, pb = gpu
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    h, w = torch.randn(rows, d, generator=gen, device="cuda").to(dt), (torch.randn(vocab, d, generator=gen, device="cuda") * d ** -0.5).to(dt)
+    g = (0.5 + torch.rand(rows, generator=gen, device="cuda")) / rows
+    if weights == "of all sizes":
+        g = g * 2.0 ** torch.randint(-6, 1, (rows,), generator=gen, device="cuda")
+    labels = _words(torch, 3, rows, vocab)
+    # scaled so that the gradients are ordinary fp16 numbers, whose smallest steps do not count here
+    g = g * rows
+    loss, dh, dw = torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(w)
+    print("head_loss as exact as rounding", rows, vocab, d, dtype, weights, flush=True)
+    pb.head_loss(h, w, labels, loss, _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, dt, True)), row_weight=g, dh=dh, dweight=dw)
+    x, y = h.double(), w.double()
+    live = (labels >= 0) & (labels < vocab)
+    p = torch.softmax(x @ y.t().contiguous(), 1)
+    assert float(p.max()) < 0.25
+    p[live.nonzero()[:, 0], labels[live]] -= 1.0
+    p *= torch.where(live, g.double(), 0.0)[:, None]
+    for name, got, ref in (("dh", dh, p @ y), ("dweight", dw, p.t().contiguous() @ x)):
+        off, least = (float((t.double() - ref).norm() / ref.norm()) for t in (got, ref.to(dt)))
+        print(name, f"{off:.6f} {least:.6f}", flush=True)
+        assert off < 1.15 * least, (name, off, least)
+
+
+# dz at the labels in fp32: rows found among all by one launch (up to 2048), or sorted; whole vectors of a row and tails; sums that go on over pieces of the sorted list
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(700, 5000, 264, "bf16"), (2048, 1003, 520, "f16"), (2049, 3000, 136, "f16"), (5000, 2001, 91, "bf16"), (17000, 400, 128, "bf16")])
+@pytest.mark.parametrize("kind", ["words", "one", "two in turn", "all", "none"])
+def test_head_loss_labels_of_every_kind(gpu, rows, vocab, d, dtype, kind):
+    torch, pb = gpu
+    assert rows * vocab * d > 8e8
+    h, w, labels, g = _head_inputs(torch, rows, vocab, d, dtype)
+    i = torch.arange(rows, device="cuda")
+    labels = {"words": labels, "one": torch.full_like(labels, vocab - 1), "two in turn": i % 2 * (vocab - 1), "all": i * 7 % vocab, "none": torch.full_like(labels, -1)}[kind]
+    live = (labels >= 0) & (labels < vocab)
+
+    def run(h, w, labels, dh, dw):
+        loss = torch.full((rows,), float("nan"), device="cuda")
+        pb.head_loss(h, w, labels, loss, _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, w.dtype, True)), row_weight=g, dh=dh, dweight=dw)
+        return loss, dh, dw
+    print("head_loss labels", rows, vocab, d, dtype, kind, flush=True)
+    new = lambda t: torch.full_like(t, float("nan"))                                                 # noqa: E731
+    first = run(h, w, labels, new(h), new(w))
+    r = _head_reference(torch, h, w, labels, g, dtype, True)
+    assert bool(((first[0].double() - r["loss"]).abs() <= r["loss_err"]).all())
+    _near(torch, first[1], r["dh"], r["dh_err"], dtype, "dh")
+    _near(torch, first[2], r["dweight"], r["dweight_err"], dtype, "dweight")
+    # 32-bit labels, rows to be ignored that hold NaN, rows inside wider ones: the same bits
+    bad = torch.where(live[:, None], h, float("nan"))
+    dh, dw = _strided(torch, torch.zeros_like(h), 3, 5), _strided(torch, torch.zeros_like(w), 5, 3)
+    again = run(_strided(torch, bad, 5, 3), w, labels.int(), dh, dw)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    for t, shift in ((dh, 5), (dw, 3)):
+        assert torch.isnan(t._base[:, :shift]).all() and torch.isnan(t._base[:, shift + d:]).all()
+
+
+@pytest.mark.parametrize("rows,vocab,d", [(600, 2000, 1024), (3000, 2000, 256)])
+def test_head_loss_labels_in_a_graph_and_on_two_streams(gpu, rows, vocab, d):
+    torch, pb = gpu
+    calls = []
+    for k in range(2):                                   # the second with other labels, and a workspace of its own
+        h, w, labels, g = _head_inputs(torch, rows, vocab, d, "bf16")
+        labels = labels if k == 0 else labels.flip(0).contiguous()
+        out = torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(w)
+        calls.append((h, w, labels, g, out, _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, h.dtype, True))))
+
+    def run(k, stream=None):
+        h, w, labels, g, out, ws = calls[k]
+        pb.head_loss(h, w, labels, out[0], ws, row_weight=g, dh=out[1], dweight=out[2], stream=stream)
+    want = []
+    for k in range(2):
+        run(k)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in calls[k][4]])
+    assert not torch.equal(want[0][2], want[1][2])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for k in range(2):
+            run(k, streams[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k in range(2) for a, b in zip(want[k], calls[k][4]))
+    # one workspace after the other: what the call before left in it has no influence
+    calls[1] = calls[1][:5] + (calls[0][5],)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(0)
+        run(1)
+    for _ in range(3):
+        for k in range(2):
+            for t in calls[k][4]:
+                t.fill_(0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(want[k], calls[k][4]))
+        run(0)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("rows,vocab,d,dtype", [(40, 300, 96, "bf16"), (300, 1000, 128, "bf16"), (300, 1000, 100, "f16"), (4000, 9000, 256, "bf16"), (300, 1000, 70, "f32")])
+def test_head_loss_gradients_in_place(gpu, rows, vocab, d, dtype):
+    """A gradient may lie where its tensor does."""
+    torch, pb = gpu
+    h, w, labels, g = _head_inputs(torch, rows, vocab, d, dtype)
+    loss = _check_head(torch, pb, h, w, labels, g, dtype, ("apart", rows, dtype))[0]
+    ws = _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, h.dtype, True))
+    r = otk.head_loss(_np(h), _np(w), labels.cpu().numpy(), _np(g), HALF[dtype], 2.0 ** -38 if dtype == "f16" else 0.0)
+    for both in ((True, False), (False, True), (True, True)):
+        x, y, again = h.clone(), w.clone(), torch.empty_like(loss)
+        a, b = x if both[0] else torch.empty_like(x), y if both[1] else torch.empty_like(y)
+        pb.head_loss(x, y, labels, again, ws, row_weight=g, dh=a, dweight=b)
+        assert torch.equal(again, loss)
+        _within(_np(a), r["dh"], _round(r["dh"], r["dh_err"], dtype), "dh")
+        _within(_np(b), r["dweight"], _round(r["dweight"], r["dweight_err"], dtype), "dweight")
 
 
 # -------------------------------------------------------------------------------------- distillation from top logits
