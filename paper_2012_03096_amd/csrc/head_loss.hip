@@ -303,7 +303,7 @@ bool direct(const void *p, long long stride, int d, int dtype) {
 // pack_*: whether the operands have to be laid out (the workspace is counted as if they had).  in_place: a gradient lies where its tensor does, which the last
 // launches read where dz is not zero at the labels.
 Plan make_plan(int rows, int vocab, int d, int dtype, bool gradients, bool pack_h, bool pack_w, bool in_place) {
-  Plan p;
+  Plan p{};
   const bool f32 = dtype == PBKD_F32;
   p.pairs = f32 && (double)rows * vocab * d >= kPairsFrom;
   p.logits = p.pairs ? kPairs : f32 ? kTriples : kOne;         // products of planes for the logits, and for the gradients

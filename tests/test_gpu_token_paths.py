@@ -387,6 +387,25 @@ def test_head_loss_labels_in_a_graph_and_on_two_streams(gpu, rows, vocab, d):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("rows", [700, 2100])
+def test_head_loss_labels_of_rows_that_are_not_finite(gpu, rows):
+    """A NaN in a row that counts reaches its own loss and gradient and the weight's, one in a row without a label nothing; a row of weight zero gives nothing."""
+    torch, pb = gpu
+    vocab, d = 5000, 264
+    h, w, labels, g = _head_inputs(torch, rows, vocab, d, "bf16")
+    labels[3], labels[5], labels[7] = 17, -1, 4999
+    labels[8:20] = 4999
+    h[5, 9], g[7:20] = float("nan"), 0.0
+    loss, dh, dw = torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(w)
+    ws = _workspace(torch, pb.head_loss_workspace_bytes(rows, vocab, d, h.dtype, True))
+    pb.head_loss(h, w, labels, loss, ws, row_weight=g, dh=dh, dweight=dw)
+    assert torch.isfinite(loss).all() and torch.isfinite(dh).all() and torch.isfinite(dw).all() and (dh[5] == 0).all() and (dh[7:20] == 0).all()
+    h[3, 5] = float("nan")
+    pb.head_loss(h, w, labels, loss, ws, row_weight=g, dh=dh, dweight=dw)
+    bad = torch.arange(rows, device="cuda") == 3
+    assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(dh).all(1), bad) and not torch.isnan(dh[~bad]).any() and torch.isnan(dw).all()
+
+
 @pytest.mark.parametrize("rows,vocab,d,dtype", [(40, 300, 96, "bf16"), (300, 1000, 128, "bf16"), (300, 1000, 100, "f16"), (4000, 9000, 256, "bf16"), (300, 1000, 70, "f32")])
 def test_head_loss_gradients_in_place(gpu, rows, vocab, d, dtype):
     """A gradient may lie where its tensor does."""
