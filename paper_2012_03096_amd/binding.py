@@ -670,7 +670,7 @@ def head_loss_workspace_bytes(rows: int, vocab: int, d: int, dtype, gradients: b
 def head_loss(h, weight, labels, loss, workspace, lse=None, row_weight=None, dh=None, dweight=None, stream=None) -> None:
     """pbkd_head_loss: loss [rows] float32 <- softmax cross entropy of h weight^T against labels, without keeping the logits; labels
     outside 0..vocab-1 are ignored.  h [..., d], weight [vocab, d], labels [...] int32 or int64.  lse [rows]: the logits' log-sums.  dh and
-    dweight (like h and weight): the gradients of (row_weight * loss).sum().  workspace: a tensor of head_loss_workspace_bytes(...) bytes."""
+    dweight (like h and weight, or these themselves): the gradients of (row_weight * loss).sum().  workspace: a tensor of head_loss_workspace_bytes(...) bytes."""
     L, code, dt, shape, dev = _first(h, "h")
     if weight is None:
         _missing("weight")

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void gemm_kernel(GemmArgs G) {
   const int r32 = lane & 31, h = lane >> 5;
   // a lane's results: n = n1 + 32 j, m = m1 .. m1 + 16 MT - 1 (tile i: sixteen of them)
   const int m1 = m0 + wm * (MT * 32) + h * (16 * MT), n1 = n0 + wn * (NT * 32) + r32;
-  // Read ahead of the sum, which may be short (128 x 131072 x 8192: dW 790 us without).  The largest tile has no registers for that, and no short sums.
+  // Read ahead of the sum, which may be short (128 x 131072 x 8192: dW 726 us, without 791).  The largest tile has no registers for that, and no short sums.
   constexpr bool EARLY = EPI == kOut && MT * NT < 16;
   int slot[NT];
   auto read_slots = [&] {

@@ -7,7 +7,7 @@
 // second a piece's dz comes out of the product once, n by v: dh reads it along v with W as it lies, dW along n with a copy of h's other layout, by the
 // transposing reads of head_gemm.h.
 //
-// Measured (bf16): 8192 rows by 4096 over 131072 27.8 to 28.1 ms, 1250 to 1270 TFLOP/s over the four products; 4096 by 2048 over 65536 3.79 ms, 1160; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 71 us in nine launches.
+// Measured (bf16): 8192 rows by 4096 over 131072 27.8 to 28.1 ms, 1250 to 1270 TFLOP/s over the four products; 4096 by 2048 over 65536 3.82 ms, 1150; losses of 32 rows by 2048 over 65536 53 us, W at 5.4 TB/s; 500 by 515 over 1013 fp32 71 us in nine launches.
 //
 // dz is rounded to the operands' type, but not where a row has its label: there it is nearly the row's weight, most of both gradients, and rounding it would be
 // an error of the size that rounding the gradients has anyway (against 64 bits 0.0024 instead of 0.0017).  These numbers, one a row, stay in fp32, and dz is zero there: head_finish
